@@ -306,7 +306,7 @@ def _run_attn(s):
     top = torch.where(top == -math.inf, 0.0, top)
     p = z.sub_(top).exp_()
     total = p.sum(-1, keepdim=True)
-    lse = (top + total.log()).reshape(B * X * H, Lq)
+    lse = (top + total.log()).reshape(B, X, H, Lq)
     p.div_(torch.where(total > 0, total, 1.0))
     o = (p.reshape(B, X, Hkv, G * Lq, Lk) @ v).reshape(B, X, H, Lq, D)
 
@@ -410,7 +410,7 @@ def exact(case, seed):
             dk[b, :, :n, e] += torch.matmul(dz.transpose(1, 2), q[b, :, :, h].contiguous()) / math.sqrt(D)
             db[h] += torch.bincount(which.reshape(-1), weights=dz.sum(0).reshape(-1), minlength=c["nb"])
     flat = lambda t: t.reshape(B, X, t.shape[2], -1)  # noqa: E731
-    res = {"o": flat(o), "lse": lse.reshape(B * X * H, Lq)}
+    res = {"o": flat(o), "lse": lse}
     if c["train"]:
         res |= {"dq": flat(dq), "dk": flat(dk), "dv": flat(dv), "dbias": db.t().contiguous()}
     return res
