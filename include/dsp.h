@@ -313,6 +313,58 @@ int dsp_attn_general_bwd(const void* q, const void* k, const void* v, const void
                          void* stream);
 
 /* ------------------------------------------------------------------------
+ * dsp_qk_norm_rope -- queries and keys made ready for attention: the root mean
+ * square norm of each head with a learned gain, and the rotation by position, in
+ * one pass.  For each token (b, x, l) and head, u of width D:
+ *     n = g * u / sqrt(mean(u^2) + eps),
+ *     y = n with its first `rot` elements turned in pairs (n_a, n_b):
+ *         y_a = n_a cos - n_b sin,  y_b = n_b cos + n_a sin,
+ * cos and sin at row p of the table, column i for pair i < rot / 2.
+ * q:      H heads, element (b, x, l, h*D + d) at b*q_strides[0] + x*q_strides[1]
+ *         + l*q_strides[2] + h*D + d; k: Hkv heads with k_strides; yq, yk:
+ *         outputs of the same shapes with strides of their own.  In place
+ *         (yq == q or yk == k with equal strides) is allowed; k and yk may be
+ *         columns of q's or yq's buffer ([Q | K | V]), any other overlap is
+ *         DSP_ERR_ARG.  Hkv = 0: queries only (k, yk, gk unused); H = 0 keys only.
+ * gq, gk: gains [D] of dtype, or NULL (1).
+ * cos, sin: DEVICE fp32 [P][rot / 2]; unused when rot is 0.
+ * pos:    DEVICE int32 [B][L], the table's row of each token, or NULL (row l,
+ *         L <= P).  A token whose position has no row (outside 0 .. P - 1) gets
+ *         NaN in the elements that turn; nothing outside the table is read.
+ * rot:    even, 0 .. D.  flags: 0 pairs element i with i + rot/2,
+ *         DSP_ROPE_ADJACENT pairs 2i with 2i + 1.
+ * Arithmetic is fp32, each output is rounded once.  D is 1 .. 256 for both
+ * dtypes at any alignment of an element; 16-byte aligned tensors and tables, with
+ * strides, D and rot multiples of 16 bytes, are fastest.
+ *
+ * dsp_qk_norm_rope_bwd -- its gradient: with dn the turn back of dy and w = g dn,
+ *     dg = sum over tokens and heads of dn * u * r,  r = 1/sqrt(mean(u^2) + eps),
+ *     du = r (w - u r^2 mean(w u)).
+ *   dq and dk may be in place of dyq and dyk, or of q and k (equal strides).
+ *   dgq, dgk: fp32 [D], or NULL.  workspace: at least
+ *   dsp_qk_norm_rope_bwd_workspace_bytes(B, X, L, H, Hkv, D) bytes, 16-byte
+ *   aligned, needed when dgq or dgk is given.  Deterministic.
+ * Errors: DSP_ERR_NULL, DSP_ERR_SHAPE (a size < 0, D outside 1 .. 256, no heads,
+ *   rot odd or past D, P < 1 or (pos NULL) P < L with rot > 0, 2^31 rows of
+ *   B X L heads or more), DSP_ERR_DTYPE, DSP_ERR_ALIGN (off an element),
+ *   DSP_ERR_ARG (eps < 0 or not finite, unknown flags, overlapping outputs),
+ *   DSP_ERR_WORKSPACE, DSP_ERR_HIP.  An empty input launches nothing and may come
+ *   with NULL pointers; the gradient then writes dgq = dgk = 0.
+ * ------------------------------------------------------------------------ */
+enum { DSP_ROPE_ADJACENT = 1 };
+int dsp_qk_norm_rope(const void* q, const void* k, void* yq, void* yk, const void* gq, const void* gk,
+                     const float* cos, const float* sin, const int32_t* pos, int64_t P, int rot, int flags, int64_t B,
+                     int64_t X, int64_t L, int H, int Hkv, int D, const int64_t* q_strides, const int64_t* k_strides,
+                     const int64_t* yq_strides, const int64_t* yk_strides, float eps, int dtype, void* stream);
+size_t dsp_qk_norm_rope_bwd_workspace_bytes(int64_t B, int64_t X, int64_t L, int H, int Hkv, int D);
+int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const void* dyk, void* dq, void* dk,
+                         float* dgq, float* dgk, const void* gq, const void* gk, const float* cos, const float* sin,
+                         const int32_t* pos, int64_t P, int rot, int flags, void* workspace, size_t ws_bytes,
+                         int64_t B, int64_t X, int64_t L, int H, int Hkv, int D, const int64_t* q_strides,
+                         const int64_t* k_strides, const int64_t* dyq_strides, const int64_t* dyk_strides,
+                         const int64_t* dq_strides, const int64_t* dk_strides, float eps, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
  * dsp_layernorm -- per-row normalisation over C (Eq. 4, 6):
  *   y = (x - mean) / sqrt(var + eps), biased variance, no affine part,
  *   statistics in fp32.

@@ -11,7 +11,7 @@ binding's functions raises.
 Entry points (see ``include/dsp.h`` for the exact contracts):
 ``dsp_switch``, ``dsp_exchange_unpack``, ``dsp_split``, ``dsp_gather``,
 ``dsp_spatial_attn``, ``dsp_temporal_attn``, ``dsp_attn_strided``,
-``dsp_attn_fwd_lse``, ``dsp_attn_bwd``, ``dsp_attn_general``, ``dsp_attn_general_bwd``, ``dsp_layernorm_bwd``, ``dsp_linear_bwd_data``, ``dsp_linear_bwd_weight``,
+``dsp_attn_fwd_lse``, ``dsp_attn_bwd``, ``dsp_attn_general``, ``dsp_attn_general_bwd``, ``dsp_qk_norm_rope``, ``dsp_qk_norm_rope_bwd``, ``dsp_layernorm_bwd``, ``dsp_linear_bwd_data``, ``dsp_linear_bwd_weight``,
 ``dsp_layernorm``, ``dsp_linear``, ``dsp_st_block_forward``.
 """
 from __future__ import annotations
@@ -29,6 +29,7 @@ DSP_OK, DSP_ERR_NULL, DSP_ERR_DIM, DSP_ERR_SHAPE, DSP_ERR_DTYPE, DSP_ERR_ALIGN, 
 DSP_F32, DSP_BF16 = 0, 1
 DSP_EPI_NONE, DSP_EPI_GELU, DSP_EPI_RESID, DSP_EPI_F32, DSP_EPI_RELU = 0, 1, 2, 3, 4
 DSP_BLOCK_NO_MLP_LN, DSP_BLOCK_ATTN_ONLY, DSP_BLOCK_POST_LN, DSP_BLOCK_RELU = 1, 2, 4, 8
+DSP_ROPE_ADJACENT = 1
 DSP_GRAD_EPI_F32, DSP_GRAD_EPI_BF16, DSP_GRAD_EPI_GELU_BWD, DSP_GRAD_EPI_RELU_BWD = 0, 1, 2, 3
 
 BLOCK_WEIGHT_FIELDS = ("wqkv_s", "bqkv_s", "wo_s", "bo_s", "wqkv_t", "bqkv_t", "wo_t", "bo_t",
@@ -72,6 +73,11 @@ _SIGNATURES = {
     "dsp_attn_bwd_noalloc_max_rows": (_I64, []),
     "dsp_attn_bwd_noalloc": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I, _I,
                                   _c.POINTER(_I64), _c.POINTER(_I64), _F, _I, _P]),
+    "dsp_qk_norm_rope": (_I, [_P] * 9 + [_I64, _I, _I, _I64, _I64, _I64, _I, _I, _I] + [_c.POINTER(_I64)] * 4
+                         + [_F, _I, _P]),
+    "dsp_qk_norm_rope_bwd_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I, _I, _I]),
+    "dsp_qk_norm_rope_bwd": (_I, [_P] * 13 + [_I64, _I, _I, _P, _SZ, _I64, _I64, _I64, _I, _I, _I]
+                             + [_c.POINTER(_I64)] * 6 + [_F, _I, _P]),
     "dsp_layernorm": (_I, [_P, _I, _P, _I, _I64, _I, _F, _P]),
     "dsp_attn_general": (_I, [_P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I, _I, _I, _c.POINTER(_I64),
                               _c.POINTER(_I64), _c.POINTER(_I64), _F, _I, _P]),
@@ -176,6 +182,35 @@ class _on:
     def __exit__(self, *exc):
         if self.guard is not None:
             self.guard.__exit__(*exc)
+        return False
+
+
+class _on_device:
+    """`_on` for calls whose tensors may be on another device than the current one: that
+    device is current meanwhile (its current stream, or the given `stream` of it)."""
+    __slots__ = ("dev", "on")
+
+    def __init__(self, t, stream):
+        torch = _torch()
+        if stream is not None and stream.device != t.device:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
+        self.dev = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
+        if self.dev is not None:
+            self.dev.__enter__()
+        try:
+            self.on = _on(stream)
+        except BaseException:
+            if self.dev is not None:
+                self.dev.__exit__(None, None, None)
+            raise
+
+    def __enter__(self):
+        return self.on.__enter__()
+
+    def __exit__(self, *exc):
+        self.on.__exit__(*exc)
+        if self.dev is not None:
+            self.dev.__exit__(*exc)
         return False
 
 
@@ -599,6 +634,107 @@ def dsp_attn_general_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, dq=None, dk=No
                                                  _ptr(dq), _ptr(dk), _ptr(dv), _ptr(delta), B, X, Lq, Lk, H, Hkv, D,
                                                  _st3(q), _st3(k), _st3(o), float(scale), _dtype_code(q), s), w)
     return dq, dk, dv
+
+
+def _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos):
+    """Checks what dsp_qk_norm_rope and its gradient share; returns (B, X, L, D, P, rot)."""
+    torch = _torch()
+    x, n = (q, H) if q is not None else (k, Hkv)
+    _check(w, "q" if q is not None else "k", x, contiguous=False)
+    _float_dtype(w, x)
+    if (q is None) != (H == 0) or (k is None) != (Hkv == 0):
+        raise ValueError(f"{w}: q has H heads and k has Hkv heads (None: 0)")
+    if x.dim() != 4 or n < 1 or x.shape[3] % n:
+        raise ValueError(f"{w}: q and k must be 4-D views [B, X, L, heads * D]")
+    B, X, L, C = x.shape
+    D = C // n
+    for name, t, heads, g in (("q", q, H, gq), ("k", k, Hkv, gk)):
+        if t is None:
+            continue
+        _check(w, name, t, dtype=x.dtype, shape=(B, X, L, heads * D), contiguous=False, like=x)
+        if t.stride(3) != 1:
+            raise ValueError(f"{w}: {name} must have a unit last stride")
+        if g is not None:
+            _check(w, "g" + name, g, dtype=x.dtype, shape=(D,), like=x)
+    if (cos is None) != (sin is None):
+        raise ValueError(f"{w}: cos and sin come together")
+    P = rot = 0
+    if cos is not None:
+        _check(w, "cos", cos, dtype=torch.float32, like=x)
+        if cos.dim() != 2:
+            raise ValueError(f"{w}: cos must be [P, rot / 2]")
+        _check(w, "sin", sin, dtype=torch.float32, shape=cos.shape, like=x)
+        P, rot = cos.shape[0], 2 * cos.shape[1]
+    if pos is not None:
+        _check(w, "pos", pos, dtype=torch.int32, shape=(B, L), like=x)
+    return B, X, L, D, P, rot
+
+
+def dsp_qk_norm_rope(q, k, H: int, Hkv: int, gq=None, gk=None, cos=None, sin=None, pos=None,
+                     interleaved: bool = False, eps: float = 1e-6, out_q=None, out_k=None, stream=None):
+    """Norm of queries and keys for each head and the rotation by position in one
+    pass (see dsp.h): q [B, X, L, H*D] and k [B, X, L, Hkv*D], 4-D views with any
+    strides (columns of a packed projection among them) and a unit last one; either
+    may be None with 0 heads.  ``gq``, ``gk``: gains [D] of q's dtype.  ``cos``,
+    ``sin``: float32 [P, rot/2]; the first rot elements of a head turn, in pairs
+    (i, i + rot/2) or, ``interleaved``, (2i, 2i + 1).  ``pos``: int32 [B, L], the
+    table's row of each token (default: its place l; without a row: NaN).  Returns
+    (yq, yk): new contiguous tensors, or ``out_q`` and ``out_k`` (q and k
+    themselves: in place)."""
+    torch = _torch()
+    w = "dsp_qk_norm_rope"
+    B, X, L, D, P, rot = _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos)
+    like = q if q is not None else k
+    with _on_device(like, stream) as s:
+        outs = []
+        for t, o, name in ((q, out_q, "out_q"), (k, out_k, "out_k")):
+            if t is not None:
+                o = torch.empty(t.shape, dtype=t.dtype, device=t.device) if o is None else o
+                _like_view(w, o, t, name)
+            outs.append(o if t is not None else None)
+        yq, yk = outs
+        st = [_st3(t) if t is not None else None for t in (q, k, yq, yk)]
+        _check_status(lib().dsp_qk_norm_rope(_ptr(q), _ptr(k), _ptr(yq), _ptr(yk), _ptr(gq), _ptr(gk), _ptr(cos),
+                                             _ptr(sin), _ptr(pos), P, rot, DSP_ROPE_ADJACENT if interleaved else 0,
+                                             B, X, L, H, Hkv, D, *st, float(eps), _dtype_code(like), s), w)
+    return yq, yk
+
+
+def dsp_qk_norm_rope_bwd(q, k, dyq, dyk, H: int, Hkv: int, gq=None, gk=None, cos=None, sin=None, pos=None,
+                         interleaved: bool = False, eps: float = 1e-6, dq=None, dk=None, gains: bool = True,
+                         workspace=None, stream=None):
+    """Gradient of dsp_qk_norm_rope at its inputs q and k: (dq, dk, dgq, dgk) from
+    the gradients dyq, dyk of its outputs (views of any strides).  dq and dk are new
+    contiguous tensors, or views given (dyq and dyk themselves: in place); dgq and
+    dgk are float32 [D], None without ``gains`` or without the side."""
+    torch = _torch()
+    w = "dsp_qk_norm_rope_bwd"
+    B, X, L, D, P, rot = _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos)
+    like = q if q is not None else k
+    with _on_device(like, stream) as s:
+        outs, dg = [], []
+        for t, dy, o, name in ((q, dyq, dq, "q"), (k, dyk, dk, "k")):
+            if t is not None:
+                _like_view(w, dy, t, "dy" + name)
+                o = torch.empty(t.shape, dtype=t.dtype, device=t.device) if o is None else o
+                _like_view(w, o, t, "d" + name)
+            elif dy is not None:
+                raise ValueError(f"{w}: dy{name} without {name}")
+            outs.append(o if t is not None else None)
+            dg.append(torch.empty(D, dtype=torch.float32, device=like.device) if gains and t is not None else None)
+        dq, dk = outs
+        need = lib().dsp_qk_norm_rope_bwd_workspace_bytes(B, X, L, H, Hkv, D) if gains else 0
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
+        if workspace is not None:
+            _check(w, "workspace", workspace, like=like)
+        st = [_st3(t) if t is not None else None for t in (q, k, dyq, dyk, dq, dk)]
+        _check_status(lib().dsp_qk_norm_rope_bwd(
+            _ptr(q), _ptr(k), _ptr(dyq), _ptr(dyk), _ptr(dq), _ptr(dk), _ptr(dg[0]), _ptr(dg[1]), _ptr(gq), _ptr(gk),
+            _ptr(cos), _ptr(sin), _ptr(pos), P, rot, DSP_ROPE_ADJACENT if interleaved else 0, _ptr(workspace),
+            _nbytes(workspace) if workspace is not None else 0, B, X, L, H, Hkv, D, *st, float(eps),
+            _dtype_code(like), s), w)
+    return dq, dk, dg[0], dg[1]
 
 
 def dsp_layernorm_bwd(x, dy, eps: float = 1e-6, dres=None, out=None, stream=None):

@@ -294,6 +294,106 @@ int attn_impl(const void* q, const void* k, const void* v, void* o, int64_t B, i
   return attn_impl_strided(q, k, v, o, B, X, L, H, D, in_st, out_st, scale, dtype, stream);
 }
 
+// offsets_ok with room to spare: sums of the terms in bytes stay below 2^63
+bool spans_ok(int64_t B, int64_t X, int64_t L, const int64_t* st) {
+  const int64_t n[3] = {B, X, L};
+  for (int i = 0; i < 3; ++i) {
+    int64_t t;
+    if (st[i] < 0 || !mul_ok(n[i] - 1, st[i], &t) || t > (int64_t(1) << 58)) return false;
+  }
+  return true;
+}
+
+// Two row tensors of the same (B, X, L) grid share no element: their spans are
+// apart, or they have one layout and lie in different columns of its rows.
+bool rows_apart(const void* a, const int64_t* sa, int64_t wa, const void* b, const int64_t* sb, int64_t wb, int64_t B,
+                int64_t X, int64_t L, int es) {
+  auto span = [&](const int64_t* st, int64_t w) {
+    return (size_t)((B - 1) * st[0] + (X - 1) * st[1] + (L - 1) * st[2] + w) * es;
+  };
+  if (!wa || !wb || !overlap(a, span(sa, wa), b, span(sb, wb))) return true;
+  const int64_t ext[3] = {B, X, L};
+  int64_t pitch = INT64_MAX;
+  for (int i = 0; i < 3; ++i) {
+    if (ext[i] <= 1) continue;
+    if (sa[i] != sb[i]) return false;
+    pitch = sa[i] < pitch ? sa[i] : pitch;
+  }
+  const int64_t off = ((intptr_t)b - (intptr_t)a) / es;
+  if (((intptr_t)b - (intptr_t)a) % es) return false;
+  return off >= 0 ? off >= wa && off <= pitch - wb : -off >= wb && -off <= pitch - wa;
+}
+bool same_rows(const void* a, const int64_t* sa, const void* b, const int64_t* sb, int64_t B, int64_t X, int64_t L) {
+  const int64_t ext[3] = {B, X, L};
+  for (int i = 0; i < 3; ++i)
+    if (ext[i] > 1 && sa[i] != sb[i]) return false;
+  return a == b;
+}
+
+int qk_norm_impl(QkNormArgs& a, bool bwd, int flags, int H, int Hkv, const int64_t* const (&xs)[2],
+                 const int64_t* const (&ds)[2], const int64_t* const (&ys)[2], void* workspace, size_t ws_bytes,
+                 int dtype, void* stream) {
+  if (!valid_dtype(dtype)) return DSP_ERR_DTYPE;
+  if (a.B < 0 || a.X < 0 || a.L < 0 || H < 0 || Hkv < 0 || (int64_t)H + Hkv < 1) return DSP_ERR_SHAPE;
+  if (a.D < 1 || a.D > 256 || a.rot < 0 || a.rot % 2 || a.rot > a.D) return DSP_ERR_SHAPE;
+  if (!(a.eps >= 0.0f) || isinf(a.eps) || (flags & ~DSP_ROPE_ADJACENT)) return DSP_ERR_ARG;
+  const int es = elem_size(dtype);
+  const int heads[2] = {H, Hkv};
+  hipStream_t s = as_stream(stream);
+  int64_t tokens, rows, width;
+  if (!mul_ok(a.B, a.X, &tokens) || !mul_ok(tokens, a.L, &tokens)) return DSP_ERR_SHAPE;
+  for (int i = 0; i < 2; ++i)
+    if (!mul_ok(tokens, heads[i], &rows) || rows >= (int64_t(1) << 31) || !mul_ok(heads[i], a.D, &width))
+      return DSP_ERR_SHAPE;
+  if (a.rot && tokens && (a.P < 1 || a.P > INT32_MAX || (!a.pos && a.P < a.L))) return DSP_ERR_SHAPE;
+  bool gains = false;
+  for (int i = 0; i < 2; ++i) {
+    QkNormSide& d = a.side[i];
+    d.heads = heads[i];
+    if (!heads[i]) { d.dgain = nullptr; continue; }
+    if (!aligned(d.gain, es) || !aligned(d.dgain, 4)) return DSP_ERR_ALIGN;
+    gains = gains || d.dgain;
+    if (!tokens) continue;
+    if (!xs[i] || !ys[i] || (bwd && !ds[i]) || !d.x || !d.y || (bwd && !d.dy)) return DSP_ERR_NULL;
+    if (!aligned(d.x, es) || !aligned(d.y, es) || !aligned(d.dy, es)) return DSP_ERR_ALIGN;
+    for (int k = 0; k < 3; ++k) {
+      d.x_strides[k] = xs[i][k];
+      d.y_strides[k] = ys[i][k];
+      d.dy_strides[k] = bwd ? ds[i][k] : 0;
+      if (d.x_strides[k] < 0 || d.y_strides[k] < 0 || d.dy_strides[k] < 0) return DSP_ERR_SHAPE;
+    }
+    for (const int64_t* st : {d.x_strides, d.y_strides, d.dy_strides})
+      if (!spans_ok(a.B, a.X, a.L, st)) return DSP_ERR_SHAPE;
+    if (!rows_disjoint(a.B, a.X, a.L, d.y_strides, (int64_t)heads[i] * a.D)) return DSP_ERR_ARG;
+  }
+  if (!tokens) return gains ? launch_qk_norm(a, bwd, nullptr, s) : DSP_OK;  // no rows: dg is a sum of nothing
+  if (a.rot && (!a.cos || !a.sin)) return DSP_ERR_NULL;
+  if (!aligned(a.cos, 4) || !aligned(a.sin, 4) || !aligned(a.pos, 4)) return DSP_ERR_ALIGN;
+  for (int i = 0; i < 2; ++i) {  // an output is apart from everything else, or in place of its own input
+    const QkNormSide& d = a.side[i];
+    if (!heads[i]) continue;
+    const int64_t w = (int64_t)heads[i] * a.D;
+    for (int j = 0; j < 2; ++j) {
+      const QkNormSide& o = a.side[j];
+      if (!heads[j]) continue;
+      const int64_t ow = (int64_t)heads[j] * a.D;
+      auto clear = [&](const void* ptr, const int64_t* st) {
+        return (i == j && same_rows(d.y, d.y_strides, ptr, st, a.B, a.X, a.L)) ||
+               rows_apart(d.y, d.y_strides, w, ptr, st, ow, a.B, a.X, a.L, es);
+      };
+      if (!clear(o.x, o.x_strides) || (bwd && !clear(o.dy, o.dy_strides))) return DSP_ERR_ARG;
+      if (i != j && !rows_apart(d.y, d.y_strides, w, o.y, o.y_strides, ow, a.B, a.X, a.L, es)) return DSP_ERR_ARG;
+    }
+  }
+  if (gains) {
+    const size_t need = qk_norm_workspace_bytes(tokens, H, Hkv, a.D);
+    if (!workspace || ws_bytes < need || !aligned(workspace, 16)) return DSP_ERR_WORKSPACE;
+  }
+  a.half = !(flags & DSP_ROPE_ADJACENT);
+  a.bf16 = dtype == DSP_BF16;
+  return launch_qk_norm(a, bwd, static_cast<float*>(workspace), s);
+}
+
 // pre (GELU/ReLU epilogue, may be null): also receives the pre-activation.
 // rs (optional): the output rows permuted from (B, T, S) to (B, S, T) token order
 // (the switch T -> S in the epilogue); the residual is read in the input's order,
@@ -677,6 +777,43 @@ int dsp_attn_general_bwd(const void* q, const void* k, const void* v, const void
                          void* stream) {
   return attn_bwd_general_impl(q, k, v, o, dout, lse, dq, dk, dv, delta, B, X, Lq, Lk, H, Hkv, D, q_strides,
                                kv_strides, o_strides, scale, dtype, stream);
+}
+
+int dsp_qk_norm_rope(const void* q, const void* k, void* yq, void* yk, const void* gq, const void* gk,
+                     const float* cos, const float* sin, const int32_t* pos, int64_t P, int rot, int flags, int64_t B,
+                     int64_t X, int64_t L, int H, int Hkv, int D, const int64_t* q_strides, const int64_t* k_strides,
+                     const int64_t* yq_strides, const int64_t* yk_strides, float eps, int dtype, void* stream) {
+  QkNormArgs a = {};
+  a.side[0].x = q, a.side[0].y = yq, a.side[0].gain = gq;
+  a.side[1].x = k, a.side[1].y = yk, a.side[1].gain = gk;
+  a.cos = cos, a.sin = sin, a.pos = pos;
+  a.P = P, a.B = B, a.X = X, a.L = L, a.D = D, a.rot = rot, a.eps = eps;
+  return qk_norm_impl(a, false, flags, H, Hkv, {q_strides, k_strides}, {nullptr, nullptr}, {yq_strides, yk_strides},
+                      nullptr, 0, dtype, stream);
+}
+
+size_t dsp_qk_norm_rope_bwd_workspace_bytes(int64_t B, int64_t X, int64_t L, int H, int Hkv, int D) {
+  int64_t tokens, rows;
+  if (!mul_ok(B, X, &tokens) || !mul_ok(tokens, L, &tokens) || H < 0 || Hkv < 0 || D < 1 || D > 256 ||
+      !mul_ok(tokens, H, &rows) || rows >= (int64_t(1) << 31) || !mul_ok(tokens, Hkv, &rows) ||
+      rows >= (int64_t(1) << 31))
+    return 0;
+  return qk_norm_workspace_bytes(tokens, H, Hkv, D);
+}
+
+int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const void* dyk, void* dq, void* dk,
+                         float* dgq, float* dgk, const void* gq, const void* gk, const float* cos, const float* sin,
+                         const int32_t* pos, int64_t P, int rot, int flags, void* workspace, size_t ws_bytes,
+                         int64_t B, int64_t X, int64_t L, int H, int Hkv, int D, const int64_t* q_strides,
+                         const int64_t* k_strides, const int64_t* dyq_strides, const int64_t* dyk_strides,
+                         const int64_t* dq_strides, const int64_t* dk_strides, float eps, int dtype, void* stream) {
+  QkNormArgs a = {};
+  a.side[0].x = q, a.side[0].dy = dyq, a.side[0].y = dq, a.side[0].gain = gq, a.side[0].dgain = dgq;
+  a.side[1].x = k, a.side[1].dy = dyk, a.side[1].y = dk, a.side[1].gain = gk, a.side[1].dgain = dgk;
+  a.cos = cos, a.sin = sin, a.pos = pos;
+  a.P = P, a.B = B, a.X = X, a.L = L, a.D = D, a.rot = rot, a.eps = eps;
+  return qk_norm_impl(a, true, flags, H, Hkv, {q_strides, k_strides}, {dyq_strides, dyk_strides},
+                      {dq_strides, dk_strides}, workspace, ws_bytes, dtype, stream);
 }
 
 int dsp_linear_bwd_data(const void* dy, const void* w, const void* u, void* dx, int64_t M, int N, int K,

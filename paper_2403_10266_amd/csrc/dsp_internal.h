@@ -91,6 +91,32 @@ constexpr int kShortAttnMaxL = 128;
 bool attn_bf16_short_fits(const AttnArgs& a);
 int launch_attn_bf16_short(const AttnArgs& a, hipStream_t s);
 
+// Norm of queries and keys for each head with the position rotation, and its
+// gradient (qk_norm.hip).  Row (b, x, l, head) of x (and dy, y) sits at
+// b * st[0] + x * st[1] + l * st[2] + head * D.  part: qk_norm_workspace_bytes()
+// bytes of fp32 when a gain's gradient is wanted.
+struct QkNormSide {
+  const void* x;
+  const void* dy;    // gradient only
+  void* y;           // y, or dx
+  const void* gain;  // or null: 1
+  float* dgain;      // gradient only, or null
+  int heads;         // 0: this side is absent
+  int64_t x_strides[3], dy_strides[3], y_strides[3];
+};
+struct QkNormArgs {
+  QkNormSide side[2];  // queries, keys
+  const float* cos;
+  const float* sin;
+  const int32_t* pos;
+  int64_t P, B, X, L;
+  int D, rot;
+  bool half, bf16;
+  float eps;
+};
+size_t qk_norm_workspace_bytes(int64_t tokens, int H, int Hkv, int D);
+int launch_qk_norm(const QkNormArgs& a, bool bwd, float* part, hipStream_t s);
+
 int launch_layernorm(const void* x, int x_bf16, void* y, int y_bf16, int64_t rows, int C, float eps,
                      hipStream_t s);
 

@@ -1,0 +1,468 @@
+// Norm of queries and keys for each head, with the position rotation in the same
+// pass, and its gradient.  For each token and head, x of width D:
+//   n = g * x * r,  r = 1 / sqrt(mean(x^2) + eps)
+//   y = R(p) n: for pair i of the first `rot` elements, with (c, s) = row p of
+//       the table,  (a, b) -> (a c - b s, b c + a s).
+// Gradient, with dn = R(p)^T dy (the turn back) and w = g * dn:
+//   dg = sum over tokens and heads of dn * x * r,
+//   dx = r * (w - x * r^2 * mean(w * x)).
+// Everything between the loads and the stores is fp32; y and dx are rounded once.
+//
+// The pass is bound by HBM: each element is read once and written once (the
+// gradient reads x and dy).  A row (one head of one token) is cut into chunks of
+// 16 bytes, one per lane, and consecutive rows follow each other in a wave (seven
+// rows of nine chunks at D = 72 in bf16), so a wave's loads cover one contiguous
+// stretch of memory whatever D is.  The sums over a row are segmented wave
+// reductions.  A chunk always holds whole pairs: adjacent pairs lie in one 16-byte
+// run, pairs (i, i + rot/2) in two runs of 8 bytes, one of each half, so no lane
+// needs another's elements.  A lane keeps its gains in registers and, for the
+// gradient, its share of dg; the lanes' shares are added in a fixed order.
+// Sizes that have no such chunks (widths or offsets off 16 bytes) take a wave per
+// row, element by element.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "dsp_internal.h"
+
+namespace dsp {
+namespace {
+
+typedef __bf16 bf16;
+
+constexpr int kNT = 256;   // threads of a work-group
+constexpr int kUnr = 4;    // row groups a wave has in flight
+constexpr int kMaxD = 256;
+
+// n / d for n < 2^31 by a multiplication
+struct FastDiv {
+  uint32_t d, m, s;
+};
+FastDiv fast_div(uint32_t d) {
+  uint32_t s = 0;
+  while ((uint64_t(1) << s) < d) ++s;
+  return {d, (uint32_t)(((uint64_t(1) << 32) * ((uint64_t(1) << s) - d)) / d + 1), s};
+}
+__device__ __forceinline__ uint32_t div(uint32_t n, const FastDiv& f) { return (__umulhi(n, f.m) + n) >> f.s; }
+
+struct Side {  // queries or keys
+  const void* x;
+  const void* dy;  // gradient only
+  void* y;         // y, or dx
+  const void* g;   // gains, or null
+  int64_t xs[3], ds[3], ys[3];  // element strides of x, dy and y along b, x, l
+  FastDiv heads;
+  uint32_t rows;   // tokens x heads
+  uint32_t blocks;
+};
+
+struct NormParams {
+  Side side[2];
+  const float* cos;
+  const float* sin;
+  const int32_t* pos;  // [B][L], or null: position l
+  float* part;         // gradient of the gains: [blocks of both sides][D], or null
+  uint32_t P, R, D;
+  uint32_t G, HP;      // lanes of a row, rows of a wave
+  FastDiv L, X;
+  float eps;
+};
+
+template <typename T>
+struct Vec;  // E elements of 16 bytes; half of them
+template <>
+struct Vec<bf16> {
+  static constexpr int E = 8;
+  typedef bf16 whole __attribute__((ext_vector_type(8)));
+  typedef bf16 half __attribute__((ext_vector_type(4)));
+};
+template <>
+struct Vec<float> {
+  static constexpr int E = 4;
+  typedef float whole __attribute__((ext_vector_type(4)));
+  typedef float half __attribute__((ext_vector_type(2)));
+};
+
+struct Where {
+  uint32_t h, l, x, b;
+};
+__device__ __forceinline__ Where where(const NormParams& p, const Side& s, uint32_t row) {
+  Where w;
+  const uint32_t t = div(row, s.heads);
+  w.h = row - t * s.heads.d;
+  const uint32_t bx = div(t, p.L);
+  w.l = t - bx * p.L.d;
+  w.b = div(bx, p.X);
+  w.x = bx - w.b * p.X.d;
+  return w;
+}
+__device__ __forceinline__ int64_t at(const Where& w, const int64_t* st, uint32_t D) {
+  return (int64_t)w.b * st[0] + (int64_t)w.x * st[1] + (int64_t)w.l * st[2] + (int64_t)w.h * D;
+}
+// the table's row of a token, or -1 where its position has none
+__device__ __forceinline__ int64_t table_row(const NormParams& p, const Where& w) {
+  if (!p.pos) return w.l;
+  const int32_t q = p.pos[(int64_t)w.b * p.L.d + w.l];
+  return (uint32_t)q < p.P ? q : -1;
+}
+
+// a lane's E elements in pair order: a[i], b[i] are the two of its i-th pair
+template <typename T, bool HALF>
+__device__ __forceinline__ void load(const T* x, uint32_t o0, uint32_t o1, float (&a)[Vec<T>::E / 2],
+                                     float (&b)[Vec<T>::E / 2]) {
+  using V = Vec<T>;
+  if constexpr (HALF) {
+    const typename V::half u = *reinterpret_cast<const typename V::half*>(x + o0);
+    const typename V::half v = *reinterpret_cast<const typename V::half*>(x + o1);
+#pragma unroll
+    for (int i = 0; i < V::E / 2; ++i) a[i] = (float)u[i], b[i] = (float)v[i];
+  } else {
+    const typename V::whole u = *reinterpret_cast<const typename V::whole*>(x + o0);
+#pragma unroll
+    for (int i = 0; i < V::E / 2; ++i) a[i] = (float)u[2 * i], b[i] = (float)u[2 * i + 1];
+  }
+}
+template <typename T, bool HALF>
+__device__ __forceinline__ void store(T* y, uint32_t o0, uint32_t o1, const float (&a)[Vec<T>::E / 2],
+                                      const float (&b)[Vec<T>::E / 2]) {
+  using V = Vec<T>;
+  if constexpr (HALF) {
+    typename V::half u, v;
+#pragma unroll
+    for (int i = 0; i < V::E / 2; ++i) u[i] = (T)a[i], v[i] = (T)b[i];
+    *reinterpret_cast<typename V::half*>(y + o0) = u;
+    *reinterpret_cast<typename V::half*>(y + o1) = v;
+  } else {
+    typename V::whole u;
+#pragma unroll
+    for (int i = 0; i < V::E / 2; ++i) u[2 * i] = (T)a[i], u[2 * i + 1] = (T)b[i];
+    *reinterpret_cast<typename V::whole*>(y + o0) = u;
+  }
+}
+
+// sum over the G lanes of a row (j: this lane's place in it), in every one of them
+__device__ __forceinline__ float row_sum(float v, uint32_t G, uint32_t j, int lane) {
+  for (uint32_t off = 1; off < G; off <<= 1) {
+    const float t = __shfl_down(v, off);
+    v += j + off < G ? t : 0.0f;
+  }
+  return __shfl(v, lane - (int)j);
+}
+
+template <typename T, bool HALF, bool BWD>
+__global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
+  constexpr int E = Vec<T>::E, N = E / 2;
+  __shared__ float red[BWD ? kNT * E : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int which = blockIdx.x >= p.side[0].blocks;
+  const Side& s = p.side[which];
+  const uint32_t blk = blockIdx.x - (which ? p.side[0].blocks : 0);
+  const uint32_t slot = lane / p.G, j = lane - slot * p.G;
+  const bool on = slot < p.HP;
+  const bool turns = E * j < p.R;  // R is a multiple of E
+  const uint32_t o0 = HALF && turns ? N * j : E * j;
+  const uint32_t o1 = HALF && turns ? p.R / 2 + N * j : E * j + N;
+  const float inv_d = 1.0f / (float)p.D;
+
+  float ga[N], gb[N], da[N], db[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) ga[i] = gb[i] = 1.0f, da[i] = db[i] = 0.0f;
+  if (s.g && on) load<T, HALF>(static_cast<const T*>(s.g), o0, o1, ga, gb);
+
+  const uint32_t group = (kNT / 64) * p.HP * kUnr;  // rows of a work-group's pass
+  for (uint64_t first = (uint64_t)blk * group; first < s.rows; first += (uint64_t)s.blocks * group) {
+    float a[kUnr][N], b[kUnr][N], ya[kUnr][N], yb[kUnr][N], c[kUnr][N], sn[kUnr][N];
+    int64_t to[kUnr];
+    bool ok[kUnr];
+#pragma unroll
+    for (int u = 0; u < kUnr; ++u) {
+      const uint64_t row = first + ((uint32_t)wave * kUnr + u) * p.HP + slot;
+      ok[u] = on && row < s.rows;
+#pragma unroll
+      for (int i = 0; i < N; ++i) a[u][i] = b[u][i] = ya[u][i] = yb[u][i] = sn[u][i] = 0.0f, c[u][i] = 1.0f;
+      to[u] = 0;
+      if (ok[u]) {
+        const Where w = where(p, s, (uint32_t)row);
+        to[u] = at(w, s.ys, p.D);
+        load<T, HALF>(static_cast<const T*>(s.x) + at(w, s.xs, p.D), o0, o1, a[u], b[u]);
+        if (BWD) load<T, HALF>(static_cast<const T*>(s.dy) + at(w, s.ds, p.D), o0, o1, ya[u], yb[u]);
+        if (turns) {
+          typedef float fv __attribute__((ext_vector_type(N)));
+          const int64_t t = table_row(p, w);
+          if (t >= 0) {
+            const int64_t e = t * (p.R / 2) + N * j;
+            const fv cv = *reinterpret_cast<const fv*>(p.cos + e), sv = *reinterpret_cast<const fv*>(p.sin + e);
+#pragma unroll
+            for (int i = 0; i < N; ++i) c[u][i] = cv[i], sn[u][i] = sv[i];
+          } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) c[u][i] = sn[u][i] = NAN;
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnr; ++u) {
+      float sq = 0.0f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) sq += a[u][i] * a[u][i] + b[u][i] * b[u][i];
+      float wx = 0.0f;
+      if (BWD) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {  // dn, then w = g dn
+          const float na = ya[u][i] * c[u][i] + yb[u][i] * sn[u][i];
+          const float nb = yb[u][i] * c[u][i] - ya[u][i] * sn[u][i];
+          ya[u][i] = na, yb[u][i] = nb;
+          wx += ga[i] * na * a[u][i] + gb[i] * nb * b[u][i];
+        }
+        wx = row_sum(wx, p.G, j, lane);
+      }
+      sq = row_sum(sq, p.G, j, lane);
+      const float r = 1.0f / sqrtf(sq * inv_d + p.eps);
+      float oa[N], ob[N];
+      if constexpr (BWD) {
+        const float k = r * r * inv_d * wx;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          da[i] += ya[u][i] * (a[u][i] * r);
+          db[i] += yb[u][i] * (b[u][i] * r);
+          oa[i] = r * (ga[i] * ya[u][i] - a[u][i] * k);
+          ob[i] = r * (gb[i] * yb[u][i] - b[u][i] * k);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float na = a[u][i] * r * ga[i], nb = b[u][i] * r * gb[i];
+          oa[i] = na * c[u][i] - nb * sn[u][i];
+          ob[i] = nb * c[u][i] + na * sn[u][i];
+        }
+      }
+      if (ok[u]) store<T, HALF>(static_cast<T*>(s.y) + to[u], o0, o1, oa, ob);
+    }
+  }
+  if constexpr (BWD) {
+    if (!p.part) return;
+    // the lanes' shares of dg: element e of chunk j from every slot of every wave
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      red[threadIdx.x * E + i] = on ? da[i] : 0.0f;
+      red[threadIdx.x * E + N + i] = on ? db[i] : 0.0f;
+    }
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < p.D; e += kNT) {
+      const uint32_t jj = e / E, i = e % E;  // chunk, element of its registers
+      float v = 0.0f;
+      for (int w = 0; w < kNT / 64; ++w)
+        for (uint32_t sl = 0; sl < p.HP; ++sl) v += red[(w * 64 + sl * p.G + jj) * E + i];
+      const bool half_turn = HALF && E * jj < p.R;
+      // registers i < N hold the first elements of the pairs
+      const uint32_t d = HALF ? (i < N ? (half_turn ? N * jj : E * jj) + i
+                                       : (half_turn ? p.R / 2 + N * jj : E * jj + N) + i - N)
+                              : E * jj + (i < N ? 2 * i : 2 * (i - N) + 1);
+      p.part[(uint64_t)blockIdx.x * p.D + d] = v;
+    }
+  }
+}
+
+// The same pass for any width up to 256, rotation and alignment: a wave per row,
+// lane e + 64 t the element d = e + 64 t with its pair's partner.
+template <typename T, bool BWD>
+__global__ __launch_bounds__(kNT) void qk_norm_any_kernel(NormParams p, int half) {
+  constexpr int NE = kMaxD / 64;
+  __shared__ float red[BWD ? (kNT / 64) * kMaxD : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int which = blockIdx.x >= p.side[0].blocks;
+  const Side& s = p.side[which];
+  const uint32_t blk = blockIdx.x - (which ? p.side[0].blocks : 0);
+  const float inv_d = 1.0f / (float)p.D;
+  uint32_t mate[NE], pair[NE];
+  float sign[NE], g[NE], gm[NE], dg[NE];
+#pragma unroll
+  for (int t = 0; t < NE; ++t) {
+    const uint32_t d = lane + 64 * t;
+    const bool turns = d < p.R;
+    const bool second = half ? d >= p.R / 2 : (d & 1);
+    pair[t] = half ? (second ? d - p.R / 2 : d) : d / 2;
+    mate[t] = !turns ? d : half ? (second ? d - p.R / 2 : d + p.R / 2) : (d ^ 1u);
+    sign[t] = second ? 1.0f : -1.0f;
+    const bool in = d < p.D;
+    g[t] = s.g && in ? (float)static_cast<const T*>(s.g)[d] : 1.0f;
+    gm[t] = s.g && in ? (float)static_cast<const T*>(s.g)[mate[t]] : 1.0f;
+    dg[t] = 0.0f;
+  }
+  for (uint64_t row = (uint64_t)blk * (kNT / 64) + wave; row < s.rows; row += (uint64_t)s.blocks * (kNT / 64)) {
+    const Where w = where(p, s, (uint32_t)row);
+    const T* x = static_cast<const T*>(s.x) + at(w, s.xs, p.D);
+    const T* dy = BWD ? static_cast<const T*>(s.dy) + at(w, s.ds, p.D) : nullptr;
+    const int64_t tr = p.R ? table_row(p, w) : 0;
+    float v[NE], vm[NE], u[NE], um[NE], c[NE], sn[NE], sq = 0.0f, wx = 0.0f;
+#pragma unroll
+    for (int t = 0; t < NE; ++t) {
+      const uint32_t d = lane + 64 * t;
+      v[t] = vm[t] = u[t] = um[t] = sn[t] = 0.0f;
+      c[t] = 1.0f;
+      if (d < p.D) {
+        v[t] = (float)x[d];
+        vm[t] = (float)x[mate[t]];
+        if (BWD) u[t] = (float)dy[d], um[t] = (float)dy[mate[t]];
+        if (d < p.R) {
+          c[t] = tr >= 0 ? p.cos[tr * (p.R / 2) + pair[t]] : NAN;
+          sn[t] = tr >= 0 ? p.sin[tr * (p.R / 2) + pair[t]] : NAN;
+        }
+      }
+      sq += v[t] * v[t];
+    }
+    float dn[NE];
+#pragma unroll
+    for (int t = 0; t < NE; ++t) {
+      dn[t] = u[t] * c[t] - sign[t] * um[t] * sn[t];
+      wx += g[t] * dn[t] * v[t];
+    }
+#pragma unroll
+    for (int off = 32; off; off >>= 1) {
+      sq += __shfl_xor(sq, off);
+      if (BWD) wx += __shfl_xor(wx, off);
+    }
+    const float r = 1.0f / sqrtf(sq * inv_d + p.eps);
+    T* y = static_cast<T*>(s.y) + at(w, s.ys, p.D);
+#pragma unroll
+    for (int t = 0; t < NE; ++t) {
+      const uint32_t d = lane + 64 * t;
+      float o;
+      if (BWD) {
+        dg[t] += dn[t] * (v[t] * r);
+        o = r * (g[t] * dn[t] - v[t] * (r * r * inv_d * wx));
+      } else {
+        o = v[t] * r * g[t] * c[t] + sign[t] * (vm[t] * r * gm[t]) * sn[t];
+      }
+      if (d < p.D) y[d] = (T)o;
+    }
+  }
+  if constexpr (BWD) {
+    if (!p.part) return;
+#pragma unroll
+    for (int t = 0; t < NE; ++t) red[wave * kMaxD + lane + 64 * t] = dg[t];
+    __syncthreads();
+    for (uint32_t d = threadIdx.x; d < p.D; d += kNT) {
+      float v = 0.0f;
+      for (int w = 0; w < kNT / 64; ++w) v += red[w * kMaxD + d];
+      p.part[(uint64_t)blockIdx.x * p.D + d] = v;
+    }
+  }
+}
+
+// dg[d] = sum over a side's work-groups of part[w][d], in a fixed order: 16 lanes
+// of columns by 64 interleaved rows, then the 64 sums in turn.
+__global__ __launch_bounds__(1024) void qk_norm_gain_kernel(const float* part, float* dgq, float* dgk, uint32_t bq,
+                                                            uint32_t bk, uint32_t D) {
+  __shared__ float red[64][17];
+  const uint32_t col = threadIdx.x & 15, r = threadIdx.x >> 4, d = blockIdx.x * 16 + col;
+  const bool key = blockIdx.y;
+  float* dg = key ? dgk : dgq;
+  if (!dg) return;
+  const float* src = part + (key ? (uint64_t)bq * D : 0);
+  const uint32_t n = key ? bk : bq;
+  float v = 0.0f;
+  if (d < D)
+    for (uint32_t w = r; w < n; w += 64) v += src[(uint64_t)w * D + d];
+  red[r][col] = v;
+  __syncthreads();
+  if (r == 0 && d < D) {
+    for (int i = 1; i < 64; ++i) v += red[i][col];
+    dg[d] = v;
+  }
+}
+
+// work-groups a side's gradient runs on: enough to fill the chip, few enough
+// that their shares of dg stay small
+constexpr uint32_t kGradBlocks = 1024;
+
+bool chunked(const QkNormArgs& a, bool bwd) {
+  const int es = a.bf16 ? 2 : 4, E = 16 / es;
+  if (a.D % E || a.rot % E) return false;
+  auto ok = [&](const void* ptr, const int64_t* st) {
+    return reinterpret_cast<uintptr_t>(ptr) % 16 == 0 && st[0] % E == 0 && st[1] % E == 0 && st[2] % E == 0;
+  };
+  for (int i = 0; i < 2; ++i) {
+    const QkNormSide& s = a.side[i];
+    if (!s.heads) continue;
+    if (!ok(s.x, s.x_strides) || !ok(s.y, s.y_strides) || (bwd && !ok(s.dy, s.dy_strides))) return false;
+    if (s.gain && reinterpret_cast<uintptr_t>(s.gain) % 16) return false;
+  }
+  return !a.rot || (reinterpret_cast<uintptr_t>(a.cos) % 16 == 0 && reinterpret_cast<uintptr_t>(a.sin) % 16 == 0);
+}
+
+struct Plan {
+  bool chunks;
+  uint32_t G, HP, blocks[2];
+};
+Plan plan(const QkNormArgs& a, bool bwd) {
+  Plan r = {};
+  r.chunks = chunked(a, bwd);
+  r.G = r.chunks ? a.D / (a.bf16 ? 8 : 4) : 64;
+  r.HP = 64 / r.G;
+  const int64_t per = r.chunks ? (kNT / 64) * r.HP * kUnr : kNT / 64;
+  for (int i = 0; i < 2; ++i) {
+    const int64_t rows = a.B * a.X * a.L * a.side[i].heads;
+    int64_t n = (rows + per - 1) / per;
+    n = std::min<int64_t>(n, bwd ? kGradBlocks : (int64_t(1) << 22));
+    r.blocks[i] = (uint32_t)n;
+  }
+  return r;
+}
+
+template <typename T>
+void launch(const NormParams& p, const Plan& pl, bool half, bool bwd, hipStream_t s) {
+  const dim3 grid(pl.blocks[0] + pl.blocks[1]);
+  if (!pl.chunks) {
+    if (bwd) qk_norm_any_kernel<T, true><<<grid, kNT, 0, s>>>(p, half);
+    else qk_norm_any_kernel<T, false><<<grid, kNT, 0, s>>>(p, half);
+  } else if (half) {
+    if (bwd) qk_norm_kernel<T, true, true><<<grid, kNT, 0, s>>>(p);
+    else qk_norm_kernel<T, true, false><<<grid, kNT, 0, s>>>(p);
+  } else {
+    if (bwd) qk_norm_kernel<T, false, true><<<grid, kNT, 0, s>>>(p);
+    else qk_norm_kernel<T, false, false><<<grid, kNT, 0, s>>>(p);
+  }
+}
+
+}  // namespace
+
+size_t qk_norm_workspace_bytes(int64_t tokens, int H, int Hkv, int D) {
+  // at most kGradBlocks work-groups of each side, at least four rows in each
+  auto n = [&](int64_t heads) { return std::min<int64_t>(kGradBlocks, (tokens * heads + 3) / 4); };
+  return (size_t)(n(H) + n(Hkv)) * (size_t)D * 4;
+}
+
+int launch_qk_norm(const QkNormArgs& a, bool bwd, float* part, hipStream_t s) {
+  const Plan pl = plan(a, bwd);
+  NormParams p = {};
+  for (int i = 0; i < 2; ++i) {
+    const QkNormSide& in = a.side[i];
+    Side& o = p.side[i];
+    o.x = in.x, o.dy = in.dy, o.y = in.y, o.g = in.gain;
+    for (int k = 0; k < 3; ++k) o.xs[k] = in.x_strides[k], o.ys[k] = in.y_strides[k], o.ds[k] = in.dy_strides[k];
+    o.heads = fast_div(std::max(in.heads, 1));
+    o.rows = (uint32_t)(a.B * a.X * a.L * in.heads);
+    o.blocks = pl.blocks[i];
+  }
+  p.cos = a.cos, p.sin = a.sin, p.pos = a.pos;
+  const bool gains = bwd && (a.side[0].dgain || a.side[1].dgain);
+  p.part = gains ? part : nullptr;
+  p.P = (uint32_t)a.P, p.R = a.rot, p.D = a.D, p.G = pl.G, p.HP = pl.HP;
+  p.L = fast_div((uint32_t)std::max<int64_t>(a.L, 1)), p.X = fast_div((uint32_t)std::max<int64_t>(a.X, 1));
+  p.eps = a.eps;
+  if (pl.blocks[0] + pl.blocks[1] == 0) {
+    // no rows
+  } else if (a.bf16) launch<bf16>(p, pl, a.half, bwd, s);
+  else launch<float>(p, pl, a.half, bwd, s);
+  const int st = last_launch_status();
+  if (st != DSP_OK || !gains) return st;
+  qk_norm_gain_kernel<<<dim3((a.D + 15) / 16, 2), 1024, 0, s>>>(part, a.side[0].dgain, a.side[1].dgain, pl.blocks[0],
+                                                                pl.blocks[1], a.D);
+  return last_launch_status();
+}
+
+}  // namespace dsp
