@@ -365,6 +365,73 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
                          const int64_t* dq_strides, const int64_t* dk_strides, float eps, int dtype, void* stream);
 
 /* ------------------------------------------------------------------------
+ * dsp_attn_relpos -- attention with a learned relative position bias by buckets:
+ *     s_ij = scale * q_i . k_j + bias[bucket(j - i - q_pos)][h],
+ *     o_i = softmax over j (s_i) v,
+ * on the units, heads and layouts of dsp_attn_general (Hkv key/value heads shared
+ * by H / Hkv query heads each, lengths Lq and Lk, any strides, 0 to broadcast keys
+ * and values).
+ * bias:    [n_buckets][H] of dtype.  A value of -1e30 or less (-inf, or the type's
+ *          lowest) takes the keys of its distances out.
+ * buckets: DEVICE int32 [2 * max_dist + 1], the bucket of each distance
+ *          -max_dist .. max_dist (key position - query position); further
+ *          distances take the nearest end's.  An entry outside
+ *          0 .. n_buckets - 1 means no bias.  dsp_relpos_buckets fills the usual
+ *          map.
+ * q_pos:   DEVICE int32 [B], the key index of each sequence's first query (a new
+ *          token's place in a cache), or NULL (0).
+ * kv_len:  DEVICE int32 [B], the keys that each sequence has, 0 .. Lk (clamped),
+ *          or NULL (Lk).  Keys and values past it are never used, whatever they
+ *          hold; the others must be finite.
+ * flags:   DSP_RELPOS_CAUSAL keeps the keys j <= i + q_pos only.
+ * A query without keys (kv_len 0, or none before it) gives o = 0 and lse = -inf.
+ * lse:     fp32 [B * X * H][Lq], the row log-sum-exp of s, or NULL.
+ * dtype:   DSP_BF16 (fp32 scores, softmax and accumulation; probabilities are
+ *          rounded to bf16 for the product with v), D a multiple of 8 up to 128,
+ *          16-byte aligned tensors and strides multiples of 8; or DSP_F32, any D up
+ *          to 128.  max_dist <= 1024, Lq and Lk below 2^30, and 64 rows of k within
+ *          2^31 bytes.
+ * workspace: dsp_attn_relpos_workspace_bytes(...) bytes, 16-byte aligned (0 except
+ *          for a few queries against many keys: there the keys are cut among
+ *          work-groups, whose sums are joined).
+ *
+ * dsp_attn_relpos_bwd -- the gradients dq, dk, dv (strides of q and k) and
+ * dbias [n_buckets][H] of dtype, from the forward's o and lse and from dout (o's
+ * strides).  Deterministic: no sum depends on timing.  Rows of dk and dv past kv_len
+ * are 0, as is dbias where bias masks.  workspace:
+ * dsp_attn_relpos_bwd_workspace_bytes(...) bytes, 16-byte aligned.  dq, dk and dv
+ * may be columns of one buffer; other overlaps are DSP_ERR_ARG, as are broadcast keys.
+ *
+ * dsp_relpos_buckets -- fills buckets[2 * max_dist + 1] in HOST memory: with
+ * n = n_buckets (bidirectional: half of them for each direction, keys after the
+ * query in the second half; otherwise keys after the query share bucket 0),
+ * distances below n / 2 have a bucket each, and the other buckets divide
+ * n / 2 .. max_dist evenly in the logarithm.
+ * Errors: DSP_ERR_NULL, DSP_ERR_SHAPE (sizes < 0 or unsupported, H % Hkv,
+ *   n_buckets < 1), DSP_ERR_DTYPE, DSP_ERR_ALIGN, DSP_ERR_ARG (scale not finite,
+ *   unknown flags, overlapping outputs), DSP_ERR_WORKSPACE, DSP_ERR_HIP.  An empty
+ *   input launches nothing and may come with NULL pointers (the gradient of no
+ *   queries writes 0 into dk, dv and dbias).
+ * ------------------------------------------------------------------------ */
+enum { DSP_RELPOS_CAUSAL = 1 };
+int dsp_relpos_buckets(int32_t* buckets, int max_dist, int n_buckets, int bidirectional);
+size_t dsp_attn_relpos_workspace_bytes(int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D,
+                                       int dtype);
+int dsp_attn_relpos(const void* q, const void* k, const void* v, void* o, float* lse, const void* bias,
+                    const int32_t* buckets, int n_buckets, int max_dist, const int32_t* q_pos,
+                    const int32_t* kv_len, int flags, void* workspace, size_t ws_bytes, int64_t B, int64_t X,
+                    int64_t Lq, int64_t Lk, int H, int Hkv, int D, const int64_t* q_strides,
+                    const int64_t* kv_strides, const int64_t* o_strides, float scale, int dtype, void* stream);
+size_t dsp_attn_relpos_bwd_workspace_bytes(int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D,
+                                           int max_dist, int dtype);
+int dsp_attn_relpos_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                        const float* lse, void* dq, void* dk, void* dv, void* dbias, const void* bias,
+                        const int32_t* buckets, int n_buckets, int max_dist, const int32_t* q_pos,
+                        const int32_t* kv_len, int flags, void* workspace, size_t ws_bytes, int64_t B, int64_t X,
+                        int64_t Lq, int64_t Lk, int H, int Hkv, int D, const int64_t* q_strides,
+                        const int64_t* kv_strides, const int64_t* o_strides, float scale, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
  * dsp_layernorm -- per-row normalisation over C (Eq. 4, 6):
  *   y = (x - mean) / sqrt(var + eps), biased variance, no affine part,
  *   statistics in fp32.

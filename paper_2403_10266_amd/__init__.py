@@ -11,7 +11,7 @@ binding's functions raises.
 Entry points (see ``include/dsp.h`` for the exact contracts):
 ``dsp_switch``, ``dsp_exchange_unpack``, ``dsp_split``, ``dsp_gather``,
 ``dsp_spatial_attn``, ``dsp_temporal_attn``, ``dsp_attn_strided``,
-``dsp_attn_fwd_lse``, ``dsp_attn_bwd``, ``dsp_attn_general``, ``dsp_attn_general_bwd``, ``dsp_qk_norm_rope``, ``dsp_qk_norm_rope_bwd``, ``dsp_layernorm_bwd``, ``dsp_linear_bwd_data``, ``dsp_linear_bwd_weight``,
+``dsp_attn_fwd_lse``, ``dsp_attn_bwd``, ``dsp_attn_general``, ``dsp_attn_general_bwd``, ``dsp_attn_relpos``, ``dsp_attn_relpos_bwd``, ``dsp_relpos_buckets``, ``dsp_qk_norm_rope``, ``dsp_qk_norm_rope_bwd``, ``dsp_layernorm_bwd``, ``dsp_linear_bwd_data``, ``dsp_linear_bwd_weight``,
 ``dsp_layernorm``, ``dsp_linear``, ``dsp_st_block_forward``.
 """
 from __future__ import annotations
@@ -30,6 +30,7 @@ DSP_F32, DSP_BF16 = 0, 1
 DSP_EPI_NONE, DSP_EPI_GELU, DSP_EPI_RESID, DSP_EPI_F32, DSP_EPI_RELU = 0, 1, 2, 3, 4
 DSP_BLOCK_NO_MLP_LN, DSP_BLOCK_ATTN_ONLY, DSP_BLOCK_POST_LN, DSP_BLOCK_RELU = 1, 2, 4, 8
 DSP_ROPE_ADJACENT = 1
+DSP_RELPOS_CAUSAL = 1
 DSP_GRAD_EPI_F32, DSP_GRAD_EPI_BF16, DSP_GRAD_EPI_GELU_BWD, DSP_GRAD_EPI_RELU_BWD = 0, 1, 2, 3
 
 BLOCK_WEIGHT_FIELDS = ("wqkv_s", "bqkv_s", "wo_s", "bo_s", "wqkv_t", "bqkv_t", "wo_t", "bo_t",
@@ -73,6 +74,13 @@ _SIGNATURES = {
     "dsp_attn_bwd_noalloc_max_rows": (_I64, []),
     "dsp_attn_bwd_noalloc": (_I, [_P, _P, _P, _P, _P, _P, _P, _P, _P, _I64, _I64, _I64, _I, _I,
                                   _c.POINTER(_I64), _c.POINTER(_I64), _F, _I, _P]),
+    "dsp_relpos_buckets": (_I, [_P, _I, _I, _I]),
+    "dsp_attn_relpos_workspace_bytes": (_SZ, [_I64] * 4 + [_I] * 4),
+    "dsp_attn_relpos": (_I, [_P] * 7 + [_I, _I, _P, _P, _I, _P, _SZ] + [_I64] * 4 + [_I] * 3
+                        + [_c.POINTER(_I64)] * 3 + [_F, _I, _P]),
+    "dsp_attn_relpos_bwd_workspace_bytes": (_SZ, [_I64] * 4 + [_I] * 5),
+    "dsp_attn_relpos_bwd": (_I, [_P] * 12 + [_I, _I, _P, _P, _I, _P, _SZ] + [_I64] * 4 + [_I] * 3
+                            + [_c.POINTER(_I64)] * 3 + [_F, _I, _P]),
     "dsp_qk_norm_rope": (_I, [_P] * 9 + [_I64, _I, _I, _I64, _I64, _I64, _I, _I, _I] + [_c.POINTER(_I64)] * 4
                          + [_F, _I, _P]),
     "dsp_qk_norm_rope_bwd_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I, _I, _I]),
@@ -636,6 +644,102 @@ def dsp_attn_general_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, dq=None, dk=No
     return dq, dk, dv
 
 
+def dsp_relpos_buckets(max_dist: int, n_buckets: int, bidirectional: bool = True):
+    """The usual map of distances -max_dist .. max_dist to buckets (see dsp.h): int32
+    [2 * max_dist + 1] on the CPU, for `.cuda()` once."""
+    torch = _torch()
+    w = "dsp_relpos_buckets"
+    if max_dist < 0:
+        raise ValueError(f"{w}: max_dist must not be negative")
+    out = torch.empty(2 * max_dist + 1, dtype=torch.int32)
+    _check_status(lib().dsp_relpos_buckets(_ptr(out), max_dist, n_buckets, 1 if bidirectional else 0), w)
+    return out
+
+
+def _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len):
+    torch = _torch()
+    dims = _general_views(w, q, k, v, H, Hkv)
+    _check(w, "bias", bias, dtype=q.dtype, like=q)
+    if bias.dim() != 2 or bias.shape[0] < 1 or bias.shape[1] != H:
+        raise ValueError(f"{w}: bias must be [n_buckets, H = {H}]")
+    _check(w, "buckets", buckets, dtype=torch.int32, like=q)
+    if buckets.dim() != 1 or buckets.numel() % 2 == 0:
+        raise ValueError(f"{w}: buckets must be [2 * max_dist + 1]")
+    for name, t in (("q_pos", q_pos), ("kv_len", kv_len)):
+        if t is not None:
+            _check(w, name, t, dtype=torch.int32, shape=(dims[0],), like=q)
+    return dims
+
+
+def _workspace(w, need, workspace, like):
+    """The given workspace, or a new one of `need` bytes (None where none is needed)."""
+    torch = _torch()
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device) if need else None
+    return _check(w, "workspace", workspace, like=like)
+
+
+def dsp_attn_relpos(q, k, v, H: int, Hkv: int, bias, buckets, causal: bool = False, q_pos=None, kv_len=None, out=None,
+                    lse=None, with_lse: bool = False, scale: float = 0.0, workspace=None, stream=None):
+    """Attention with a learned relative position bias (see dsp.h) over dim 2 of 4-D
+    views q [B, X, Lq, H*D], k and v [B, X, Lk, Hkv*D].  ``bias`` [n_buckets, H] of
+    q's dtype, ``buckets`` int32 [2 * max_dist + 1] (dsp_relpos_buckets), ``q_pos``
+    and ``kv_len`` int32 [B]: the key index of the first query and the keys of each
+    sequence (default 0 and Lk).  Returns out [B, X, Lq, H*D] (and lse
+    [B, X, H, Lq] fp32 when with_lse or lse is given)."""
+    torch = _torch()
+    w = "dsp_attn_relpos"
+    B, X, Lq, Lk, C, D = _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len)
+    with _on_device(q, stream) as s:
+        if out is None:
+            out = torch.empty((B, X, Lq, C), dtype=q.dtype, device=q.device)
+        _like_view(w, out, q, "out")
+        if with_lse and lse is None:
+            lse = torch.empty((B, X, H, Lq), dtype=torch.float32, device=q.device)
+        if lse is not None:
+            _check(w, "lse", lse, dtype=torch.float32, numel=B * X * H * Lq, like=q)
+        dt = _dtype_code(q)
+        ws = _workspace(w, lib().dsp_attn_relpos_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, dt), workspace, q)
+        _check_status(lib().dsp_attn_relpos(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(bias), _ptr(buckets), bias.shape[0],
+            buckets.numel() // 2, _ptr(q_pos), _ptr(kv_len), DSP_RELPOS_CAUSAL if causal else 0, _ptr(ws),
+            _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv, D, _st3(q), _st3(k), _st3(out), float(scale),
+            dt, s), w)
+    return (out, lse) if lse is not None else out
+
+
+def dsp_attn_relpos_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, bias, buckets, causal: bool = False, q_pos=None,
+                        kv_len=None, dq=None, dk=None, dv=None, dbias=None, scale: float = 0.0, workspace=None,
+                        stream=None):
+    """Gradients of dsp_attn_relpos, given its o and lse and the gradient dout (o's
+    strides): (dq like q, dk and dv like k and v, dbias like bias)."""
+    torch = _torch()
+    w = "dsp_attn_relpos_bwd"
+    B, X, Lq, Lk, C, D = _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len)
+    _like_view(w, o, q, "o")
+    _like_view(w, dout, q, "dout")
+    if dout.stride() != o.stride():
+        raise ValueError(f"{w}: dout must have the strides of o")
+    _check(w, "lse", lse, dtype=torch.float32, numel=B * X * H * Lq, like=q)
+    with _on_device(q, stream) as s:
+        dq = torch.empty_like(q) if dq is None else dq
+        dk = torch.empty_like(k) if dk is None else dk
+        dv = torch.empty_like(v) if dv is None else dv
+        _check(w, "dq", dq, dtype=q.dtype, shape=q.shape, strides=q.stride(), contiguous=False, like=q)
+        _check(w, "dk", dk, dtype=q.dtype, shape=k.shape, strides=k.stride(), contiguous=False, like=q)
+        _check(w, "dv", dv, dtype=q.dtype, shape=k.shape, strides=k.stride(), contiguous=False, like=q)
+        dbias = torch.empty_like(bias) if dbias is None else dbias
+        _check(w, "dbias", dbias, dtype=q.dtype, shape=bias.shape, like=q)
+        dt, M = _dtype_code(q), buckets.numel() // 2
+        ws = _workspace(w, lib().dsp_attn_relpos_bwd_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, M, dt), workspace, q)
+        _check_status(lib().dsp_attn_relpos_bwd(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias),
+            _ptr(bias), _ptr(buckets), bias.shape[0], M, _ptr(q_pos), _ptr(kv_len),
+            DSP_RELPOS_CAUSAL if causal else 0, _ptr(ws), _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv,
+            D, _st3(q), _st3(k), _st3(o), float(scale), dt, s), w)
+    return dq, dk, dv, dbias
+
+
 def _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos):
     """Checks what dsp_qk_norm_rope and its gradient share; returns (B, X, L, D, P, rot)."""
     torch = _torch()
@@ -724,10 +828,7 @@ def dsp_qk_norm_rope_bwd(q, k, dyq, dyk, H: int, Hkv: int, gq=None, gk=None, cos
             dg.append(torch.empty(D, dtype=torch.float32, device=like.device) if gains and t is not None else None)
         dq, dk = outs
         need = lib().dsp_qk_norm_rope_bwd_workspace_bytes(B, X, L, H, Hkv, D) if gains else 0
-        if workspace is None and need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=like.device)
-        if workspace is not None:
-            _check(w, "workspace", workspace, like=like)
+        workspace = _workspace(w, need, workspace, like)
         st = [_st3(t) if t is not None else None for t in (q, k, dyq, dyk, dq, dk)]
         _check_status(lib().dsp_qk_norm_rope_bwd(
             _ptr(q), _ptr(k), _ptr(dyq), _ptr(dyk), _ptr(dq), _ptr(dk), _ptr(dg[0]), _ptr(dg[1]), _ptr(gq), _ptr(gk),

@@ -304,14 +304,16 @@ bool spans_ok(int64_t B, int64_t X, int64_t L, const int64_t* st) {
   return true;
 }
 
-// Two row tensors of the same (B, X, L) grid share no element: their spans are
-// apart, or they have one layout and lie in different columns of its rows.
-bool rows_apart(const void* a, const int64_t* sa, int64_t wa, const void* b, const int64_t* sb, int64_t wb, int64_t B,
-                int64_t X, int64_t L, int es) {
-  auto span = [&](const int64_t* st, int64_t w) {
+// Two row tensors of (B, X, La) and (B, X, Lb) rows share no element: their spans
+// are apart, or they have one grid and layout and lie in different columns of its rows.
+bool rows_apart(const void* a, const int64_t* sa, int64_t wa, int64_t La, const void* b, const int64_t* sb, int64_t wb,
+                int64_t Lb, int64_t B, int64_t X, int es) {
+  auto span = [&](const int64_t* st, int64_t w, int64_t L) {
     return (size_t)((B - 1) * st[0] + (X - 1) * st[1] + (L - 1) * st[2] + w) * es;
   };
-  if (!wa || !wb || !overlap(a, span(sa, wa), b, span(sb, wb))) return true;
+  if (!wa || !wb || !La || !Lb || !overlap(a, span(sa, wa, La), b, span(sb, wb, Lb))) return true;
+  if (La != Lb) return false;
+  const int64_t L = La;
   const int64_t ext[3] = {B, X, L};
   int64_t pitch = INT64_MAX;
   for (int i = 0; i < 3; ++i) {
@@ -379,10 +381,10 @@ int qk_norm_impl(QkNormArgs& a, bool bwd, int flags, int H, int Hkv, const int64
       const int64_t ow = (int64_t)heads[j] * a.D;
       auto clear = [&](const void* ptr, const int64_t* st) {
         return (i == j && same_rows(d.y, d.y_strides, ptr, st, a.B, a.X, a.L)) ||
-               rows_apart(d.y, d.y_strides, w, ptr, st, ow, a.B, a.X, a.L, es);
+               rows_apart(d.y, d.y_strides, w, a.L, ptr, st, ow, a.L, a.B, a.X, es);
       };
       if (!clear(o.x, o.x_strides) || (bwd && !clear(o.dy, o.dy_strides))) return DSP_ERR_ARG;
-      if (i != j && !rows_apart(d.y, d.y_strides, w, o.y, o.y_strides, ow, a.B, a.X, a.L, es)) return DSP_ERR_ARG;
+      if (i != j && !rows_apart(d.y, d.y_strides, w, a.L, o.y, o.y_strides, ow, a.L, a.B, a.X, es)) return DSP_ERR_ARG;
     }
   }
   if (gains) {
@@ -392,6 +394,102 @@ int qk_norm_impl(QkNormArgs& a, bool bwd, int flags, int H, int Hkv, const int64
   a.half = !(flags & DSP_ROPE_ADJACENT);
   a.bf16 = dtype == DSP_BF16;
   return launch_qk_norm(a, bwd, static_cast<float*>(workspace), s);
+}
+
+// Sizes of dsp_attn_relpos that its workspace depends on, checked.
+int relpos_sizes(RelposArgs& a, int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D, int max_dist,
+                 int dtype) {
+  constexpr int64_t kMaxL = int64_t(1) << 30;
+  if (!valid_dtype(dtype)) return DSP_ERR_DTYPE;
+  if (B < 0 || X < 0 || Lq < 0 || Lk < 0 || H < 1 || Hkv < 1 || H % Hkv || D < 1 || D > kRelposMaxD) return DSP_ERR_SHAPE;
+  if (dtype == DSP_BF16 && D % 8) return DSP_ERR_SHAPE;
+  if (Lq >= kMaxL || Lk >= kMaxL || max_dist < 0 || max_dist > kRelposMaxDist) return DSP_ERR_SHAPE;
+  int64_t units, n;
+  if (!mul_ok(B, X, &units) || units >= kMaxL || !mul_ok(units, H, &n) || n >= (int64_t(1) << 31) || !mul_ok(n, Lq, &n) ||
+      n > (int64_t(1) << 48))
+    return DSP_ERR_SHAPE;
+  a.B = B, a.X = X, a.Lq = Lq, a.Lk = Lk, a.H = H, a.Hkv = Hkv, a.D = D, a.max_dist = max_dist;
+  a.bf16 = dtype == DSP_BF16;
+  return DSP_OK;
+}
+
+int relpos_impl(RelposArgs& a, bool bwd, int flags, void* workspace, size_t ws_bytes, const int64_t* q_st,
+                const int64_t* kv_st, const int64_t* o_st, float scale, int dtype, void* stream) {
+  const int es = elem_size(dtype);
+  if (!q_st || !kv_st || !o_st) return DSP_ERR_NULL;
+  if (a.n_buckets < 1) return DSP_ERR_SHAPE;
+  if (isnan(scale) || isinf(scale) || (flags & ~DSP_RELPOS_CAUSAL)) return DSP_ERR_ARG;
+  for (int i = 0; i < 3; ++i)
+    if (q_st[i] < 0 || kv_st[i] < 0 || o_st[i] < 0) return DSP_ERR_SHAPE;
+  const bool no_units = a.B == 0 || a.X == 0;
+  const bool no_q = no_units || a.Lq == 0, no_k = no_units || a.Lk == 0;
+  const bool nothing = bwd ? no_q && no_k && !a.dbias : no_q;
+  if (nothing) return DSP_OK;
+  // what each tensor's rows are there for
+  const void* q_side[] = {a.q, bwd ? a.dout : a.q, bwd ? a.o : a.q, bwd ? a.dq : a.o};
+  const void* k_side[] = {a.k, a.v, bwd ? a.dk : a.k, bwd ? a.dv : a.v};
+  for (const void* p : q_side)
+    if (!no_q && !p) return DSP_ERR_NULL;
+  for (const void* p : k_side)
+    if (!no_k && !p) return DSP_ERR_NULL;
+  if (!a.bias || !a.buckets || (bwd && (!a.dbias || (!no_q && !a.lse)))) return DSP_ERR_NULL;
+  if (!aligned(a.bias, es) || !aligned(a.buckets, 4) || !aligned(a.q_pos, 4) || !aligned(a.kv_len, 4) ||
+      !aligned(a.lse, 4) || !aligned(a.dbias, es))
+    return DSP_ERR_ALIGN;
+  const int64_t wq = (int64_t)a.H * a.D, wk = (int64_t)a.Hkv * a.D;
+  bool vec = a.D % (16 / es) == 0;
+  auto side = [&](const void* const (&side)[4], int64_t L, const int64_t* st) {
+    for (const void* p : side) {
+      if (!aligned(p, es)) return false;
+      vec = vec && aligned(p, 16);
+    }
+    for (int i = 0; i < 3; ++i) vec = vec && st[i] % (16 / es) == 0;
+    return true;
+  };
+  if (!side(q_side, a.Lq, q_st) || !side(k_side, a.Lk, kv_st) || !side(q_side, a.Lq, o_st)) return DSP_ERR_ALIGN;
+  if (dtype == DSP_BF16 && !vec) return DSP_ERR_ALIGN;
+  if (!no_q && (!spans_ok(a.B, a.X, a.Lq, q_st) || !spans_ok(a.B, a.X, a.Lq, o_st))) return DSP_ERR_SHAPE;
+  if (!no_k && !spans_ok(a.B, a.X, a.Lk, kv_st)) return DSP_ERR_SHAPE;
+  for (int i = 0; i < 3; ++i) a.q_strides[i] = q_st[i], a.kv_strides[i] = kv_st[i], a.o_strides[i] = o_st[i];
+  // the stride of a single row is never used as one; the kernels read whole rows by it
+  if (a.Lq <= 1) a.q_strides[2] = a.o_strides[2] = wq;
+  if (a.Lk <= 1) a.kv_strides[2] = wk;
+  const int64_t far = (int64_t(1) << 31) / 64 / es;   // 64 rows lie within 2^31 bytes
+  if (a.kv_strides[2] >= far || (bwd && (a.q_strides[2] >= far || a.o_strides[2] >= far))) return DSP_ERR_SHAPE;
+  auto disjoint = [&](int64_t L, const int64_t* st, int64_t w) { return rows_disjoint(a.B, a.X, L, st, w); };
+  const int64_t B = a.B, X = a.X;
+  auto apart = [&](const void* p, const int64_t* sp, int64_t wp, int64_t Lp, const void* r, const int64_t* sr,
+                   int64_t wr, int64_t Lr) { return rows_apart(p, sp, wp, Lp, r, sr, wr, Lr, B, X, es); };
+  const int64_t Lq = no_q ? 0 : a.Lq, Lk = no_k ? 0 : a.Lk;
+  const int64_t *sq = a.q_strides, *sk = a.kv_strides, *so = a.o_strides;
+  if (!bwd) {
+    if (!disjoint(a.Lq, so, wq)) return DSP_ERR_ARG;
+    if (!apart(a.o, so, wq, Lq, a.q, sq, wq, Lq) || !apart(a.o, so, wq, Lq, a.k, sk, wk, Lk) ||
+        !apart(a.o, so, wq, Lq, a.v, sk, wk, Lk))
+      return DSP_ERR_ARG;
+  } else {
+    if ((!no_q && !disjoint(a.Lq, sq, wq)) || (!no_k && !disjoint(a.Lk, sk, wk))) return DSP_ERR_ARG;
+    struct Rows { const void* p; const int64_t* st; int64_t w, L; };
+    const Rows in[] = {{a.q, sq, wq, Lq}, {a.k, sk, wk, Lk}, {a.v, sk, wk, Lk}, {a.o, so, wq, Lq}, {a.dout, so, wq, Lq}};
+    const Rows out[] = {{a.dq, sq, wq, Lq}, {a.dk, sk, wk, Lk}, {a.dv, sk, wk, Lk}};
+    for (int i = 0; i < 3; ++i) {
+      for (const Rows& r : in)
+        if (!apart(out[i].p, out[i].st, out[i].w, out[i].L, r.p, r.st, r.w, r.L)) return DSP_ERR_ARG;
+      for (int j = 0; j < i; ++j)
+        if (!apart(out[i].p, out[i].st, out[i].w, out[i].L, out[j].p, out[j].st, out[j].w, out[j].L)) return DSP_ERR_ARG;
+    }
+    if (overlap(a.dbias, (size_t)a.n_buckets * a.H * es, a.bias, (size_t)a.n_buckets * a.H * es)) return DSP_ERR_ARG;
+  }
+  const size_t need = bwd ? attn_relpos_bwd_workspace_bytes(a) : attn_relpos_workspace_bytes(a);
+  if (need && (!workspace || ws_bytes < need || !aligned(workspace, 16))) return DSP_ERR_WORKSPACE;
+  a.workspace = static_cast<float*>(workspace);
+  a.scale = scale > 0.0f ? scale : (float)(1.0 / sqrt((double)a.D));
+  a.causal = flags & DSP_RELPOS_CAUSAL;
+  a.vec = vec;
+  if (no_q) a.Lq = 0;
+  if (no_k) a.Lk = 0;
+  hipStream_t s = as_stream(stream);
+  return bwd ? launch_attn_relpos_bwd(a, s) : launch_attn_relpos(a, s);
 }
 
 // pre (GELU/ReLU epilogue, may be null): also receives the pre-activation.
@@ -777,6 +875,65 @@ int dsp_attn_general_bwd(const void* q, const void* k, const void* v, const void
                          void* stream) {
   return attn_bwd_general_impl(q, k, v, o, dout, lse, dq, dk, dv, delta, B, X, Lq, Lk, H, Hkv, D, q_strides,
                                kv_strides, o_strides, scale, dtype, stream);
+}
+
+int dsp_relpos_buckets(int32_t* buckets, int max_dist, int n_buckets, int bidirectional) {
+  if (!buckets) return DSP_ERR_NULL;
+  if (max_dist < 0 || max_dist > kRelposMaxDist || n_buckets < (bidirectional ? 2 : 1)) return DSP_ERR_SHAPE;
+  const int half = bidirectional ? n_buckets / 2 : n_buckets, near = half / 2;
+  for (int d = -max_dist; d <= max_dist; ++d) {
+    int n = bidirectional ? abs(d) : d < 0 ? -d : 0;
+    if (n >= near && near > 0 && max_dist > near) {
+      // steps of equal ratio; the margin keeps distances on a step's border in it
+      const double t = log((double)n / near) / log((double)max_dist / near) * (half - near);
+      const int step = (int)floor(t + 1e-9);
+      n = near + (step < half - near ? step : half - near - 1);
+    } else if (n >= near) {
+      n = n < half ? n : half - 1;
+    }
+    buckets[d + max_dist] = (bidirectional && d > 0 ? half : 0) + n;
+  }
+  return DSP_OK;
+}
+
+size_t dsp_attn_relpos_workspace_bytes(int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D,
+                                       int dtype) {
+  RelposArgs a = {};
+  if (relpos_sizes(a, B, X, Lq, Lk, H, Hkv, D, 0, dtype) != DSP_OK || B == 0 || X == 0 || Lq == 0) return 0;
+  return attn_relpos_workspace_bytes(a);
+}
+
+int dsp_attn_relpos(const void* q, const void* k, const void* v, void* o, float* lse, const void* bias,
+                    const int32_t* buckets, int n_buckets, int max_dist, const int32_t* q_pos,
+                    const int32_t* kv_len, int flags, void* workspace, size_t ws_bytes, int64_t B, int64_t X,
+                    int64_t Lq, int64_t Lk, int H, int Hkv, int D, const int64_t* q_strides,
+                    const int64_t* kv_strides, const int64_t* o_strides, float scale, int dtype, void* stream) {
+  RelposArgs a = {};
+  if (int st = relpos_sizes(a, B, X, Lq, Lk, H, Hkv, D, max_dist, dtype)) return st;
+  a.q = q, a.k = k, a.v = v, a.o = o, a.lse = lse;
+  a.bias = bias, a.buckets = buckets, a.n_buckets = n_buckets, a.q_pos = q_pos, a.kv_len = kv_len;
+  return relpos_impl(a, false, flags, workspace, ws_bytes, q_strides, kv_strides, o_strides, scale, dtype, stream);
+}
+
+size_t dsp_attn_relpos_bwd_workspace_bytes(int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D,
+                                           int max_dist, int dtype) {
+  RelposArgs a = {};
+  if (relpos_sizes(a, B, X, Lq, Lk, H, Hkv, D, max_dist, dtype) != DSP_OK) return 0;
+  return attn_relpos_bwd_workspace_bytes(a);
+}
+
+int dsp_attn_relpos_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout,
+                        const float* lse, void* dq, void* dk, void* dv, void* dbias, const void* bias,
+                        const int32_t* buckets, int n_buckets, int max_dist, const int32_t* q_pos,
+                        const int32_t* kv_len, int flags, void* workspace, size_t ws_bytes, int64_t B, int64_t X,
+                        int64_t Lq, int64_t Lk, int H, int Hkv, int D, const int64_t* q_strides,
+                        const int64_t* kv_strides, const int64_t* o_strides, float scale, int dtype, void* stream) {
+  RelposArgs a = {};
+  if (int st = relpos_sizes(a, B, X, Lq, Lk, H, Hkv, D, max_dist, dtype)) return st;
+  a.q = q, a.k = k, a.v = v, a.o = const_cast<void*>(o), a.lse = const_cast<float*>(lse);
+  a.dout = dout, a.dq = dq, a.dk = dk, a.dv = dv, a.dbias = dbias;
+  a.bias = bias, a.buckets = buckets, a.n_buckets = n_buckets, a.q_pos = q_pos, a.kv_len = kv_len;
+  return relpos_impl(a, true, flags, workspace, ws_bytes, q_strides, kv_strides, o_strides, scale, dtype, stream);
 }
 
 int dsp_qk_norm_rope(const void* q, const void* k, void* yq, void* yk, const void* gq, const void* gk,

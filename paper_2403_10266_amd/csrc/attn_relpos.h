@@ -1,0 +1,314 @@
+// Pieces shared by the forward and the gradient of attention with a relative
+// position bias (not installed).
+//
+// Both types run on 32 x 32 matrix instructions whose accumulator gives lane
+// (n + 32 g) column n, rows 8 (r / 4) + 4 g + r % 4 for its registers r = 0 .. 15:
+// bf16 on 32x32x16, fp32 on 32x32x2.  Tensors sit row-major in LDS.
+//  * Row products (scores): A and B fragments are 16 bytes of a row, lane (n + 32 g)
+//    holding row n, bytes 32 s + 16 g .. + 15 of step s.  A contraction may take its
+//    terms in any order that both sides share, so in fp32 the four elements of a
+//    fragment are four instructions.
+//  * Column products (P V and the gradients'): the A operand is the tensor's
+//    transpose, the B operand the accumulator of a row product as it stands (rounded
+//    to bf16 for bf16), again in the row order that both sides share.
+#pragma once
+
+#include <math.h>
+
+#include "attn_bf16_common.h"
+#include "dsp_internal.h"
+
+namespace dsp {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kMasked = -1e30f;   // a bias this low takes its keys out
+
+template <typename T>
+struct Mx;
+template <>
+struct Mx<bf16> {
+  static constexpr int E = 8;       // elements of 16 bytes
+  typedef bf16x8 frag;
+  static __device__ __forceinline__ floatx16 mma(frag a, frag b, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mx<float> {
+  static constexpr int E = 4;
+  typedef floatx4 frag;
+  static __device__ __forceinline__ floatx16 mma(frag a, frag b, floatx16 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+
+// Head widths are rounded up to a class DC; columns D .. are zero in LDS.
+template <typename T, int DC>
+struct Geo {
+  static constexpr int E = Mx<T>::E;
+  static constexpr int NS = DC / (2 * E);              // steps of a row product
+  static constexpr bool SLAB = DC % 32 != 0;           // bf16: last 16 columns on 16x16x32
+  static constexpr int NT = DC / 32;                   // 32-column tiles of a column product
+  static constexpr int P = DC + E;                     // LDS row pitch: an odd number of 16 bytes
+  static constexpr int CHM = DC / E;                   // 16-byte chunks of a row, at most
+  static_assert(DC % 16 == 0 && (!SLAB || E == 8), "class");
+};
+
+// A B operand of a column product made of a 32 x 32 accumulator
+template <typename T>
+struct ColB;
+template <>
+struct ColB<bf16> {
+  bf16x8 v[2];
+  __device__ __forceinline__ void set(int r, float x) { v[r / 8][r % 8] = (bf16)x; }
+};
+template <>
+struct ColB<float> {
+  floatx16 v;
+  __device__ __forceinline__ void set(int r, float x) { v[r] = x; }
+};
+
+// acc[col][n] += sum over the 32 rows of t from row0 of t[row][col0 + col] b[row][n]
+__device__ __forceinline__ floatx16 col_mma(const bf16* t, int pitch, int row0, int col0, int lane,
+                                            const ColB<bf16>& b, floatx16 acc) {
+  const int j16 = lane & 15, g = lane >> 5, mbase = 16 * ((lane >> 4) & 1);
+#pragma unroll
+  for (int kk = 0; kk < 2; ++kk) {
+    const int row = row0 + 16 * kk + 4 * g + (j16 >> 2);
+    const int col = col0 + mbase + 4 * (j16 & 3);
+    const shortx4 lo = lds_read_tr(t + row * pitch + col);
+    const shortx4 hi = lds_read_tr(t + (row + 8) * pitch + col);
+    const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b.v[kk], acc, 0, 0, 0);
+  }
+  return acc;
+}
+__device__ __forceinline__ floatx16 col_mma(const float* t, int pitch, int row0, int col0, int lane,
+                                            const ColB<float>& b, floatx16 acc) {
+  const int l32 = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(t[(row0 + 8 * (r / 4) + 4 * g + r % 4) * pitch + col0 + l32], b.v[r],
+                                               acc, 0, 0, 0);
+  return acc;
+}
+
+// The last 16 columns (col0 ..) on 16x16x32: accumulator h holds columns col0 +
+// 4 (lane / 16) + r of n = 16 h + lane % 16.  One permlane16 swap of the two 16-row
+// halves of b gives the B operands, whose row order the A operand shares.
+__device__ __forceinline__ void slab_mma(const bf16* t, int pitch, int row0, int col0, int lane,
+                                         const ColB<bf16>& b, floatx4 (&acc)[2]) {
+  const int j16 = lane & 15, c = lane >> 4;
+  const int row = row0 + ((c & 1) ? 16 : 0) + ((c & 2) ? 4 : 0) + (j16 >> 2);
+  const int col = col0 + 4 * (j16 & 3);
+  const shortx4 lo = lds_read_tr(t + row * pitch + col);
+  const shortx4 hi = lds_read_tr(t + (row + 8) * pitch + col);
+  const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  const u32x4 x = __builtin_bit_cast(u32x4, b.v[0]), y = __builtin_bit_cast(u32x4, b.v[1]);
+  u32x4 b0, b1;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x[w], y[w], false, false);
+    b0[w] = r[0];
+    b1[w] = r[1];
+  }
+  acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b0), acc[0], 0, 0, 0);
+  acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b1), acc[1], 0, 0, 0);
+}
+
+// The accumulators of a column product for one 32-row block: its tiles and slab.
+template <typename T, int DC>
+struct ColAcc {
+  using G = Geo<T, DC>;
+  floatx16 t[G::NT > 0 ? G::NT : 1];
+  floatx4 s[2];
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < G::NT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) t[i][r] = 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[h][r] = 0.0f;
+  }
+  __device__ __forceinline__ void add(const T* lds, int row0, int lane, const ColB<T>& b) {
+#pragma unroll
+    for (int i = 0; i < G::NT; ++i) t[i] = col_mma(lds, G::P, row0, 32 * i, lane, b, t[i]);
+    if constexpr (G::SLAB) slab_mma(lds, G::P, row0, 32 * G::NT, lane, b, s);
+  }
+  // times a factor that each lane holds for its own column n = lane % 32
+  __device__ __forceinline__ void scale(float f, int lane) {
+#pragma unroll
+    for (int i = 0; i < G::NT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) t[i][r] *= f;
+    if constexpr (G::SLAB) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float fh = __shfl(f, 16 * h + (lane & 15));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[h][r] *= fh;
+      }
+    }
+  }
+};
+
+// Stores four consecutive elements of a row from column d0, those below D.
+__device__ __forceinline__ void store4(bf16* row, int d0, int D, bool, float a, float b, float c, float d) {
+  if (d0 >= D) return;   // D is a multiple of 8
+  const bf16x2 lo = {(bf16)a, (bf16)b}, hi = {(bf16)c, (bf16)d};
+  uint2 w;
+  w.x = __builtin_bit_cast(uint32_t, lo);
+  w.y = __builtin_bit_cast(uint32_t, hi);
+  *reinterpret_cast<uint2*>(row + d0) = w;
+}
+__device__ __forceinline__ void store4(float* row, int d0, int D, bool vec, float a, float b, float c, float d) {
+  if (vec) {
+    if (d0 < D) *reinterpret_cast<floatx4*>(row + d0) = floatx4{a, b, c, d};
+    return;
+  }
+  if (d0 < D) row[d0] = a;
+  if (d0 + 1 < D) row[d0 + 1] = b;
+  if (d0 + 2 < D) row[d0 + 2] = c;
+  if (d0 + 3 < D) row[d0 + 3] = d;
+}
+
+// Writes the rows of a ColAcc: `row_of(n)` gives column n's row, or null.
+template <typename T, int DC, typename F>
+__device__ __forceinline__ void store_rows(const ColAcc<T, DC>& a, int lane, int D, bool vec, F row_of) {
+  using G = Geo<T, DC>;
+  const int g = lane >> 5;
+  auto* row = row_of(lane & 31);
+  if (row) {
+#pragma unroll
+    for (int i = 0; i < G::NT; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        store4(row, 32 * i + 8 * q + 4 * g, D, vec, a.t[i][4 * q], a.t[i][4 * q + 1], a.t[i][4 * q + 2],
+               a.t[i][4 * q + 3]);
+  }
+  if constexpr (G::SLAB) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      auto* rs = row_of(16 * h + (lane & 15));
+      if (rs) store4(rs, 32 * G::NT + 4 * (lane >> 4), D, vec, a.s[h][0], a.s[h][1], a.s[h][2], a.s[h][3]);
+    }
+  }
+}
+
+// The fragments of one row in registers, columns D .. as 0; row null: all 0.
+template <typename T, int DC>
+__device__ __forceinline__ void row_frags(const T* row, int g, int D, bool vec,
+                                          typename Mx<T>::frag (&f)[Geo<T, DC>::NS]) {
+  constexpr int E = Mx<T>::E;
+#pragma unroll
+  for (int s = 0; s < Geo<T, DC>::NS; ++s) {
+    const int d = 2 * E * s + E * g;
+#pragma unroll
+    for (int e = 0; e < E; ++e) f[s][e] = (T)0.0f;
+    if (!row) continue;
+    if (vec) {
+      if (d < D) f[s] = *reinterpret_cast<const typename Mx<T>::frag*>(row + d);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (d + e < D) f[s][e] = row[d + e];
+    }
+  }
+}
+
+// A tile of up to R rows of one tensor on its way from memory to LDS: NT threads,
+// 16-byte chunks, rows past `rows` and columns past D as 0 (the columns are cleared
+// once, by clear_pad).  vec: whole chunks at 16-byte offsets; otherwise (fp32) an
+// element at a time.
+template <typename T, int DC, int R, int NT>
+struct Tile {
+  using G = Geo<T, DC>;
+  static constexpr int N = (R * G::CHM + NT - 1) / NT;
+  u32x4 pre[N];
+
+  // where this thread's chunks lie: byte offset in the tensor's rows, element offset in LDS
+  struct Map {
+    uint32_t at[N];
+    int to[N];
+    uint32_t n;  // chunks of a full tile
+  };
+  static __device__ __forceinline__ Map map(int D, uint32_t row_bytes) {
+    Map m;
+    const uint32_t ch = (uint32_t)(D + G::E - 1) / G::E;
+    m.n = R * ch;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t c = threadIdx.x + i * NT;
+      const uint32_t row = c / ch, col = c - row * ch;
+      m.at[i] = row * row_bytes + col * 16u;
+      m.to[i] = (int)(row * G::P + col * G::E);
+    }
+    return m;
+  }
+  __device__ __forceinline__ void fetch(const Map& m, const T* base, uint32_t rows, uint32_t row_bytes, int D,
+                                        bool vec) {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, rows * row_bytes);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (threadIdx.x + i * NT >= m.n) continue;
+      if (sizeof(T) == 2 || vec) {
+        pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, m.at[i], 0, 0);
+      } else {
+        const int col = m.to[i] % G::P;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          pre[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, col + e < D ? m.at[i] + 4u * e : 0xFFFFFFF0u, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void stash(const Map& m, T* lds) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (threadIdx.x + i * NT < m.n) *reinterpret_cast<u32x4*>(lds + m.to[i]) = pre[i];
+  }
+};
+// zero in columns D .. P - 1 of `rows` LDS rows (fp32: past the chunk that holds D - 1)
+template <typename T, int DC>
+__device__ __forceinline__ void clear_pad(T* lds, int rows, int D, int nt) {
+  using G = Geo<T, DC>;
+  const int d0 = (D + G::E - 1) / G::E * G::E, w = G::P - d0;
+  for (int e = threadIdx.x; e < rows * w; e += nt) lds[e / w * G::P + d0 + e % w] = (T)0.0f;
+}
+
+struct BiasArgs {
+  const void* bias;        // [n_buckets][H]
+  const int32_t* buckets;  // [2 M + 1]
+  int32_t M, nb;
+};
+// the bias of a distance for head h in the exp2 domain
+template <typename T>
+__device__ __forceinline__ float bias_at(const BiasArgs& b, uint32_t H, uint32_t h, int32_t d) {
+  d = d < -b.M ? -b.M : d > b.M ? b.M : d;
+  const int32_t k = b.buckets[d + b.M];
+  const float v = (uint32_t)k < (uint32_t)b.nb ? (float)static_cast<const T*>(b.bias)[(int64_t)k * H + h] : 0.0f;
+  return v <= kMasked ? -INFINITY : v * kLog2e;
+}
+// A 32 x 32 block of scores whose keys start d0 positions after its queries holds the
+// distances d0 - 31 .. d0 + 31.  Where they all lie at or past one end of the table
+// the bias is one value; the other blocks' distances lie within M + kEdge.
+constexpr int kEdge = 62;
+// q_pos and kv_len come from the device: kept where differences cannot overflow
+__device__ __forceinline__ int32_t position(const int32_t* q_pos, uint32_t b) {
+  if (!q_pos) return 0;
+  const int32_t v = q_pos[b];
+  return v < -(1 << 30) ? -(1 << 30) : v > (1 << 30) ? (1 << 30) : v;
+}
+__device__ __forceinline__ uint32_t length(const int32_t* kv_len, uint32_t b, uint32_t Lk) {
+  if (!kv_len) return Lk;
+  const int32_t v = kv_len[b];
+  return v < 0 ? 0u : (uint32_t)v < Lk ? (uint32_t)v : Lk;
+}
+
+}  // namespace
+}  // namespace dsp

@@ -91,6 +91,38 @@ constexpr int kShortAttnMaxL = 128;
 bool attn_bf16_short_fits(const AttnArgs& a);
 int launch_attn_bf16_short(const AttnArgs& a, hipStream_t s);
 
+// Attention with a relative position bias (attn_relpos.hip) and its gradient
+// (attn_relpos_bwd.hip).  Layouts as in AttnArgs; workspace: fp32, the sizes below.
+struct RelposArgs {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;
+  const void* bias;        // [n_buckets][H]
+  const int32_t* buckets;  // [2 max_dist + 1]
+  const int32_t* q_pos;    // [B] or null
+  const int32_t* kv_len;   // [B] or null
+  float* workspace;
+  int64_t B, X, Lq, Lk;
+  int H, Hkv, D, n_buckets, max_dist;
+  int64_t q_strides[3], kv_strides[3], o_strides[3];
+  float scale;
+  bool causal, bf16;
+  bool vec;                // every row of every tensor starts on 16 bytes, D whole 16-byte chunks
+  // gradient
+  const void* dout;
+  void* dq;
+  void* dk;
+  void* dv;
+  void* dbias;
+};
+constexpr int kRelposMaxD = 128, kRelposMaxDist = 1024;
+size_t attn_relpos_workspace_bytes(const RelposArgs& a);
+int launch_attn_relpos(const RelposArgs& a, hipStream_t s);
+size_t attn_relpos_bwd_workspace_bytes(const RelposArgs& a);
+int launch_attn_relpos_bwd(const RelposArgs& a, hipStream_t s);
+
 // Norm of queries and keys for each head with the position rotation, and its
 // gradient (qk_norm.hip).  Row (b, x, l, head) of x (and dy, y) sits at
 // b * st[0] + x * st[1] + l * st[2] + head * D.  part: qk_norm_workspace_bytes()

@@ -101,3 +101,121 @@ def test_norm_binding_refusals():
     x = torch.zeros(1, 1, 2, 144)
     with pytest.raises(ValueError, match="device tensor"):
         dsp.dsp_qk_norm_rope(x, x, 2, 2)
+
+
+def _relpos(lib, bwd=False, **kw):
+    """A valid call (B2 X3, 5 queries, 7 keys, 4 and 2 heads of 72) with some arguments
+    replaced."""
+    d = dict(q=A[0], k=A[1], v=A[2], o=A[3], lse=A[4], bias=A[5], bk=A[6], nb=8, M=16, q_pos=None, kv_len=None, flags=0,
+             ws=A[7], nws=1 << 30, B=2, X=3, Lq=5, Lk=7, H=4, Hkv=2, D=72, qs=_st(15 * 288, 5 * 288, 288),
+             ks=_st(21 * 144, 7 * 144, 144), os=_st(15 * 288, 5 * 288, 288), scale=0.0, dt=BF, do=A[8], dq=A[9], dk=A[10],
+             dv=A[11], db=A[12])
+    assert set(kw) <= set(d)
+    d |= kw
+    mid = [d["bias"], d["bk"], d["nb"], d["M"], d["q_pos"], d["kv_len"], d["flags"], d["ws"], d["nws"], d["B"], d["X"],
+           d["Lq"], d["Lk"], d["H"], d["Hkv"], d["D"], d["qs"], d["ks"], d["os"], d["scale"], d["dt"], None]
+    if not bwd:
+        return lib.dsp_attn_relpos(d["q"], d["k"], d["v"], d["o"], d["lse"], *mid)
+    return lib.dsp_attn_relpos_bwd(d["q"], d["k"], d["v"], d["o"], d["do"], d["lse"], d["dq"], d["dk"], d["dv"], d["db"],
+                                   *mid)
+
+
+@pytest.mark.parametrize("bwd", [False, True])
+@pytest.mark.parametrize("status,kw", [
+    (dsp.DSP_ERR_DTYPE, dict(dt=2)),
+    (dsp.DSP_ERR_NULL, dict(q=None)),
+    (dsp.DSP_ERR_NULL, dict(v=None)),
+    (dsp.DSP_ERR_NULL, dict(o=None)),
+    (dsp.DSP_ERR_NULL, dict(bias=None)),
+    (dsp.DSP_ERR_NULL, dict(bk=None)),
+    (dsp.DSP_ERR_NULL, dict(ks=None)),
+    (dsp.DSP_ERR_SHAPE, dict(B=-1)),
+    (dsp.DSP_ERR_SHAPE, dict(H=0)),
+    (dsp.DSP_ERR_SHAPE, dict(Hkv=3)),
+    (dsp.DSP_ERR_SHAPE, dict(D=0)),
+    (dsp.DSP_ERR_SHAPE, dict(D=136)),
+    (dsp.DSP_ERR_SHAPE, dict(D=70)),                        # bf16: multiples of 8
+    (dsp.DSP_ERR_SHAPE, dict(D=129, dt=F32)),
+    (dsp.DSP_ERR_SHAPE, dict(nb=0)),
+    (dsp.DSP_ERR_SHAPE, dict(M=-1)),
+    (dsp.DSP_ERR_SHAPE, dict(M=1025)),
+    (dsp.DSP_ERR_SHAPE, dict(Lq=1 << 30)),
+    (dsp.DSP_ERR_SHAPE, dict(Lk=1 << 30)),
+    (dsp.DSP_ERR_SHAPE, dict(B=1 << 20, X=1 << 20)),
+    (dsp.DSP_ERR_SHAPE, dict(ks=_st(21 * 144, 7 * 144, -8))),
+    (dsp.DSP_ERR_SHAPE, dict(ks=_st(1 << 40, 1 << 30, 1 << 24))),   # 64 rows past 2^31 bytes
+    (dsp.DSP_ERR_ARG, dict(scale=float("nan"))),
+    (dsp.DSP_ERR_ARG, dict(scale=float("inf"))),
+    (dsp.DSP_ERR_ARG, dict(flags=2)),
+    (dsp.DSP_ERR_ALIGN, dict(q=A[0] + 8)),
+    (dsp.DSP_ERR_ALIGN, dict(k=A[1] + 1)),
+    (dsp.DSP_ERR_ALIGN, dict(bias=A[5] + 1)),
+    (dsp.DSP_ERR_ALIGN, dict(bk=A[6] + 2)),
+    (dsp.DSP_ERR_ALIGN, dict(q_pos=A[13] + 2)),
+    (dsp.DSP_ERR_ALIGN, dict(kv_len=A[13] + 1)),
+    (dsp.DSP_ERR_ALIGN, dict(lse=A[4] + 2)),
+    (dsp.DSP_ERR_ALIGN, dict(qs=_st(15 * 288, 5 * 288, 292))),
+])
+def test_relpos_refusals(lib, bwd, status, kw):
+    assert _relpos(lib, bwd, **kw) == status
+
+
+def test_relpos_output_overlaps(lib):
+    assert _relpos(lib, o=A[0]) == dsp.DSP_ERR_ARG
+    assert _relpos(lib, o=A[2]) == dsp.DSP_ERR_ARG
+    assert _relpos(lib, os=_st(15 * 288, 5 * 288, 280)) == dsp.DSP_ERR_ARG
+    for kw in (dict(dq=A[0]), dict(dk=A[1]), dict(dv=A[10]), dict(dq=A[3]), dict(dk=A[8]), dict(db=A[5]),
+               dict(ks=_st(21 * 144, 0, 144)), dict(qs=_st(0, 5 * 288, 288))):
+        assert _relpos(lib, True, **kw) == dsp.DSP_ERR_ARG, kw
+
+
+def test_relpos_gradient_refusals(lib):
+    for n in ("do", "dq", "dk", "dv", "db", "lse"):
+        assert _relpos(lib, True, **{n: None}) == dsp.DSP_ERR_NULL, n
+    need = lib.dsp_attn_relpos_bwd_workspace_bytes(2, 3, 5, 7, 4, 2, 72, 16, BF)
+    assert need >= 2 * 3 * 4 * 5 * 4
+    for kw in (dict(ws=None), dict(nws=need - 1), dict(ws=A[7] + 8)):
+        assert _relpos(lib, True, **kw) == dsp.DSP_ERR_WORKSPACE, kw
+    assert _relpos(lib, True, qs=_st(15 << 30, 5 << 26, 1 << 26), Lq=5) == dsp.DSP_ERR_SHAPE
+
+
+def test_relpos_workspaces(lib):
+    size = lib.dsp_attn_relpos_workspace_bytes
+    assert size(2, 1, 1, 100, 8, 2, 72, BF) == 0 and size(2, 1, 300, 5000, 8, 2, 72, BF) == 0
+    need = size(2, 1, 1, 5000, 8, 2, 72, BF)
+    assert need > 0
+    long = dict(X=1, Lq=1, Lk=5000, H=8, Hkv=2, qs=_st(576, 576, 576), os=_st(576, 576, 576), ks=_st(5000 * 144, 5000 * 144, 144))
+    for kw in (dict(ws=None), dict(nws=need - 1)):
+        assert _relpos(lib, **long, **kw) == dsp.DSP_ERR_WORKSPACE
+    assert size(1, 1, 1, 5000, 8, 3, 72, BF) == 0 and size(-1, 1, 1, 5000, 8, 2, 72, BF) == 0
+
+
+def test_relpos_of_nothing(lib):
+    assert _relpos(lib, Lq=0, q=None, o=None, lse=None) == dsp.DSP_OK
+    assert _relpos(lib, B=0, q=None, k=None, v=None, o=None, bias=None, bk=None) == dsp.DSP_OK
+
+
+def test_buckets_refusals(lib):
+    buf = (ctypes.c_int32 * 9)()
+    assert lib.dsp_relpos_buckets(None, 4, 8, 1) == dsp.DSP_ERR_NULL
+    assert lib.dsp_relpos_buckets(buf, -1, 8, 1) == dsp.DSP_ERR_SHAPE
+    assert lib.dsp_relpos_buckets(buf, 1025, 8, 1) == dsp.DSP_ERR_SHAPE
+    assert lib.dsp_relpos_buckets(buf, 4, 1, 1) == dsp.DSP_ERR_SHAPE
+    assert lib.dsp_relpos_buckets(buf, 4, 0, 0) == dsp.DSP_ERR_SHAPE
+    assert lib.dsp_relpos_buckets(buf, 4, 1, 0) == dsp.DSP_OK and not any(buf)
+    with pytest.raises(ValueError):
+        dsp.dsp_relpos_buckets(-1, 8)
+
+
+@pytest.mark.parametrize("M,nb", [(8, 4), (128, 32), (128, 8), (40, 15), (200, 33), (1024, 64)])
+@pytest.mark.parametrize("both", [False, True])
+def test_buckets_follow_the_oracle(M, nb, both):
+    from oracle import position as po
+    assert dsp.dsp_relpos_buckets(M, nb, both).tolist() == po.relpos_buckets(M, nb, both).tolist()
+
+
+def test_relpos_binding_refusals():
+    import torch
+    x = torch.zeros(1, 1, 2, 144)
+    with pytest.raises(ValueError, match="device tensor"):
+        dsp.dsp_attn_relpos(x, x, x, 2, 2, torch.zeros(3, 2), torch.zeros(5, dtype=torch.int32))
