@@ -39,7 +39,7 @@ def hipcc() -> str:
 # Per-file extra flags.  The attention kernels never see NaN by contract (a NaN
 # input makes the output undefined anyway), which lets the softmax maxima skip
 # NaN canonicalisation.
-FILE_FLAGS = {"attn_bf16.hip": ["-fno-honor-nans"]}
+FILE_FLAGS = {"attn_bf16.hip": ["-fno-honor-nans"], "attn_relpos.hip": ["-fno-honor-nans"]}
 
 
 def _compile(src: Path, verbose: bool) -> Path:

@@ -201,6 +201,25 @@ __device__ __forceinline__ void store_rows(const ColAcc<T, DC>& a, int lane, int
   }
 }
 
+// The same through LDS: `so` holds 32 rows of pitch P for this wave alone, and the rows
+// leave as whole 16-byte chunks, consecutive lanes along a row (from the accumulators
+// a store would write 8 or 16 bytes of 32 rows each).  One wave's LDS accesses complete
+// in order.
+template <typename T, int DC, typename F>
+__device__ __forceinline__ void store_rows_lds(T* so, const ColAcc<T, DC>& a, int lane, int D, F row_of) {
+  using G = Geo<T, DC>;
+  store_rows<T, DC>(a, lane, DC, true, [&](int n) { return so + n * G::P; });
+  const int ch = D / G::E;   // whole chunks: the callers' rows are aligned
+  int row = lane / ch, col = lane - row * ch;
+  const int dr = 64 / ch, dc = 64 - dr * ch;
+  for (int c = lane; c < 32 * ch; c += 64) {
+    T* to = row_of(row);
+    if (to) *reinterpret_cast<u32x4*>(to + col * G::E) = *reinterpret_cast<const u32x4*>(so + row * G::P + col * G::E);
+    row += dr, col += dc;
+    if (col >= ch) col -= ch, ++row;
+  }
+}
+
 // The fragments of one row in registers, columns D .. as 0; row null: all 0.
 template <typename T, int DC>
 __device__ __forceinline__ void row_frags(const T* row, int g, int D, bool vec,
@@ -222,7 +241,7 @@ __device__ __forceinline__ void row_frags(const T* row, int g, int D, bool vec,
   }
 }
 
-// A tile of up to R rows of one tensor on its way from memory to LDS: NT threads,
+// A tile of up to R rows of one tensor on its way from memory to LDS: NT threads (tid),
 // 16-byte chunks, rows past `rows` and columns past D as 0 (the columns are cleared
 // once, by clear_pad).  vec: whole chunks at 16-byte offsets; otherwise (fp32) an
 // element at a time.
@@ -238,13 +257,13 @@ struct Tile {
     int to[N];
     uint32_t n;  // chunks of a full tile
   };
-  static __device__ __forceinline__ Map map(int D, uint32_t row_bytes) {
+  static __device__ __forceinline__ Map map(int D, uint32_t row_bytes, uint32_t tid) {
     Map m;
     const uint32_t ch = (uint32_t)(D + G::E - 1) / G::E;
     m.n = R * ch;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const uint32_t c = threadIdx.x + i * NT;
+      const uint32_t c = tid + i * NT;
       const uint32_t row = c / ch, col = c - row * ch;
       m.at[i] = row * row_bytes + col * 16u;
       m.to[i] = (int)(row * G::P + col * G::E);
@@ -252,11 +271,11 @@ struct Tile {
     return m;
   }
   __device__ __forceinline__ void fetch(const Map& m, const T* base, uint32_t rows, uint32_t row_bytes, int D,
-                                        bool vec) {
+                                        bool vec, uint32_t tid) {
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, rows * row_bytes);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (threadIdx.x + i * NT >= m.n) continue;
+      if (tid + i * NT >= m.n) continue;
       if (sizeof(T) == 2 || vec) {
         pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, m.at[i], 0, 0);
       } else {
@@ -267,18 +286,18 @@ struct Tile {
       }
     }
   }
-  __device__ __forceinline__ void stash(const Map& m, T* lds) const {
+  __device__ __forceinline__ void stash(const Map& m, T* lds, uint32_t tid) const {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (threadIdx.x + i * NT < m.n) *reinterpret_cast<u32x4*>(lds + m.to[i]) = pre[i];
+      if (tid + i * NT < m.n) *reinterpret_cast<u32x4*>(lds + m.to[i]) = pre[i];
   }
 };
 // zero in columns D .. P - 1 of `rows` LDS rows (fp32: past the chunk that holds D - 1)
 template <typename T, int DC>
-__device__ __forceinline__ void clear_pad(T* lds, int rows, int D, int nt) {
+__device__ __forceinline__ void clear_pad(T* lds, int rows, int D, int tid, int nt) {
   using G = Geo<T, DC>;
   const int d0 = (D + G::E - 1) / G::E * G::E, w = G::P - d0;
-  for (int e = threadIdx.x; e < rows * w; e += nt) lds[e / w * G::P + d0 + e % w] = (T)0.0f;
+  for (int e = tid; e < rows * w; e += nt) lds[e / w * G::P + d0 + e % w] = (T)0.0f;
 }
 
 struct BiasArgs {
@@ -286,14 +305,49 @@ struct BiasArgs {
   const int32_t* buckets;  // [2 M + 1]
   int32_t M, nb;
 };
-// the bias of a distance for head h in the exp2 domain
+__device__ __forceinline__ int32_t bucket_at(const BiasArgs& b, int32_t d) {
+  return b.buckets[(d < -b.M ? -b.M : d > b.M ? b.M : d) + b.M];
+}
+// the bias of bucket k, and of a distance, for head h in the exp2 domain
 template <typename T>
-__device__ __forceinline__ float bias_at(const BiasArgs& b, uint32_t H, uint32_t h, int32_t d) {
-  d = d < -b.M ? -b.M : d > b.M ? b.M : d;
-  const int32_t k = b.buckets[d + b.M];
+__device__ __forceinline__ float bias_of(const BiasArgs& b, uint32_t H, uint32_t h, int32_t k) {
   const float v = (uint32_t)k < (uint32_t)b.nb ? (float)static_cast<const T*>(b.bias)[(int64_t)k * H + h] : 0.0f;
   return v <= kMasked ? -INFINITY : v * kLog2e;
 }
+template <typename T>
+__device__ __forceinline__ float bias_at(const BiasArgs& b, uint32_t H, uint32_t h, int32_t d) {
+  return bias_of<T>(b, H, h, bucket_at(b, d));
+}
+// The table of distances lo .. lo + n - 1 for nh heads from h0, `stride` apart in LDS, by
+// NT threads.  Loads return in order: the buckets are asked for before a work-group's
+// first keys and the biases after them, so that neither wait is added to the keys'.
+template <typename T, int NT>
+struct Table {
+  static constexpr int N = 2;
+  int32_t k[N];
+  __device__ __forceinline__ void fetch(const BiasArgs& b, int32_t lo, int32_t n) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int32_t t = (int32_t)threadIdx.x + i * NT;
+      k[i] = t < n ? bucket_at(b, lo + t) : -1;
+    }
+  }
+  __device__ __forceinline__ void build(const BiasArgs& b, int32_t lo, int32_t n, float* tab, uint32_t stride,
+                                        uint32_t H, uint32_t h0, uint32_t nh) const {
+    for (uint32_t hh = 0; hh < nh; ++hh) {
+      float v[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] = bias_of<T>(b, H, h0 + hh, k[i]);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int32_t t = (int32_t)threadIdx.x + i * NT;
+        if (t < n) tab[hh * stride + t] = v[i];
+      }
+      for (int32_t t = (int32_t)threadIdx.x + N * NT; t < n; t += NT)
+        tab[hh * stride + t] = bias_at<T>(b, H, h0 + hh, lo + t);
+    }
+  }
+};
 // A 32 x 32 block of scores whose keys start d0 positions after its queries holds the
 // distances d0 - 31 .. d0 + 31.  Where they all lie at or past one end of the table
 // the bias is one value; the other blocks' distances lie within M + kEdge.

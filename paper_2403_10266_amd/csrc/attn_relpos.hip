@@ -15,9 +15,9 @@
 // register; for long sequences that is nearly all of them, and the bias costs them
 // nothing beyond the multiply-add that the scale needs anyway.
 //
-// The subtracted reference follows the running maximum lazily: it moves (and the sums
-// are rescaled) only when a score exceeds it by 2^8, so the usual tile pays one
-// comparison.
+// The subtracted reference follows the running maximum lazily: it is the maximum of the
+// first tile until a tile's probabilities sum to more than 2^16 (one comparison for
+// each column and tile); only then are the tile's maxima taken and the sums rescaled.
 //
 // Few queries against many keys (a new token against a cache): the queries of a
 // key/value head's group share one block of 32 columns, and the keys are cut among
@@ -30,175 +30,124 @@
 namespace dsp {
 namespace {
 
-constexpr float kMove = 8.0f;   // exp2 units a score may exceed the reference by
-
 struct FwdParams {
   const void* q;
   const void* k;
   const void* v;
   void* o;
   float* lse;
-  float* part;   // split keys: per work-group 32 maxima, 32 sums, 32 rows of D
+  float* part;       // split keys: the columns' references, sums and rows of each work-group
   const int32_t* q_pos;
   const int32_t* kv_len;
   int64_t qs[3], ks[3], os[3];
   BiasArgs bias;
   uint32_t X, H, grp, Lq, Lk, n_qb, n_split, split_keys, n_blocks, D;
   uint32_t tab;      // distances of the LDS table, for each head of a work-group
-  uint32_t cols;     // packed: queries x group heads of a unit; 0: one head's queries
+  uint32_t cols;     // few queries: queries x heads of a group
   float c;           // scale * log2(e)
-  bool vec, vec_o, causal;
+  bool vec, causal;
 };
 
-template <typename T, int DC, int NW, int QT, int KB, int NBUF, int MINW>
-__global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) {
+// The softmax of QT blocks of 32 query columns over NKT blocks of 32 keys at a time.
+// LAZY: the reference moves only when it has to (long runs of keys); otherwise every
+// tile takes its maxima (few keys, and passes that memory bounds).
+template <typename T, int DC, int QT, int NKT, bool LAZY>
+struct Softmax {
   using G = Geo<T, DC>;
   using M = Mx<T>;
-  constexpr int NT = NW * 64, QB = NW * 32 * QT, NKT = KB / 32;
-  constexpr int TILE = KB * G::P;
-  extern __shared__ __attribute__((aligned(16))) char smem[];
-  T* lds = reinterpret_cast<T*>(smem);                       // [NBUF][K, V][KB][P]
-  float* tab = reinterpret_cast<float*>(lds + NBUF * 2 * TILE);
-
-  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // work-group -> (unit, query block, split); each XCD takes a contiguous range
-  uint32_t bid = blockIdx.x;
-  if ((p.n_blocks & 7u) == 0) bid = (bid & 7u) * (p.n_blocks >> 3) + (bid >> 3);
-  const uint32_t split = bid % p.n_split, ub = bid / p.n_split;
-  const uint32_t unit = ub / p.n_qb;
-  // causal: the last query blocks have the most keys and start first
-  const uint32_t qb = p.causal ? p.n_qb - 1 - ub % p.n_qb : ub % p.n_qb;
-  const uint32_t per_bx = p.cols ? p.H / p.grp : p.H;
-  const uint32_t bx = unit / per_bx, h0 = p.cols ? unit % per_bx * p.grp : unit % per_bx;
-  const uint32_t b = bx / p.X, x = bx % p.X;
-  const int D = (int)p.D;
-  const T* kg = static_cast<const T*>(p.k) + (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)(h0 / p.grp) * D;
-  const T* vg = static_cast<const T*>(p.v) + (kg - static_cast<const T*>(p.k));
-  const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.qs[0] + (int64_t)x * p.qs[1] + (int64_t)h0 * D;
-
-  const int32_t q0 = position(p.q_pos, b) + (int32_t)(qb * QB);   // position of the block's first query
-  const uint32_t len = length(p.kv_len, b, p.Lk);
-  const uint32_t nq = p.cols ? p.Lq : min(p.Lq - qb * QB, (uint32_t)QB);
-  // keys [k0, k1) of this work-group: whole tiles from its split's first key on
-  const uint32_t k0 = split * p.split_keys;
-  uint32_t k1 = min(len, p.n_split > 1 ? k0 + p.split_keys : len);
-  if (p.causal) {
-    const int32_t last = q0 + (int32_t)nq;   // keys before it
-    k1 = last <= 0 ? 0u : min(k1, (uint32_t)last);
-  }
-  const uint32_t row_bytes = (uint32_t)p.ks[2] * (uint32_t)sizeof(T);
-  using TileT = Tile<T, DC, KB, NT>;
-  const typename TileT::Map map = TileT::map(D, row_bytes);
-  TileT tk, tv;
-  auto fetch = [&](uint32_t kb) {
-    const uint32_t rows = kb < k1 ? min(k1 - kb, (uint32_t)KB) : 0u;
-    tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
-    tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
-  };
-  auto stash = [&](int buf) {
-    tk.stash(map, lds + buf * 2 * TILE);
-    tv.stash(map, lds + buf * 2 * TILE + TILE);
-  };
-  if (k0 < k1) fetch(k0);
-
-  // the columns: head (in the unit) and query of this lane's column of tile j
-  uint32_t ch[QT], cq[QT];
-#pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    const uint32_t col = 32 * (wave * QT + j) + l32;
-    ch[j] = p.cols ? min(col / p.Lq, p.grp - 1) : 0u;
-    cq[j] = p.cols ? col - ch[j] * p.Lq : col;
-  }
-  auto row_at = [&](uint32_t c, uint32_t h, int64_t rs) { return (int64_t)(qb * QB + c) * rs + (int64_t)h * D; };
-  typename M::frag qf[QT][G::NS];
-#pragma unroll
-  for (int j = 0; j < QT; ++j)
-    row_frags<T, DC>(cq[j] < nq ? qg + row_at(cq[j], ch[j], p.qs[2]) : nullptr, g, D, p.vec, qf[j]);
-
-  // the table: distances lo .. of each head of the work-group
-  const int32_t kend = (int32_t)((k1 + KB - 1) / KB * KB);
-  const int32_t lo = max(-(p.bias.M + kEdge), (int32_t)k0 - (q0 + QB - 1));
-  const int32_t hi = min(p.bias.M + kEdge, kend - 1 - q0);
-  const uint32_t nh = p.cols ? p.grp : 1;
-  if (k0 < k1)
-    for (uint32_t hh = 0; hh < nh; ++hh)
-      for (int32_t d = lo + (int32_t)threadIdx.x; d <= hi; d += NT)
-        tab[hh * p.tab + (uint32_t)(d - lo)] = bias_at<T>(p.bias, p.H, h0 + hh, d);
-  float left[QT], right[QT];
-#pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    left[j] = bias_at<T>(p.bias, p.H, h0 + ch[j], -p.bias.M);
-    right[j] = bias_at<T>(p.bias, p.H, h0 + ch[j], p.bias.M);
-  }
-
+  // a tile's sum of probabilities past this moves the reference: every probability
+  // then stays below it, far inside both types' range
+  static constexpr float kMove = 65536.0f;
   ColAcc<T, DC> o[QT];
-  float ref[QT], sum[QT];
-  bool set[QT];
+  float ref[QT], sum[QT];   // exp2 units; the sum of this lane's keys
+  bool set;                 // every column has a reference
+
+  __device__ __forceinline__ void init() {
 #pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    o[j].zero();
-    ref[j] = sum[j] = 0.0f;
-    set[j] = false;
+    for (int j = 0; j < QT; ++j) {
+      o[j].zero();
+      ref[j] = -INFINITY;
+      sum[j] = 0.0f;
+    }
+    set = false;
+  }
+  // what a tile of keys needs besides its LDS rows
+  struct Keys {
+    int32_t key0;           // its first key
+    int32_t stop;           // keys of the work-group end here
+    int32_t M;
+    bool causal;
+  };
+
+  // scores of the tile in exp2 units, less `minus`
+  template <typename Q>
+  static __device__ __forceinline__ void scores(floatx16 (&s)[NKT][QT], const T* kl, const Q& qf, const Keys& k, float c,
+                                         const int32_t (&first)[QT], const int32_t (&at)[QT],
+                                         const float* const (&tab)[QT], const float (&left)[QT],
+                                         const float (&right)[QT], const float (&minus)[QT], int lane) {
+    const int l32 = lane & 31, g = lane >> 5;
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int j = 0; j < QT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][j][r] = 0.0f;
+#pragma unroll
+    for (int st = 0; st < G::NS; ++st)
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        const auto a =
+            *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
+#pragma unroll
+        for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(a, qf[j][st], s[kt][j]);
+      }
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int j = 0; j < QT; ++j) {
+        const int32_t key0 = k.key0 + 32 * kt;
+        const int32_t d0 = key0 - first[j];
+        if (d0 + 31 <= -k.M || d0 - 31 >= k.M) {
+          const float t = (d0 < 0 ? left[j] : right[j]) - minus[j];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][j][r] = fmaf(s[kt][j][r], c, t);
+        } else {
+          const float* tb = tab[j] + key0 + 4 * g;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][j][r] = fmaf(s[kt][j][r], c, tb[8 * (r / 4) + r % 4] - minus[j]);
+        }
+        if ((k.causal && d0 + 31 > 0) || key0 + 32 > k.stop) {
+          const int32_t stop = k.causal ? min(k.stop, at[j] + 1) : k.stop;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (key0 + 8 * (r / 4) + 4 * g + r % 4 >= stop) s[kt][j][r] = -INFINITY;
+        }
+      }
   }
 
-  clear_pad<T, DC>(lds, NBUF * 2 * KB, D, NT);
-  if (k0 < k1) stash(0);
-  __syncthreads();
-  const uint32_t n_it = k0 < k1 ? (k1 - k0 + KB - 1) / KB : 0;
-  for (uint32_t it = 0; it < n_it; ++it) {
-    const uint32_t kb = k0 + it * KB;
-    const bool more = NBUF > 1 && it + 1 < n_it;
-    if (more) fetch(kb + KB);
-    const T* kl = lds + (NBUF > 1 ? (it & 1) : 0) * 2 * TILE;
-    const T* vl = kl + TILE;
-    // queries of this wave are all before the tile: nothing to see
-    const int32_t wq = q0 + (p.cols ? 0 : 32 * QT * wave);          // the wave's first query
-    const int32_t wl = wq + (p.cols ? (int32_t)p.Lq : 32 * QT) - 1;   // and its last
-    if (!(p.causal && (int32_t)kb > wl)) {
+  // One tile: first[j] is the position of block j's first query, at[j] of this lane's
+  // own, tab[j] the table at its distance from key 0.
+  template <typename Q>
+  __device__ __forceinline__ void step(const T* kl, const T* vl, const Q& qf, const Keys& k, float c,
+                                       const int32_t (&first)[QT], const int32_t (&at)[QT],
+                                       const float* const (&tab)[QT], const float (&left)[QT],
+                                       const float (&right)[QT], int lane) {
+    ColB<T> pf[NKT][QT];
+    float add[QT];
+    bool move = !LAZY || !set;
+    if (LAZY && set) {
       floatx16 s[NKT][QT];
+      scores(s, kl, qf, k, c, first, at, tab, left, right, ref, lane);
+      move = probabilities(s, pf, add);
+    }
+    if (!LAZY || __any(move)) {
+      // the scores themselves, their maxima, and the sums moved to those
+      floatx16 s[NKT][QT];
+      float zero[QT];
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int j = 0; j < QT; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[kt][j][r] = 0.0f;
-#pragma unroll
-      for (int st = 0; st < G::NS; ++st)
-#pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) {
-          const auto a =
-              *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
-#pragma unroll
-          for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(a, qf[j][st], s[kt][j]);
-        }
-      // scores relative to the reference, in the exp2 domain
-#pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-        for (int j = 0; j < QT; ++j) {
-          const int32_t key0 = (int32_t)kb + 32 * kt;
-          const int32_t bq = p.cols ? q0 : wq + 32 * j;   // the block's first query
-          const int32_t d0 = key0 - bq;
-          if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
-            const float t = (d0 < 0 ? left[j] : right[j]) - ref[j];
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][j][r] = fmaf(s[kt][j][r], p.c, t);
-          } else {
-            const float* tb = tab + ch[j] * p.tab + (key0 + 4 * g - (q0 + (int32_t)cq[j]) - lo);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              s[kt][j][r] = fmaf(s[kt][j][r], p.c, tb[8 * (r / 4) + r % 4] - ref[j]);
-          }
-          if ((p.causal && d0 + 31 > 0) || key0 + 32 > (int32_t)k1) {
-            const int32_t stop = p.causal ? min((int32_t)k1, q0 + (int32_t)cq[j] + 1) : (int32_t)k1;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (key0 + 8 * (r / 4) + 4 * g + r % 4 >= stop) s[kt][j][r] = -INFINITY;
-          }
-        }
-      bool move = false;
-      float top[QT];
+      for (int j = 0; j < QT; ++j) zero[j] = 0.0f;
+      scores(s, kl, qf, k, c, first, at, tab, left, right, zero, lane);
+      bool all = true;
 #pragma unroll
       for (int j = 0; j < QT; ++j) {
         float m = s[0][j][0];
@@ -206,157 +155,421 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
         for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
           for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kt][j][r]);
-        top[j] = fmaxf(m, swap_halves(m));
-        move |= top[j] > (set[j] ? kMove : -INFINITY);
+        m = fmaxf(fmaxf(m, swap_halves(m)), ref[j]);
+        const float f = ref[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[j] - m);
+        sum[j] *= f;
+        o[j].scale(f, lane);
+        ref[j] = m;
+        all &= m != -INFINITY;
+        const float by = m == -INFINITY ? 0.0f : m;   // nothing yet: every score is -inf
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][j][r] -= by;
       }
-      if (__any(move)) {
+      set = __all(all);
+      probabilities(s, pf, add);
+    }
 #pragma unroll
-        for (int j = 0; j < QT; ++j) {
-          const bool mv = top[j] > (set[j] ? kMove : -INFINITY);
-          const float d = mv ? top[j] : 0.0f;
-          const float f = mv && set[j] ? __builtin_amdgcn_exp2f(-d) : 1.0f;
-          ref[j] += d;
-          set[j] |= mv;
-          sum[j] *= f;
-          o[j].scale(f, lane);
+    for (int j = 0; j < QT; ++j) sum[j] += add[j];
 #pragma unroll
-          for (int kt = 0; kt < NKT; ++kt)
+    for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][j][r] -= d;
-        }
-      }
+      for (int j = 0; j < QT; ++j) o[j].add(vl, 32 * kt, lane, pf[kt][j]);
+  }
+  // exp2 of the scores, as operands and summed; whether some column's are too large
+  static __device__ __forceinline__ bool probabilities(const floatx16 (&s)[NKT][QT], ColB<T> (&pf)[NKT][QT],
+                                                       float (&add)[QT]) {
+    bool over = false;
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+      float a = 0.0f;
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
-        for (int j = 0; j < QT; ++j) {
-          ColB<T> pf;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float e = __builtin_amdgcn_exp2f(s[kt][j][r]);
-            sum[j] += e;
-            pf.set(r, e);
-          }
-          o[j].add(vl, 32 * kt, lane, pf);
+        for (int r = 0; r < 16; ++r) {
+          const float e = __builtin_amdgcn_exp2f(s[kt][j][r]);
+          a += e;
+          pf[kt][j].set(r, e);
         }
+      add[j] = a;
+      over |= a > kMove;
     }
+    return over;
+  }
+};
+
+// Many queries: QT blocks of 32 queries of one head per wave, the keys in LDS tiles
+// that all waves share, the next tile on its way in registers.
+template <typename T, int DC, int NW, int QT, int KB, int NBUF, int MINW>
+__global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) {
+  // NBUF == 1: one tile holds all keys
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  constexpr int NT = NW * 64, QB = NW * 32 * QT, NKT = KB / 32;
+  constexpr int TILE = KB * G::P;
+  static_assert(NW * QT * 32 <= NBUF * 2 * KB || QT > 1 || NW <= NBUF * 2 * NKT, "the output rows fit the tiles");
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* lds = reinterpret_cast<T*>(smem);                       // [NBUF][K, V][KB][P]
+  float* tab = reinterpret_cast<float*>(lds + NBUF * 2 * TILE);
+
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // work-group -> (unit, query block); each XCD takes a contiguous range
+  uint32_t bid = blockIdx.x;
+  if ((p.n_blocks & 7u) == 0) bid = (bid & 7u) * (p.n_blocks >> 3) + (bid >> 3);
+  const uint32_t unit = bid / p.n_qb;
+  // causal: the last query blocks have the most keys and start first
+  const uint32_t qb = p.causal ? p.n_qb - 1 - bid % p.n_qb : bid % p.n_qb;
+  const uint32_t bx = unit / p.H, h = unit % p.H, b = bx / p.X, x = bx % p.X;
+  const int D = (int)p.D;
+  const int64_t k_at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)(h / p.grp) * D;
+  const T* kg = static_cast<const T*>(p.k) + k_at;
+  const T* vg = static_cast<const T*>(p.v) + k_at;
+  const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.qs[0] + (int64_t)x * p.qs[1] + (int64_t)h * D;
+
+  const int32_t q0 = position(p.q_pos, b) + (int32_t)(qb * QB);   // position of the block's first query
+  const uint32_t nq = min(p.Lq - qb * QB, (uint32_t)QB);
+  uint32_t k1 = length(p.kv_len, b, p.Lk);
+  if (p.causal) {
+    const int32_t last = q0 + (int32_t)nq;   // keys before it
+    k1 = last <= 0 ? 0u : min(k1, (uint32_t)last);
+  }
+  const uint32_t row_bytes = (uint32_t)p.ks[2] * (uint32_t)sizeof(T);
+  using TileT = Tile<T, DC, KB, NT>;
+  const typename TileT::Map map = TileT::map(D, row_bytes, threadIdx.x);
+  TileT tk, tv;
+  auto fetch = [&](uint32_t kb) {
+    const uint32_t rows = kb < k1 ? min(k1 - kb, (uint32_t)KB) : 0u;
+    tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
+    tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
+  };
+  auto stash = [&](int buf) {
+    tk.stash(map, lds + buf * 2 * TILE, threadIdx.x);
+    tv.stash(map, lds + buf * 2 * TILE + TILE, threadIdx.x);
+  };
+  // the table: distances lo .. hi
+  const int32_t lo = max(-(p.bias.M + kEdge), -(q0 + QB - 1));
+  const int32_t hi = min(p.bias.M + kEdge, (int32_t)((k1 + KB - 1) / KB * KB) - 1 - q0);
+  const int32_t n_tab = k1 ? hi - lo + 1 : 0;
+  Table<T, NT> table;
+  table.fetch(p.bias, lo, n_tab);
+  if (k1) fetch(0);
+
+  const int32_t wq = q0 + 32 * QT * wave;   // the wave's first query
+  typename M::frag qf[QT][G::NS];
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    const uint32_t i = 32 * (wave * QT + j) + l32;
+    row_frags<T, DC>(i < nq ? qg + (int64_t)(qb * QB + i) * p.qs[2] : nullptr, g, D, p.vec, qf[j]);
+  }
+  table.build(p.bias, lo, n_tab, tab, 0, p.H, h, 1);
+  float left[QT], right[QT];
+  int32_t first[QT], at[QT];
+  const float* tb[QT];
+  left[0] = bias_at<T>(p.bias, p.H, h, -p.bias.M);
+  right[0] = bias_at<T>(p.bias, p.H, h, p.bias.M);
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    left[j] = left[0], right[j] = right[0];
+    first[j] = wq + 32 * j;
+    at[j] = first[j] + l32;
+    tb[j] = tab - lo - at[j];
+  }
+  Softmax<T, DC, QT, NKT, NBUF != 1> sm;
+  sm.init();
+  clear_pad<T, DC>(lds, NBUF * 2 * KB, D, threadIdx.x, NT);
+  if (k1) stash(0);
+  __syncthreads();
+  const uint32_t n_it = (k1 + KB - 1) / KB;
+  for (uint32_t it = 0; it < n_it; ++it) {
+    const uint32_t kb = it * KB;
+    const bool more = NBUF > 1 && it + 1 < n_it;
+    if (more) fetch(kb + KB);
+    const T* kl = lds + (NBUF > 1 ? (it & 1) : 0) * 2 * TILE;
+    // queries of this wave are all before the tile, or past the end: nothing to do
+    if (!(p.causal && (int32_t)kb > wq + 32 * QT - 1) && 32u * QT * wave < nq)
+      sm.step(kl, kl + TILE, qf, {(int32_t)kb, (int32_t)k1, p.bias.M, p.causal}, p.c, first, at, tb, left,
+              right, lane);
     if (more) stash((it + 1) & 1);
     __syncthreads();
   }
 
+  T* og = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)h * D;
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
-    const float l = sum[j] + swap_halves(sum[j]);
-    if (p.n_split > 1) {   // one block of columns: the sums as they are
-      float* w = p.part + (uint64_t)(unit * p.n_split + split) * (64 + 32 * p.D);
-      if (g == 0) {
-        w[l32] = set[j] ? ref[j] : -INFINITY;
-        w[32 + l32] = l;
-      }
-      store_rows<T, DC>(o[j], lane, D, false, [&](int n) { return w + 64 + n * (int)p.D; });
-      continue;
-    }
-    o[j].scale(l > 0.0f ? 1.0f / l : 0.0f, lane);
-    T* og = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)h0 * D;
-    store_rows<T, DC>(o[j], lane, D, p.vec_o, [&](int n) -> T* {
-      const uint32_t col = 32 * (wave * QT + j) + n;
-      const uint32_t hh = p.cols ? col / p.Lq : 0, i = p.cols ? col - hh * p.Lq : col;
-      return (p.cols ? col < p.cols : i < nq) ? og + row_at(i, hh, p.os[2]) : nullptr;
-    });
-    const bool mine = p.cols ? 32u * (wave * QT + j) + l32 < p.cols : cq[j] < nq;
-    if (p.lse && g == 0 && mine)
-      p.lse[((uint64_t)bx * p.H + h0 + ch[j]) * p.Lq + qb * QB + cq[j]] =
-          l > 0.0f ? kLn2 * (ref[j] + log2f(l)) : -INFINITY;
+    const float l = sm.sum[j] + swap_halves(sm.sum[j]);
+    sm.o[j].scale(l > 0.0f ? 1.0f / l : 0.0f, lane);
+    const uint32_t c0 = 32 * (wave * QT + j);
+    auto row = [&](int n) -> T* { return c0 + n < nq ? og + (int64_t)(qb * QB + c0 + n) * p.os[2] : nullptr; };
+    if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, sm.o[j], lane, D, row);
+    else store_rows<T, DC>(sm.o[j], lane, D, false, row);
+    if (p.lse && g == 0 && c0 + l32 < nq)
+      p.lse[((uint64_t)bx * p.H + h) * p.Lq + qb * QB + c0 + l32] = l > 0.0f ? kLn2 * (sm.ref[j] + log2f(l)) : -INFINITY;
   }
 }
 
-// Joins the splits of a unit's columns: with the splits' references m_s, sums l_s and
-// rows o_s, o = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.  A wave per column.
-template <typename T>
-__global__ __launch_bounds__(256) void relpos_join_kernel(FwdParams p, uint32_t n_cols) {
-  const uint32_t wid = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (wid >= n_cols) return;
-  const uint32_t unit = wid / p.cols, col = wid - unit * p.cols;
-  const uint32_t stride = 64 + 32 * p.D;
+// Few queries: the queries of a key/value head's group (at most 32 in all) are the
+// columns of one block.  Each wave takes every NW-th tile of 32 keys through LDS rows
+// of its own, with no barrier until the waves' sums are joined; the whole chip's loads
+// are in flight at once, which is what bounds a pass over a cache.
+template <typename T, int DC, int NW, int MINW>
+__global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  constexpr int TILE = 32 * G::P;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  T* kl = reinterpret_cast<T*>(smem) + wave * 2 * TILE;   // [NW][K, V][32][P]
+  T* vl = kl + TILE;
+  float* tab = reinterpret_cast<float*>(reinterpret_cast<T*>(smem) + NW * 2 * TILE);
+
+  uint32_t bid = blockIdx.x;
+  if ((p.n_blocks & 7u) == 0) bid = (bid & 7u) * (p.n_blocks >> 3) + (bid >> 3);
+  const uint32_t unit = bid / p.n_split, split = bid - unit * p.n_split;
+  const uint32_t kvh = p.H / p.grp, bx = unit / kvh, e = unit - bx * kvh, h0 = e * p.grp;
+  const uint32_t b = bx / p.X, x = bx - b * p.X;
+  const int D = (int)p.D;
+  const int64_t k_at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)e * D;
+  const T* kg = static_cast<const T*>(p.k) + k_at;
+  const T* vg = static_cast<const T*>(p.v) + k_at;
+
+  const int32_t q0 = position(p.q_pos, b);
+  const uint32_t k0 = split * p.split_keys;
+  uint32_t k1 = min(length(p.kv_len, b, p.Lk), k0 + p.split_keys);
+  if (p.causal) {
+    const int32_t last = q0 + (int32_t)p.Lq;
+    k1 = last <= 0 ? 0u : min(k1, (uint32_t)last);
+  }
+  const uint32_t row_bytes = (uint32_t)p.ks[2] * (uint32_t)sizeof(T);
+  using TileT = Tile<T, DC, 32, 64>;
+  const typename TileT::Map map = TileT::map(D, row_bytes, lane);
+  TileT tk, tv;
+  auto fetch = [&](uint32_t kb) {
+    const uint32_t rows = kb < k1 ? min(k1 - kb, 32u) : 0u;
+    tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, lane);
+    tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, lane);
+  };
+  const int32_t lo = max(-(p.bias.M + kEdge), (int32_t)k0 - (q0 + 31));
+  const int32_t hi = min(p.bias.M + kEdge, (int32_t)(k0 + (max(k1, k0) - k0 + 31) / 32 * 32) - 1 - q0);
+  const int32_t n_tab = k0 < k1 ? hi - lo + 1 : 0;
+  Table<T, NW * 64> table;
+  table.fetch(p.bias, lo, n_tab);
+  const uint32_t mine = k0 + 32 * wave;
+  if (mine < k1) fetch(mine);
+
+  // this lane's column: head ch of the group, query cq
+  const uint32_t ch = min(l32 / p.Lq, p.grp - 1), cq = l32 - ch * p.Lq;
+  const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.qs[0] + (int64_t)x * p.qs[1];
+  auto at_row = [&](uint32_t hh, uint32_t i, int64_t rs) { return (int64_t)i * rs + (int64_t)(h0 + hh) * D; };
+  typename M::frag qf[1][G::NS];
+  row_frags<T, DC>((uint32_t)l32 < p.cols ? qg + at_row(ch, cq, p.qs[2]) : nullptr, g, D, p.vec, qf[0]);
+  table.build(p.bias, lo, n_tab, tab, p.tab, p.H, h0, p.grp);
+  const float left[1] = {bias_at<T>(p.bias, p.H, h0 + ch, -p.bias.M)};
+  const float right[1] = {bias_at<T>(p.bias, p.H, h0 + ch, p.bias.M)};
+  const int32_t first[1] = {q0}, at[1] = {q0 + (int32_t)cq};
+  const float* const tb[1] = {tab + (int64_t)ch * p.tab - lo - at[0]};
+
+  Softmax<T, DC, 1, 1, false> sm;
+  sm.init();
+  clear_pad<T, DC>(kl, 64, D, lane, 64);
+  __syncthreads();   // the table
+  for (uint32_t kb = mine; kb < k1; kb += 32 * NW) {
+    tk.stash(map, kl, lane);
+    tv.stash(map, vl, lane);
+    if (kb + 32 * NW < k1) fetch(kb + 32 * NW);
+    sm.step(kl, vl, qf, {(int32_t)kb, (int32_t)k1, p.bias.M, p.causal}, p.c, first, at, tb, left, right, lane);
+  }
+  float l = sm.sum[0] + swap_halves(sm.sum[0]);
+
+  T* og = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1];
+  if constexpr (NW == 1) {
+    sm.o[0].scale(l > 0.0f ? 1.0f / l : 0.0f, lane);
+    auto row = [&](int n) -> T* {
+      const uint32_t hh = (uint32_t)n / p.Lq;
+      return (uint32_t)n < p.cols ? og + at_row(hh, n - hh * p.Lq, p.os[2]) : nullptr;
+    };
+    if (p.vec) store_rows_lds<T, DC>(kl, sm.o[0], lane, D, row);
+    else store_rows<T, DC>(sm.o[0], lane, D, false, row);
+    if (p.lse && g == 0 && (uint32_t)l32 < p.cols)
+      p.lse[((uint64_t)bx * p.H + h0 + ch) * p.Lq + cq] = l > 0.0f ? kLn2 * (sm.ref[0] + log2f(l)) : -INFINITY;
+  } else {
+    // the waves' columns meet at the largest of their references, and are added in
+    // the waves' order
+    __syncthreads();
+    float* ms = tab;   // the table is done with: [NW][32] references, [NW][32] sums, [2][32] joined
+    if (g == 0) {
+      ms[wave * 32 + l32] = sm.ref[0];
+      ms[(NW + wave) * 32 + l32] = l;
+    }
+    __syncthreads();
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, ms[w * 32 + l32]);
+    const float base = top == -INFINITY ? 0.0f : top;
+    l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) l += __builtin_amdgcn_exp2f(ms[w * 32 + l32] - base) * ms[(NW + w) * 32 + l32];
+    sm.o[0].scale(__builtin_amdgcn_exp2f(sm.ref[0] - base), lane);
+    float* rows = reinterpret_cast<float*>(smem);   // [NW][32][DC]
+    store_rows<T, DC>(sm.o[0], lane, DC, true, [&](int n) -> float* {
+      return (uint32_t)n < p.cols ? rows + (wave * 32 + n) * DC : nullptr;
+    });
+    if (wave == 0 && g == 0) {
+      ms[2 * NW * 32 + l32] = top;
+      ms[(2 * NW + 1) * 32 + l32] = l;
+    }
+    __syncthreads();
+    float* part = p.part + (uint64_t)bid * p.cols * (2 + p.D);   // maxima, sums, rows
+    for (uint32_t i = threadIdx.x; i < p.cols * p.D; i += NW * 64) {
+      const uint32_t col = i / p.D, d = i - col * p.D;
+      float v = 0.0f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) v += rows[(w * 32 + col) * DC + d];
+      if (p.n_split > 1) {
+        part[2 * p.cols + i] = v;
+      } else {
+        const float s = ms[(2 * NW + 1) * 32 + col];
+        const uint32_t hh = col / p.Lq;
+        og[at_row(hh, col - hh * p.Lq, p.os[2]) + d] = (T)(s > 0.0f ? v / s : 0.0f);
+      }
+    }
+    if (threadIdx.x < p.cols) {
+      const float m = ms[2 * NW * 32 + threadIdx.x], s = ms[(2 * NW + 1) * 32 + threadIdx.x];
+      if (p.n_split > 1) part[threadIdx.x] = m, part[p.cols + threadIdx.x] = s;
+      else if (p.lse) {
+        const uint32_t hh = threadIdx.x / p.Lq;
+        p.lse[((uint64_t)bx * p.H + h0 + hh) * p.Lq + threadIdx.x - hh * p.Lq] =
+            s > 0.0f ? kLn2 * (m + log2f(s)) : -INFINITY;
+      }
+    }
+  }
+}
+
+// Joins the splits of one column: with their references m_s, sums l_s and rows o_s,
+// o = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.  A work-group per column; 256 / DP
+// groups of threads take every such split, and their sums are added in order.
+constexpr int kMaxSplit = 512;
+template <typename T, int DP>
+__global__ __launch_bounds__(256) void relpos_join_kernel(FwdParams p) {
+  constexpr int GR = 256 / DP;
+  __shared__ float f[kMaxSplit], red[256], m4[4];
+  const uint32_t unit = blockIdx.x / p.cols, col = blockIdx.x - unit * p.cols;
+  const uint32_t stride = p.cols * (2 + p.D);
   const float* w = p.part + (uint64_t)unit * p.n_split * stride;
   float m = -INFINITY;
-  for (uint32_t s = lane; s < p.n_split; s += 64) m = fmaxf(m, w[(uint64_t)s * stride + col]);
+  for (uint32_t s = threadIdx.x; s < p.n_split; s += 256) {
+    f[s] = w[(uint64_t)s * stride + col];
+    m = fmaxf(m, f[s]);
+  }
 #pragma unroll
   for (int off = 32; off; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  if ((threadIdx.x & 63) == 0) m4[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
   const float top = m == -INFINITY ? 0.0f : m;
-  float l = 0.0f, a0 = 0.0f, a1 = 0.0f;
-  for (uint32_t s = 0; s < p.n_split; ++s) {
-    const float* ws = w + (uint64_t)s * stride;
-    const float f = __builtin_amdgcn_exp2f(ws[col] - top);   // no keys: exp2(-inf) = 0
-    l += f * ws[32 + col];
-    const float* row = ws + 64 + col * p.D;
-    if (lane < p.D) a0 += f * row[lane];
-    if (lane + 64 < p.D) a1 += f * row[lane + 64];
+  for (uint32_t s = threadIdx.x; s < p.n_split; s += 256) f[s] = __builtin_amdgcn_exp2f(f[s] - top);   // no keys: 0
+  __syncthreads();
+  const uint32_t d = threadIdx.x % DP, gr = threadIdx.x / DP;
+  float a = 0.0f, l = 0.0f;
+  if (d < p.D) {
+#pragma unroll 4
+    for (uint32_t s = gr; s < p.n_split; s += GR) {
+      const float* ws = w + (uint64_t)s * stride;
+      l += f[s] * ws[p.cols + col];
+      a += f[s] * ws[2 * p.cols + col * p.D + d];
+    }
   }
-  const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+  red[threadIdx.x] = a;
+  __syncthreads();
+  if (gr == 0) {
+#pragma unroll
+    for (int i = 1; i < GR; ++i) a += red[i * DP + d];
+  }
+  __syncthreads();
+  red[threadIdx.x] = l;
+  __syncthreads();
+  if (gr || d >= p.D) return;
+#pragma unroll
+  for (int i = 1; i < GR; ++i) l += red[i * DP + d];
   const uint32_t kvh = p.H / p.grp, bx = unit / kvh, hh = col / p.Lq, i = col - hh * p.Lq;
   const uint32_t h = unit % kvh * p.grp + hh, b = bx / p.X, x = bx % p.X;
-  T* o = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)i * p.os[2] + (int64_t)h * p.D;
-  if (lane < p.D) o[lane] = (T)(a0 * inv);
-  if (lane + 64 < p.D) o[lane + 64] = (T)(a1 * inv);
-  if (p.lse && lane == 0) p.lse[((uint64_t)bx * p.H + h) * p.Lq + i] = l > 0.0f ? kLn2 * (top + log2f(l)) : -INFINITY;
+  static_cast<T*>(p.o)[(int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)i * p.os[2] + (int64_t)h * p.D + d] =
+      (T)(l > 0.0f ? a / l : 0.0f);
+  if (p.lse && d == 0) p.lse[((uint64_t)bx * p.H + h) * p.Lq + i] = l > 0.0f ? kLn2 * (top + log2f(l)) : -INFINITY;
 }
 
 struct Choice {
-  bool pack;
+  bool few;
   int64_t n_split, split_keys;
 };
 
-// Packed columns and split keys: the queries of a group share a block of 32 columns
-// where they fit in one, and the keys are cut while there are fewer work-groups than
-// the chip holds at once, into pieces of at least 256 keys.
+// The few-queries form where a group's queries fit the 32 columns of a block.  Its keys
+// are cut while there are fewer work-groups than 8 for each CU (lengths differ, so more
+// than the chip holds at once), into pieces of at least 256 keys.
 Choice choose(const RelposArgs& a) {
   Choice c = {};
   const int64_t grp = a.H / a.Hkv;
   c.n_split = 1;
   c.split_keys = a.Lk;
-  c.pack = a.Lq * grp <= 32 && a.Lq > 0;
-  if (!c.pack) return c;
-  const int64_t units = a.B * a.X * a.Hkv;
-  const int64_t want = (256 * 6 + units - 1) / units;
-  const int64_t n = std::min<int64_t>(std::min<int64_t>(want, (a.Lk + 255) / 256), 1024);
+  c.few = a.Lq * grp <= 32;
+  if (!c.few) return c;
+  const int64_t units = std::max<int64_t>(a.B * a.X * a.Hkv, 1);
+  const int64_t n = std::min<int64_t>({(256 * 8 + units - 1) / units, a.Lk / 256, kMaxSplit});
   if (n > 1) {
-    c.split_keys = ((a.Lk + n - 1) / n + 63) / 64 * 64;
+    c.split_keys = ((a.Lk + n - 1) / n + 127) / 128 * 128;
     c.n_split = (a.Lk + c.split_keys - 1) / c.split_keys;
   }
   return c;
 }
 
-template <typename T, int DC, int NW, int QT, int KB, int NBUF, int MINW>
-int start(FwdParams& p, const RelposArgs& a, const Choice& c, hipStream_t s) {
-  using G = Geo<T, DC>;
-  constexpr int QB = NW * 32 * QT;
-  const int64_t grp = a.H / a.Hkv;
-  p.n_qb = (uint32_t)((a.Lq + QB - 1) / QB);
-  if (p.cols) p.n_qb = 1;
-  const int64_t span = QB + (a.Lk + KB - 1) / KB * KB;
-  p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, span);
-  const size_t lds = (size_t)NBUF * 2 * KB * G::P * sizeof(T) + (size_t)p.tab * 4 * (p.cols ? grp : 1);
-  const int64_t blocks = a.B * a.X * (p.cols ? a.Hkv : a.H) * p.n_qb * p.n_split;
-  if (!grid_fits(blocks, NW * 64)) return DSP_ERR_SHAPE;
+template <typename K>
+int launch(K* kernel, int64_t blocks, int threads, size_t lds, FwdParams& p, hipStream_t s) {
+  if (!grid_fits(blocks, threads)) return DSP_ERR_SHAPE;
   p.n_blocks = (uint32_t)blocks;
-  auto* kernel = relpos_fwd_kernel<T, DC, NW, QT, KB, NBUF, MINW>;
   if (lds > 64 * 1024) {
     const hipError_t e =
         hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return DSP_ERR_HIP;
   }
-  kernel<<<dim3(p.n_blocks), NW * 64, lds, s>>>(p);
-  int st = last_launch_status();
+  kernel<<<dim3(p.n_blocks), threads, lds, s>>>(p);
+  return last_launch_status();
+}
+
+template <typename T, int DC, int NW, int QT, int KB, int NBUF, int MINW>
+int start_many(FwdParams& p, const RelposArgs& a, hipStream_t s) {
+  constexpr int QB = NW * 32 * QT;
+  p.n_qb = (uint32_t)((a.Lq + QB - 1) / QB);
+  p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, QB + (a.Lk + KB - 1) / KB * KB);
+  const size_t lds = (size_t)NBUF * 2 * KB * Geo<T, DC>::P * sizeof(T) + (size_t)p.tab * 4;
+  return launch(relpos_fwd_kernel<T, DC, NW, QT, KB, NBUF, MINW>, a.B * a.X * a.H * p.n_qb, NW * 64, lds, p, s);
+}
+
+template <typename T, int DC, int NW>
+int start_few(FwdParams& p, const RelposArgs& a, hipStream_t s) {
+  p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, 32 + ((int64_t)p.split_keys + 31) / 32 * 32);
+  const size_t tab = std::max<size_t>((size_t)p.tab * p.grp, (2 * NW + 2) * 32);
+  const size_t lds = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T) + tab * 4;
+  int st = launch(relpos_few_kernel<T, DC, NW, sizeof(T) == 2 ? (DC <= 80 ? 3 : 2) : 1>, a.B * a.X * a.Hkv * p.n_split, NW * 64, lds, p, s);
   if (st != DSP_OK || p.n_split == 1) return st;
-  const int64_t cols = a.B * a.X * a.Hkv * p.cols;
-  relpos_join_kernel<T><<<dim3((uint32_t)((cols + 3) / 4)), 256, 0, s>>>(p, (uint32_t)cols);
+  const int64_t cols = a.B * a.X * a.Hkv * p.cols;   // few units: they are why the keys are split
+  if (a.D <= 64) relpos_join_kernel<T, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p);
+  else relpos_join_kernel<T, 128><<<dim3((uint32_t)cols), 256, 0, s>>>(p);
   return last_launch_status();
 }
 
 template <typename T, int DC>
-int start_class(FwdParams& p, const RelposArgs& a, const Choice& c, hipStream_t s) {
-  if (a.Lq <= 32 || p.cols) return start<T, DC, 1, 1, 32, 2, 1>(p, a, c, s);
-  return start<T, DC, 4, 1, 32, 2, 1>(p, a, c, s);
+int start(FwdParams& p, const RelposArgs& a, hipStream_t s) {
+  if (p.cols) {
+    if (a.Lk <= 32) return start_few<T, DC, 1>(p, a, s);
+    if (a.Lk <= 64) return start_few<T, DC, 2>(p, a, s);
+    return start_few<T, DC, 4>(p, a, s);
+  }
+  constexpr bool B16 = sizeof(T) == 2;
+  if (a.Lq <= 64 && a.Lk <= 64) return start_many<T, DC, 2, 1, 64, 1, 1>(p, a, s);
+  if (a.Lq <= 128) return start_many<T, DC, 4, 1, B16 ? 64 : 32, 2, 1>(p, a, s);
+  return start_many<T, DC, B16 ? 8 : 4, B16 && DC <= 96 ? 2 : 1, B16 ? 64 : 32, 2, B16 ? 2 : 1>(p, a, s);
 }
 
 }  // namespace
@@ -369,27 +582,27 @@ int launch_attn_relpos(const RelposArgs& a, hipStream_t s) {
   for (int i = 0; i < 3; ++i) p.qs[i] = a.q_strides[i], p.ks[i] = a.kv_strides[i], p.os[i] = a.o_strides[i];
   p.bias = {a.bias, a.buckets, a.max_dist, a.n_buckets};
   p.X = (uint32_t)a.X, p.H = a.H, p.grp = a.H / a.Hkv, p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk, p.D = a.D;
-  p.cols = c.pack ? (uint32_t)(a.Lq * p.grp) : 0;
+  p.cols = c.few ? (uint32_t)(a.Lq * p.grp) : 0;
   p.n_split = (uint32_t)c.n_split, p.split_keys = (uint32_t)c.split_keys;
   p.c = a.scale * kLog2e;
-  p.vec = a.vec, p.vec_o = a.vec, p.causal = a.causal;
+  p.vec = a.vec, p.causal = a.causal;
   if (a.bf16) {
-    if (a.D <= 32) return start_class<bf16, 32>(p, a, c, s);
-    if (a.D <= 48) return start_class<bf16, 48>(p, a, c, s);
-    if (a.D <= 64) return start_class<bf16, 64>(p, a, c, s);
-    if (a.D <= 80) return start_class<bf16, 80>(p, a, c, s);
-    if (a.D <= 96) return start_class<bf16, 96>(p, a, c, s);
-    return start_class<bf16, 128>(p, a, c, s);
+    if (a.D <= 32) return start<bf16, 32>(p, a, s);
+    if (a.D <= 48) return start<bf16, 48>(p, a, s);
+    if (a.D <= 64) return start<bf16, 64>(p, a, s);
+    if (a.D <= 80) return start<bf16, 80>(p, a, s);
+    if (a.D <= 96) return start<bf16, 96>(p, a, s);
+    return start<bf16, 128>(p, a, s);
   }
-  if (a.D <= 32) return start_class<float, 32>(p, a, c, s);
-  if (a.D <= 64) return start_class<float, 64>(p, a, c, s);
-  if (a.D <= 96) return start_class<float, 96>(p, a, c, s);
-  return start_class<float, 128>(p, a, c, s);
+  if (a.D <= 32) return start<float, 32>(p, a, s);
+  if (a.D <= 64) return start<float, 64>(p, a, s);
+  if (a.D <= 96) return start<float, 96>(p, a, s);
+  return start<float, 128>(p, a, s);
 }
 
 size_t attn_relpos_workspace_bytes(const RelposArgs& a) {
   const Choice c = choose(a);
-  return c.n_split > 1 ? (size_t)(a.B * a.X * a.Hkv * c.n_split) * (64 + 32 * (size_t)a.D) * 4 : 0;
+  return c.n_split > 1 ? (size_t)(a.B * a.X * a.H * c.n_split * a.Lq) * (2 + (size_t)a.D) * 4 : 0;
 }
 
 }  // namespace dsp

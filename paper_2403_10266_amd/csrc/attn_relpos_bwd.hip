@@ -76,12 +76,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
   const int D = (int)p.D;
   const uint32_t row_bytes = (uint32_t)p.ks[2] * (uint32_t)sizeof(T);
   using TileT = Tile<T, DC, KB, NT>;
-  const typename TileT::Map map = TileT::map(D, row_bytes);
+  const typename TileT::Map map = TileT::map(D, row_bytes, threadIdx.x);
   TileT tk, tv;
 
   for (int32_t e = threadIdx.x; e < n_tab; e += NT) tab[e] = bias_at<T>(p.bias, p.H, h, e - near);
   for (int32_t e = threadIdx.x; e < 2 * NW * n_tab; e += NT) acc[e] = 0.0f;
-  clear_pad<T, DC>(lds, 4 * KB, D, NT);
+  clear_pad<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
   const float left = bias_at<T>(p.bias, p.H, h, -p.bias.M), right = bias_at<T>(p.bias, p.H, h, p.bias.M);
   float* mine = acc + (2 * wave + g) * n_tab + near;
   float sum_l = 0.0f, sum_r = 0.0f;
@@ -103,12 +103,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
     }
     auto fetch = [&](uint32_t kb) {
       const uint32_t rows = kb < k1 ? min(k1 - kb, (uint32_t)KB) : 0u;
-      tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
-      tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
+      tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
+      tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
     };
     auto stash = [&](int buf) {
-      tk.stash(map, lds + buf * 2 * TILE);
-      tv.stash(map, lds + buf * 2 * TILE + TILE);
+      tk.stash(map, lds + buf * 2 * TILE, threadIdx.x);
+      tv.stash(map, lds + buf * 2 * TILE + TILE, threadIdx.x);
     };
     if (k1) fetch(0);
     const uint32_t row = blk * QB + 32 * wave + l32;
@@ -291,10 +291,10 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
 
   const uint32_t q_row = (uint32_t)p.qs[2] * (uint32_t)sizeof(T), o_row = (uint32_t)p.os[2] * (uint32_t)sizeof(T);
   using TileT = Tile<T, DC, QB, NT>;
-  const typename TileT::Map mq = TileT::map(D, q_row), mo = TileT::map(D, o_row);
+  const typename TileT::Map mq = TileT::map(D, q_row, threadIdx.x), mo = TileT::map(D, o_row, threadIdx.x);
   TileT tq, to;
   float pre = 0.0f;
-  clear_pad<T, DC>(lds, 4 * QB, D, NT);
+  clear_pad<T, DC>(lds, 4 * QB, D, threadIdx.x, NT);
 
   ColAcc<T, DC> dk, dv;
   dk.zero();
@@ -312,8 +312,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
     const float left = bias_at<T>(p.bias, p.H, h, -p.bias.M), right = bias_at<T>(p.bias, p.H, h, p.bias.M);
     auto fetch = [&](uint32_t it) {
       const uint32_t q0 = it * QB, rows = min(p.Lq - q0, (uint32_t)QB);
-      tq.fetch(mq, qg + (int64_t)q0 * p.qs[2], rows, q_row, D, p.vec);
-      to.fetch(mo, og + (int64_t)q0 * p.os[2], rows, o_row, D, p.vec);
+      tq.fetch(mq, qg + (int64_t)q0 * p.qs[2], rows, q_row, D, p.vec, threadIdx.x);
+      to.fetch(mo, og + (int64_t)q0 * p.os[2], rows, o_row, D, p.vec, threadIdx.x);
       if (threadIdx.x < 2 * QB) {
         const uint32_t i = threadIdx.x % QB;
         const bool is_delta = threadIdx.x >= QB;
@@ -322,8 +322,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
       }
     };
     auto stash = [&](int buf) {
-      tq.stash(mq, lds + buf * 2 * TILE);
-      to.stash(mo, lds + buf * 2 * TILE + TILE);
+      tq.stash(mq, lds + buf * 2 * TILE, threadIdx.x);
+      to.stash(mo, lds + buf * 2 * TILE + TILE, threadIdx.x);
       if (threadIdx.x < 2 * QB) stat[buf * 2 * QB + threadIdx.x] = pre;
     };
     fetch(it0);
