@@ -323,7 +323,7 @@ __device__ __forceinline__ float bias_at(const BiasArgs& b, uint32_t H, uint32_t
 // first keys and the biases after them, so that neither wait is added to the keys'.
 template <typename T, int NT>
 struct Table {
-  static constexpr int N = 2;
+  static constexpr int N = NT < 128 ? 4 : 2;
   int32_t k[N];
   __device__ __forceinline__ void fetch(const BiasArgs& b, int32_t lo, int32_t n) {
 #pragma unroll
@@ -334,17 +334,24 @@ struct Table {
   }
   __device__ __forceinline__ void build(const BiasArgs& b, int32_t lo, int32_t n, float* tab, uint32_t stride,
                                         uint32_t H, uint32_t h0, uint32_t nh) const {
-    for (uint32_t hh = 0; hh < nh; ++hh) {
-      float v[N];
+    for (uint32_t h4 = 0; h4 < nh; h4 += 4) {   // four heads' loads at a time
+      float v[4][N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = bias_of<T>(b, H, h0 + hh, k[i]);
+      for (int q = 0; q < 4; ++q)
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int32_t t = (int32_t)threadIdx.x + i * NT;
-        if (t < n) tab[hh * stride + t] = v[i];
-      }
-      for (int32_t t = (int32_t)threadIdx.x + N * NT; t < n; t += NT)
-        tab[hh * stride + t] = bias_at<T>(b, H, h0 + hh, lo + t);
+        for (int i = 0; i < N; ++i)
+          v[q][i] = h4 + q < nh ? bias_of<T>(b, H, h0 + h4 + q, k[i]) : 0.0f;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int32_t t = (int32_t)threadIdx.x + i * NT;
+          if (t < n && h4 + q < nh) tab[(h4 + q) * stride + t] = v[q][i];
+        }
+    }
+    for (int32_t t = (int32_t)threadIdx.x + N * NT; t < n; t += NT) {
+      const int32_t far = bucket_at(b, lo + t);
+      for (uint32_t hh = 0; hh < nh; ++hh) tab[hh * stride + t] = bias_of<T>(b, H, h0 + hh, far);
     }
   }
 };

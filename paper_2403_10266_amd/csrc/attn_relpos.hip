@@ -80,8 +80,8 @@ struct Softmax {
   };
 
   // scores of the tile in exp2 units, less `minus`
-  template <typename Q>
-  static __device__ __forceinline__ void scores(floatx16 (&s)[NKT][QT], const T* kl, const Q& qf, const Keys& k, float c,
+  template <typename KF, typename Q>
+  static __device__ __forceinline__ void scores(floatx16 (&s)[NKT][QT], const KF& kf, const Q& qf, const Keys& k, float c,
                                          const int32_t (&first)[QT], const int32_t (&at)[QT],
                                          const float* const (&tab)[QT], const float (&left)[QT],
                                          const float (&right)[QT], const float (&minus)[QT], int lane) {
@@ -96,8 +96,7 @@ struct Softmax {
     for (int st = 0; st < G::NS; ++st)
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt) {
-        const auto a =
-            *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
+        const auto a = kf(kt, st);
 #pragma unroll
         for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(a, qf[j][st], s[kt][j]);
       }
@@ -125,10 +124,11 @@ struct Softmax {
       }
   }
 
-  // One tile: first[j] is the position of block j's first query, at[j] of this lane's
-  // own, tab[j] the table at its distance from key 0.
-  template <typename Q>
-  __device__ __forceinline__ void step(const T* kl, const T* vl, const Q& qf, const Keys& k, float c,
+  // One tile: kf(kt, st) the fragments of its keys, vl its values in LDS; first[j] is the
+  // position of block j's first query, at[j] of this lane's own, tab[j] the table at
+  // its distance from key 0.
+  template <typename KF, typename Q>
+  __device__ __forceinline__ void step(const KF& kf, const T* vl, const Q& qf, const Keys& k, float c,
                                        const int32_t (&first)[QT], const int32_t (&at)[QT],
                                        const float* const (&tab)[QT], const float (&left)[QT],
                                        const float (&right)[QT], int lane) {
@@ -137,7 +137,7 @@ struct Softmax {
     bool move = !LAZY || !set;
     if (LAZY && set) {
       floatx16 s[NKT][QT];
-      scores(s, kl, qf, k, c, first, at, tab, left, right, ref, lane);
+      scores(s, kf, qf, k, c, first, at, tab, left, right, ref, lane);
       move = probabilities(s, pf, add);
     }
     if (!LAZY || __any(move)) {
@@ -146,7 +146,7 @@ struct Softmax {
       float zero[QT];
 #pragma unroll
       for (int j = 0; j < QT; ++j) zero[j] = 0.0f;
-      scores(s, kl, qf, k, c, first, at, tab, left, right, zero, lane);
+      scores(s, kf, qf, k, c, first, at, tab, left, right, zero, lane);
       bool all = true;
 #pragma unroll
       for (int j = 0; j < QT; ++j) {
@@ -289,8 +289,11 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
     const T* kl = lds + (NBUF > 1 ? (it & 1) : 0) * 2 * TILE;
     // queries of this wave are all before the tile, or past the end: nothing to do
     if (!(p.causal && (int32_t)kb > wq + 32 * QT - 1) && 32u * QT * wave < nq)
-      sm.step(kl, kl + TILE, qf, {(int32_t)kb, (int32_t)k1, p.bias.M, p.causal}, p.c, first, at, tb, left,
-              right, lane);
+      sm.step(
+          [&](int kt, int st) {
+            return *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
+          },
+          kl + TILE, qf, {(int32_t)kb, (int32_t)k1, p.bias.M, p.causal}, p.c, first, at, tb, left, right, lane);
     if (more) stash((it + 1) & 1);
     __syncthreads();
   }
@@ -310,10 +313,13 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
 }
 
 // Few queries: the queries of a key/value head's group (at most 32 in all) are the
-// columns of one block.  Each wave takes every NW-th tile of 32 keys through LDS rows
-// of its own, with no barrier until the waves' sums are joined; the whole chip's loads
-// are in flight at once, which is what bounds a pass over a cache.
-template <typename T, int DC, int NW, int MINW>
+// columns of one block.  Each wave takes every NW-th tile of 32 keys through LDS rows of
+// its own, with no barrier until the waves' sums are joined.  A pass over a cache is
+// bound by memory: what counts is how many waves a CU holds, that each has its next
+// tile on its way, and that every load runs along rows (the operands' own layout,
+// loaded directly, asks L2 for each line four times: 61 -> 81 us for the token
+// against long caches).  ONE: the keys are one tile.
+template <typename T, int DC, int NW, bool ONE, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) {
   using G = Geo<T, DC>;
   using M = Mx<T>;
@@ -356,15 +362,37 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
   const int32_t n_tab = k0 < k1 ? hi - lo + 1 : 0;
   Table<T, NW * 64> table;
   table.fetch(p.bias, lo, n_tab);
-  const uint32_t mine = k0 + 32 * wave;
-  if (mine < k1) fetch(mine);
-
   // this lane's column: head ch of the group, query cq
   const uint32_t ch = min(l32 / p.Lq, p.grp - 1), cq = l32 - ch * p.Lq;
   const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.qs[0] + (int64_t)x * p.qs[1];
   auto at_row = [&](uint32_t hh, uint32_t i, int64_t rs) { return (int64_t)i * rs + (int64_t)(h0 + hh) * D; };
+  // the columns' rows, on their way to LDS like the keys'
+  u32x4 qp[TileT::N];
+  const uint32_t chunks = (uint32_t)(D / G::E);
+  if (p.vec)
+#pragma unroll
+    for (int i = 0; i < TileT::N; ++i) {
+      const uint32_t c = lane + 64 * i, col = c / chunks, hh = col / p.Lq;
+      if (col < p.cols)
+        qp[i] = *reinterpret_cast<const u32x4*>(qg + at_row(hh, col - hh * p.Lq, p.qs[2]) + (c - col * chunks) * G::E);
+    }
+  const uint32_t mine = k0 + 32 * wave;
+  if (mine < k1) fetch(mine);
+  clear_pad<T, DC>(kl, 64, D, lane, 64);
   typename M::frag qf[1][G::NS];
-  row_frags<T, DC>((uint32_t)l32 < p.cols ? qg + at_row(ch, cq, p.qs[2]) : nullptr, g, D, p.vec, qf[0]);
+  if (p.vec) {
+#pragma unroll
+    for (int i = 0; i < TileT::N; ++i) {
+      const uint32_t c = lane + 64 * i, col = c / chunks;
+      if (col < p.cols) *reinterpret_cast<u32x4*>(vl + col * G::P + (c - col * chunks) * G::E) = qp[i];
+    }
+    // columns past the last hold what the LDS held: their results are dropped
+#pragma unroll
+    for (int st = 0; st < G::NS; ++st)
+      qf[0][st] = *reinterpret_cast<const typename M::frag*>(vl + l32 * G::P + 2 * G::E * st + G::E * g);
+  } else {
+    row_frags<T, DC>((uint32_t)l32 < p.cols ? qg + at_row(ch, cq, p.qs[2]) : nullptr, g, D, false, qf[0]);
+  }
   table.build(p.bias, lo, n_tab, tab, p.tab, p.H, h0, p.grp);
   const float left[1] = {bias_at<T>(p.bias, p.H, h0 + ch, -p.bias.M)};
   const float right[1] = {bias_at<T>(p.bias, p.H, h0 + ch, p.bias.M)};
@@ -373,13 +401,17 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
 
   Softmax<T, DC, 1, 1, false> sm;
   sm.init();
-  clear_pad<T, DC>(kl, 64, D, lane, 64);
   __syncthreads();   // the table
   for (uint32_t kb = mine; kb < k1; kb += 32 * NW) {
     tk.stash(map, kl, lane);
     tv.stash(map, vl, lane);
-    if (kb + 32 * NW < k1) fetch(kb + 32 * NW);
-    sm.step(kl, vl, qf, {(int32_t)kb, (int32_t)k1, p.bias.M, p.causal}, p.c, first, at, tb, left, right, lane);
+    if (!ONE && kb + 32 * NW < k1) fetch(kb + 32 * NW);
+    sm.step(
+        [&](int, int st) {
+          return *reinterpret_cast<const typename M::frag*>(kl + l32 * G::P + 2 * G::E * st + G::E * g);
+        },
+        vl, qf, {(int32_t)kb, (int32_t)k1, p.bias.M, p.causal}, p.c, first, at, tb, left, right, lane);
+    if (ONE) break;
   }
   float l = sm.sum[0] + swap_halves(sm.sum[0]);
 
@@ -390,15 +422,15 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
       const uint32_t hh = (uint32_t)n / p.Lq;
       return (uint32_t)n < p.cols ? og + at_row(hh, n - hh * p.Lq, p.os[2]) : nullptr;
     };
-    if (p.vec) store_rows_lds<T, DC>(kl, sm.o[0], lane, D, row);
+    if (p.vec) store_rows_lds<T, DC>(vl, sm.o[0], lane, D, row);
     else store_rows<T, DC>(sm.o[0], lane, D, false, row);
     if (p.lse && g == 0 && (uint32_t)l32 < p.cols)
       p.lse[((uint64_t)bx * p.H + h0 + ch) * p.Lq + cq] = l > 0.0f ? kLn2 * (sm.ref[0] + log2f(l)) : -INFINITY;
   } else {
     // the waves' columns meet at the largest of their references, and are added in
-    // the waves' order
+    // the waves' order; the tiles and the table are done with
     __syncthreads();
-    float* ms = tab;   // the table is done with: [NW][32] references, [NW][32] sums, [2][32] joined
+    float* ms = reinterpret_cast<float*>(smem);   // [NW][32] references, [NW][32] sums, [2][32] joined
     if (g == 0) {
       ms[wave * 32 + l32] = sm.ref[0];
       ms[(NW + wave) * 32 + l32] = l;
@@ -412,9 +444,9 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
 #pragma unroll
     for (int w = 0; w < NW; ++w) l += __builtin_amdgcn_exp2f(ms[w * 32 + l32] - base) * ms[(NW + w) * 32 + l32];
     sm.o[0].scale(__builtin_amdgcn_exp2f(sm.ref[0] - base), lane);
-    float* rows = reinterpret_cast<float*>(smem);   // [NW][32][DC]
+    float* rows = ms + (2 * NW + 2) * 32;   // [NW][cols][DC]
     store_rows<T, DC>(sm.o[0], lane, DC, true, [&](int n) -> float* {
-      return (uint32_t)n < p.cols ? rows + (wave * 32 + n) * DC : nullptr;
+      return (uint32_t)n < p.cols ? rows + (wave * p.cols + n) * DC : nullptr;
     });
     if (wave == 0 && g == 0) {
       ms[2 * NW * 32 + l32] = top;
@@ -426,7 +458,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
       const uint32_t col = i / p.D, d = i - col * p.D;
       float v = 0.0f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) v += rows[(w * 32 + col) * DC + d];
+      for (int w = 0; w < NW; ++w) v += rows[(w * p.cols + col) * DC + d];
       if (p.n_split > 1) {
         part[2 * p.cols + i] = v;
       } else {
@@ -546,12 +578,13 @@ int start_many(FwdParams& p, const RelposArgs& a, hipStream_t s) {
   return launch(relpos_fwd_kernel<T, DC, NW, QT, KB, NBUF, MINW>, a.B * a.X * a.H * p.n_qb, NW * 64, lds, p, s);
 }
 
-template <typename T, int DC, int NW>
+template <typename T, int DC, int NW, bool ONE>
 int start_few(FwdParams& p, const RelposArgs& a, hipStream_t s) {
+  constexpr int MINW = sizeof(T) == 4 ? 1 : ONE ? (DC <= 80 ? 4 : 3) : DC <= 80 ? 3 : 2;
   p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, 32 + ((int64_t)p.split_keys + 31) / 32 * 32);
-  const size_t tab = std::max<size_t>((size_t)p.tab * p.grp, (2 * NW + 2) * 32);
-  const size_t lds = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T) + tab * 4;
-  int st = launch(relpos_few_kernel<T, DC, NW, sizeof(T) == 2 ? (DC <= 80 ? 3 : 2) : 1>, a.B * a.X * a.Hkv * p.n_split, NW * 64, lds, p, s);
+  size_t lds = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T) + (size_t)p.tab * p.grp * 4;
+  if (NW > 1) lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * p.cols * DC) * 4);
+  int st = launch(relpos_few_kernel<T, DC, NW, ONE, MINW>, a.B * a.X * a.Hkv * p.n_split, NW * 64, lds, p, s);
   if (st != DSP_OK || p.n_split == 1) return st;
   const int64_t cols = a.B * a.X * a.Hkv * p.cols;   // few units: they are why the keys are split
   if (a.D <= 64) relpos_join_kernel<T, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p);
@@ -562,9 +595,12 @@ int start_few(FwdParams& p, const RelposArgs& a, hipStream_t s) {
 template <typename T, int DC>
 int start(FwdParams& p, const RelposArgs& a, hipStream_t s) {
   if (p.cols) {
-    if (a.Lk <= 32) return start_few<T, DC, 1>(p, a, s);
-    if (a.Lk <= 64) return start_few<T, DC, 2>(p, a, s);
-    return start_few<T, DC, 4>(p, a, s);
+    // a wave per unit where the units alone fill the chip
+    const bool full = a.B * a.X * a.Hkv >= 256 * 12;
+    if (a.Lk <= 32) return start_few<T, DC, 1, true>(p, a, s);
+    if (full) return start_few<T, DC, 1, false>(p, a, s);
+    if (a.Lk <= 64) return start_few<T, DC, 2, true>(p, a, s);
+    return start_few<T, DC, 4, false>(p, a, s);
   }
   constexpr bool B16 = sizeof(T) == 2;
   if (a.Lq <= 64 && a.Lk <= 64) return start_many<T, DC, 2, 1, 64, 1, 1>(p, a, s);
