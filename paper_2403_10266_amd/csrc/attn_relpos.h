@@ -300,6 +300,56 @@ __device__ __forceinline__ void clear_pad(T* lds, int rows, int D, int tid, int 
   for (int e = tid; e < rows * w; e += nt) lds[e / w * G::P + d0 + e % w] = (T)0.0f;
 }
 
+// Which work-group does what.  Work-group i runs on XCD i % 8, each with an L2 of its
+// own.  Work comes in chunks that share cached rows: the heads of one key/value head's
+// group, or of a whole token row where a unit has few blocks (heads lie side by side in
+// a row's cache lines).  Chunk c goes to XCD c % 8, so that sequences of different
+// lengths spread over all of them.  A chunk's blocks follow each other; where the
+// blocks differ in cost (causal masks) every chunk's most costly ones come first.
+struct Order {
+  uint32_t n_chunks, per_xcd;   // chunks in all, and (rounded up) of an XCD
+  uint32_t heads, blocks;       // of a chunk: heads, blocks of each head
+  uint32_t chunks_bx;           // chunks of one (b, x)
+  bool costly_first;
+};
+inline Order make_order(int64_t bx, int64_t groups, int64_t grp, int64_t blocks, bool costly_first) {
+  const int64_t rows = blocks <= 2 && bx >= 64 ? groups : 1;   // key/value heads of a chunk
+  Order o;
+  o.chunks_bx = (uint32_t)(groups / rows);
+  o.n_chunks = (uint32_t)(bx * o.chunks_bx);
+  o.per_xcd = (o.n_chunks + 7) / 8;
+  o.heads = (uint32_t)(rows * grp);
+  o.blocks = (uint32_t)blocks;
+  o.costly_first = costly_first;
+  return o;
+}
+inline int64_t order_blocks(const Order& o) { return (int64_t)8 * o.per_xcd * o.heads * o.blocks; }
+struct Place {
+  uint32_t bx, h, block;   // block 0 is the most costly
+  bool any;                // the grid is rounded up: nothing to do
+};
+__device__ __forceinline__ Place place(const Order& o) {
+  const uint32_t xcd = blockIdx.x & 7u, j = blockIdx.x >> 3;
+  Place p;
+  uint32_t local, head;
+  if (o.costly_first) {
+    const uint32_t n = o.per_xcd * o.heads, r = j % n;
+    p.block = j / n;
+    local = r / o.heads;
+    head = r - local * o.heads;
+  } else {
+    const uint32_t n = o.heads * o.blocks, r = j % n;
+    local = j / n;
+    head = r / o.blocks;
+    p.block = r - head * o.blocks;
+  }
+  const uint32_t chunk = local * 8 + xcd;
+  p.any = chunk < o.n_chunks;
+  p.bx = chunk / o.chunks_bx;
+  p.h = (chunk - p.bx * o.chunks_bx) * o.heads + head;
+  return p;
+}
+
 struct BiasArgs {
   const void* bias;        // [n_buckets][H]
   const int32_t* buckets;  // [2 M + 1]

@@ -41,7 +41,9 @@ struct FwdParams {
   const int32_t* kv_len;
   int64_t qs[3], ks[3], os[3];
   BiasArgs bias;
-  uint32_t X, H, grp, Lq, Lk, n_qb, n_split, split_keys, n_blocks, D;
+  uint32_t X, H, grp, Lq, Lk, n_split, split_keys, D;
+  Order order;       // many queries
+  uint32_t pieces;   // few queries: (b, x) times splits
   uint32_t tab;      // distances of the LDS table, for each head of a work-group
   uint32_t cols;     // few queries: queries x heads of a group
   float c;           // scale * log2(e)
@@ -215,13 +217,11 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
 
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // work-group -> (unit, query block); each XCD takes a contiguous range
-  uint32_t bid = blockIdx.x;
-  if ((p.n_blocks & 7u) == 0) bid = (bid & 7u) * (p.n_blocks >> 3) + (bid >> 3);
-  const uint32_t unit = bid / p.n_qb;
-  // causal: the last query blocks have the most keys and start first
-  const uint32_t qb = p.causal ? p.n_qb - 1 - bid % p.n_qb : bid % p.n_qb;
-  const uint32_t bx = unit / p.H, h = unit % p.H, b = bx / p.X, x = bx % p.X;
+  const Place pl = place(p.order);
+  if (!pl.any) return;
+  // causal: the last queries have the most keys
+  const uint32_t bx = pl.bx, h = pl.h, qb = p.causal ? p.order.blocks - 1 - pl.block : pl.block;
+  const uint32_t b = bx / p.X, x = bx % p.X;
   const int D = (int)p.D;
   const int64_t k_at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)(h / p.grp) * D;
   const T* kg = static_cast<const T*>(p.k) + k_at;
@@ -331,10 +331,10 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
   T* vl = kl + TILE;
   float* tab = reinterpret_cast<float*>(reinterpret_cast<T*>(smem) + NW * 2 * TILE);
 
-  uint32_t bid = blockIdx.x;
-  if ((p.n_blocks & 7u) == 0) bid = (bid & 7u) * (p.n_blocks >> 3) + (bid >> 3);
-  const uint32_t unit = bid / p.n_split, split = bid - unit * p.n_split;
-  const uint32_t kvh = p.H / p.grp, bx = unit / kvh, e = unit - bx * kvh, h0 = e * p.grp;
+  // an XCD takes the heads of a stretch of keys, which together read whole token rows
+  const uint32_t kvh = p.H / p.grp, j8 = blockIdx.x >> 3, piece = j8 / kvh * 8 + (blockIdx.x & 7u);
+  if (piece >= p.pieces) return;
+  const uint32_t e = j8 % kvh, split = piece % p.n_split, bx = piece / p.n_split, h0 = e * p.grp;
   const uint32_t b = bx / p.X, x = bx - b * p.X;
   const int D = (int)p.D;
   const int64_t k_at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)e * D;
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
       ms[(2 * NW + 1) * 32 + l32] = l;
     }
     __syncthreads();
-    float* part = p.part + (uint64_t)bid * p.cols * (2 + p.D);   // maxima, sums, rows
+    float* part = p.part + ((uint64_t)(bx * kvh + e) * p.n_split + split) * p.cols * (2 + p.D);   // maxima, sums, rows
     for (uint32_t i = threadIdx.x; i < p.cols * p.D; i += NW * 64) {
       const uint32_t col = i / p.D, d = i - col * p.D;
       float v = 0.0f;
@@ -559,32 +559,33 @@ Choice choose(const RelposArgs& a) {
 template <typename K>
 int launch(K* kernel, int64_t blocks, int threads, size_t lds, FwdParams& p, hipStream_t s) {
   if (!grid_fits(blocks, threads)) return DSP_ERR_SHAPE;
-  p.n_blocks = (uint32_t)blocks;
   if (lds > 64 * 1024) {
     const hipError_t e =
         hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (e != hipSuccess) return DSP_ERR_HIP;
   }
-  kernel<<<dim3(p.n_blocks), threads, lds, s>>>(p);
+  kernel<<<dim3((uint32_t)blocks), threads, lds, s>>>(p);
   return last_launch_status();
 }
 
 template <typename T, int DC, int NW, int QT, int KB, int NBUF, int MINW>
 int start_many(FwdParams& p, const RelposArgs& a, hipStream_t s) {
   constexpr int QB = NW * 32 * QT;
-  p.n_qb = (uint32_t)((a.Lq + QB - 1) / QB);
+  p.order = make_order(a.B * a.X, a.Hkv, a.H / a.Hkv, (a.Lq + QB - 1) / QB, a.causal);
   p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, QB + (a.Lk + KB - 1) / KB * KB);
   const size_t lds = (size_t)NBUF * 2 * KB * Geo<T, DC>::P * sizeof(T) + (size_t)p.tab * 4;
-  return launch(relpos_fwd_kernel<T, DC, NW, QT, KB, NBUF, MINW>, a.B * a.X * a.H * p.n_qb, NW * 64, lds, p, s);
+  return launch(relpos_fwd_kernel<T, DC, NW, QT, KB, NBUF, MINW>, order_blocks(p.order), NW * 64, lds, p, s);
 }
 
 template <typename T, int DC, int NW, bool ONE>
 int start_few(FwdParams& p, const RelposArgs& a, hipStream_t s) {
-  constexpr int MINW = sizeof(T) == 4 ? 1 : ONE ? (DC <= 80 ? 4 : 3) : DC <= 80 ? 3 : 2;
+  constexpr int MINW = sizeof(T) == 4 ? 1 : ONE ? (DC <= 80 ? 4 : DC <= 96 ? 3 : 2) : DC <= 80 ? 3 : 2;
   p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, 32 + ((int64_t)p.split_keys + 31) / 32 * 32);
   size_t lds = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T) + (size_t)p.tab * p.grp * 4;
   if (NW > 1) lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * p.cols * DC) * 4);
-  int st = launch(relpos_few_kernel<T, DC, NW, ONE, MINW>, a.B * a.X * a.Hkv * p.n_split, NW * 64, lds, p, s);
+  const int64_t pieces = a.B * a.X * p.n_split;
+  p.pieces = (uint32_t)pieces;
+  int st = launch(relpos_few_kernel<T, DC, NW, ONE, MINW>, (pieces + 7) / 8 * 8 * a.Hkv, NW * 64, lds, p, s);
   if (st != DSP_OK || p.n_split == 1) return st;
   const int64_t cols = a.B * a.X * a.Hkv * p.cols;   // few units: they are why the keys are split
   if (a.D <= 64) relpos_join_kernel<T, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p);
