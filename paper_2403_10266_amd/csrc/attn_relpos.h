@@ -50,12 +50,13 @@ struct Mx<float> {
 template <typename T, int DC>
 struct Geo {
   static constexpr int E = Mx<T>::E;
-  static constexpr int NS = DC / (2 * E);              // steps of a row product
-  static constexpr bool SLAB = DC % 32 != 0;           // bf16: last 16 columns on 16x16x32
-  static constexpr int NT = DC / 32;                   // 32-column tiles of a column product
-  static constexpr int P = DC + E;                     // LDS row pitch: an odd number of 16 bytes
+  static constexpr int DP = (DC + 15) / 16 * 16;       // columns the products take
+  static constexpr int NS = DP / (2 * E);              // steps of a row product
+  static constexpr bool SLAB = DP % 32 != 0;           // bf16: last 16 columns on 16x16x32
+  static constexpr int NT = DP / 32;                   // 32-column tiles of a column product
+  static constexpr int P = DP + E;                     // LDS row pitch: an odd number of 16 bytes
   static constexpr int CHM = DC / E;                   // 16-byte chunks of a row, at most
-  static_assert(DC % 16 == 0 && (!SLAB || E == 8), "class");
+  static_assert(DC % 8 == 0 && (!SLAB || E == 8), "class");
 };
 
 // A B operand of a column product made of a 32 x 32 accumulator
@@ -208,7 +209,7 @@ __device__ __forceinline__ void store_rows(const ColAcc<T, DC>& a, int lane, int
 template <typename T, int DC, typename F>
 __device__ __forceinline__ void store_rows_lds(T* so, const ColAcc<T, DC>& a, int lane, int D, F row_of) {
   using G = Geo<T, DC>;
-  store_rows<T, DC>(a, lane, DC, true, [&](int n) { return so + n * G::P; });
+  store_rows<T, DC>(a, lane, G::DP, true, [&](int n) { return so + n * G::P; });
   const int ch = D / G::E;   // whole chunks: the callers' rows are aligned
   int row = lane / ch, col = lane - row * ch;
   const int dr = 64 / ch, dc = 64 - dr * ch;
@@ -243,53 +244,53 @@ __device__ __forceinline__ void row_frags(const T* row, int g, int D, bool vec,
 
 // A tile of up to R rows of one tensor on its way from memory to LDS: NT threads (tid),
 // 16-byte chunks, rows past `rows` and columns past D as 0 (the columns are cleared
-// once, by clear_pad).  vec: whole chunks at 16-byte offsets; otherwise (fp32) an
-// element at a time.
+// once, by clear_pad).  A thread keeps to one column of chunks and takes every n-th
+// row, so its places are one offset and a scalar step.  vec: whole chunks at 16-byte
+// offsets; otherwise (fp32) an element at a time.
 template <typename T, int DC, int R, int NT>
 struct Tile {
   using G = Geo<T, DC>;
-  static constexpr int N = (R * G::CHM + NT - 1) / NT;
+  static constexpr int STEP = NT / G::CHM;               // rows of a pass, at least
+  static constexpr int N = (R + STEP - 1) / STEP;
   u32x4 pre[N];
 
   // where this thread's chunks lie: byte offset in the tensor's rows, element offset in LDS
   struct Map {
-    uint32_t at[N];
-    int to[N];
-    uint32_t n;  // chunks of a full tile
+    uint32_t at, row, step;   // step: rows of a pass
+    int to, col;
   };
   static __device__ __forceinline__ Map map(int D, uint32_t row_bytes, uint32_t tid) {
     Map m;
     const uint32_t ch = (uint32_t)(D + G::E - 1) / G::E;
-    m.n = R * ch;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t c = tid + i * NT;
-      const uint32_t row = c / ch, col = c - row * ch;
-      m.at[i] = row * row_bytes + col * 16u;
-      m.to[i] = (int)(row * G::P + col * G::E);
-    }
+    m.step = min(NT / ch, (uint32_t)R);
+    m.row = tid / ch;
+    const uint32_t col = tid - m.row * ch;
+    if (m.row >= m.step) m.row = R;   // a thread without chunks
+    m.at = m.row * row_bytes + col * 16u;
+    m.col = (int)(col * G::E);
+    m.to = (int)(m.row * G::P) + m.col;
     return m;
   }
   __device__ __forceinline__ void fetch(const Map& m, const T* base, uint32_t rows, uint32_t row_bytes, int D,
-                                        bool vec, uint32_t tid) {
+                                        bool vec) {
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, rows * row_bytes);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (tid + i * NT >= m.n) continue;
+      if (m.row + i * m.step >= R) continue;
+      const uint32_t skip = i * m.step * row_bytes;
       if (sizeof(T) == 2 || vec) {
-        pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, m.at[i], 0, 0);
+        pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, m.at, skip, 0);
       } else {
-        const int col = m.to[i] % G::P;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          pre[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, col + e < D ? m.at[i] + 4u * e : 0xFFFFFFF0u, 0, 0);
+          pre[i][e] = m.col + e < D ? __builtin_amdgcn_raw_buffer_load_b32(rs, m.at + 4u * e, skip, 0) : 0u;
       }
     }
   }
-  __device__ __forceinline__ void stash(const Map& m, T* lds, uint32_t tid) const {
+  __device__ __forceinline__ void stash(const Map& m, T* lds) const {
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (tid + i * NT < m.n) *reinterpret_cast<u32x4*>(lds + m.to[i]) = pre[i];
+      if (m.row + i * m.step < R) *reinterpret_cast<u32x4*>(lds + m.to + i * (int)m.step * G::P) = pre[i];
   }
 };
 // zero in columns D .. P - 1 of `rows` LDS rows (fp32: past the chunk that holds D - 1)

@@ -87,7 +87,7 @@ struct Softmax {
                                          const int32_t (&first)[QT], const int32_t (&at)[QT],
                                          const float* const (&tab)[QT], const float (&left)[QT],
                                          const float (&right)[QT], const float (&minus)[QT], int lane) {
-    const int l32 = lane & 31, g = lane >> 5;
+    const int g = lane >> 5;
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
@@ -241,12 +241,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
   TileT tk, tv;
   auto fetch = [&](uint32_t kb) {
     const uint32_t rows = kb < k1 ? min(k1 - kb, (uint32_t)KB) : 0u;
-    tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
-    tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
+    tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
+    tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
   };
   auto stash = [&](int buf) {
-    tk.stash(map, lds + buf * 2 * TILE, threadIdx.x);
-    tv.stash(map, lds + buf * 2 * TILE + TILE, threadIdx.x);
+    tk.stash(map, lds + buf * 2 * TILE);
+    tv.stash(map, lds + buf * 2 * TILE + TILE);
   };
   // the table: distances lo .. hi
   const int32_t lo = max(-(p.bias.M + kEdge), -(q0 + QB - 1));
@@ -354,8 +354,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
   TileT tk, tv;
   auto fetch = [&](uint32_t kb) {
     const uint32_t rows = kb < k1 ? min(k1 - kb, 32u) : 0u;
-    tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, lane);
-    tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, lane);
+    tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
+    tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
   };
   const int32_t lo = max(-(p.bias.M + kEdge), (int32_t)k0 - (q0 + 31));
   const int32_t hi = min(p.bias.M + kEdge, (int32_t)(k0 + (max(k1, k0) - k0 + 31) / 32 * 32) - 1 - q0);
@@ -367,11 +367,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
   const T* qg = static_cast<const T*>(p.q) + (int64_t)b * p.qs[0] + (int64_t)x * p.qs[1];
   auto at_row = [&](uint32_t hh, uint32_t i, int64_t rs) { return (int64_t)i * rs + (int64_t)(h0 + hh) * D; };
   // the columns' rows, on their way to LDS like the keys'
-  u32x4 qp[TileT::N];
+  constexpr int NQ = (32 * G::CHM + 63) / 64;
+  u32x4 qp[NQ];
   const uint32_t chunks = (uint32_t)(D / G::E);
   if (p.vec)
 #pragma unroll
-    for (int i = 0; i < TileT::N; ++i) {
+    for (int i = 0; i < NQ; ++i) {
       const uint32_t c = lane + 64 * i, col = c / chunks, hh = col / p.Lq;
       if (col < p.cols)
         qp[i] = *reinterpret_cast<const u32x4*>(qg + at_row(hh, col - hh * p.Lq, p.qs[2]) + (c - col * chunks) * G::E);
@@ -382,7 +383,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
   typename M::frag qf[1][G::NS];
   if (p.vec) {
 #pragma unroll
-    for (int i = 0; i < TileT::N; ++i) {
+    for (int i = 0; i < NQ; ++i) {
       const uint32_t c = lane + 64 * i, col = c / chunks;
       if (col < p.cols) *reinterpret_cast<u32x4*>(vl + col * G::P + (c - col * chunks) * G::E) = qp[i];
     }
@@ -403,8 +404,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
   sm.init();
   __syncthreads();   // the table
   for (uint32_t kb = mine; kb < k1; kb += 32 * NW) {
-    tk.stash(map, kl, lane);
-    tv.stash(map, vl, lane);
+    tk.stash(map, kl);
+    tv.stash(map, vl);
     if (!ONE && kb + 32 * NW < k1) fetch(kb + 32 * NW);
     sm.step(
         [&](int, int st) {
@@ -445,8 +446,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
     for (int w = 0; w < NW; ++w) l += __builtin_amdgcn_exp2f(ms[w * 32 + l32] - base) * ms[(NW + w) * 32 + l32];
     sm.o[0].scale(__builtin_amdgcn_exp2f(sm.ref[0] - base), lane);
     float* rows = ms + (2 * NW + 2) * 32;   // [NW][cols][DC]
-    store_rows<T, DC>(sm.o[0], lane, DC, true, [&](int n) -> float* {
-      return (uint32_t)n < p.cols ? rows + (wave * p.cols + n) * DC : nullptr;
+    store_rows<T, DC>(sm.o[0], lane, G::DP, true, [&](int n) -> float* {
+      return (uint32_t)n < p.cols ? rows + (wave * p.cols + n) * G::DP : nullptr;
     });
     if (wave == 0 && g == 0) {
       ms[2 * NW * 32 + l32] = top;
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
       const uint32_t col = i / p.D, d = i - col * p.D;
       float v = 0.0f;
 #pragma unroll
-      for (int w = 0; w < NW; ++w) v += rows[(w * p.cols + col) * DC + d];
+      for (int w = 0; w < NW; ++w) v += rows[(w * p.cols + col) * G::DP + d];
       if (p.n_split > 1) {
         part[2 * p.cols + i] = v;
       } else {
@@ -582,7 +583,7 @@ int start_few(FwdParams& p, const RelposArgs& a, hipStream_t s) {
   constexpr int MINW = sizeof(T) == 4 ? 1 : ONE ? (DC <= 80 ? 4 : DC <= 96 ? 3 : 2) : DC <= 80 ? 3 : 2;
   p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, 32 + ((int64_t)p.split_keys + 31) / 32 * 32);
   size_t lds = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T) + (size_t)p.tab * p.grp * 4;
-  if (NW > 1) lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * p.cols * DC) * 4);
+  if (NW > 1) lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * p.cols * Geo<T, DC>::DP) * 4);
   const int64_t pieces = a.B * a.X * p.n_split;
   p.pieces = (uint32_t)pieces;
   int st = launch(relpos_few_kernel<T, DC, NW, ONE, MINW>, (pieces + 7) / 8 * 8 * a.Hkv, NW * 64, lds, p, s);
@@ -627,6 +628,7 @@ int launch_attn_relpos(const RelposArgs& a, hipStream_t s) {
     if (a.D <= 32) return start<bf16, 32>(p, a, s);
     if (a.D <= 48) return start<bf16, 48>(p, a, s);
     if (a.D <= 64) return start<bf16, 64>(p, a, s);
+    if (a.D <= 72) return start<bf16, 72>(p, a, s);
     if (a.D <= 80) return start<bf16, 80>(p, a, s);
     if (a.D <= 96) return start<bf16, 96>(p, a, s);
     return start<bf16, 128>(p, a, s);

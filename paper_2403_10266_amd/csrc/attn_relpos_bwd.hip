@@ -48,6 +48,62 @@ __device__ __forceinline__ int64_t bx_at(const BwdParams& p, uint32_t bx, const 
   return (int64_t)(bx / p.X) * st[0] + (int64_t)(bx % p.X) * st[1];
 }
 
+// The probabilities of a block with queries on rows and keys on columns, in place of its
+// raw scores: lse2 (LDS) at this lane's first row, d0 the first key's place after the
+// first query.  `key0`, len: keys from len on have none.
+__device__ __forceinline__ void block_probabilities(const BwdParams& p, floatx16& s, const float* lse2,
+                                                    const float* tab0, float left, float right, int32_t d0, int l32,
+                                                    int g, uint32_t key0, uint32_t len) {
+  const bool far = d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M;
+  const float t = d0 < 0 ? left : right;
+  const float* tb = tab0 + d0 + l32 - 4 * g;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const floatx4 l = *reinterpret_cast<const floatx4*>(lse2 + 8 * q);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[4 * q + i] = fmaf(s[4 * q + i], p.c, (far ? t : tb[-(8 * q + i)]) - l[i]);
+  }
+  if (p.causal && d0 + 31 > 0) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (d0 + l32 > 8 * (r / 4) + 4 * g + r % 4) s[r] = -INFINITY;
+  }
+  if (key0 + 32 > len) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = key0 + l32 < len ? s[r] : -INFINITY;
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]);
+}
+
+// A work-group's sums of one head into its part: the half-waves' arrays, the sums past
+// the table's ends ([2][NT]) and the table's own entries past M, in a fixed order.
+template <int NT>
+__device__ __forceinline__ void fold_sums(const BwdParams& p, float* acc, int n_acc, const float* ends, uint32_t h,
+                                          uint32_t part) {
+  const int32_t near = p.bias.M + kEdge, n_tab = 2 * near + 1;
+  for (int32_t e = threadIdx.x; e < n_tab; e += NT) {
+    float v = acc[e];
+    for (int w = 1; w < n_acc; ++w) v += acc[w * n_tab + e];
+    acc[e] = v;
+  }
+  __syncthreads();
+  const int32_t n_out = 2 * p.bias.M + 1;
+  float* w = p.part + ((uint64_t)h * p.parts + part) * n_out;
+  for (int32_t e = threadIdx.x; e < n_out; e += NT) {
+    float v = acc[e + kEdge];
+    if (e == 0) {
+      for (int t = 0; t < NT; ++t) v += ends[t];
+      for (int i = 0; i < kEdge; ++i) v += acc[i];
+    }
+    if (e == n_out - 1) {   // M = 0: both ends are the one distance
+      for (int t = 0; t < NT; ++t) v += ends[NT + t];
+      for (int i = 0; i < kEdge; ++i) v += acc[n_tab - 1 - i];
+    }
+    w[e] = v;
+  }
+}
+
 // ---------------------------------------------------------------------------
 // dQ, Delta and the sums of dZ by distance: 32 queries of one head per wave.
 template <typename T, int DC, int NW, int KB, int MINW>
@@ -103,12 +159,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
     }
     auto fetch = [&](uint32_t kb) {
       const uint32_t rows = kb < k1 ? min(k1 - kb, (uint32_t)KB) : 0u;
-      tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
-      tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec, threadIdx.x);
+      tk.fetch(map, kg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
+      tv.fetch(map, vg + (int64_t)kb * p.ks[2], rows, row_bytes, D, p.vec);
     };
     auto stash = [&](int buf) {
-      tk.stash(map, lds + buf * 2 * TILE, threadIdx.x);
-      tv.stash(map, lds + buf * 2 * TILE + TILE, threadIdx.x);
+      tk.stash(map, lds + buf * 2 * TILE);
+      tv.stash(map, lds + buf * 2 * TILE + TILE);
     };
     if (k1) fetch(0);
     const uint32_t row = blk * QB + 32 * wave + l32;
@@ -207,55 +263,43 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
     });
   }
 
-  // the work-group's sums: the half-waves' arrays, the far registers, and the ends
-  // of the table past M, in a fixed order
   __syncthreads();
-  float* far = reinterpret_cast<float*>(lds);   // [2][NT]
-  far[threadIdx.x] = sum_l;
-  far[NT + threadIdx.x] = sum_r;
-  for (int32_t e = threadIdx.x; e < n_tab; e += NT) {
-    float v = acc[e];
-    for (int w = 1; w < 2 * NW; ++w) v += acc[w * n_tab + e];
-    acc[e] = v;
-  }
+  float* ends = reinterpret_cast<float*>(lds);   // [2][NT]
+  ends[threadIdx.x] = sum_l;
+  ends[NT + threadIdx.x] = sum_r;
   __syncthreads();
-  if (threadIdx.x < 2) {
-    const int right_end = threadIdx.x;
-    float v = 0.0f;
-    for (int t = 0; t < NT; ++t) v += far[right_end * NT + t];
-    for (int e = 0; e < kEdge; ++e) v += acc[right_end ? n_tab - 1 - e : e];
-    // M = 0: both ends are the one distance
-    if (p.bias.M == 0) far[2 * NT + right_end] = v;
-    else acc[right_end ? near + p.bias.M : near - p.bias.M] += v;
-  }
-  __syncthreads();
-  if (p.bias.M == 0 && threadIdx.x == 0) acc[near] += far[2 * NT] + far[2 * NT + 1];
-  __syncthreads();
-  const int32_t n_out = 2 * p.bias.M + 1;
-  float* w = p.part + ((uint64_t)h * p.parts + part) * n_out;
-  for (int32_t e = threadIdx.x; e < n_out; e += NT) w[e] = acc[e + kEdge];
+  fold_sums<NT>(p, acc, 2 * NW, ends, h, part);
 }
 
-// dbias[t][h]: the parts of each distance in order, then the distances of each bucket.
+// dbias[t][h]: the parts of each distance, then the distances of each bucket, in a fixed
+// order: 4 interleaved runs of parts for each distance, 64 lanes to a bucket.
 template <typename T>
 __global__ __launch_bounds__(1024) void relpos_bias_grad_kernel(BwdParams p, T* dbias) {
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  float* sums = reinterpret_cast<float*>(smem);
   const uint32_t h = blockIdx.x;
   const int32_t n = 2 * p.bias.M + 1;
+  float* sums = reinterpret_cast<float*>(smem);             // [4][n]
+  int32_t* which = reinterpret_cast<int32_t*>(sums + 4 * n);  // [n]
   const float* w = p.part + (uint64_t)h * p.parts * n;
-  for (int32_t e = threadIdx.x; e < n; e += blockDim.x) {
+  for (int32_t e = threadIdx.x; e < n; e += 1024) which[e] = p.bias.buckets[e];
+  const uint32_t run = threadIdx.x >> 8;
+  for (int32_t e = threadIdx.x & 255; e < n; e += 256) {
     float v = 0.0f;
-    for (uint32_t s = 0; s < p.parts; ++s) v += w[(uint64_t)s * n + e];
-    sums[e] = v;
+#pragma unroll 8
+    for (uint32_t s = run; s < p.parts; s += 4) v += w[(uint64_t)s * n + e];
+    sums[run * n + e] = v;
   }
   __syncthreads();
-  for (int32_t t = threadIdx.x; t < p.bias.nb; t += blockDim.x) {
+  for (int32_t e = threadIdx.x; e < n; e += 1024) sums[e] = (sums[e] + sums[n + e]) + (sums[2 * n + e] + sums[3 * n + e]);
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  for (int32_t t = threadIdx.x >> 6; t < p.bias.nb; t += 16) {
     float v = 0.0f;
-    bool masked = (float)static_cast<const T*>(p.bias.bias)[(int64_t)t * p.H + h] <= kMasked;
-    for (int32_t e = 0; e < n; ++e)
-      if (p.bias.buckets[e] == t) v += sums[e];
-    dbias[(int64_t)t * p.H + h] = (T)(masked ? 0.0f : v);
+    for (int32_t e = lane; e < n; e += 64) v += which[e] == t ? sums[e] : 0.0f;
+#pragma unroll
+    for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off);
+    const bool masked = (float)static_cast<const T*>(p.bias.bias)[(int64_t)t * p.H + h] <= kMasked;
+    if (lane == 0) dbias[(int64_t)t * p.H + h] = (T)(masked ? 0.0f : v);
   }
 }
 
@@ -312,8 +356,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
     const float left = bias_at<T>(p.bias, p.H, h, -p.bias.M), right = bias_at<T>(p.bias, p.H, h, p.bias.M);
     auto fetch = [&](uint32_t it) {
       const uint32_t q0 = it * QB, rows = min(p.Lq - q0, (uint32_t)QB);
-      tq.fetch(mq, qg + (int64_t)q0 * p.qs[2], rows, q_row, D, p.vec, threadIdx.x);
-      to.fetch(mo, og + (int64_t)q0 * p.os[2], rows, o_row, D, p.vec, threadIdx.x);
+      tq.fetch(mq, qg + (int64_t)q0 * p.qs[2], rows, q_row, D, p.vec);
+      to.fetch(mo, og + (int64_t)q0 * p.os[2], rows, o_row, D, p.vec);
       if (threadIdx.x < 2 * QB) {
         const uint32_t i = threadIdx.x % QB;
         const bool is_delta = threadIdx.x >= QB;
@@ -322,8 +366,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
       }
     };
     auto stash = [&](int buf) {
-      tq.stash(mq, lds + buf * 2 * TILE, threadIdx.x);
-      to.stash(mo, lds + buf * 2 * TILE + TILE, threadIdx.x);
+      tq.stash(mq, lds + buf * 2 * TILE);
+      to.stash(mo, lds + buf * 2 * TILE + TILE);
       if (threadIdx.x < 2 * QB) stat[buf * 2 * QB + threadIdx.x] = pre;
     };
     fetch(it0);
@@ -352,38 +396,16 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
         }
         // lane (n + 32 g): key n, queries 8 (r / 4) + 4 g + r % 4
         const int32_t d0 = (int32_t)key0 - q0;
-        float lse2[16], dl[16];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const floatx4 a = *reinterpret_cast<const floatx4*>(sl + 32 * sub + 8 * q + 4 * g);
-          const floatx4 d = *reinterpret_cast<const floatx4*>(sl + QB + 32 * sub + 8 * q + 4 * g);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) lse2[4 * q + i] = a[i], dl[4 * q + i] = d[i];
-        }
-        if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
-          const float t = d0 < 0 ? left : right;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, t - lse2[r]);
-        } else {
-          const float* tb = tab + near + d0 + l32 - 4 * g;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, tb[-(8 * (r / 4) + r % 4)] - lse2[r]);
-        }
-        if (p.causal && d0 + 31 > 0) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (d0 + l32 > 8 * (r / 4) + 4 * g + r % 4) s[r] = -INFINITY;
-        }
-        if (key0 + 32 > len) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = on ? s[r] : -INFINITY;
-        }
+        block_probabilities(p, s, sl + 32 * sub + 4 * g, tab + near, left, right, d0, l32, g, key0, len);
         ColB<T> pb, zb;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float e2 = __builtin_amdgcn_exp2f(s[r]);
-          pb.set(r, e2);
-          zb.set(r, e2 * (dp[r] - dl[r]));
+        for (int q = 0; q < 4; ++q) {
+          const floatx4 dl = *reinterpret_cast<const floatx4*>(sl + QB + 32 * sub + 8 * q + 4 * g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pb.set(4 * q + i, s[4 * q + i]);
+            zb.set(4 * q + i, s[4 * q + i] * (dp[4 * q + i] - dl[i]));
+          }
         }
         dv.add(ol, 32 * sub, lane, pb);
         dk.add(ql, 32 * sub, lane, zb);
@@ -399,14 +421,241 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
   store_rows<T, DC>(dv, lane, D, p.vec, [&](int n) { return key0 + n < p.Lk ? vo + (int64_t)(key0 + n) * p.ks[2] : nullptr; });
 }
 
-// Work-groups of a head: enough for the chip to hold two rounds of, no more than
-// there are blocks of queries.
-int64_t parts_of(const RelposArgs& a, int64_t qb) {
-  const int64_t items = a.B * a.X * ((a.Lq + qb - 1) / qb);
+// ---------------------------------------------------------------------------
+// Units of at most 32 NB queries and keys (temporal attention): one work-group holds a
+// unit's Q, K, V and dO in LDS, so each row crosses HBM once.  Wave w first takes queries
+// 32 w .. against all keys (dQ, dbias), with the whole row of P and dP in registers, so
+// Delta_i = sum_j P_ij dP_ij needs no o and none of its rounding; then keys 32 w ..
+// against all queries (dK, dV), with the scores computed again the other way round.
+// A work-group stays with one head (which has keys of its own) and runs through units.
+template <typename T, int DC, int NB, int MINW>
+__global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  constexpr int NT = NB * 64, R = NB * 32, TILE = R * G::P;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* kl = reinterpret_cast<T*>(smem);
+  T* vl = kl + TILE;
+  T* ql = vl + TILE;
+  T* ol = ql + TILE;
+  float* st_lse = reinterpret_cast<float*>(ol + TILE);    // [R]
+  float* st_del = st_lse + R;                             // [R]
+  const int32_t near = p.bias.M + kEdge, n_tab = 2 * near + 1;
+  float* tab = st_del + R;                                // [n_tab]
+  float* acc = tab + n_tab;                               // [2 NB][n_tab]
+  float* ends = acc + 2 * NB * n_tab;                     // [2][NT]: sums past the table's ends
+
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // work-group -> (head, part); an XCD takes whole token rows
+  const uint32_t j8 = blockIdx.x >> 3;
+  const uint32_t h = j8 % p.H, part = j8 / p.H * 8 + (blockIdx.x & 7u);
+  const int D = (int)p.D;
+  const uint32_t k_row = (uint32_t)p.ks[2] * (uint32_t)sizeof(T), q_row = (uint32_t)p.qs[2] * (uint32_t)sizeof(T),
+                 o_row = (uint32_t)p.os[2] * (uint32_t)sizeof(T);
+  using TileT = Tile<T, DC, R, NT>;
+  const typename TileT::Map mk = TileT::map(D, k_row, threadIdx.x), mq = TileT::map(D, q_row, threadIdx.x),
+                            mo = TileT::map(D, o_row, threadIdx.x);
+
+  for (int32_t t = threadIdx.x; t < n_tab; t += NT) tab[t] = bias_at<T>(p.bias, p.H, h, t - near);
+  for (int32_t t = threadIdx.x; t < 2 * NB * n_tab + 2 * NT; t += NT) acc[t] = 0.0f;   // and the ends
+  clear_pad<T, DC>(kl, 4 * R, D, threadIdx.x, NT);
+
+  for (uint32_t bx = part; bx < p.BX; bx += p.parts) {
+    const uint32_t b = bx / p.X;
+    const int32_t q0 = position(p.q_pos, b);
+    const uint32_t len = length(p.kv_len, b, p.Lk);
+    const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)h * D, q_at = bx_at(p, bx, p.qs) + (int64_t)h * D,
+                  o_at = bx_at(p, bx, p.os) + (int64_t)h * D;
+    {
+      TileT tk, tv, tq, to;
+      tk.fetch(mk, static_cast<const T*>(p.k) + k_at, len, k_row, D, p.vec);
+      tv.fetch(mk, static_cast<const T*>(p.v) + k_at, len, k_row, D, p.vec);
+      tq.fetch(mq, static_cast<const T*>(p.q) + q_at, p.Lq, q_row, D, p.vec);
+      to.fetch(mo, static_cast<const T*>(p.dout) + o_at, p.Lq, o_row, D, p.vec);
+      float l = -INFINITY;
+      if (threadIdx.x < p.Lq) l = p.lse[((uint64_t)bx * p.H + h) * p.Lq + threadIdx.x];
+      __syncthreads();   // the rows are free
+      tk.stash(mk, kl);
+      tv.stash(mk, vl);
+      tq.stash(mq, ql);
+      to.stash(mo, ol);
+      if (threadIdx.x < R) st_lse[threadIdx.x] = l == -INFINITY ? INFINITY : l * kLog2e;
+    }
+    __syncthreads();
+    const float* tb0 = tab + near;
+    const float left = tb0[-p.bias.M], right = tb0[p.bias.M];
+    ColAcc<T, DC> dq;
+    dq.zero();
+    if (32u * wave < p.Lq) {
+      const int32_t wq = q0 + 32 * wave;
+      typename M::frag qf[G::NS], df[G::NS];
+#pragma unroll
+      for (int s = 0; s < G::NS; ++s) {
+        const int at = (32 * wave + l32) * G::P + 2 * G::E * s + G::E * g;
+        qf[s] = *reinterpret_cast<const typename M::frag*>(ql + at);
+        df[s] = *reinterpret_cast<const typename M::frag*>(ol + at);
+      }
+      const float lse2 = st_lse[32 * wave + l32];
+      floatx16 s[NB], dp[NB];
+      float delta = 0.0f;
+#pragma unroll
+      for (int kt = 0; kt < NB; ++kt) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][r] = dp[kt][r] = 0.0f;
+        if (32u * kt >= len) continue;
+#pragma unroll
+        for (int i = 0; i < G::NS; ++i) {
+          const int at = (32 * kt + l32) * G::P + 2 * G::E * i + G::E * g;
+          s[kt] = M::mma(*reinterpret_cast<const typename M::frag*>(kl + at), qf[i], s[kt]);
+          dp[kt] = M::mma(*reinterpret_cast<const typename M::frag*>(vl + at), df[i], dp[kt]);
+        }
+        const int32_t d0 = 32 * kt - wq;
+        if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
+          const float t = (d0 < 0 ? left : right) - lse2;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], p.c, t);
+        } else {
+          const float* tb = tb0 + d0 + 4 * g - l32;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], p.c, tb[8 * (r / 4) + r % 4] - lse2);
+        }
+        if ((p.causal && d0 + 31 > 0) || 32u * kt + 32 > len) {
+          const int32_t stop = p.causal ? min((int32_t)len, wq + l32 + 1) : (int32_t)len;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (32 * kt + 8 * (r / 4) + 4 * g + r % 4 >= stop) s[kt][r] = -INFINITY;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          s[kt][r] = __builtin_amdgcn_exp2f(s[kt][r]);
+          delta += s[kt][r] * dp[kt][r];
+        }
+      }
+      delta += swap_halves(delta);
+      if (g == 0) st_del[32 * wave + l32] = delta;
+      float* mine = acc + (2 * wave + g) * n_tab + near;
+#pragma unroll
+      for (int kt = 0; kt < NB; ++kt) {
+        if (32u * kt >= len) continue;
+        ColB<T> z;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dp[kt][r] = s[kt][r] * (dp[kt][r] - delta);
+          z.set(r, dp[kt][r]);
+        }
+        const int32_t d0 = 32 * kt - wq;
+        if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
+          float v = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) v += dp[kt][r];
+          ends[(d0 < 0 ? 0 : NT) + threadIdx.x] += v;
+        } else {
+          float* to = mine + d0 + 4 * g - l32;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) atomicAdd(to + 8 * (r / 4) + r % 4, dp[kt][r]);
+        }
+        dq.add(kl, 32 * kt, lane, z);
+      }
+      dq.scale(p.scale, lane);
+    }
+    __syncthreads();   // Delta is there
+    typename M::frag kf[G::NS], vf[G::NS];
+#pragma unroll
+    for (int s = 0; s < G::NS; ++s) {
+      const int at = (32 * wave + l32) * G::P + 2 * G::E * s + G::E * g;
+      kf[s] = *reinterpret_cast<const typename M::frag*>(kl + at);
+      vf[s] = *reinterpret_cast<const typename M::frag*>(vl + at);
+    }
+    __syncthreads();   // the rows of K are free
+    auto q_out = [&](int n) -> T* {
+      const uint32_t r = 32 * wave + n;
+      return r < p.Lq ? static_cast<T*>(p.dq) + q_at + (int64_t)r * p.qs[2] : nullptr;
+    };
+    if (p.vec) store_rows_lds<T, DC>(kl + 32 * wave * G::P, dq, lane, D, q_out);
+    else store_rows<T, DC>(dq, lane, D, false, q_out);
+    ColAcc<T, DC> dk, dv;
+    dk.zero();
+    dv.zero();
+    if (32u * wave < len) {
+#pragma unroll
+      for (int qt = 0; qt < NB; ++qt) {
+        const int32_t d0 = 32 * wave - q0 - 32 * qt;
+        if (32u * qt >= p.Lq || (p.causal && d0 > 31)) continue;
+        floatx16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < G::NS; ++i) {
+          const int at = (32 * qt + l32) * G::P + 2 * G::E * i + G::E * g;
+          s = M::mma(*reinterpret_cast<const typename M::frag*>(ql + at), kf[i], s);
+          dp = M::mma(*reinterpret_cast<const typename M::frag*>(ol + at), vf[i], dp);
+        }
+        block_probabilities(p, s, st_lse + 32 * qt + 4 * g, tb0, left, right, d0, l32, g, 32 * wave, len);
+        ColB<T> pb, zb;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const floatx4 dl = *reinterpret_cast<const floatx4*>(st_del + 32 * qt + 8 * q + 4 * g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pb.set(4 * q + i, s[4 * q + i]);
+            zb.set(4 * q + i, s[4 * q + i] * (dp[4 * q + i] - dl[i]));
+          }
+        }
+        dv.add(ol, 32 * qt, lane, pb);
+        dk.add(ql, 32 * qt, lane, zb);
+      }
+    }
+    // the rows of K and V serve to write: this wave's own, which it alone reads now
+    dk.scale(p.scale, lane);
+    auto out = [&](void* base) {
+      return [&, base](int n) -> T* {
+        const uint32_t r = 32 * wave + n;
+        return r < p.Lk ? static_cast<T*>(base) + k_at + (int64_t)r * p.ks[2] : nullptr;
+      };
+    };
+    if (p.vec) {
+      store_rows_lds<T, DC>(kl + 32 * wave * G::P, dk, lane, D, out(p.dk));
+      store_rows_lds<T, DC>(vl + 32 * wave * G::P, dv, lane, D, out(p.dv));
+    } else {
+      store_rows<T, DC>(dk, lane, D, false, out(p.dk));
+      store_rows<T, DC>(dv, lane, D, false, out(p.dv));
+    }
+  }
+  __syncthreads();
+  fold_sums<NT>(p, acc, 2 * NB, ends, h, part);
+}
+
+constexpr int kQB = 128;   // queries of a work-group of the dQ kernel
+
+// LDS of the short-unit kernel, and the blocks of 32 it takes the call with (0: not at
+// all): at most 64 queries and keys, heads with keys of their own (fp32 up to 64 wide:
+// a wider one's rows and sums do not fit the registers).
+size_t short_lds(const RelposArgs& a, int nb, int row_bytes) {
+  const size_t n_tab = 2 * ((size_t)a.max_dist + kEdge) + 1;
+  return (size_t)4 * 32 * nb * row_bytes + (size_t)2 * 32 * nb * 4 + (n_tab * (1 + 2 * nb) + 2 * 64 * nb) * 4;
+}
+int row_bytes_of(const RelposArgs& a) {
+  const int dc = a.bf16 ? (a.D <= 32 ? 32 : a.D <= 48 ? 48 : a.D <= 64 ? 64 : a.D <= 80 ? 80 : a.D <= 96 ? 96 : 128)
+                        : (a.D + 31) / 32 * 32;
+  return a.bf16 ? (dc + 8) * 2 : (dc + 4) * 4;
+}
+int short_blocks(const RelposArgs& a) {
+  const int64_t l = std::max(a.Lq, a.Lk);
+  return a.H != a.Hkv || a.Lq == 0 || l > 64 || (!a.bf16 && a.D > 64) ? 0 : l <= 32 ? 1 : 2;
+}
+// Work-groups of a head (parts of its dbias): enough to fill the chip, no more than
+// there is work.
+int64_t parts_of(const RelposArgs& a) {
+  if (const int nb = short_blocks(a)) {
+    const int64_t per_cu = std::max<int64_t>(1, 160 * 1024 / (int64_t)short_lds(a, nb, row_bytes_of(a)));
+    const int64_t want = (256 * std::min<int64_t>(per_cu, 8 / nb) + a.Hkv - 1) / a.Hkv;
+    return (std::min(a.B * a.X, want) + 7) / 8 * 8;
+  }
+  const int64_t items = a.B * a.X * ((a.Lq + kQB - 1) / kQB);
   const int64_t want = (1024 + a.H - 1) / a.H;
   return std::max<int64_t>(1, std::min(items, want));
 }
-constexpr int kQB = 128;
 
 template <typename K>
 int lds_limit(K* kernel, size_t lds) {
@@ -415,10 +664,31 @@ int lds_limit(K* kernel, size_t lds) {
       hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
 }
 
+template <typename T>
+int bias_grad(BwdParams& p, const RelposArgs& a, hipStream_t s) {
+  const size_t n = 2 * (size_t)p.bias.M + 1;
+  relpos_bias_grad_kernel<T><<<dim3(p.H), 1024, n * 5 * 4, s>>>(p, static_cast<T*>(a.dbias));
+  return last_launch_status();
+}
+
+template <typename T, int DC, int NB>
+int start_short(BwdParams& p, const RelposArgs& a, hipStream_t s) {
+  auto* kernel = relpos_bwd_short_kernel<T, DC, NB, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
+  const size_t lds = short_lds(a, NB, Geo<T, DC>::P * sizeof(T));
+  if (int st = lds_limit(kernel, lds)) return st;
+  const int64_t blocks = (int64_t)p.parts * a.Hkv;
+  if (!grid_fits(blocks, NB * 64)) return DSP_ERR_SHAPE;
+  kernel<<<dim3((uint32_t)blocks), NB * 64, lds, s>>>(p);
+  if (int st = last_launch_status()) return st;
+  return bias_grad<T>(p, a, s);
+}
+
 template <typename T, int DC>
 int start(BwdParams& p, const RelposArgs& a, hipStream_t s) {
   using G = Geo<T, DC>;
   constexpr int NW = 4, KB = 32;
+  if constexpr (sizeof(T) == 2 || DC <= 64)
+    if (const int nb = short_blocks(a)) return nb == 1 ? start_short<T, DC, 1>(p, a, s) : start_short<T, DC, 2>(p, a, s);
   const size_t n_tab = 2 * ((size_t)p.bias.M + kEdge) + 1;
   if (a.Lq > 0) {
     p.n_blk = (uint32_t)((a.Lq + 32 * NW - 1) / (32 * NW));
@@ -428,8 +698,7 @@ int start(BwdParams& p, const RelposArgs& a, hipStream_t s) {
     kernel<<<dim3(p.H * p.parts), NW * 64, lds, s>>>(p);
     if (int st = last_launch_status()) return st;
   }
-  relpos_bias_grad_kernel<T><<<dim3(p.H), 1024, (2 * (size_t)p.bias.M + 1) * 4, s>>>(p, static_cast<T*>(a.dbias));
-  if (int st = last_launch_status()) return st;
+  if (int st = bias_grad<T>(p, a, s)) return st;
   if (a.Lk > 0) {
     constexpr int QT = 1;
     p.n_blk = (uint32_t)((a.Lk + 32 * NW - 1) / (32 * NW));
@@ -448,7 +717,7 @@ int start(BwdParams& p, const RelposArgs& a, hipStream_t s) {
 
 size_t attn_relpos_bwd_workspace_bytes(const RelposArgs& a) {
   const int64_t stats = (a.B * a.X * a.H * a.Lq + 63) / 64 * 64;
-  return (size_t)(stats + a.H * parts_of(a, kQB) * (2 * (int64_t)a.max_dist + 1)) * 4;
+  return (size_t)(stats + a.H * parts_of(a) * (2 * (int64_t)a.max_dist + 1)) * 4;
 }
 
 int launch_attn_relpos_bwd(const RelposArgs& a, hipStream_t s) {
@@ -462,13 +731,14 @@ int launch_attn_relpos_bwd(const RelposArgs& a, hipStream_t s) {
   p.bias = {a.bias, a.buckets, a.max_dist, a.n_buckets};
   p.X = (uint32_t)a.X, p.H = a.H, p.grp = a.H / a.Hkv, p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk, p.D = a.D;
   p.BX = (uint32_t)(a.B * a.X);
-  p.parts = a.Lq > 0 ? (uint32_t)parts_of(a, kQB) : 0;   // no queries: sums of nothing
+  p.parts = a.Lq > 0 ? (uint32_t)parts_of(a) : 0;   // no queries: sums of nothing
   p.c = a.scale * kLog2e, p.scale = a.scale;
   p.vec = a.vec, p.causal = a.causal;
   if (a.bf16) {
     if (a.D <= 32) return start<bf16, 32>(p, a, s);
     if (a.D <= 48) return start<bf16, 48>(p, a, s);
     if (a.D <= 64) return start<bf16, 64>(p, a, s);
+    if (a.D <= 72) return start<bf16, 72>(p, a, s);
     if (a.D <= 80) return start<bf16, 80>(p, a, s);
     if (a.D <= 96) return start<bf16, 96>(p, a, s);
     return start<bf16, 128>(p, a, s);
