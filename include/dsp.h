@@ -389,8 +389,8 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
  * dtype:   DSP_BF16 (fp32 scores, softmax and accumulation; probabilities are
  *          rounded to bf16 for the product with v), D a multiple of 8 up to 128,
  *          16-byte aligned tensors and strides multiples of 8; or DSP_F32, any D up
- *          to 128.  max_dist <= 1024, Lq and Lk below 2^30, and 64 rows of k within
- *          2^31 bytes.
+ *          to 128.  max_dist <= 1024, Lq and Lk below 2^30, and 64 rows of each tensor
+ *          within 2^31 bytes.
  * workspace: dsp_attn_relpos_workspace_bytes(...) bytes, 16-byte aligned (0 except
  *          for a few queries against many keys: there the keys are cut among
  *          work-groups, whose sums are joined).

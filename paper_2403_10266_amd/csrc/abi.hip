@@ -455,7 +455,8 @@ int relpos_impl(RelposArgs& a, bool bwd, int flags, void* workspace, size_t ws_b
   if (a.Lq <= 1) a.q_strides[2] = a.o_strides[2] = wq;
   if (a.Lk <= 1) a.kv_strides[2] = wk;
   const int64_t far = (int64_t(1) << 31) / 64 / es;   // 64 rows lie within 2^31 bytes
-  if (a.kv_strides[2] >= far || (bwd && (a.q_strides[2] >= far || a.o_strides[2] >= far))) return DSP_ERR_SHAPE;
+  for (const int64_t* st : {a.q_strides, a.kv_strides, a.o_strides})
+    if (st[2] >= far) return DSP_ERR_SHAPE;
   auto disjoint = [&](int64_t L, const int64_t* st, int64_t w) { return rows_disjoint(a.B, a.X, L, st, w); };
   const int64_t B = a.B, X = a.X;
   auto apart = [&](const void* p, const int64_t* sp, int64_t wp, int64_t Lp, const void* r, const int64_t* sr,

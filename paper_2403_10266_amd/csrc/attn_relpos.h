@@ -273,17 +273,17 @@ struct Tile {
   }
   __device__ __forceinline__ void fetch(const Map& m, const T* base, uint32_t rows, uint32_t row_bytes, int D,
                                         bool vec) {
+    // an offset past the resource instead of a branch: all loads go out at once
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, rows * row_bytes);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      if (m.row + i * m.step >= R) continue;
-      const uint32_t skip = i * m.step * row_bytes;
+      const uint32_t off = m.row + i * m.step < rows ? m.at + i * m.step * row_bytes : 0xFFFFFFF0u;
       if (sizeof(T) == 2 || vec) {
-        pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, m.at, skip, 0);
+        pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          pre[i][e] = m.col + e < D ? __builtin_amdgcn_raw_buffer_load_b32(rs, m.at + 4u * e, skip, 0) : 0u;
+          pre[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, m.col + e < D ? off + 4u * e : 0xFFFFFFF0u, 0, 0);
       }
     }
   }

@@ -254,14 +254,36 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
   const int32_t n_tab = k1 ? hi - lo + 1 : 0;
   Table<T, NT> table;
   table.fetch(p.bias, lo, n_tab);
-  if (k1) fetch(0);
-
   const int32_t wq = q0 + 32 * QT * wave;   // the wave's first query
   typename M::frag qf[QT][G::NS];
+  if constexpr (NBUF == 1) {
+    // short units are bound by memory: Q, too, comes along its rows, through the
+    // rows of V
+    static_assert(QB == KB && QT == 1, "one tile of queries");
+    const uint32_t q_row = (uint32_t)p.qs[2] * (uint32_t)sizeof(T);
+    const typename TileT::Map mq = TileT::map(D, q_row, threadIdx.x);
+    TileT tq;
+    tq.fetch(mq, qg + (int64_t)(qb * QB) * p.qs[2], nq, q_row, D, p.vec);
+    if (k1) fetch(0);
+    clear_pad<T, DC>(lds, 2 * KB, D, threadIdx.x, NT);
+    tq.stash(mq, lds + TILE);
+    if (k1) tk.stash(map, lds);
+    __syncthreads();
 #pragma unroll
-  for (int j = 0; j < QT; ++j) {
-    const uint32_t i = 32 * (wave * QT + j) + l32;
-    row_frags<T, DC>(i < nq ? qg + (int64_t)(qb * QB + i) * p.qs[2] : nullptr, g, D, p.vec, qf[j]);
+    for (int st = 0; st < G::NS; ++st)
+      qf[0][st] = *reinterpret_cast<const typename M::frag*>(lds + TILE + (32 * wave + l32) * G::P + 2 * G::E * st +
+                                                             G::E * g);
+    __syncthreads();
+    if (k1) tv.stash(map, lds + TILE);
+  } else {
+    if (k1) fetch(0);
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+      const uint32_t i = 32 * (wave * QT + j) + l32;
+      row_frags<T, DC>(i < nq ? qg + (int64_t)(qb * QB + i) * p.qs[2] : nullptr, g, D, p.vec, qf[j]);
+    }
+    clear_pad<T, DC>(lds, NBUF * 2 * KB, D, threadIdx.x, NT);
+    if (k1) stash(0);
   }
   table.build(p.bias, lo, n_tab, tab, 0, p.H, h, 1);
   float left[QT], right[QT];
@@ -278,8 +300,6 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
   }
   Softmax<T, DC, QT, NKT, NBUF != 1> sm;
   sm.init();
-  clear_pad<T, DC>(lds, NBUF * 2 * KB, D, threadIdx.x, NT);
-  if (k1) stash(0);
   __syncthreads();
   const uint32_t n_it = (k1 + KB - 1) / KB;
   for (uint32_t it = 0; it < n_it; ++it) {
@@ -605,8 +625,8 @@ int start(FwdParams& p, const RelposArgs& a, hipStream_t s) {
     return start_few<T, DC, 4, false>(p, a, s);
   }
   constexpr bool B16 = sizeof(T) == 2;
-  if (a.Lq <= 64 && a.Lk <= 64) return start_many<T, DC, 2, 1, 64, 1, 1>(p, a, s);
-  if (a.Lq <= 128) return start_many<T, DC, 4, 1, B16 ? 64 : 32, 2, 1>(p, a, s);
+  if (a.Lq <= 64 && a.Lk <= 64) return start_many<T, DC, 2, 1, 64, 1, B16 ? (DC <= 80 ? 3 : 2) : 1>(p, a, s);
+  if (a.Lq <= 128) return start_many<T, DC, 4, 1, B16 ? 64 : 32, 2, B16 ? 2 : 1>(p, a, s);
   return start_many<T, DC, B16 ? 8 : 4, B16 && DC <= 96 ? 2 : 1, B16 ? 64 : 32, 2, B16 ? 2 : 1>(p, a, s);
 }
 

@@ -427,7 +427,9 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
 // 32 w .. against all keys (dQ, dbias), with the whole row of P and dP in registers, so
 // Delta_i = sum_j P_ij dP_ij needs no o and none of its rounding; then keys 32 w ..
 // against all queries (dK, dV), with the scores computed again the other way round.
-// A work-group stays with one head (which has keys of its own) and runs through units.
+// A work-group stays with one head (which has keys of its own) and runs through units;
+// a wave's dZ is summed over them in registers, element by element, and goes to the
+// sums by distance only when the queries' first position changes and at the end.
 template <typename T, int DC, int NB, int MINW>
 __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdParams p) {
   using G = Geo<T, DC>;
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
   float* acc = tab + n_tab;                               // [2 NB][n_tab]
   float* ends = acc + 2 * NB * n_tab;                     // [2][NT]: sums past the table's ends
 
-  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int lane0 = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // work-group -> (head, part); an XCD takes whole token rows
   const uint32_t j8 = blockIdx.x >> 3;
@@ -461,9 +463,42 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
   for (int32_t t = threadIdx.x; t < 2 * NB * n_tab + 2 * NT; t += NT) acc[t] = 0.0f;   // and the ends
   clear_pad<T, DC>(kl, 4 * R, D, threadIdx.x, NT);
 
-  for (uint32_t bx = part; bx < p.BX; bx += p.parts) {
-    const uint32_t b = bx / p.X;
+  floatx16 sum[NB];   // of dZ, queries 32 wave .. against keys 32 kt ..
+#pragma unroll
+  for (int kt = 0; kt < NB; ++kt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum[kt][r] = 0.0f;
+  int32_t sum_q0 = 0;
+  for (uint32_t bx = part;; bx += p.parts) {
+    const bool done = bx >= p.BX;
+    const uint32_t b = done ? 0 : bx / p.X;
     const int32_t q0 = position(p.q_pos, b);
+    if (done || q0 != sum_q0) {
+      __syncthreads();   // the sums by distance are set
+      const int l32 = lane0 & 31, g = lane0 >> 5;
+      float* mine = acc + (2 * wave + g) * n_tab + near;
+#pragma unroll
+      for (int kt = 0; kt < NB; ++kt) {
+        const int32_t d0 = 32 * kt - sum_q0 - 32 * wave;
+        if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
+          float v = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) v += sum[kt][r];
+          ends[(d0 < 0 ? 0 : NT) + threadIdx.x] += v;
+        } else {
+          float* to = mine + d0 + 4 * g - l32;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) atomicAdd(to + 8 * (r / 4) + r % 4, sum[kt][r]);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sum[kt][r] = 0.0f;
+      }
+      sum_q0 = q0;
+    }
+    if (done) break;
+    int lane = lane0;
+    asm volatile("" : "+v"(lane));   // the addresses made of it are cheaper to form again than to keep over the loop
+    const int l32 = lane & 31, g = lane >> 5;
     const uint32_t len = length(p.kv_len, b, p.Lk);
     const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)h * D, q_at = bx_at(p, bx, p.qs) + (int64_t)h * D,
                   o_at = bx_at(p, bx, p.os) + (int64_t)h * D;
@@ -534,26 +569,15 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
       }
       delta += swap_halves(delta);
       if (g == 0) st_del[32 * wave + l32] = delta;
-      float* mine = acc + (2 * wave + g) * n_tab + near;
 #pragma unroll
       for (int kt = 0; kt < NB; ++kt) {
         if (32u * kt >= len) continue;
         ColB<T> z;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          dp[kt][r] = s[kt][r] * (dp[kt][r] - delta);
-          z.set(r, dp[kt][r]);
-        }
-        const int32_t d0 = 32 * kt - wq;
-        if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
-          float v = 0.0f;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) v += dp[kt][r];
-          ends[(d0 < 0 ? 0 : NT) + threadIdx.x] += v;
-        } else {
-          float* to = mine + d0 + 4 * g - l32;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) atomicAdd(to + 8 * (r / 4) + r % 4, dp[kt][r]);
+          const float dz = s[kt][r] * (dp[kt][r] - delta);
+          sum[kt][r] += dz;
+          z.set(r, dz);
         }
         dq.add(kl, 32 * kt, lane, z);
       }

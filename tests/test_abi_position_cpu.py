@@ -144,6 +144,8 @@ def _relpos(lib, bwd=False, **kw):
     (dsp.DSP_ERR_SHAPE, dict(B=1 << 20, X=1 << 20)),
     (dsp.DSP_ERR_SHAPE, dict(ks=_st(21 * 144, 7 * 144, -8))),
     (dsp.DSP_ERR_SHAPE, dict(ks=_st(1 << 40, 1 << 30, 1 << 24))),   # 64 rows past 2^31 bytes
+    (dsp.DSP_ERR_SHAPE, dict(qs=_st(1 << 40, 1 << 30, 1 << 24))),
+    (dsp.DSP_ERR_SHAPE, dict(os=_st(1 << 40, 1 << 30, 1 << 24))),
     (dsp.DSP_ERR_ARG, dict(scale=float("nan"))),
     (dsp.DSP_ERR_ARG, dict(scale=float("inf"))),
     (dsp.DSP_ERR_ARG, dict(flags=2)),
