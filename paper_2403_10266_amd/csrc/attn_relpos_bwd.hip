@@ -8,13 +8,13 @@
 // second owns blocks of keys and loops over the queries of its group's heads (dK, dV).
 //
 // dbias is a sum along diagonals of dZ.  Blocks wholly past the table's end add to one
-// register per lane.  In the others each lane adds its dZ to an LDS array over the
-// distances; the array is private to a half of a wave, whose 32 lanes hold 32
-// different distances of each register, so every element is added by one lane at a
-// time in program order and the sum does not depend on timing.  A work-group stays
-// with one head and runs through several blocks of queries, so the arrays are folded
-// once; a last kernel adds the work-groups' sums in order and folds distances into
-// buckets.
+// register per lane.  The others go through LDS: a wave writes its 32 x 32 block and
+// reads it back along the diagonals, lane c the distance c - 31 from the block's, and
+// adds the 63 sums to an array over the distances of its own (no atomics: LDS atomics
+// took 85 ns an instruction here, half of the kernel's time).  A work-group stays with
+// one head and runs through several blocks of queries, so the waves' arrays are folded
+// once, in order; a last kernel adds the work-groups' sums in order and folds distances
+// into buckets.
 #include <algorithm>
 #include <type_traits>
 
@@ -39,7 +39,8 @@ struct BwdParams {
   const int32_t* kv_len;
   int64_t qs[3], ks[3], os[3];
   BiasArgs bias;
-  uint32_t X, H, grp, Lq, Lk, n_blk, n_blocks, D, BX, parts;
+  uint32_t X, H, grp, Lq, Lk, n_blk, D, BX, parts;
+  Order order;       // dK, dV
   float c, scale;
   bool vec, causal;
 };
@@ -76,7 +77,37 @@ __device__ __forceinline__ void block_probabilities(const BwdParams& p, floatx16
   for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r]);
 }
 
-// A work-group's sums of one head into its part: the half-waves' arrays, the sums past
+// Adds a block of dZ (lane (n + 32 g): query n, keys 8 (r / 4) + 4 g + r % 4) to the sums
+// by distance: `at` is the sum of the first key's distance from the first query, `room`
+// 32 rows of 32 floats of this wave's.  Row k is written rotated by k, so that column c
+// holds the elements of two distances: k - q = -c where k <= q, and 32 - c past the wrap.
+constexpr int kDiag = 32 * 32;
+__device__ __forceinline__ void add_diagonals(float* at, float* room, const floatx16& z, int lane) {
+  asm volatile("" : "+v"(lane));   // what is made of it below is not worth keeping in registers
+  const int l32 = lane & 31, g = lane >> 5;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int k = 8 * (r / 4) + r % 4;
+    room[(k + 4 * g) * 32 + ((l32 - 4 * g - k) & 31)] = z[r];
+  }
+  // lane (c + 32 g): column c, rows 16 g ..; row k of it is query k + c, or k + c - 32
+  float low = 0.0f, high = 0.0f;
+  const int split = 32 - l32 - 16 * g;   // rows from here on have wrapped
+  const float* from = room + 16 * g * 32 + l32;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) {
+    const float e = from[i * 32];
+    low += i < split ? e : 0.0f;
+    high += i < split ? 0.0f : e;
+  }
+  low += swap_halves(low);
+  high += swap_halves(high);
+  // distance -c from the first half's lanes, 32 - c (c > 0) from the second's
+  if (g == 0) at[-l32] += low;
+  else if (l32) at[32 - l32] += high;
+}
+
+// A work-group's sums of one head into its part: the waves' arrays, the sums past
 // the table's ends ([2][NT]) and the table's own entries past M, in a fixed order.
 template <int NT>
 __device__ __forceinline__ void fold_sums(const BwdParams& p, float* acc, int n_acc, const float* ends, uint32_t h,
@@ -114,8 +145,9 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
   extern __shared__ __attribute__((aligned(16))) char smem[];
   T* lds = reinterpret_cast<T*>(smem);   // [2][K, V][KB][P]
   const int32_t near = p.bias.M + kEdge, n_tab = 2 * near + 1;
-  float* tab = reinterpret_cast<float*>(lds + 4 * TILE);   // bias of distance d at near + d
-  float* acc = tab + n_tab;                                // [2 NW][n_tab]: the half-waves' sums
+  float* room = reinterpret_cast<float*>(lds + 4 * TILE);  // [NW][kDiag]
+  float* tab = room + NW * kDiag;                     // bias of distance d at near + d
+  float* acc = tab + n_tab;                                // [NW][n_tab]: the waves' sums
 
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -136,16 +168,17 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
   TileT tk, tv;
 
   for (int32_t e = threadIdx.x; e < n_tab; e += NT) tab[e] = bias_at<T>(p.bias, p.H, h, e - near);
-  for (int32_t e = threadIdx.x; e < 2 * NW * n_tab; e += NT) acc[e] = 0.0f;
+  for (int32_t e = threadIdx.x; e < NW * n_tab; e += NT) acc[e] = 0.0f;
   clear_pad<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
   const float left = bias_at<T>(p.bias, p.H, h, -p.bias.M), right = bias_at<T>(p.bias, p.H, h, p.bias.M);
-  float* mine = acc + (2 * wave + g) * n_tab + near;
+  float* mine = acc + wave * n_tab + near;
   float sum_l = 0.0f, sum_r = 0.0f;
 
+  // a work-group's items: with one each, the costly ones (causal: the last blocks of
+  // every unit) come first
   const uint32_t n_items = p.BX * p.n_blk;
   for (uint32_t item = part; item < n_items; item += p.parts) {
-    const uint32_t bx = item / p.n_blk;
-    const uint32_t blk = p.causal ? p.n_blk - 1 - item % p.n_blk : item % p.n_blk;
+    const uint32_t blk = p.n_blk - 1 - item / p.BX, bx = item - item / p.BX * p.BX;
     const uint32_t b = bx / p.X;
     const int64_t q_at = bx_at(p, bx, p.qs) + (int64_t)h * D, o_at = bx_at(p, bx, p.os) + (int64_t)h * D;
     const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)(h / p.grp) * D;
@@ -169,15 +202,18 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
     if (k1) fetch(0);
     const uint32_t row = blk * QB + 32 * wave + l32;
     const bool on = row < p.Lq;
-    typename M::frag qf[G::NS], df[G::NS], of[G::NS];
+    typename M::frag qf[G::NS], df[G::NS];
     row_frags<T, DC>(on ? static_cast<const T*>(p.q) + q_at + (int64_t)row * p.qs[2] : nullptr, g, D, p.vec, qf);
     row_frags<T, DC>(on ? static_cast<const T*>(p.dout) + o_at + (int64_t)row * p.os[2] : nullptr, g, D, p.vec, df);
-    row_frags<T, DC>(on ? static_cast<const T*>(p.o) + o_at + (int64_t)row * p.os[2] : nullptr, g, D, p.vec, of);
     float delta = 0.0f;
+    {
+      typename M::frag of[G::NS];
+      row_frags<T, DC>(on ? static_cast<const T*>(p.o) + o_at + (int64_t)row * p.os[2] : nullptr, g, D, p.vec, of);
 #pragma unroll
-    for (int s = 0; s < G::NS; ++s)
+      for (int s = 0; s < G::NS; ++s)
 #pragma unroll
-      for (int e = 0; e < G::E; ++e) delta += (float)df[s][e] * (float)of[s][e];
+        for (int e = 0; e < G::E; ++e) delta += (float)df[s][e] * (float)of[s][e];
+    }
     delta += swap_halves(delta);
     const uint64_t stat = ((uint64_t)bx * p.H + h) * p.Lq + row;
     // a row without keys, or past the end: P = exp2(-inf) = 0
@@ -198,77 +234,71 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
       if (more) fetch(kb + KB);
       const T* kl = lds + (it & 1) * 2 * TILE;
       const T* vl = kl + TILE;
-      if (!(p.causal && (int32_t)kb > wq + 31)) {
-        floatx16 s[NKT], dp[NKT];
 #pragma unroll
-        for (int kt = 0; kt < NKT; ++kt)
+      for (int kt = 0; kt < NKT; ++kt) {
+        const int32_t key0 = (int32_t)kb + 32 * kt, d0 = key0 - wq;
+        if (key0 >= (int32_t)k1 || (p.causal && d0 > 31)) continue;
+        floatx16 s, dp;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kt][r] = dp[kt][r] = 0.0f;
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
 #pragma unroll
-        for (int st = 0; st < G::NS; ++st)
-#pragma unroll
-          for (int kt = 0; kt < NKT; ++kt) {
-            const int at = (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g;
-            s[kt] = M::mma(*reinterpret_cast<const typename M::frag*>(kl + at), qf[st], s[kt]);
-            dp[kt] = M::mma(*reinterpret_cast<const typename M::frag*>(vl + at), df[st], dp[kt]);
-          }
-#pragma unroll
-        for (int kt = 0; kt < NKT; ++kt) {
-          const int32_t key0 = (int32_t)kb + 32 * kt, d0 = key0 - wq;
-          const bool far = d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M;
-          const int32_t at = d0 + 4 * g - l32;   // the distance of register 0
-          if (far) {
-            const float t = (d0 < 0 ? left : right) - lse2;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], p.c, t);
-          } else {
-            const float* tb = tab + near + at;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[kt][r] = fmaf(s[kt][r], p.c, tb[8 * (r / 4) + r % 4] - lse2);
-          }
-          if ((p.causal && d0 + 31 > 0) || key0 + 32 > (int32_t)k1) {
-            const int32_t stop = p.causal ? min((int32_t)k1, wq + l32 + 1) : (int32_t)k1;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (key0 + 8 * (r / 4) + 4 * g + r % 4 >= stop) s[kt][r] = -INFINITY;
-          }
-          ColB<T> z;
-          float row_z = 0.0f;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const float dz = __builtin_amdgcn_exp2f(s[kt][r]) * (dp[kt][r] - delta);
-            dp[kt][r] = dz;
-            z.set(r, dz);
-          }
-          if (far) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) row_z += dp[kt][r];
-            if (d0 < 0) sum_l += row_z;
-            else sum_r += row_z;
-          } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) atomicAdd(mine + at + 8 * (r / 4) + r % 4, dp[kt][r]);
-          }
-          dq.add(kl, 32 * kt, lane, z);
+        for (int st = 0; st < G::NS; ++st) {
+          const int at = (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g;
+          s = M::mma(*reinterpret_cast<const typename M::frag*>(kl + at), qf[st], s);
+          dp = M::mma(*reinterpret_cast<const typename M::frag*>(vl + at), df[st], dp);
         }
+        const bool far = d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M;
+        if (far) {
+          const float t = (d0 < 0 ? left : right) - lse2;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, t);
+        } else {
+          const float* tb = tab + near + d0 + 4 * g - l32;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, tb[8 * (r / 4) + r % 4] - lse2);
+        }
+        if ((p.causal && d0 + 31 > 0) || key0 + 32 > (int32_t)k1) {
+          const int32_t stop = (p.causal ? min((int32_t)k1, wq + l32 + 1) : (int32_t)k1) - key0 - 4 * g;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (8 * (r / 4) + r % 4 >= stop) s[r] = -INFINITY;
+        }
+        ColB<T> z;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          dp[r] = __builtin_amdgcn_exp2f(s[r]) * (dp[r] - delta);
+          z.set(r, dp[r]);
+        }
+        if (far) {
+          float v = 0.0f;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) v += dp[r];
+          if (d0 < 0) sum_l += v;
+          else sum_r += v;
+        } else {
+          add_diagonals(mine + d0, room + wave * kDiag, dp, lane);
+        }
+        dq.add(kl, 32 * kt, lane, z);
       }
       if (more) stash((it + 1) & 1);
       __syncthreads();
     }
     dq.scale(p.scale, lane);
     T* out = static_cast<T*>(p.dq) + q_at;
-    store_rows<T, DC>(dq, lane, D, p.vec, [&](int n) -> T* {
+    auto q_out = [&](int n) -> T* {
       const uint32_t r = blk * QB + 32 * wave + n;
       return r < p.Lq ? out + (int64_t)r * p.qs[2] : nullptr;
-    });
+    };
+    if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, dq, lane, D, q_out);   // this wave's rows of the tiles
+    else store_rows<T, DC>(dq, lane, D, false, q_out);
   }
 
   __syncthreads();
-  float* ends = reinterpret_cast<float*>(lds);   // [2][NT]
+  float* ends = room;   // [2][NT]
   ends[threadIdx.x] = sum_l;
   ends[NT + threadIdx.x] = sum_r;
   __syncthreads();
-  fold_sums<NT>(p, acc, 2 * NW, ends, h, part);
+  fold_sums<NT>(p, acc, NW, ends, h, part);
 }
 
 // dbias[t][h]: the parts of each distance, then the distances of each bucket, in a fixed
@@ -304,12 +334,16 @@ __global__ __launch_bounds__(1024) void relpos_bias_grad_kernel(BwdParams p, T* 
 }
 
 // ---------------------------------------------------------------------------
-// dK and dV: 32 keys of one key/value head per wave, over the queries of the group.
-template <typename T, int DC, int NW, int QT, int MINW>
-__global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams p) {
+// dK and dV, over the queries of every head of the key/value head's group: KW blocks of
+// 32 keys, the queries of a tile shared out among QS waves for each, whose sums are
+// joined at the end.  KW = 4 reads the queries least often; QS = 4 makes four times the
+// work-groups, each a quarter as long, which is what few, long, causal or ragged units
+// need to fill the chip evenly.
+template <typename T, int DC, int KW, int QS, int MINW>
+__global__ __launch_bounds__(KW * QS * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams p) {
   using G = Geo<T, DC>;
   using M = Mx<T>;
-  constexpr int NT = NW * 64, QB = 32 * QT, TILE = QB * G::P;
+  constexpr int NT = KW * QS * 64, QT = QS > 1 ? QS : sizeof(T) == 2 ? 2 : 1, QB = 32 * QT, TILE = QB * G::P;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   T* lds = reinterpret_cast<T*>(smem);                            // [2][Q, dO][QB][P]
   float* stat = reinterpret_cast<float*>(lds + 4 * TILE);         // [2][lse2, Delta][QB]
@@ -318,25 +352,25 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
 
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  uint32_t bid = blockIdx.x;
-  if ((p.n_blocks & 7u) == 0) bid = (bid & 7u) * (p.n_blocks >> 3) + (bid >> 3);
-  const uint32_t unit = bid / p.n_blk, blk = bid - unit * p.n_blk;
-  const uint32_t hkv = p.H / p.grp, bx = unit / hkv, e = unit % hkv, b = bx / p.X;
+  const int kw = wave / QS, qs = wave % QS;
+  const Place pl = place(p.order);   // heads of the order: key/value heads
+  if (!pl.any) return;
+  const uint32_t blk = pl.block, bx = pl.bx, e = pl.h, b = bx / p.X;
   const int D = (int)p.D;
   const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D;
   const int64_t q_bx = bx_at(p, bx, p.qs), o_bx = bx_at(p, bx, p.os);
-  const uint32_t key0 = blk * 32 * NW + 32 * wave, key = key0 + l32;
+  const uint32_t first_key = blk * 32 * KW, key0 = first_key + 32 * kw, key = key0 + l32;
   const uint32_t len = length(p.kv_len, b, p.Lk);
   const int32_t pos = position(p.q_pos, b);
-  const bool on = key < len;
   typename M::frag kf[G::NS], vf[G::NS];
-  row_frags<T, DC>(on ? static_cast<const T*>(p.k) + k_at + (int64_t)key * p.ks[2] : nullptr, g, D, p.vec, kf);
-  row_frags<T, DC>(on ? static_cast<const T*>(p.v) + k_at + (int64_t)key * p.ks[2] : nullptr, g, D, p.vec, vf);
+  row_frags<T, DC>(key < len ? static_cast<const T*>(p.k) + k_at + (int64_t)key * p.ks[2] : nullptr, g, D, p.vec, kf);
+  row_frags<T, DC>(key < len ? static_cast<const T*>(p.v) + k_at + (int64_t)key * p.ks[2] : nullptr, g, D, p.vec, vf);
 
   const uint32_t q_row = (uint32_t)p.qs[2] * (uint32_t)sizeof(T), o_row = (uint32_t)p.os[2] * (uint32_t)sizeof(T);
   using TileT = Tile<T, DC, QB, NT>;
   const typename TileT::Map mq = TileT::map(D, q_row, threadIdx.x), mo = TileT::map(D, o_row, threadIdx.x);
   TileT tq, to;
+  static_assert(NT >= 2 * QB || QB == 128, "a statistic for each thread");
   float pre = 0.0f;
   clear_pad<T, DC>(lds, 4 * QB, D, threadIdx.x, NT);
 
@@ -344,10 +378,10 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
   dk.zero();
   dv.zero();
   // the first tile of queries that sees the work-group's first key
-  const int32_t first = p.causal ? (int32_t)(blk * 32 * NW) - pos : 0;
+  const int32_t first = p.causal ? (int32_t)first_key - pos : 0;
   const uint32_t it0 = first > 0 ? (uint32_t)first / QB : 0u;
   const uint32_t n_it = (p.Lq + QB - 1) / QB;
-  const bool any = blk * 32 * NW < len && it0 < n_it;
+  const bool any = first_key < len && it0 < n_it;
   for (uint32_t hh = 0; any && hh < p.grp; ++hh) {
     const uint32_t h = e * p.grp + hh;
     const T* qg = static_cast<const T*>(p.q) + q_bx + (int64_t)h * D;
@@ -382,9 +416,10 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
       const T* ol = ql + TILE;
       const float* sl = stat + (it & 1) * 2 * QB;
 #pragma unroll
-      for (int sub = 0; sub < QT; ++sub) {
+      for (int i = 0; i < QT / QS; ++i) {
+        const int sub = i * QS + qs;
         const int32_t q0 = pos + (int32_t)(it * QB) + 32 * sub;   // position of the block's first query
-        if (key0 >= len || (p.causal && (int32_t)key0 > q0 + 31)) continue;
+        if (key0 >= len || it * QB + 32 * sub >= p.Lq || (p.causal && (int32_t)key0 > q0 + 31)) continue;
         floatx16 s, dp;
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
@@ -395,16 +430,15 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
           dp = M::mma(*reinterpret_cast<const typename M::frag*>(ol + at), vf[st], dp);
         }
         // lane (n + 32 g): key n, queries 8 (r / 4) + 4 g + r % 4
-        const int32_t d0 = (int32_t)key0 - q0;
-        block_probabilities(p, s, sl + 32 * sub + 4 * g, tab + near, left, right, d0, l32, g, key0, len);
+        block_probabilities(p, s, sl + 32 * sub + 4 * g, tab + near, left, right, (int32_t)key0 - q0, l32, g, key0, len);
         ColB<T> pb, zb;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const floatx4 dl = *reinterpret_cast<const floatx4*>(sl + QB + 32 * sub + 8 * q + 4 * g);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            pb.set(4 * q + i, s[4 * q + i]);
-            zb.set(4 * q + i, s[4 * q + i] * (dp[4 * q + i] - dl[i]));
+          for (int j = 0; j < 4; ++j) {
+            pb.set(4 * q + j, s[4 * q + j]);
+            zb.set(4 * q + j, s[4 * q + j] * (dp[4 * q + j] - dl[j]));
           }
         }
         dv.add(ol, 32 * sub, lane, pb);
@@ -415,10 +449,39 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams
     }
   }
   dk.scale(p.scale, lane);
-  T* ko = static_cast<T*>(p.dk) + k_at;
-  T* vo = static_cast<T*>(p.dv) + k_at;
-  store_rows<T, DC>(dk, lane, D, p.vec, [&](int n) { return key0 + n < p.Lk ? ko + (int64_t)(key0 + n) * p.ks[2] : nullptr; });
-  store_rows<T, DC>(dv, lane, D, p.vec, [&](int n) { return key0 + n < p.Lk ? vo + (int64_t)(key0 + n) * p.ks[2] : nullptr; });
+  T* const out[2] = {static_cast<T*>(p.dk) + k_at, static_cast<T*>(p.dv) + k_at};
+  auto row = [&](T* base, int n) -> T* { return key0 + n < p.Lk ? base + (int64_t)(key0 + n) * p.ks[2] : nullptr; };
+  if constexpr (QS == 1) {
+    if (p.vec) {
+      T* so = lds + wave * 32 * G::P;   // the tiles are done with
+      static_assert(KW * 32 <= 4 * QB, "rows to write through");
+      __syncthreads();
+      store_rows_lds<T, DC>(so, dk, lane, D, [&](int n) { return row(out[0], n); });
+      store_rows_lds<T, DC>(so, dv, lane, D, [&](int n) { return row(out[1], n); });
+    } else {
+      store_rows<T, DC>(dk, lane, D, false, [&](int n) { return row(out[0], n); });
+      store_rows<T, DC>(dv, lane, D, false, [&](int n) { return row(out[1], n); });
+    }
+  } else {
+    // the QS waves' sums of a key, added in order
+    float* sums = reinterpret_cast<float*>(smem);   // [QS][KW * 32][DP]
+    constexpr int W = G::DP, ROWS = KW * 32;
+    static_assert((size_t)QS * ROWS * W * 4 <= (size_t)4 * TILE * sizeof(T), "the sums fit the tiles");
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      __syncthreads();
+      store_rows<T, DC>(which ? dv : dk, lane, W, true, [&](int n) { return sums + (qs * ROWS + kw * 32 + n) * W; });
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < ROWS * W / 4; i += NT) {
+        const uint32_t n = i / (W / 4), d = i % (W / 4) * 4;
+        floatx4 v = *reinterpret_cast<const floatx4*>(sums + n * W + d);
+#pragma unroll
+        for (int q = 1; q < QS; ++q) v += *reinterpret_cast<const floatx4*>(sums + (q * ROWS + n) * W + d);
+        if (first_key + n < p.Lk)
+          store4(out[which] + (int64_t)(first_key + n) * p.ks[2], (int)d, D, p.vec, v[0], v[1], v[2], v[3]);
+      }
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------
@@ -444,8 +507,8 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
   float* st_del = st_lse + R;                             // [R]
   const int32_t near = p.bias.M + kEdge, n_tab = 2 * near + 1;
   float* tab = st_del + R;                                // [n_tab]
-  float* acc = tab + n_tab;                               // [2 NB][n_tab]
-  float* ends = acc + 2 * NB * n_tab;                     // [2][NT]: sums past the table's ends
+  float* acc = tab + n_tab;                               // [NB][n_tab]: the waves' sums
+  float* ends = acc + NB * n_tab;                         // [2][NT]: sums past the table's ends
 
   const int lane0 = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -460,7 +523,7 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
                             mo = TileT::map(D, o_row, threadIdx.x);
 
   for (int32_t t = threadIdx.x; t < n_tab; t += NT) tab[t] = bias_at<T>(p.bias, p.H, h, t - near);
-  for (int32_t t = threadIdx.x; t < 2 * NB * n_tab + 2 * NT; t += NT) acc[t] = 0.0f;   // and the ends
+  for (int32_t t = threadIdx.x; t < NB * n_tab + 2 * NT; t += NT) acc[t] = 0.0f;   // and the ends
   clear_pad<T, DC>(kl, 4 * R, D, threadIdx.x, NT);
 
   floatx16 sum[NB];   // of dZ, queries 32 wave .. against keys 32 kt ..
@@ -474,9 +537,10 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
     const uint32_t b = done ? 0 : bx / p.X;
     const int32_t q0 = position(p.q_pos, b);
     if (done || q0 != sum_q0) {
-      __syncthreads();   // the sums by distance are set
-      const int l32 = lane0 & 31, g = lane0 >> 5;
-      float* mine = acc + (2 * wave + g) * n_tab + near;
+      __syncthreads();   // the sums by distance are set, the rows of K, V, Q and dO free
+      float* mine = acc + wave * n_tab + near;
+      float* room = reinterpret_cast<float*>(smem) + wave * kDiag;
+      static_assert((size_t)NB * kDiag * 4 <= (size_t)4 * TILE * sizeof(T), "blocks of dZ fit the rows");
 #pragma unroll
       for (int kt = 0; kt < NB; ++kt) {
         const int32_t d0 = 32 * kt - sum_q0 - 32 * wave;
@@ -486,14 +550,14 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
           for (int r = 0; r < 16; ++r) v += sum[kt][r];
           ends[(d0 < 0 ? 0 : NT) + threadIdx.x] += v;
         } else {
-          float* to = mine + d0 + 4 * g - l32;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) atomicAdd(to + 8 * (r / 4) + r % 4, sum[kt][r]);
+          add_diagonals(mine + d0, room, sum[kt], lane0);
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum[kt][r] = 0.0f;
       }
       sum_q0 = q0;
+      __syncthreads();
+      clear_pad<T, DC>(kl, 4 * R, D, threadIdx.x, NT);   // the blocks went over it
     }
     if (done) break;
     int lane = lane0;
@@ -647,7 +711,7 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
     }
   }
   __syncthreads();
-  fold_sums<NT>(p, acc, 2 * NB, ends, h, part);
+  fold_sums<NT>(p, acc, NB, ends, h, part);
 }
 
 constexpr int kQB = 128;   // queries of a work-group of the dQ kernel
@@ -657,7 +721,7 @@ constexpr int kQB = 128;   // queries of a work-group of the dQ kernel
 // a wider one's rows and sums do not fit the registers).
 size_t short_lds(const RelposArgs& a, int nb, int row_bytes) {
   const size_t n_tab = 2 * ((size_t)a.max_dist + kEdge) + 1;
-  return (size_t)4 * 32 * nb * row_bytes + (size_t)2 * 32 * nb * 4 + (n_tab * (1 + 2 * nb) + 2 * 64 * nb) * 4;
+  return (size_t)4 * 32 * nb * row_bytes + (size_t)2 * 32 * nb * 4 + (n_tab * (1 + nb) + 2 * 64 * nb) * 4;
 }
 int row_bytes_of(const RelposArgs& a) {
   const int dc = a.bf16 ? (a.D <= 32 ? 32 : a.D <= 48 ? 48 : a.D <= 64 ? 64 : a.D <= 80 ? 80 : a.D <= 96 ? 96 : 128)
@@ -677,7 +741,7 @@ int64_t parts_of(const RelposArgs& a) {
     return (std::min(a.B * a.X, want) + 7) / 8 * 8;
   }
   const int64_t items = a.B * a.X * ((a.Lq + kQB - 1) / kQB);
-  const int64_t want = (1024 + a.H - 1) / a.H;
+  const int64_t want = (4096 + a.H - 1) / a.H;
   return std::max<int64_t>(1, std::min(items, want));
 }
 
@@ -707,34 +771,42 @@ int start_short(BwdParams& p, const RelposArgs& a, hipStream_t s) {
   return bias_grad<T>(p, a, s);
 }
 
+template <typename T, int DC, int KW, int QS>
+int start_dkv(BwdParams& p, const RelposArgs& a, hipStream_t s) {
+  constexpr int QB = 32 * (QS > 1 ? QS : sizeof(T) == 2 ? 2 : 1);
+  p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lk + 32 * KW - 1) / (32 * KW), a.causal);
+  if (!grid_fits(order_blocks(p.order), KW * QS * 64)) return DSP_ERR_SHAPE;
+  const size_t lds = (size_t)4 * QB * Geo<T, DC>::P * sizeof(T) + (size_t)4 * QB * 4 +
+                     (2 * ((size_t)p.bias.M + kEdge) + 1) * 4;
+  auto* kernel = relpos_bwd_dkv_kernel<T, DC, KW, QS, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
+  if (int st = lds_limit(kernel, lds)) return st;
+  kernel<<<dim3((uint32_t)order_blocks(p.order)), KW * QS * 64, lds, s>>>(p);
+  return last_launch_status();
+}
+
 template <typename T, int DC>
 int start(BwdParams& p, const RelposArgs& a, hipStream_t s) {
   using G = Geo<T, DC>;
-  constexpr int NW = 4, KB = 32;
+  constexpr int NW = kQB / 32, KB = sizeof(T) == 2 ? 64 : 32;
   if constexpr (sizeof(T) == 2 || DC <= 64)
     if (const int nb = short_blocks(a)) return nb == 1 ? start_short<T, DC, 1>(p, a, s) : start_short<T, DC, 2>(p, a, s);
   const size_t n_tab = 2 * ((size_t)p.bias.M + kEdge) + 1;
   if (a.Lq > 0) {
-    p.n_blk = (uint32_t)((a.Lq + 32 * NW - 1) / (32 * NW));
-    const size_t lds = (size_t)4 * KB * G::P * sizeof(T) + n_tab * 4 * (1 + 2 * NW);
-    auto* kernel = relpos_bwd_dq_kernel<T, DC, NW, KB, 1>;
+    p.n_blk = (uint32_t)((a.Lq + kQB - 1) / kQB);
+    const size_t lds = (size_t)4 * KB * G::P * sizeof(T) + (size_t)NW * kDiag * 4 + n_tab * 4 * (1 + NW);
+    auto* kernel = relpos_bwd_dq_kernel<T, DC, NW, KB, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
     if (int st = lds_limit(kernel, lds)) return st;
     kernel<<<dim3(p.H * p.parts), NW * 64, lds, s>>>(p);
     if (int st = last_launch_status()) return st;
   }
   if (int st = bias_grad<T>(p, a, s)) return st;
-  if (a.Lk > 0) {
-    constexpr int QT = 1;
-    p.n_blk = (uint32_t)((a.Lk + 32 * NW - 1) / (32 * NW));
-    const int64_t blocks = a.B * a.X * a.Hkv * p.n_blk;
-    if (!grid_fits(blocks, NW * 64)) return DSP_ERR_SHAPE;
-    p.n_blocks = (uint32_t)blocks;
-    const size_t lds = (size_t)4 * 32 * QT * G::P * sizeof(T) + (size_t)4 * 32 * QT * 4 + n_tab * 4;
-    auto* kernel = relpos_bwd_dkv_kernel<T, DC, NW, QT, 1>;
-    if (int st = lds_limit(kernel, lds)) return st;
-    kernel<<<dim3(p.n_blocks), NW * 64, lds, s>>>(p);
-  }
-  return last_launch_status();
+  if (a.Lk == 0) return DSP_OK;
+  // as many work-groups as fill the chip four times over, where splitting makes them
+  const int64_t wide = a.B * a.X * a.Hkv * ((a.Lk + 127) / 128);
+  if (wide >= 2048) return start_dkv<T, DC, 4, 1>(p, a, s);
+  if (wide >= 1024 || sizeof(T) == 4) return start_dkv<T, DC, 2, 2>(p, a, s);   // fp32: four tiles are past the LDS
+  if constexpr (sizeof(T) == 2) return start_dkv<T, DC, 1, 4>(p, a, s);
+  return DSP_ERR_HIP;
 }
 
 }  // namespace
