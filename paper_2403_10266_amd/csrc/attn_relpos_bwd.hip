@@ -334,23 +334,23 @@ __global__ __launch_bounds__(1024) void relpos_bias_grad_kernel(BwdParams p, T* 
 }
 
 // ---------------------------------------------------------------------------
-// dK and dV, over the queries of every head of the key/value head's group: KW blocks of
-// 32 keys, the queries of a tile shared out among QS waves for each, whose sums are
-// joined at the end.  KW = 4 reads the queries least often; QS = 4 makes four times the
-// work-groups, each a quarter as long, which is what few, long, causal or ragged units
-// need to fill the chip evenly.
-template <typename T, int DC, int KW, int QS, int MINW>
+// dK and dV, over the queries of every head of the key/value head's group, in tiles of
+// 32 QT: KW blocks of 32 keys, each tile's queries shared out among QS waves for each,
+// whose sums are joined at the end.  More keys read the queries less often; more waves
+// to a key make more work-groups, each shorter, which is what few, long, causal or
+// ragged units need to fill the chip evenly.
+template <typename T, int DC, int KW, int QS, int QT, int MINW>
 __global__ __launch_bounds__(KW * QS * 64, MINW) void relpos_bwd_dkv_kernel(BwdParams p) {
   using G = Geo<T, DC>;
   using M = Mx<T>;
-  constexpr int NT = KW * QS * 64, QT = QS > 1 ? QS : sizeof(T) == 2 ? 2 : 1, QB = 32 * QT, TILE = QB * G::P;
+  constexpr int NT = KW * QS * 64, QB = 32 * QT, TILE = QB * G::P;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   T* lds = reinterpret_cast<T*>(smem);                            // [2][Q, dO][QB][P]
   float* stat = reinterpret_cast<float*>(lds + 4 * TILE);         // [2][lse2, Delta][QB]
   const int32_t near = p.bias.M + kEdge, n_tab = 2 * near + 1;
   float* tab = stat + 4 * QB;
 
-  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int lane0 = threadIdx.x & 63, lane = lane0, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kw = wave / QS, qs = wave % QS;
   const Place pl = place(p.order);   // heads of the order: key/value heads
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void relpos_bwd_dkv_kernel(BwdP
   using TileT = Tile<T, DC, QB, NT>;
   const typename TileT::Map mq = TileT::map(D, q_row, threadIdx.x), mo = TileT::map(D, o_row, threadIdx.x);
   TileT tq, to;
-  static_assert(NT >= 2 * QB || QB == 128, "a statistic for each thread");
+  static_assert(NT >= 2 * QB, "a statistic for each thread");
   float pre = 0.0f;
   clear_pad<T, DC>(lds, 4 * QB, D, threadIdx.x, NT);
 
@@ -412,6 +412,9 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void relpos_bwd_dkv_kernel(BwdP
     for (uint32_t it = it0; it < n_it; ++it) {
       const bool more = it + 1 < n_it;
       if (more) fetch(it + 1);
+      int lane = lane0;
+      asm volatile("" : "+v"(lane));
+      const int l32 = lane & 31, g = lane >> 5;
       const T* ql = lds + (it & 1) * 2 * TILE;
       const T* ol = ql + TILE;
       const float* sl = stat + (it & 1) * 2 * QB;
@@ -714,7 +717,7 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
   fold_sums<NT>(p, acc, NB, ends, h, part);
 }
 
-constexpr int kQB = 128;   // queries of a work-group of the dQ kernel
+constexpr int kDqWaves = 4;   // of a work-group of the dQ kernel, 32 queries each
 
 // LDS of the short-unit kernel, and the blocks of 32 it takes the call with (0: not at
 // all): at most 64 queries and keys, heads with keys of their own (fp32 up to 64 wide:
@@ -740,7 +743,8 @@ int64_t parts_of(const RelposArgs& a) {
     const int64_t want = (256 * std::min<int64_t>(per_cu, 8 / nb) + a.Hkv - 1) / a.Hkv;
     return (std::min(a.B * a.X, want) + 7) / 8 * 8;
   }
-  const int64_t items = a.B * a.X * ((a.Lq + kQB - 1) / kQB);
+  constexpr int64_t qb = 32 * kDqWaves;
+  const int64_t items = a.B * a.X * ((a.Lq + qb - 1) / qb);
   const int64_t want = (4096 + a.H - 1) / a.H;
   return std::max<int64_t>(1, std::min(items, want));
 }
@@ -771,14 +775,26 @@ int start_short(BwdParams& p, const RelposArgs& a, hipStream_t s) {
   return bias_grad<T>(p, a, s);
 }
 
-template <typename T, int DC, int KW, int QS>
+template <typename T, int DC, int NW>
+int start_dq(BwdParams& p, const RelposArgs& a, hipStream_t s) {
+  constexpr int KB = sizeof(T) == 2 ? 64 : 32;
+  const size_t n_tab = 2 * ((size_t)p.bias.M + kEdge) + 1;
+  p.n_blk = (uint32_t)((a.Lq + 32 * NW - 1) / (32 * NW));
+  const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T) + (size_t)NW * kDiag * 4 + n_tab * 4 * (1 + NW);
+  auto* kernel = relpos_bwd_dq_kernel<T, DC, NW, KB, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
+  if (int st = lds_limit(kernel, lds)) return st;
+  kernel<<<dim3(p.H * p.parts), NW * 64, lds, s>>>(p);
+  return last_launch_status();
+}
+
+template <typename T, int DC, int KW, int QS, int QT>
 int start_dkv(BwdParams& p, const RelposArgs& a, hipStream_t s) {
-  constexpr int QB = 32 * (QS > 1 ? QS : sizeof(T) == 2 ? 2 : 1);
+  constexpr int QB = 32 * QT;
   p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lk + 32 * KW - 1) / (32 * KW), a.causal);
   if (!grid_fits(order_blocks(p.order), KW * QS * 64)) return DSP_ERR_SHAPE;
   const size_t lds = (size_t)4 * QB * Geo<T, DC>::P * sizeof(T) + (size_t)4 * QB * 4 +
                      (2 * ((size_t)p.bias.M + kEdge) + 1) * 4;
-  auto* kernel = relpos_bwd_dkv_kernel<T, DC, KW, QS, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
+  auto* kernel = relpos_bwd_dkv_kernel<T, DC, KW, QS, QT, KW * QS == 8 ? 2 : 1>;
   if (int st = lds_limit(kernel, lds)) return st;
   kernel<<<dim3((uint32_t)order_blocks(p.order)), KW * QS * 64, lds, s>>>(p);
   return last_launch_status();
@@ -786,27 +802,30 @@ int start_dkv(BwdParams& p, const RelposArgs& a, hipStream_t s) {
 
 template <typename T, int DC>
 int start(BwdParams& p, const RelposArgs& a, hipStream_t s) {
-  using G = Geo<T, DC>;
-  constexpr int NW = kQB / 32, KB = sizeof(T) == 2 ? 64 : 32;
   if constexpr (sizeof(T) == 2 || DC <= 64)
     if (const int nb = short_blocks(a)) return nb == 1 ? start_short<T, DC, 1>(p, a, s) : start_short<T, DC, 2>(p, a, s);
-  const size_t n_tab = 2 * ((size_t)p.bias.M + kEdge) + 1;
   if (a.Lq > 0) {
-    p.n_blk = (uint32_t)((a.Lq + kQB - 1) / kQB);
-    const size_t lds = (size_t)4 * KB * G::P * sizeof(T) + (size_t)NW * kDiag * 4 + n_tab * 4 * (1 + NW);
-    auto* kernel = relpos_bwd_dq_kernel<T, DC, NW, KB, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
-    if (int st = lds_limit(kernel, lds)) return st;
-    kernel<<<dim3(p.H * p.parts), NW * 64, lds, s>>>(p);
-    if (int st = last_launch_status()) return st;
+    if (int st = start_dq<T, DC, kDqWaves>(p, a, s)) return st;
   }
   if (int st = bias_grad<T>(p, a, s)) return st;
   if (a.Lk == 0) return DSP_OK;
-  // as many work-groups as fill the chip four times over, where splitting makes them
-  const int64_t wide = a.B * a.X * a.Hkv * ((a.Lk + 127) / 128);
-  if (wide >= 2048) return start_dkv<T, DC, 4, 1>(p, a, s);
-  if (wide >= 1024 || sizeof(T) == 4) return start_dkv<T, DC, 2, 2>(p, a, s);   // fp32: four tiles are past the LDS
-  if constexpr (sizeof(T) == 2) return start_dkv<T, DC, 1, 4>(p, a, s);
-  return DSP_ERR_HIP;
+  // The most keys to a work-group that still fill the chip, which holds 256 of eight
+  // waves: once where units are alike, twice where masks or lengths make them differ.
+  // 4 x 2000 tokens, 32 heads of 64 over 8, causal and ragged: gradients 478, 385 and
+  // 445 us with 8, 4 and 2 blocks of keys; 16 heads of 72 over 4: 484, 349, 273; not
+  // causal, 8 x 16 units of 4096: 3170, 3417, 3940.
+  auto fills = [&](int64_t keys) {
+    return a.B * a.X * a.Hkv * ((a.Lk + keys - 1) / keys) >= (a.causal || a.kv_len ? 512 : 256);
+  };
+  if constexpr (sizeof(T) == 2 && DC <= 80) {
+    if (fills(256)) return start_dkv<T, DC, 8, 1, 2>(p, a, s);
+    if (fills(128)) return start_dkv<T, DC, 4, 2, 4>(p, a, s);
+    return start_dkv<T, DC, 2, 4, 4>(p, a, s);
+  } else {
+    // wide heads and fp32: registers for four waves, in fp32 LDS for 64 queries
+    if (fills(128)) return start_dkv<T, DC, 4, 1, sizeof(T) == 2 ? 2 : 1>(p, a, s);
+    return start_dkv<T, DC, 2, 2, 2>(p, a, s);
+  }
 }
 
 }  // namespace
