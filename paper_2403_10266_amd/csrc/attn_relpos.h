@@ -59,6 +59,11 @@ struct Geo {
   static_assert(DC % 8 == 0 && (!SLAB || E == 8), "class");
 };
 
+// Between LDS accesses of different lanes of one wave to the same words: the hardware
+// keeps their order; the compiler does where it cannot tell a lane's addresses apart,
+// and has to be told to where it can.
+__device__ __forceinline__ void wave_order() { asm volatile("" ::: "memory"); }
+
 // A B operand of a column product made of a 32 x 32 accumulator
 template <typename T>
 struct ColB;
@@ -204,8 +209,7 @@ __device__ __forceinline__ void store_rows(const ColAcc<T, DC>& a, int lane, int
 
 // The same through LDS: `so` holds 32 rows of pitch P for this wave alone, and the rows
 // leave as whole 16-byte chunks, consecutive lanes along a row (from the accumulators
-// a store would write 8 or 16 bytes of 32 rows each).  One wave's LDS accesses complete
-// in order.
+// a store would write 8 or 16 bytes of 32 rows each).
 template <typename T, int DC, typename F>
 __device__ __forceinline__ void store_rows_lds(T* so, const ColAcc<T, DC>& a, int lane, int D, F row_of) {
   using G = Geo<T, DC>;

@@ -90,6 +90,7 @@ __device__ __forceinline__ void add_diagonals(float* at, float* room, const floa
     const int k = 8 * (r / 4) + r % 4;
     room[(k + 4 * g) * 32 + ((l32 - 4 * g - k) & 31)] = z[r];
   }
+  wave_order();
   // lane (c + 32 g): column c, rows 16 g ..; row k of it is query k + c, or k + c - 32
   float low = 0.0f, high = 0.0f;
   const int split = 32 - l32 - 16 * g;   // rows from here on have wrapped
@@ -105,6 +106,7 @@ __device__ __forceinline__ void add_diagonals(float* at, float* room, const floa
   // distance -c from the first half's lanes, 32 - c (c > 0) from the second's
   if (g == 0) at[-l32] += low;
   else if (l32) at[32 - l32] += high;
+  wave_order();
 }
 
 // A work-group's sums of one head into its part: the waves' arrays, the sums past
@@ -540,10 +542,11 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
     const uint32_t b = done ? 0 : bx / p.X;
     const int32_t q0 = position(p.q_pos, b);
     if (done || q0 != sum_q0) {
-      __syncthreads();   // the sums by distance are set, the rows of K, V, Q and dO free
+      __syncthreads();   // the sums by distance are set
+      int lane = lane0;
+      asm volatile("" : "+v"(lane));
+      const int l32 = lane & 31, g = lane >> 5;
       float* mine = acc + wave * n_tab + near;
-      float* room = reinterpret_cast<float*>(smem) + wave * kDiag;
-      static_assert((size_t)NB * kDiag * 4 <= (size_t)4 * TILE * sizeof(T), "blocks of dZ fit the rows");
 #pragma unroll
       for (int kt = 0; kt < NB; ++kt) {
         const int32_t d0 = 32 * kt - sum_q0 - 32 * wave;
@@ -553,14 +556,20 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
           for (int r = 0; r < 16; ++r) v += sum[kt][r];
           ends[(d0 < 0 ? 0 : NT) + threadIdx.x] += v;
         } else {
-          add_diagonals(mine + d0, room, sum[kt], lane0);
+          // rare: one register of one half of the wave (32 distances) at a time
+          float* to = mine + d0 + 4 * g - l32;
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              if (g == half) to[8 * (r / 4) + r % 4] += sum[kt][r];
+              wave_order();
+            }
         }
 #pragma unroll
         for (int r = 0; r < 16; ++r) sum[kt][r] = 0.0f;
       }
       sum_q0 = q0;
-      __syncthreads();
-      clear_pad<T, DC>(kl, 4 * R, D, threadIdx.x, NT);   // the blocks went over it
     }
     if (done) break;
     int lane = lane0;
