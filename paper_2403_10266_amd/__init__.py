@@ -193,33 +193,52 @@ class _on:
         return False
 
 
-class _on_device:
+_I3 = ctypes.c_int64 * 3
+
+
+class _on_device(_on):
     """`_on` for calls whose tensors may be on another device than the current one: that
-    device is current meanwhile (its current stream, or the given `stream` of it)."""
-    __slots__ = ("dev", "on")
+    device is current meanwhile (its current stream, or the given `stream` of it).
+    Yields the stream's handle as a number."""
+    __slots__ = ("device",)
 
     def __init__(self, t, stream):
         torch = _torch()
         if stream is not None and stream.device != t.device:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {t.device}")
-        self.dev = torch.cuda.device(t.device) if t.device.index != torch.cuda.current_device() else None
-        if self.dev is not None:
-            self.dev.__enter__()
+        dev = t.get_device()
+        if stream is not None or dev == torch.cuda.current_device():
+            self.device = None
+            super().__init__(stream)
+            return
+        self.device = torch.cuda.device(dev)
+        self.device.__enter__()
         try:
-            self.on = _on(stream)
+            super().__init__(None)
         except BaseException:
-            if self.dev is not None:
-                self.dev.__exit__(None, None, None)
+            self.device.__exit__(None, None, None)
             raise
 
     def __enter__(self):
-        return self.on.__enter__()
+        super().__enter__()
+        return self.handle
 
     def __exit__(self, *exc):
-        self.on.__exit__(*exc)
-        if self.dev is not None:
-            self.dev.__exit__(*exc)
+        super().__exit__(*exc)
+        if self.device is not None:
+            self.device.__exit__(*exc)
         return False
+
+
+def _as(t, dtype, shape, device) -> bool:
+    """Whether t has this dtype, shape and device index: most of `_check` at a third of
+    its time, for calls of a few microseconds (`_check` then says what is wrong)."""
+    return t is not None and t.dtype is dtype and t.shape == shape and t.get_device() == device
+
+
+def _at(t):
+    """A tensor's address for an argument of pointer type, None for None."""
+    return None if t is None else t.data_ptr()
 
 
 def _check(where, name, t, *, dtype=None, shape=None, numel=None, contiguous=True, like=None, strides=None):
@@ -659,15 +678,18 @@ def dsp_relpos_buckets(max_dist: int, n_buckets: int, bidirectional: bool = True
 def _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len):
     torch = _torch()
     dims = _general_views(w, q, k, v, H, Hkv)
-    _check(w, "bias", bias, dtype=q.dtype, like=q)
-    if bias.dim() != 2 or bias.shape[0] < 1 or bias.shape[1] != H:
+    dev = q.get_device()
+    if not (_as(bias, q.dtype, (bias.shape[0] if bias is not None and bias.dim() else 0, H), dev)
+            and bias.shape[0] > 0 and bias.is_contiguous()):
+        _check(w, "bias", bias, dtype=q.dtype, like=q)
         raise ValueError(f"{w}: bias must be [n_buckets, H = {H}]")
-    _check(w, "buckets", buckets, dtype=torch.int32, like=q)
-    if buckets.dim() != 1 or buckets.numel() % 2 == 0:
+    if not (_as(buckets, torch.int32, (buckets.numel() | 1 if buckets is not None else 0,), dev)
+            and buckets.is_contiguous()):
+        _check(w, "buckets", buckets, dtype=torch.int32, like=q)
         raise ValueError(f"{w}: buckets must be [2 * max_dist + 1]")
     for name, t in (("q_pos", q_pos), ("kv_len", kv_len)):
-        if t is not None:
-            _check(w, name, t, dtype=torch.int32, shape=(dims[0],), like=q)
+        if t is not None and not (_as(t, torch.int32, dims[:1], dev) and t.is_contiguous()):
+            _check(w, name, t, dtype=torch.int32, shape=dims[:1], like=q)
     return dims
 
 
@@ -699,12 +721,13 @@ def dsp_attn_relpos(q, k, v, H: int, Hkv: int, bias, buckets, causal: bool = Fal
         if lse is not None:
             _check(w, "lse", lse, dtype=torch.float32, numel=B * X * H * Lq, like=q)
         dt = _dtype_code(q)
-        ws = _workspace(w, lib().dsp_attn_relpos_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, dt), workspace, q)
-        _check_status(lib().dsp_attn_relpos(
-            _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(bias), _ptr(buckets), bias.shape[0],
-            buckets.numel() // 2, _ptr(q_pos), _ptr(kv_len), DSP_RELPOS_CAUSAL if causal else 0, _ptr(ws),
-            _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv, D, _st3(q), _st3(k), _st3(out), float(scale),
-            dt, s), w)
+        L = lib()
+        ws = _workspace(w, L.dsp_attn_relpos_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, dt), workspace, q)
+        _check_status(L.dsp_attn_relpos(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _at(lse), bias.data_ptr(), buckets.data_ptr(),
+            bias.shape[0], buckets.numel() // 2, _at(q_pos), _at(kv_len), DSP_RELPOS_CAUSAL if causal else 0, _at(ws),
+            _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv, D, _I3(*q.stride()[:3]), _I3(*k.stride()[:3]),
+            _I3(*out.stride()[:3]), scale, dt, s), w)
     return (out, lse) if lse is not None else out
 
 
@@ -731,12 +754,14 @@ def dsp_attn_relpos_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, bias, buckets, 
         dbias = torch.empty_like(bias) if dbias is None else dbias
         _check(w, "dbias", dbias, dtype=q.dtype, shape=bias.shape, like=q)
         dt, M = _dtype_code(q), buckets.numel() // 2
-        ws = _workspace(w, lib().dsp_attn_relpos_bwd_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, M, dt), workspace, q)
-        _check_status(lib().dsp_attn_relpos_bwd(
-            _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(lse), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dbias),
-            _ptr(bias), _ptr(buckets), bias.shape[0], M, _ptr(q_pos), _ptr(kv_len),
-            DSP_RELPOS_CAUSAL if causal else 0, _ptr(ws), _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv,
-            D, _st3(q), _st3(k), _st3(o), float(scale), dt, s), w)
+        L = lib()
+        ws = _workspace(w, L.dsp_attn_relpos_bwd_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, M, dt), workspace, q)
+        _check_status(L.dsp_attn_relpos_bwd(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), dout.data_ptr(), lse.data_ptr(), dq.data_ptr(),
+            dk.data_ptr(), dv.data_ptr(), dbias.data_ptr(), bias.data_ptr(), buckets.data_ptr(), bias.shape[0], M,
+            _at(q_pos), _at(kv_len), DSP_RELPOS_CAUSAL if causal else 0, _at(ws),
+            _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv, D, _I3(*q.stride()[:3]), _I3(*k.stride()[:3]),
+            _I3(*o.stride()[:3]), scale, dt, s), w)
     return dq, dk, dv, dbias
 
 
@@ -745,7 +770,7 @@ def _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos):
     torch = _torch()
     x, n = (q, H) if q is not None else (k, Hkv)
     _check(w, "q" if q is not None else "k", x, contiguous=False)
-    _float_dtype(w, x)
+    dt, dev = _float_dtype(w, x), x.get_device()
     if (q is None) != (H == 0) or (k is None) != (Hkv == 0):
         raise ValueError(f"{w}: q has H heads and k has Hkv heads (None: 0)")
     if x.dim() != 4 or n < 1 or x.shape[3] % n:
@@ -755,23 +780,41 @@ def _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos):
     for name, t, heads, g in (("q", q, H, gq), ("k", k, Hkv, gk)):
         if t is None:
             continue
-        _check(w, name, t, dtype=x.dtype, shape=(B, X, L, heads * D), contiguous=False, like=x)
+        if not _as(t, dt, (B, X, L, heads * D), dev):
+            _check(w, name, t, dtype=dt, shape=(B, X, L, heads * D), contiguous=False, like=x)
         if t.stride(3) != 1:
             raise ValueError(f"{w}: {name} must have a unit last stride")
-        if g is not None:
-            _check(w, "g" + name, g, dtype=x.dtype, shape=(D,), like=x)
+        if g is not None and not (_as(g, dt, (D,), dev) and g.is_contiguous()):
+            _check(w, "g" + name, g, dtype=dt, shape=(D,), like=x)
     if (cos is None) != (sin is None):
         raise ValueError(f"{w}: cos and sin come together")
     P = rot = 0
     if cos is not None:
-        _check(w, "cos", cos, dtype=torch.float32, like=x)
-        if cos.dim() != 2:
+        shape, f32 = cos.shape, torch.float32
+        if len(shape) != 2:
             raise ValueError(f"{w}: cos must be [P, rot / 2]")
-        _check(w, "sin", sin, dtype=torch.float32, shape=cos.shape, like=x)
-        P, rot = cos.shape[0], 2 * cos.shape[1]
-    if pos is not None:
+        for name, t in (("cos", cos), ("sin", sin)):
+            if not (_as(t, f32, shape, dev) and t.is_contiguous()):
+                _check(w, name, t, dtype=f32, shape=shape, like=x)
+        P, rot = shape[0], 2 * shape[1]
+    if pos is not None and not (_as(pos, torch.int32, (B, L), dev) and pos.is_contiguous()):
         _check(w, "pos", pos, dtype=torch.int32, shape=(B, L), like=x)
     return B, X, L, D, P, rot
+
+
+def _norm_rope_out(w, name, o, t):
+    """The given output for t, checked, or a new one; None without t."""
+    if t is None:
+        return None
+    if o is None:
+        return _torch().empty(t.shape, dtype=t.dtype, device=t.device)
+    if not (_as(o, t.dtype, t.shape, t.get_device()) and o.stride(3) == 1):
+        _like_view(w, o, t, name)
+    return o
+
+
+def _strides(t):
+    return None if t is None else _I3(*t.stride()[:3])
 
 
 def dsp_qk_norm_rope(q, k, H: int, Hkv: int, gq=None, gk=None, cos=None, sin=None, pos=None,
@@ -790,17 +833,11 @@ def dsp_qk_norm_rope(q, k, H: int, Hkv: int, gq=None, gk=None, cos=None, sin=Non
     B, X, L, D, P, rot = _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos)
     like = q if q is not None else k
     with _on_device(like, stream) as s:
-        outs = []
-        for t, o, name in ((q, out_q, "out_q"), (k, out_k, "out_k")):
-            if t is not None:
-                o = torch.empty(t.shape, dtype=t.dtype, device=t.device) if o is None else o
-                _like_view(w, o, t, name)
-            outs.append(o if t is not None else None)
-        yq, yk = outs
-        st = [_st3(t) if t is not None else None for t in (q, k, yq, yk)]
-        _check_status(lib().dsp_qk_norm_rope(_ptr(q), _ptr(k), _ptr(yq), _ptr(yk), _ptr(gq), _ptr(gk), _ptr(cos),
-                                             _ptr(sin), _ptr(pos), P, rot, DSP_ROPE_ADJACENT if interleaved else 0,
-                                             B, X, L, H, Hkv, D, *st, float(eps), _dtype_code(like), s), w)
+        yq, yk = _norm_rope_out(w, "out_q", out_q, q), _norm_rope_out(w, "out_k", out_k, k)
+        _check_status(lib().dsp_qk_norm_rope(
+            _at(q), _at(k), _at(yq), _at(yk), _at(gq), _at(gk), _at(cos), _at(sin), _at(pos), P, rot,
+            DSP_ROPE_ADJACENT if interleaved else 0, B, X, L, H, Hkv, D, _strides(q), _strides(k), _strides(yq),
+            _strides(yk), eps, _dtype_code(like), s), w)
     return yq, yk
 
 
@@ -816,25 +853,22 @@ def dsp_qk_norm_rope_bwd(q, k, dyq, dyk, H: int, Hkv: int, gq=None, gk=None, cos
     B, X, L, D, P, rot = _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos)
     like = q if q is not None else k
     with _on_device(like, stream) as s:
-        outs, dg = [], []
-        for t, dy, o, name in ((q, dyq, dq, "q"), (k, dyk, dk, "k")):
-            if t is not None:
-                _like_view(w, dy, t, "dy" + name)
-                o = torch.empty(t.shape, dtype=t.dtype, device=t.device) if o is None else o
-                _like_view(w, o, t, "d" + name)
-            elif dy is not None:
-                raise ValueError(f"{w}: dy{name} without {name}")
-            outs.append(o if t is not None else None)
+        dg = []
+        for t, dy, name in ((q, dyq, "dyq"), (k, dyk, "dyk")):
+            if t is None:
+                if dy is not None:
+                    raise ValueError(f"{w}: {name} without its input")
+            elif not (_as(dy, t.dtype, t.shape, t.get_device()) and dy.stride(3) == 1):
+                _like_view(w, dy, t, name)
             dg.append(torch.empty(D, dtype=torch.float32, device=like.device) if gains and t is not None else None)
-        dq, dk = outs
+        dq, dk = _norm_rope_out(w, "dq", dq, q), _norm_rope_out(w, "dk", dk, k)
         need = lib().dsp_qk_norm_rope_bwd_workspace_bytes(B, X, L, H, Hkv, D) if gains else 0
         workspace = _workspace(w, need, workspace, like)
-        st = [_st3(t) if t is not None else None for t in (q, k, dyq, dyk, dq, dk)]
         _check_status(lib().dsp_qk_norm_rope_bwd(
-            _ptr(q), _ptr(k), _ptr(dyq), _ptr(dyk), _ptr(dq), _ptr(dk), _ptr(dg[0]), _ptr(dg[1]), _ptr(gq), _ptr(gk),
-            _ptr(cos), _ptr(sin), _ptr(pos), P, rot, DSP_ROPE_ADJACENT if interleaved else 0, _ptr(workspace),
-            _nbytes(workspace) if workspace is not None else 0, B, X, L, H, Hkv, D, *st, float(eps),
-            _dtype_code(like), s), w)
+            _at(q), _at(k), _at(dyq), _at(dyk), _at(dq), _at(dk), _at(dg[0]), _at(dg[1]), _at(gq), _at(gk), _at(cos),
+            _at(sin), _at(pos), P, rot, DSP_ROPE_ADJACENT if interleaved else 0, _at(workspace),
+            _nbytes(workspace) if workspace is not None else 0, B, X, L, H, Hkv, D, _strides(q), _strides(k),
+            _strides(dyq), _strides(dyk), _strides(dq), _strides(dk), eps, _dtype_code(like), s), w)
     return dq, dk, dg[0], dg[1]
 
 

@@ -33,7 +33,10 @@ namespace {
 typedef __bf16 bf16;
 
 constexpr int kNT = 256;   // threads of a work-group
-constexpr int kUnr = 4;    // row groups a wave has in flight
+// Row groups a wave has in flight.  129600 tokens of 64 heads of 64: 487, 430, 410 and
+// 455 us for 1, 2, 4 and 8; gradients of 13600 tokens of 32 heads of 72: 57, 52, 56 and
+// 62 us for 1, 2, 3 and 4 (170 registers from there on).
+constexpr int unroll(bool bwd) { return bwd ? 2 : 4; }
 constexpr int kMaxD = 256;
 
 // n / d for n < 2^31 by a multiplication
@@ -108,22 +111,35 @@ __device__ __forceinline__ int64_t table_row(const NormParams& p, const Where& w
   return (uint32_t)q < p.P ? q : -1;
 }
 
-// a lane's E elements in pair order: a[i], b[i] are the two of its i-th pair
+// a lane's E elements as they lie, and in pair order: a[i], b[i] are the two of its
+// i-th pair
 template <typename T, bool HALF>
-__device__ __forceinline__ void load(const T* x, uint32_t o0, uint32_t o1, float (&a)[Vec<T>::E / 2],
-                                     float (&b)[Vec<T>::E / 2]) {
+struct Raw;
+template <typename T>
+struct Raw<T, true> {
   using V = Vec<T>;
-  if constexpr (HALF) {
-    const typename V::half u = *reinterpret_cast<const typename V::half*>(x + o0);
-    const typename V::half v = *reinterpret_cast<const typename V::half*>(x + o1);
+  typename V::half u, v;
+  __device__ __forceinline__ void load(const T* x, uint32_t o0, uint32_t o1) {
+    u = *reinterpret_cast<const typename V::half*>(x + o0);
+    v = *reinterpret_cast<const typename V::half*>(x + o1);
+  }
+  __device__ __forceinline__ void pairs(float (&a)[V::E / 2], float (&b)[V::E / 2]) const {
 #pragma unroll
     for (int i = 0; i < V::E / 2; ++i) a[i] = (float)u[i], b[i] = (float)v[i];
-  } else {
-    const typename V::whole u = *reinterpret_cast<const typename V::whole*>(x + o0);
+  }
+};
+template <typename T>
+struct Raw<T, false> {
+  using V = Vec<T>;
+  typename V::whole u;
+  __device__ __forceinline__ void load(const T* x, uint32_t o0, uint32_t) {
+    u = *reinterpret_cast<const typename V::whole*>(x + o0);
+  }
+  __device__ __forceinline__ void pairs(float (&a)[V::E / 2], float (&b)[V::E / 2]) const {
 #pragma unroll
     for (int i = 0; i < V::E / 2; ++i) a[i] = (float)u[2 * i], b[i] = (float)u[2 * i + 1];
   }
-}
+};
 template <typename T, bool HALF>
 __device__ __forceinline__ void store(T* y, uint32_t o0, uint32_t o1, const float (&a)[Vec<T>::E / 2],
                                       const float (&b)[Vec<T>::E / 2]) {
@@ -153,7 +169,7 @@ __device__ __forceinline__ float row_sum(float v, uint32_t G, uint32_t j, int la
 
 template <typename T, bool HALF, bool BWD>
 __global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
-  constexpr int E = Vec<T>::E, N = E / 2;
+  constexpr int E = Vec<T>::E, N = E / 2, kUnr = unroll(BWD);
   __shared__ float red[BWD ? kNT * E : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int which = blockIdx.x >= p.side[0].blocks;
@@ -169,53 +185,59 @@ __global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
   float ga[N], gb[N], da[N], db[N];
 #pragma unroll
   for (int i = 0; i < N; ++i) ga[i] = gb[i] = 1.0f, da[i] = db[i] = 0.0f;
-  if (s.g && on) load<T, HALF>(static_cast<const T*>(s.g), o0, o1, ga, gb);
+  if (s.g) {
+    Raw<T, HALF> raw;
+    raw.load(static_cast<const T*>(s.g), o0, o1);
+    raw.pairs(ga, gb);
+  }
 
+  typedef float fv __attribute__((ext_vector_type(N)));
   const uint32_t group = (kNT / 64) * p.HP * kUnr;  // rows of a work-group's pass
   for (uint64_t first = (uint64_t)blk * group; first < s.rows; first += (uint64_t)s.blocks * group) {
-    float a[kUnr][N], b[kUnr][N], ya[kUnr][N], yb[kUnr][N], c[kUnr][N], sn[kUnr][N];
+    // everything the rows need is asked for at once, without branches: rows past the
+    // end repeat the last one and are not written
+    Raw<T, HALF> rx[kUnr], ry[kUnr];
+    fv c[kUnr], sn[kUnr];
     int64_t to[kUnr];
-    bool ok[kUnr];
+    bool ok[kUnr], known[kUnr];
 #pragma unroll
     for (int u = 0; u < kUnr; ++u) {
       const uint64_t row = first + ((uint32_t)wave * kUnr + u) * p.HP + slot;
       ok[u] = on && row < s.rows;
-#pragma unroll
-      for (int i = 0; i < N; ++i) a[u][i] = b[u][i] = ya[u][i] = yb[u][i] = sn[u][i] = 0.0f, c[u][i] = 1.0f;
-      to[u] = 0;
-      if (ok[u]) {
-        const Where w = where(p, s, (uint32_t)row);
-        to[u] = at(w, s.ys, p.D);
-        load<T, HALF>(static_cast<const T*>(s.x) + at(w, s.xs, p.D), o0, o1, a[u], b[u]);
-        if (BWD) load<T, HALF>(static_cast<const T*>(s.dy) + at(w, s.ds, p.D), o0, o1, ya[u], yb[u]);
-        if (turns) {
-          typedef float fv __attribute__((ext_vector_type(N)));
-          const int64_t t = table_row(p, w);
-          if (t >= 0) {
-            const int64_t e = t * (p.R / 2) + N * j;
-            const fv cv = *reinterpret_cast<const fv*>(p.cos + e), sv = *reinterpret_cast<const fv*>(p.sin + e);
-#pragma unroll
-            for (int i = 0; i < N; ++i) c[u][i] = cv[i], sn[u][i] = sv[i];
-          } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) c[u][i] = sn[u][i] = NAN;
-          }
-        }
+      const Where w = where(p, s, row < s.rows ? (uint32_t)row : s.rows - 1);
+      to[u] = at(w, s.ys, p.D);
+      rx[u].load(static_cast<const T*>(s.x) + at(w, s.xs, p.D), o0, o1);
+      if (BWD) ry[u].load(static_cast<const T*>(s.dy) + at(w, s.ds, p.D), o0, o1);
+      known[u] = true;
+      if (p.R) {
+        const int64_t t = table_row(p, w);
+        known[u] = t >= 0;
+        const int64_t e = (known[u] ? t : 0) * (p.R / 2) + (turns ? N * j : 0);
+        c[u] = *reinterpret_cast<const fv*>(p.cos + e);
+        sn[u] = *reinterpret_cast<const fv*>(p.sin + e);
       }
     }
 #pragma unroll
     for (int u = 0; u < kUnr; ++u) {
+      float a[N], b[N], ya[N], yb[N];
+      rx[u].pairs(a, b);
+      if (BWD) ry[u].pairs(ya, yb);
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        c[u][i] = !turns ? 1.0f : known[u] ? c[u][i] : NAN;
+        sn[u][i] = !turns ? 0.0f : known[u] ? sn[u][i] : NAN;
+      }
       float sq = 0.0f;
 #pragma unroll
-      for (int i = 0; i < N; ++i) sq += a[u][i] * a[u][i] + b[u][i] * b[u][i];
+      for (int i = 0; i < N; ++i) sq += a[i] * a[i] + b[i] * b[i];
       float wx = 0.0f;
       if (BWD) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {  // dn, then w = g dn
-          const float na = ya[u][i] * c[u][i] + yb[u][i] * sn[u][i];
-          const float nb = yb[u][i] * c[u][i] - ya[u][i] * sn[u][i];
-          ya[u][i] = na, yb[u][i] = nb;
-          wx += ga[i] * na * a[u][i] + gb[i] * nb * b[u][i];
+          const float na = ya[i] * c[u][i] + yb[i] * sn[u][i];
+          const float nb = yb[i] * c[u][i] - ya[i] * sn[u][i];
+          ya[i] = na, yb[i] = nb;
+          wx += ga[i] * na * a[i] + gb[i] * nb * b[i];
         }
         wx = row_sum(wx, p.G, j, lane);
       }
@@ -226,15 +248,15 @@ __global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
         const float k = r * r * inv_d * wx;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          da[i] += ya[u][i] * (a[u][i] * r);
-          db[i] += yb[u][i] * (b[u][i] * r);
-          oa[i] = r * (ga[i] * ya[u][i] - a[u][i] * k);
-          ob[i] = r * (gb[i] * yb[u][i] - b[u][i] * k);
+          da[i] += ok[u] ? ya[i] * (a[i] * r) : 0.0f;
+          db[i] += ok[u] ? yb[i] * (b[i] * r) : 0.0f;
+          oa[i] = r * (ga[i] * ya[i] - a[i] * k);
+          ob[i] = r * (gb[i] * yb[i] - b[i] * k);
         }
       } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const float na = a[u][i] * r * ga[i], nb = b[u][i] * r * gb[i];
+          const float na = a[i] * r * ga[i], nb = b[i] * r * gb[i];
           oa[i] = na * c[u][i] - nb * sn[u][i];
           ob[i] = nb * c[u][i] + na * sn[u][i];
         }
@@ -366,6 +388,7 @@ __global__ __launch_bounds__(1024) void qk_norm_gain_kernel(const float* part, f
   const uint32_t n = key ? bk : bq;
   float v = 0.0f;
   if (d < D)
+#pragma unroll 8
     for (uint32_t w = r; w < n; w += 64) v += src[(uint64_t)w * D + d];
   red[r][col] = v;
   __syncthreads();
@@ -403,7 +426,7 @@ Plan plan(const QkNormArgs& a, bool bwd) {
   r.chunks = chunked(a, bwd);
   r.G = r.chunks ? a.D / (a.bf16 ? 8 : 4) : 64;
   r.HP = 64 / r.G;
-  const int64_t per = r.chunks ? (kNT / 64) * r.HP * kUnr : kNT / 64;
+  const int64_t per = r.chunks ? (kNT / 64) * r.HP * unroll(bwd) : kNT / 64;
   for (int i = 0; i < 2; ++i) {
     const int64_t rows = a.B * a.X * a.L * a.side[i].heads;
     int64_t n = (rows + per - 1) / per;
