@@ -17,8 +17,8 @@
 // run, pairs (i, i + rot/2) in two runs of 8 bytes, one of each half, so no lane
 // needs another's elements.  A lane keeps its gains in registers and, for the
 // gradient, its share of dg; the lanes' shares are added in a fixed order.
-// Sizes that have no such chunks (widths or offsets off 16 bytes) take a wave per
-// row, element by element.
+// Where the width, the rotation or an offset asks for it, a chunk is 8 or 4 bytes; what
+// has no such chunk either takes a wave per row, element by element.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -73,19 +73,17 @@ struct NormParams {
   float eps;
 };
 
-template <typename T>
-struct Vec;  // E elements of 16 bytes; half of them
-template <>
-struct Vec<bf16> {
-  static constexpr int E = 8;
-  typedef bf16 whole __attribute__((ext_vector_type(8)));
-  typedef bf16 half __attribute__((ext_vector_type(4)));
+// E elements, and half of them: adjacent pairs lie in one run of E, pairs (i, i + rot/2)
+// in two of E / 2
+template <typename T, int E>
+struct Vec {
+  typedef T whole __attribute__((ext_vector_type(E)));
+  typedef T half __attribute__((ext_vector_type(E / 2)));
 };
-template <>
-struct Vec<float> {
-  static constexpr int E = 4;
-  typedef float whole __attribute__((ext_vector_type(4)));
-  typedef float half __attribute__((ext_vector_type(2)));
+template <typename T>
+struct Vec<T, 2> {
+  typedef T whole __attribute__((ext_vector_type(2)));
+  typedef T half __attribute__((ext_vector_type(1)));
 };
 
 struct Where {
@@ -113,47 +111,47 @@ __device__ __forceinline__ int64_t table_row(const NormParams& p, const Where& w
 
 // a lane's E elements as they lie, and in pair order: a[i], b[i] are the two of its
 // i-th pair
-template <typename T, bool HALF>
+template <typename T, int E, bool HALF>
 struct Raw;
-template <typename T>
-struct Raw<T, true> {
-  using V = Vec<T>;
+template <typename T, int E>
+struct Raw<T, E, true> {
+  using V = Vec<T, E>;
   typename V::half u, v;
   __device__ __forceinline__ void load(const T* x, uint32_t o0, uint32_t o1) {
     u = *reinterpret_cast<const typename V::half*>(x + o0);
     v = *reinterpret_cast<const typename V::half*>(x + o1);
   }
-  __device__ __forceinline__ void pairs(float (&a)[V::E / 2], float (&b)[V::E / 2]) const {
+  __device__ __forceinline__ void pairs(float (&a)[E / 2], float (&b)[E / 2]) const {
 #pragma unroll
-    for (int i = 0; i < V::E / 2; ++i) a[i] = (float)u[i], b[i] = (float)v[i];
+    for (int i = 0; i < E / 2; ++i) a[i] = (float)u[i], b[i] = (float)v[i];
   }
 };
-template <typename T>
-struct Raw<T, false> {
-  using V = Vec<T>;
+template <typename T, int E>
+struct Raw<T, E, false> {
+  using V = Vec<T, E>;
   typename V::whole u;
   __device__ __forceinline__ void load(const T* x, uint32_t o0, uint32_t) {
     u = *reinterpret_cast<const typename V::whole*>(x + o0);
   }
-  __device__ __forceinline__ void pairs(float (&a)[V::E / 2], float (&b)[V::E / 2]) const {
+  __device__ __forceinline__ void pairs(float (&a)[E / 2], float (&b)[E / 2]) const {
 #pragma unroll
-    for (int i = 0; i < V::E / 2; ++i) a[i] = (float)u[2 * i], b[i] = (float)u[2 * i + 1];
+    for (int i = 0; i < E / 2; ++i) a[i] = (float)u[2 * i], b[i] = (float)u[2 * i + 1];
   }
 };
-template <typename T, bool HALF>
-__device__ __forceinline__ void store(T* y, uint32_t o0, uint32_t o1, const float (&a)[Vec<T>::E / 2],
-                                      const float (&b)[Vec<T>::E / 2]) {
-  using V = Vec<T>;
+template <typename T, int E, bool HALF>
+__device__ __forceinline__ void store(T* y, uint32_t o0, uint32_t o1, const float (&a)[E / 2],
+                                      const float (&b)[E / 2]) {
+  using V = Vec<T, E>;
   if constexpr (HALF) {
     typename V::half u, v;
 #pragma unroll
-    for (int i = 0; i < V::E / 2; ++i) u[i] = (T)a[i], v[i] = (T)b[i];
+    for (int i = 0; i < E / 2; ++i) u[i] = (T)a[i], v[i] = (T)b[i];
     *reinterpret_cast<typename V::half*>(y + o0) = u;
     *reinterpret_cast<typename V::half*>(y + o1) = v;
   } else {
     typename V::whole u;
 #pragma unroll
-    for (int i = 0; i < V::E / 2; ++i) u[2 * i] = (T)a[i], u[2 * i + 1] = (T)b[i];
+    for (int i = 0; i < E / 2; ++i) u[2 * i] = (T)a[i], u[2 * i + 1] = (T)b[i];
     *reinterpret_cast<typename V::whole*>(y + o0) = u;
   }
 }
@@ -167,9 +165,9 @@ __device__ __forceinline__ float row_sum(float v, uint32_t G, uint32_t j, int la
   return __shfl(v, lane - (int)j);
 }
 
-template <typename T, bool HALF, bool BWD>
+template <typename T, int E, bool HALF, bool BWD>
 __global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
-  constexpr int E = Vec<T>::E, N = E / 2, kUnr = unroll(BWD);
+  constexpr int N = E / 2, kUnr = unroll(BWD);
   __shared__ float red[BWD ? kNT * E : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int which = blockIdx.x >= p.side[0].blocks;
@@ -186,7 +184,7 @@ __global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
 #pragma unroll
   for (int i = 0; i < N; ++i) ga[i] = gb[i] = 1.0f, da[i] = db[i] = 0.0f;
   if (s.g) {
-    Raw<T, HALF> raw;
+    Raw<T, E, HALF> raw;
     raw.load(static_cast<const T*>(s.g), o0, o1);
     raw.pairs(ga, gb);
   }
@@ -196,7 +194,7 @@ __global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
   for (uint64_t first = (uint64_t)blk * group; first < s.rows; first += (uint64_t)s.blocks * group) {
     // everything the rows need is asked for at once, without branches: rows past the
     // end repeat the last one and are not written
-    Raw<T, HALF> rx[kUnr], ry[kUnr];
+    Raw<T, E, HALF> rx[kUnr], ry[kUnr];
     fv c[kUnr], sn[kUnr];
     int64_t to[kUnr];
     bool ok[kUnr], known[kUnr];
@@ -261,7 +259,7 @@ __global__ __launch_bounds__(kNT) void qk_norm_kernel(NormParams p) {
           ob[i] = nb * c[u][i] + na * sn[u][i];
         }
       }
-      if (ok[u]) store<T, HALF>(static_cast<T*>(s.y) + to[u], o0, o1, oa, ob);
+      if (ok[u]) store<T, E, HALF>(static_cast<T*>(s.y) + to[u], o0, o1, oa, ob);
     }
   }
   if constexpr (BWD) {
@@ -402,31 +400,38 @@ __global__ __launch_bounds__(1024) void qk_norm_gain_kernel(const float* part, f
 // that their shares of dg stay small
 constexpr uint32_t kGradBlocks = 1024;
 
-bool chunked(const QkNormArgs& a, bool bwd) {
-  const int es = a.bf16 ? 2 : 4, E = 16 / es;
-  if (a.D % E || a.rot % E) return false;
-  auto ok = [&](const void* ptr, const int64_t* st) {
-    return reinterpret_cast<uintptr_t>(ptr) % 16 == 0 && st[0] % E == 0 && st[1] % E == 0 && st[2] % E == 0;
-  };
-  for (int i = 0; i < 2; ++i) {
-    const QkNormSide& s = a.side[i];
-    if (!s.heads) continue;
-    if (!ok(s.x, s.x_strides) || !ok(s.y, s.y_strides) || (bwd && !ok(s.dy, s.dy_strides))) return false;
-    if (s.gain && reinterpret_cast<uintptr_t>(s.gain) % 16) return false;
+// The elements of a lane's chunk: 16 bytes' worth, or a half or a quarter of it where the
+// width, the rotation or an alignment asks for it; 0: no such chunk (a lane for each
+// element then).
+int chunk(const QkNormArgs& a, bool bwd) {
+  const int es = a.bf16 ? 2 : 4;
+  for (int E = 16 / es; E >= 2; E /= 2) {
+    if (a.D % E || a.rot % E || a.D / E > 64) continue;
+    auto ok = [&](const void* ptr, const int64_t* st) {
+      return reinterpret_cast<uintptr_t>(ptr) % (E * es) == 0 && st[0] % E == 0 && st[1] % E == 0 && st[2] % E == 0;
+    };
+    bool all = !a.rot || (reinterpret_cast<uintptr_t>(a.cos) % (2 * E) == 0 && reinterpret_cast<uintptr_t>(a.sin) % (2 * E) == 0);
+    for (int i = 0; i < 2; ++i) {
+      const QkNormSide& s = a.side[i];
+      if (!s.heads) continue;
+      all = all && ok(s.x, s.x_strides) && ok(s.y, s.y_strides) && (!bwd || ok(s.dy, s.dy_strides)) &&
+            reinterpret_cast<uintptr_t>(s.gain) % (E * es) == 0;
+    }
+    if (all) return E;
   }
-  return !a.rot || (reinterpret_cast<uintptr_t>(a.cos) % 16 == 0 && reinterpret_cast<uintptr_t>(a.sin) % 16 == 0);
+  return 0;
 }
 
 struct Plan {
-  bool chunks;
+  int E;
   uint32_t G, HP, blocks[2];
 };
 Plan plan(const QkNormArgs& a, bool bwd) {
   Plan r = {};
-  r.chunks = chunked(a, bwd);
-  r.G = r.chunks ? a.D / (a.bf16 ? 8 : 4) : 64;
+  r.E = chunk(a, bwd);
+  r.G = r.E ? a.D / r.E : 64;
   r.HP = 64 / r.G;
-  const int64_t per = r.chunks ? (kNT / 64) * r.HP * unroll(bwd) : kNT / 64;
+  const int64_t per = r.E ? (kNT / 64) * r.HP * unroll(bwd) : kNT / 64;
   for (int i = 0; i < 2; ++i) {
     const int64_t rows = a.B * a.X * a.L * a.side[i].heads;
     int64_t n = (rows + per - 1) / per;
@@ -436,18 +441,29 @@ Plan plan(const QkNormArgs& a, bool bwd) {
   return r;
 }
 
+template <typename T, int E>
+void launch_chunks(const NormParams& p, dim3 grid, bool half, bool bwd, hipStream_t s) {
+  if (half) {
+    if (bwd) qk_norm_kernel<T, E, true, true><<<grid, kNT, 0, s>>>(p);
+    else qk_norm_kernel<T, E, true, false><<<grid, kNT, 0, s>>>(p);
+  } else {
+    if (bwd) qk_norm_kernel<T, E, false, true><<<grid, kNT, 0, s>>>(p);
+    else qk_norm_kernel<T, E, false, false><<<grid, kNT, 0, s>>>(p);
+  }
+}
 template <typename T>
 void launch(const NormParams& p, const Plan& pl, bool half, bool bwd, hipStream_t s) {
   const dim3 grid(pl.blocks[0] + pl.blocks[1]);
-  if (!pl.chunks) {
-    if (bwd) qk_norm_any_kernel<T, true><<<grid, kNT, 0, s>>>(p, half);
-    else qk_norm_any_kernel<T, false><<<grid, kNT, 0, s>>>(p, half);
-  } else if (half) {
-    if (bwd) qk_norm_kernel<T, true, true><<<grid, kNT, 0, s>>>(p);
-    else qk_norm_kernel<T, true, false><<<grid, kNT, 0, s>>>(p);
+  if (pl.E == 8) {
+    if constexpr (sizeof(T) == 2) launch_chunks<T, 8>(p, grid, half, bwd, s);
+  } else if (pl.E == 4) {
+    launch_chunks<T, 4>(p, grid, half, bwd, s);
+  } else if (pl.E == 2) {
+    launch_chunks<T, 2>(p, grid, half, bwd, s);
+  } else if (bwd) {
+    qk_norm_any_kernel<T, true><<<grid, kNT, 0, s>>>(p, half);
   } else {
-    if (bwd) qk_norm_kernel<T, false, true><<<grid, kNT, 0, s>>>(p);
-    else qk_norm_kernel<T, false, false><<<grid, kNT, 0, s>>>(p);
+    qk_norm_any_kernel<T, false><<<grid, kNT, 0, s>>>(p, half);
   }
 }
 
