@@ -626,8 +626,19 @@ int start(FwdParams& p, const RelposArgs& a, hipStream_t s) {
   }
   constexpr bool B16 = sizeof(T) == 2;
   if (a.Lq <= 64 && a.Lk <= 64) return start_many<T, DC, 2, 1, 64, 1, B16 ? (DC <= 80 ? 3 : 2) : 1>(p, a, s);
-  if (a.Lq <= 128) return start_many<T, DC, 4, 1, B16 ? 64 : 32, 2, B16 ? 2 : 1>(p, a, s);
-  return start_many<T, DC, B16 ? 8 : 4, B16 && DC <= 96 ? 2 : 1, B16 ? 64 : 32, 2, B16 ? 2 : 1>(p, a, s);
+  // Long rows.  Heads of at most 64 columns: 4 waves of 32 queries, 3 of such work-groups
+  // to a CU (8 x 16 units of 4096 x 64: 627 us; 8 waves of 64 queries 630, and 81 instead
+  // of 60 us for 64 x 16 units of 300).  Wider heads have registers for 2 waves per SIMD,
+  // and large blocks of queries, 64 to a wave up to 80 columns, ask less of LDS: 880 us
+  // against 913 for 4096 x 72, 1160 against 1215 for 4096 x 128.  Where they leave CUs
+  // idle or much of a block empty it is the other way round: 64 x 16 units of 300 x 72
+  // 106 and 96, of 300 x 128 160 and 125, four units of 2000 x 96 60 and 55.
+  if constexpr (B16 && DC > 64) {
+    constexpr int QT = DC <= 80 ? 2 : 1;
+    if (a.Lq >= 1024 && a.B * a.X * a.H * ((a.Lq + 256 * QT - 1) / (256 * QT)) >= 256)
+      return start_many<T, DC, 8, QT, 64, 2, 2>(p, a, s);
+  }
+  return start_many<T, DC, 4, 1, B16 ? 64 : 32, 2, B16 ? (DC <= 64 ? 3 : 2) : 1>(p, a, s);
 }
 
 }  // namespace
