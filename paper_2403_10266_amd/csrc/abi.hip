@@ -318,8 +318,10 @@ bool rows_apart(const void* a, const int64_t* sa, int64_t wa, int64_t La, const 
   int64_t pitch = INT64_MAX;
   for (int i = 0; i < 3; ++i) {
     if (ext[i] <= 1) continue;
-    if (sa[i] != sb[i]) return false;
+    if (sa[i] != sb[i] || sa[i] == 0) return false;
     pitch = sa[i] < pitch ? sa[i] : pitch;
+    for (int j = 0; j < 3; ++j)   // whole pitches: a larger stride starts after the smaller one's rows
+      if (j != i && ext[j] > 1 && sa[j] >= sa[i] && sa[j] / sa[i] < ext[i]) return false;
   }
   const int64_t off = ((intptr_t)b - (intptr_t)a) / es;
   if (((intptr_t)b - (intptr_t)a) % es) return false;

@@ -277,8 +277,9 @@ struct Tile {
   }
   __device__ __forceinline__ void fetch(const Map& m, const T* base, uint32_t rows, uint32_t row_bytes, int D,
                                         bool vec) {
-    // an offset past the resource instead of a branch: all loads go out at once
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, rows * row_bytes);
+    // an offset past the resource instead of a branch: all loads go out at once.  The
+    // resource ends with the last row's last element, whatever the stride (0 included).
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, rows ? (rows - 1) * row_bytes + (uint32_t)(D * sizeof(T)) : 0u);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const uint32_t off = m.row + i * m.step < rows ? m.at + i * m.step * row_bytes : 0xFFFFFFF0u;

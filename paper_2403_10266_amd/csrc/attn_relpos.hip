@@ -42,10 +42,11 @@ struct FwdParams {
   int64_t qs[3], ks[3], os[3];
   BiasArgs bias;
   uint32_t X, H, grp, Lq, Lk, n_split, split_keys, D;
+  uint32_t sub;      // few queries: parts of a key/value head's group, of grp heads each
   Order order;       // many queries
   uint32_t pieces;   // few queries: (b, x) times splits
   uint32_t tab;      // distances of the LDS table, for each head of a work-group
-  uint32_t cols;     // few queries: queries x heads of a group
+  uint32_t cols;     // few queries: queries x grp
   float c;           // scale * log2(e)
   bool vec, causal;
 };
@@ -357,7 +358,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
   const uint32_t e = j8 % kvh, split = piece % p.n_split, bx = piece / p.n_split, h0 = e * p.grp;
   const uint32_t b = bx / p.X, x = bx - b * p.X;
   const int D = (int)p.D;
-  const int64_t k_at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)e * D;
+  const int64_t k_at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)(e / p.sub) * D;
   const T* kg = static_cast<const T*>(p.k) + k_at;
   const T* vg = static_cast<const T*>(p.v) + k_at;
 
@@ -602,21 +603,29 @@ template <typename T, int DC, int NW, bool ONE>
 int start_few(FwdParams& p, const RelposArgs& a, hipStream_t s) {
   constexpr int MINW = sizeof(T) == 4 ? 1 : ONE ? (DC <= 80 ? 4 : DC <= 96 ? 3 : 2) : DC <= 80 ? 3 : 2;
   p.tab = (uint32_t)std::min<int64_t>(2 * (p.bias.M + kEdge) + 1, 32 + ((int64_t)p.split_keys + 31) / 32 * 32);
-  size_t lds = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T) + (size_t)p.tab * p.grp * 4;
+  // A group whose tables do not fit beside the tiles (long tables, many heads) is taken
+  // in parts, each of which reads the keys; one head always fits.
+  const uint32_t grp = p.grp;
+  const size_t tiles = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T);
+  p.sub = 1;
+  while (grp % p.sub || tiles + (size_t)p.tab * (grp / p.sub) * 4 > 160 * 1024) ++p.sub;
+  p.grp = grp / p.sub;
+  p.cols = (uint32_t)a.Lq * p.grp;
+  size_t lds = tiles + (size_t)p.tab * p.grp * 4;
   if (NW > 1) lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * p.cols * Geo<T, DC>::DP) * 4);
   const int64_t pieces = a.B * a.X * p.n_split;
   p.pieces = (uint32_t)pieces;
-  int st = launch(relpos_few_kernel<T, DC, NW, ONE, MINW>, (pieces + 7) / 8 * 8 * a.Hkv, NW * 64, lds, p, s);
+  int st = launch(relpos_few_kernel<T, DC, NW, ONE, MINW>, (pieces + 7) / 8 * 8 * (a.H / p.grp), NW * 64, lds, p, s);
   if (st != DSP_OK || p.n_split == 1) return st;
-  const int64_t cols = a.B * a.X * a.Hkv * p.cols;   // few units: they are why the keys are split
+  const int64_t cols = a.B * a.X * a.H * a.Lq;   // few units: they are why the keys are split
   if (a.D <= 64) relpos_join_kernel<T, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p);
   else relpos_join_kernel<T, 128><<<dim3((uint32_t)cols), 256, 0, s>>>(p);
   return last_launch_status();
 }
 
 template <typename T, int DC>
-int start(FwdParams& p, const RelposArgs& a, hipStream_t s) {
-  if (p.cols) {
+int start(FwdParams& p, const RelposArgs& a, bool few, hipStream_t s) {
+  if (few) {
     // a wave per unit where the units alone fill the chip
     const bool full = a.B * a.X * a.Hkv >= 256 * 12;
     if (a.Lk <= 32) return start_few<T, DC, 1, true>(p, a, s);
@@ -651,23 +660,22 @@ int launch_attn_relpos(const RelposArgs& a, hipStream_t s) {
   for (int i = 0; i < 3; ++i) p.qs[i] = a.q_strides[i], p.ks[i] = a.kv_strides[i], p.os[i] = a.o_strides[i];
   p.bias = {a.bias, a.buckets, a.max_dist, a.n_buckets};
   p.X = (uint32_t)a.X, p.H = a.H, p.grp = a.H / a.Hkv, p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk, p.D = a.D;
-  p.cols = c.few ? (uint32_t)(a.Lq * p.grp) : 0;
   p.n_split = (uint32_t)c.n_split, p.split_keys = (uint32_t)c.split_keys;
   p.c = a.scale * kLog2e;
   p.vec = a.vec, p.causal = a.causal;
   if (a.bf16) {
-    if (a.D <= 32) return start<bf16, 32>(p, a, s);
-    if (a.D <= 48) return start<bf16, 48>(p, a, s);
-    if (a.D <= 64) return start<bf16, 64>(p, a, s);
-    if (a.D <= 72) return start<bf16, 72>(p, a, s);
-    if (a.D <= 80) return start<bf16, 80>(p, a, s);
-    if (a.D <= 96) return start<bf16, 96>(p, a, s);
-    return start<bf16, 128>(p, a, s);
+    if (a.D <= 32) return start<bf16, 32>(p, a, c.few, s);
+    if (a.D <= 48) return start<bf16, 48>(p, a, c.few, s);
+    if (a.D <= 64) return start<bf16, 64>(p, a, c.few, s);
+    if (a.D <= 72) return start<bf16, 72>(p, a, c.few, s);
+    if (a.D <= 80) return start<bf16, 80>(p, a, c.few, s);
+    if (a.D <= 96) return start<bf16, 96>(p, a, c.few, s);
+    return start<bf16, 128>(p, a, c.few, s);
   }
-  if (a.D <= 32) return start<float, 32>(p, a, s);
-  if (a.D <= 64) return start<float, 64>(p, a, s);
-  if (a.D <= 96) return start<float, 96>(p, a, s);
-  return start<float, 128>(p, a, s);
+  if (a.D <= 32) return start<float, 32>(p, a, c.few, s);
+  if (a.D <= 64) return start<float, 64>(p, a, c.few, s);
+  if (a.D <= 96) return start<float, 96>(p, a, c.few, s);
+  return start<float, 128>(p, a, c.few, s);
 }
 
 size_t attn_relpos_workspace_bytes(const RelposArgs& a) {

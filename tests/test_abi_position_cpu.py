@@ -221,3 +221,13 @@ def test_relpos_binding_refusals():
     x = torch.zeros(1, 1, 2, 144)
     with pytest.raises(ValueError, match="device tensor"):
         dsp.dsp_attn_relpos(x, x, x, 2, 2, torch.zeros(3, 2), torch.zeros(5, dtype=torch.int32))
+
+
+def test_rows_between_rows_of_uneven_pitch(lib):
+    """Outputs in the gaps between the inputs' rows share no element only where every
+    stride is whole pitches; here x's second run of rows starts inside a gap."""
+    uneven, even = _st(10000, 2688, 600), _st(10000, 3000, 600)
+    for es, dt in ((2, BF), (4, F32)):
+        assert _norm(lib, qs=uneven, yq=A[0] + 300 * es, dt=dt) == dsp.DSP_ERR_ARG
+        assert _norm(lib, qs=even, yq=A[0] + 300 * es, dt=dt, cos=None) == dsp.DSP_ERR_NULL
+        assert _norm(lib, qs=even, yq=A[0] + 313 * es, dt=dt) == dsp.DSP_ERR_ARG

@@ -303,3 +303,91 @@ def test_empty(torch):
         dq, dk, dv, db = dsp.dsp_attn_relpos_bwd(q, k, k, q, q, z(1, 2, 2, Lq), 2, 2, bias, bk)
         torch.cuda.synchronize()
         assert not any(t.any() for t in (dq, dk, dv, db))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Lq,Lk", [(1, 200), (3, 50), (32, 32), (60, 60), (70, 150)])
+def test_rows_of_any_stride(torch, dtype, Lq, Lk):
+    """One key for every position (stride 0), key rows that overlap, one query for
+    every row: as with the same rows in their own places."""
+    import paper_2403_10266_amd as dsp
+    H, D = 2, 24
+    c = ru.case(1, 3, Lq, Lk, H, H, D, 9, 5, dtype, seed=Lq)
+    bias, bk = dev(c["bias"], dtype), torch.from_numpy(c["buckets"]).cuda()
+    q, k, v = (dev(c[n], dtype) for n in "qkv")
+    flat = [t.reshape(-1) for t in (k, v)]
+    views = dict(one=[t[:, :, :1].expand_as(t) for t in (k, v)],
+                 close=[t.as_strided(k.shape, (0, Lk * 8, 8, 1)) for t in flat])
+    for kind, (a, b) in views.items():
+        got = dsp.dsp_attn_relpos(q, a, b, H, H, bias, bk)
+        want = dsp.dsp_attn_relpos(q, a.contiguous(), b.contiguous(), H, H, bias, bk)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want), kind
+    one = q[:, :, -1:].expand_as(q)
+    assert torch.equal(dsp.dsp_attn_relpos(one, k, v, H, H, bias, bk),
+                       dsp.dsp_attn_relpos(one.contiguous(), k, v, H, H, bias, bk))
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_tables_of_wide_heads_and_groups(torch, dtype):
+    """The longest table with the widest heads, and with groups whose tables do not fit
+    a work-group together (with the keys cut among work-groups, and not)."""
+    import paper_2403_10266_amd as dsp
+    for Lq, Lk, H, Hkv, D in ((60, 60, 2, 2, 128), (150, 1300, 2, 2, 128), (1300, 150, 2, 1, 80)):
+        c = ru.case(1, 1, Lq, Lk, H, Hkv, D, 1024, 40, dtype, seed=D)
+        _check(torch, c, dtype, f"M1024 D{D}")
+    for D, H, Lq, lens in ((128, 32, 1, [2100, 1, 0]), (64, 30, 1, [2100, 2000, 7]), (72, 6, 5, [1800, 5, 900])):
+        c = ru.case(3, 1, Lq, max(lens), H, 1, D, 1024, 40, dtype, seed=H)
+        _check(torch, c, dtype, f"M1024 group {H}", causal=True, q_pos=[n - Lq for n in lens], kv_len=lens, grads=False)
+    c = ru.case(1, 2, 1, 2400, 32, 1, 32, 1024, 40, dtype, seed=6)
+    q, k, v = (dev(c[n], dtype) for n in "qkv")
+    many = lambda t: t[:, :1].expand(1, 2100, *t.shape[2:])  # noqa: E731
+    pos = torch.tensor([1200], dtype=torch.int32, device="cuda")
+    o, lse = dsp.dsp_attn_relpos(many(q), many(k), many(v), 32, 1, dev(c["bias"], dtype),
+                                 torch.from_numpy(c["buckets"]).cuda(), q_pos=pos, with_lse=True)
+    torch.cuda.synchronize()
+    assert (o == o[:, :1]).all() and (lse == lse[:, :1]).all()
+    c = {n: t[:, :1] if n in ("q", "k", "v", "do") else t for n, t in c.items()}
+    ru.compare(dict(o=host(o[:, :1]), lse=host(lse[:, :1])), ru.wanted(c, dtype, False, [1200], None, grads=False), say)
+
+
+def test_offsets_past_32_bits(torch):
+    """Rows of keys 2 MB apart, 4.6 GB of them: the bits of the same rows side by side."""
+    import paper_2403_10266_amd as dsp
+    H, D, Lk, gap = 2, 64, 2200, 1 << 20
+    def far(t):
+        wide = torch.empty(Lk * gap, dtype=t.dtype, device="cuda").as_strided(t.shape, (0, 0, gap, 1))
+        wide.copy_(t)
+        return wide
+    c = ru.case(1, 1, 100, Lk, H, H, D, 30, 8, "bf16", seed=1)
+    near = {n: dev(c[n], "bf16") for n in "qkv"}
+    k, v = far(near["k"]), far(near["v"])
+    bias, bk, do = dev(c["bias"], "bf16"), torch.from_numpy(c["buckets"]).cuda(), dev(c["do"], "bf16")
+    at = torch.tensor([Lk - 100], dtype=torch.int32, device="cuda")
+    for n in (1, 100):
+        q = near["q"][:, :, -n:].contiguous()
+        kw = dict(causal=True, q_pos=at + 100 - n, with_lse=True)
+        a = dsp.dsp_attn_relpos(q, k, v, H, H, bias, bk, **kw)
+        b = dsp.dsp_attn_relpos(q, near["k"], near["v"], H, H, bias, bk, **kw)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(a, b)), n
+    kw = dict(causal=True, q_pos=at)
+    dk, dv = far(torch.zeros_like(near["k"])), far(torch.zeros_like(near["k"]))
+    got = dsp.dsp_attn_relpos_bwd(q, k, v, a[0], do, a[1], H, H, bias, bk, dk=dk, dv=dv, **kw)
+    want = dsp.dsp_attn_relpos_bwd(q, near["k"], near["v"], a[0], do, a[1], H, H, bias, bk, **kw)
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
+def test_no_units(torch):
+    import paper_2403_10266_amd as dsp
+    z = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    bias, bk = z(4, 2) + 1, dsp.dsp_relpos_buckets(3, 4).cuda()
+    for B, X in ((0, 2), (2, 0)):
+        q, k = z(B, X, 3, 16), z(B, X, 5, 16)
+        o, lse = dsp.dsp_attn_relpos(q, k, k, 2, 2, bias, bk, with_lse=True)
+        *_, db = dsp.dsp_attn_relpos_bwd(q, k, k, q, q, lse, 2, 2, bias, bk, dbias=z(4, 2) + 9)
+        torch.cuda.synchronize()
+        assert o.shape == q.shape and not db.any()

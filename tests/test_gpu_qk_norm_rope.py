@@ -241,3 +241,28 @@ def test_infinite_and_nan_rows_stay_alone(torch):
         hit = torch.zeros_like(same)
         hit[1, 4, 2] = hit[0, 2, 0] = True
         assert torch.equal(same, ~hit)
+
+
+@pytest.mark.parametrize("D", [72, 44])
+def test_offsets_past_32_bits_and_broadcast_rows(torch, D):
+    """Tokens 2 MB apart in 4.6 GB, and one row for every token: the bits of the same
+    rows side by side, forward and gradient."""
+    import paper_2403_10266_amd as dsp
+    L, H, gap = 2200, 2, 1 << 20
+    q, dy = (torch.randn(1, 1, L, H * D, device="cuda").bfloat16() for _ in range(2))
+    cos, sin = (torch.from_numpy(t).cuda() for t in _table(L, D // 2 * 2))
+    def far(t):
+        wide = torch.empty(L * gap, dtype=t.dtype, device="cuda").as_strided(t.shape, (0, 0, gap, 1))
+        wide.copy_(t)
+        return wide
+    both = lambda x, g, **kw: (dsp.dsp_qk_norm_rope(x, None, H, 0, cos=cos, sin=sin, out_q=kw.get("y"))[0],  # noqa: E731
+                               *dsp.dsp_qk_norm_rope_bwd(x, None, g, None, H, 0, cos=cos, sin=sin, dq=kw.get("dq"))[::2])
+    want = both(q, dy)
+    got = both(far(q), far(dy), y=far(torch.zeros_like(q)), dq=far(torch.zeros_like(q)))
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+    one, g1 = q[:, :, :1].expand_as(q), dy[:, :, :1].expand_as(dy)
+    for a, b in zip(both(one, g1), both(one.contiguous(), g1.contiguous())):
+        assert torch.equal(a, b)
+    torch.cuda.synchronize()
