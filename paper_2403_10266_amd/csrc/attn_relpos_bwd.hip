@@ -490,6 +490,69 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void relpos_bwd_dkv_kernel(BwdP
 }
 
 // ---------------------------------------------------------------------------
+// Adds the gradients of keys 32 wave .. from one head's queries: rows of Q and dO in
+// LDS, the keys' and values' in registers; tb0: the bias of distance 0.
+template <typename T, int DC, int NB>
+__device__ __forceinline__ void short_dkv(const BwdParams& p, const T* ql, const T* ol,
+                                          const typename Mx<T>::frag (&kf)[Geo<T, DC>::NS],
+                                          const typename Mx<T>::frag (&vf)[Geo<T, DC>::NS], const float* st_lse,
+                                          const float* st_del, const float* tb0, int32_t q0, uint32_t len, int wave,
+                                          int lane, ColAcc<T, DC>& dk, ColAcc<T, DC>& dv) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  const int l32 = lane & 31, g = lane >> 5;
+  const float left = tb0[-p.bias.M], right = tb0[p.bias.M];
+  if (32u * wave >= len) return;
+#pragma unroll
+  for (int qt = 0; qt < NB; ++qt) {
+    const int32_t d0 = 32 * wave - q0 - 32 * qt;
+    if (32u * qt >= p.Lq || (p.causal && d0 > 31)) continue;
+    floatx16 s, dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < G::NS; ++i) {
+      const int at = (32 * qt + l32) * G::P + 2 * G::E * i + G::E * g;
+      s = M::mma(*reinterpret_cast<const typename M::frag*>(ql + at), kf[i], s);
+      dp = M::mma(*reinterpret_cast<const typename M::frag*>(ol + at), vf[i], dp);
+    }
+    block_probabilities(p, s, st_lse + 32 * qt + 4 * g, tb0, left, right, d0, l32, g, 32 * wave, len);
+    ColB<T> pb, zb;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const floatx4 dl = *reinterpret_cast<const floatx4*>(st_del + 32 * qt + 8 * q + 4 * g);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pb.set(4 * q + i, s[4 * q + i]);
+        zb.set(4 * q + i, s[4 * q + i] * (dp[4 * q + i] - dl[i]));
+      }
+    }
+    dv.add(ol, 32 * qt, lane, pb);
+    dk.add(ql, 32 * qt, lane, zb);
+  }
+}
+// and writes them, through LDS rows 32 wave .. of two tiles
+template <typename T, int DC>
+__device__ __forceinline__ void short_store(const BwdParams& p, T* kl, T* vl, int64_t k_at, int wave, int lane,
+                                            ColAcc<T, DC>& dk, const ColAcc<T, DC>& dv) {
+  using G = Geo<T, DC>;
+  const int D = (int)p.D;
+  dk.scale(p.scale, lane);
+  auto out = [&](void* base) {
+    return [&, base](int n) -> T* {
+      const uint32_t r = 32 * wave + n;
+      return r < p.Lk ? static_cast<T*>(base) + k_at + (int64_t)r * p.ks[2] : nullptr;
+    };
+  };
+  if (p.vec) {
+    store_rows_lds<T, DC>(kl + 32 * wave * G::P, dk, lane, D, out(p.dk));
+    store_rows_lds<T, DC>(vl + 32 * wave * G::P, dv, lane, D, out(p.dv));
+  } else {
+    store_rows<T, DC>(dk, lane, D, false, out(p.dk));
+    store_rows<T, DC>(dv, lane, D, false, out(p.dv));
+  }
+}
+
 // Units of at most 32 NB queries and keys (temporal attention): one work-group holds a
 // unit's Q, K, V and dO in LDS, so each row crosses HBM once.  Wave w first takes queries
 // 32 w .. against all keys (dQ, dbias), with the whole row of P and dP in registers, so
@@ -498,7 +561,9 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void relpos_bwd_dkv_kernel(BwdP
 // A work-group stays with one head (which has keys of its own) and runs through units;
 // a wave's dZ is summed over them in registers, element by element, and goes to the
 // sums by distance only when the queries' first position changes and at the end.
-template <typename T, int DC, int NB, int MINW>
+// Where heads share keys (not OWN) dK and dV are sums over heads: they are left to
+// relpos_bwd_short_dkv_kernel, and Delta goes to memory.
+template <typename T, int DC, int NB, bool OWN, int MINW>
 __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdParams p) {
   using G = Geo<T, DC>;
   using M = Mx<T>;
@@ -576,8 +641,8 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
     asm volatile("" : "+v"(lane));   // the addresses made of it are cheaper to form again than to keep over the loop
     const int l32 = lane & 31, g = lane >> 5;
     const uint32_t len = length(p.kv_len, b, p.Lk);
-    const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)h * D, q_at = bx_at(p, bx, p.qs) + (int64_t)h * D,
-                  o_at = bx_at(p, bx, p.os) + (int64_t)h * D;
+    const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)(OWN ? h : h / p.grp) * D,
+                  q_at = bx_at(p, bx, p.qs) + (int64_t)h * D, o_at = bx_at(p, bx, p.os) + (int64_t)h * D;
     {
       TileT tk, tv, tq, to;
       tk.fetch(mk, static_cast<const T*>(p.k) + k_at, len, k_row, D, p.vec);
@@ -644,7 +709,11 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
         }
       }
       delta += swap_halves(delta);
-      if (g == 0) st_del[32 * wave + l32] = delta;
+      if (OWN) {
+        if (g == 0) st_del[32 * wave + l32] = delta;
+      } else if (g == 0 && 32u * wave + l32 < p.Lq) {
+        p.delta[((uint64_t)bx * p.H + h) * p.Lq + 32 * wave + l32] = delta;
+      }
 #pragma unroll
       for (int kt = 0; kt < NB; ++kt) {
         if (32u * kt >= len) continue;
@@ -661,76 +730,118 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
     }
     __syncthreads();   // Delta is there
     typename M::frag kf[G::NS], vf[G::NS];
+    if constexpr (OWN) {
 #pragma unroll
-    for (int s = 0; s < G::NS; ++s) {
-      const int at = (32 * wave + l32) * G::P + 2 * G::E * s + G::E * g;
-      kf[s] = *reinterpret_cast<const typename M::frag*>(kl + at);
-      vf[s] = *reinterpret_cast<const typename M::frag*>(vl + at);
+      for (int s = 0; s < G::NS; ++s) {
+        const int at = (32 * wave + l32) * G::P + 2 * G::E * s + G::E * g;
+        kf[s] = *reinterpret_cast<const typename M::frag*>(kl + at);
+        vf[s] = *reinterpret_cast<const typename M::frag*>(vl + at);
+      }
+      __syncthreads();   // the rows of K are free
     }
-    __syncthreads();   // the rows of K are free
     auto q_out = [&](int n) -> T* {
       const uint32_t r = 32 * wave + n;
       return r < p.Lq ? static_cast<T*>(p.dq) + q_at + (int64_t)r * p.qs[2] : nullptr;
     };
     if (p.vec) store_rows_lds<T, DC>(kl + 32 * wave * G::P, dq, lane, D, q_out);
     else store_rows<T, DC>(dq, lane, D, false, q_out);
-    ColAcc<T, DC> dk, dv;
-    dk.zero();
-    dv.zero();
-    if (32u * wave < len) {
-#pragma unroll
-      for (int qt = 0; qt < NB; ++qt) {
-        const int32_t d0 = 32 * wave - q0 - 32 * qt;
-        if (32u * qt >= p.Lq || (p.causal && d0 > 31)) continue;
-        floatx16 s, dp;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < G::NS; ++i) {
-          const int at = (32 * qt + l32) * G::P + 2 * G::E * i + G::E * g;
-          s = M::mma(*reinterpret_cast<const typename M::frag*>(ql + at), kf[i], s);
-          dp = M::mma(*reinterpret_cast<const typename M::frag*>(ol + at), vf[i], dp);
-        }
-        block_probabilities(p, s, st_lse + 32 * qt + 4 * g, tb0, left, right, d0, l32, g, 32 * wave, len);
-        ColB<T> pb, zb;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const floatx4 dl = *reinterpret_cast<const floatx4*>(st_del + 32 * qt + 8 * q + 4 * g);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            pb.set(4 * q + i, s[4 * q + i]);
-            zb.set(4 * q + i, s[4 * q + i] * (dp[4 * q + i] - dl[i]));
-          }
-        }
-        dv.add(ol, 32 * qt, lane, pb);
-        dk.add(ql, 32 * qt, lane, zb);
-      }
-    }
-    // the rows of K and V serve to write: this wave's own, which it alone reads now
-    dk.scale(p.scale, lane);
-    auto out = [&](void* base) {
-      return [&, base](int n) -> T* {
-        const uint32_t r = 32 * wave + n;
-        return r < p.Lk ? static_cast<T*>(base) + k_at + (int64_t)r * p.ks[2] : nullptr;
-      };
-    };
-    if (p.vec) {
-      store_rows_lds<T, DC>(kl + 32 * wave * G::P, dk, lane, D, out(p.dk));
-      store_rows_lds<T, DC>(vl + 32 * wave * G::P, dv, lane, D, out(p.dv));
-    } else {
-      store_rows<T, DC>(dk, lane, D, false, out(p.dk));
-      store_rows<T, DC>(dv, lane, D, false, out(p.dv));
+    if constexpr (OWN) {
+      ColAcc<T, DC> dk, dv;
+      dk.zero();
+      dv.zero();
+      short_dkv<T, DC, NB>(p, ql, ol, kf, vf, st_lse, st_del, tb0, q0, len, wave, lane, dk, dv);
+      // the rows of K and V serve to write: this wave's own, which it alone reads now
+      short_store<T, DC>(p, kl, vl, k_at, wave, lane, dk, dv);
     }
   }
   __syncthreads();
   fold_sums<NT>(p, acc, NB, ends, h, part);
 }
 
+// dK and dV of short units whose keys several heads share: a work-group runs through
+// units of one key/value head, whose heads' tables it keeps; wave w takes keys 32 w ..
+// and adds up their gradients over the heads in registers.
+template <typename T, int DC, int NB, int MINW>
+__global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_dkv_kernel(BwdParams p, uint32_t parts) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  constexpr int NT = NB * 64, R = NB * 32, TILE = R * G::P;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* ql = reinterpret_cast<T*>(smem);                     // K at first
+  T* ol = ql + TILE;                                      // V at first
+  float* st_lse = reinterpret_cast<float*>(ol + TILE);    // [R]
+  float* st_del = st_lse + R;                             // [R]
+  const int32_t near = p.bias.M + kEdge, n_tab = 2 * near + 1;
+  float* tab = st_del + R;                                // [grp][n_tab]
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t kvh = p.H / p.grp, j8 = blockIdx.x >> 3;
+  const uint32_t e = j8 % kvh, part = j8 / kvh * 8 + (blockIdx.x & 7u);
+  const int D = (int)p.D;
+  const uint32_t k_row = (uint32_t)p.ks[2] * (uint32_t)sizeof(T), q_row = (uint32_t)p.qs[2] * (uint32_t)sizeof(T),
+                 o_row = (uint32_t)p.os[2] * (uint32_t)sizeof(T);
+  using TileT = Tile<T, DC, R, NT>;
+  const typename TileT::Map mk = TileT::map(D, k_row, threadIdx.x), mq = TileT::map(D, q_row, threadIdx.x),
+                            mo = TileT::map(D, o_row, threadIdx.x);
+  for (uint32_t hh = 0; hh < p.grp; ++hh)
+    for (int32_t t = threadIdx.x; t < n_tab; t += NT)
+      tab[hh * n_tab + t] = bias_at<T>(p.bias, p.H, e * p.grp + hh, t - near);
+  clear_pad<T, DC>(ql, 2 * R, D, threadIdx.x, NT);
+  for (uint32_t bx = part; bx < p.BX; bx += parts) {
+    const uint32_t b = bx / p.X;
+    const int32_t q0 = position(p.q_pos, b);
+    const uint32_t len = length(p.kv_len, b, p.Lk);
+    const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D;
+    TileT ta, tb;
+    ta.fetch(mk, static_cast<const T*>(p.k) + k_at, len, k_row, D, p.vec);
+    tb.fetch(mk, static_cast<const T*>(p.v) + k_at, len, k_row, D, p.vec);
+    __syncthreads();   // the rows are free
+    ta.stash(mk, ql);
+    tb.stash(mk, ol);
+    typename M::frag kf[G::NS], vf[G::NS];
+    ColAcc<T, DC> dk, dv;
+    dk.zero();
+    dv.zero();
+    for (uint32_t hh = 0; hh < p.grp; ++hh) {
+      const uint32_t h = e * p.grp + hh;
+      const int64_t q_at = bx_at(p, bx, p.qs) + (int64_t)h * D, o_at = bx_at(p, bx, p.os) + (int64_t)h * D;
+      ta.fetch(mq, static_cast<const T*>(p.q) + q_at, p.Lq, q_row, D, p.vec);
+      tb.fetch(mo, static_cast<const T*>(p.dout) + o_at, p.Lq, o_row, D, p.vec);
+      float l = -INFINITY, del = 0.0f;
+      if (threadIdx.x < p.Lq) {
+        const uint64_t stat = ((uint64_t)bx * p.H + h) * p.Lq + threadIdx.x;
+        l = p.lse[stat];
+        del = p.delta[stat];
+      }
+      __syncthreads();   // K and V, or the last head's rows, are there
+      if (hh == 0) {
+#pragma unroll
+        for (int s = 0; s < G::NS; ++s) {
+          const int at = (32 * wave + l32) * G::P + 2 * G::E * s + G::E * g;
+          kf[s] = *reinterpret_cast<const typename M::frag*>(ql + at);
+          vf[s] = *reinterpret_cast<const typename M::frag*>(ol + at);
+        }
+        __syncthreads();   // and free
+      }
+      ta.stash(mq, ql);
+      tb.stash(mo, ol);
+      if (threadIdx.x < R) {
+        st_lse[threadIdx.x] = l == -INFINITY ? INFINITY : l * kLog2e;
+        st_del[threadIdx.x] = del;
+      }
+      __syncthreads();
+      short_dkv<T, DC, NB>(p, ql, ol, kf, vf, st_lse, st_del, tab + hh * n_tab + near, q0, len, wave, lane, dk, dv);
+    }
+    __syncthreads();   // the rows serve to write
+    short_store<T, DC>(p, ql, ol, k_at, wave, lane, dk, dv);
+  }
+}
+
 constexpr int kDqWaves = 4;   // of a work-group of the dQ kernel, 32 queries each
 
 // LDS of the short-unit kernel, and the blocks of 32 it takes the call with (0: not at
-// all): at most 64 queries and keys, heads with keys of their own (fp32 up to 64 wide:
-// a wider one's rows and sums do not fit the registers).
+// all): at most 64 queries and keys (fp32 up to 64 wide: a wider one's rows and sums do
+// not fit the registers); where heads share keys, tables of a group of 32 KB at most.
 size_t short_lds(const RelposArgs& a, int nb, int row_bytes) {
   const size_t n_tab = 2 * ((size_t)a.max_dist + kEdge) + 1;
   return (size_t)4 * 32 * nb * row_bytes + (size_t)2 * 32 * nb * 4 + (n_tab * (1 + nb) + 2 * 64 * nb) * 4;
@@ -740,16 +851,21 @@ int row_bytes_of(const RelposArgs& a) {
                         : (a.D + 31) / 32 * 32;
   return a.bf16 ? (dc + 8) * 2 : (dc + 4) * 4;
 }
+size_t shared_tables(const RelposArgs& a) {
+  return (size_t)(a.H / a.Hkv) * (2 * ((size_t)a.max_dist + kEdge) + 1) * 4;
+}
 int short_blocks(const RelposArgs& a) {
   const int64_t l = std::max(a.Lq, a.Lk);
-  return a.H != a.Hkv || a.Lq == 0 || l > 64 || (!a.bf16 && a.D > 64) ? 0 : l <= 32 ? 1 : 2;
+  if (a.Lq == 0 || l > 64 || (!a.bf16 && a.D > 64)) return 0;
+  if (a.H != a.Hkv && shared_tables(a) > 32 * 1024) return 0;
+  return l <= 32 ? 1 : 2;
 }
 // Work-groups of a head (parts of its dbias): enough to fill the chip, no more than
 // there is work.
 int64_t parts_of(const RelposArgs& a) {
   if (const int nb = short_blocks(a)) {
     const int64_t per_cu = std::max<int64_t>(1, 160 * 1024 / (int64_t)short_lds(a, nb, row_bytes_of(a)));
-    const int64_t want = (256 * std::min<int64_t>(per_cu, 8 / nb) + a.Hkv - 1) / a.Hkv;
+    const int64_t want = (256 * std::min<int64_t>(per_cu, 8 / nb) + a.H - 1) / a.H;
     return (std::min(a.B * a.X, want) + 7) / 8 * 8;
   }
   constexpr int64_t qb = 32 * kDqWaves;
@@ -774,13 +890,26 @@ int bias_grad(BwdParams& p, const RelposArgs& a, hipStream_t s) {
 
 template <typename T, int DC, int NB>
 int start_short(BwdParams& p, const RelposArgs& a, hipStream_t s) {
-  auto* kernel = relpos_bwd_short_kernel<T, DC, NB, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
-  const size_t lds = short_lds(a, NB, Geo<T, DC>::P * sizeof(T));
+  constexpr int MINW = sizeof(T) == 2 && DC <= 96 ? 2 : 1;
+  const bool own = a.H == a.Hkv;
+  auto* kernel = own ? relpos_bwd_short_kernel<T, DC, NB, true, MINW> : relpos_bwd_short_kernel<T, DC, NB, false, MINW>;
+  const size_t row = Geo<T, DC>::P * sizeof(T), lds = short_lds(a, NB, row);
   if (int st = lds_limit(kernel, lds)) return st;
-  const int64_t blocks = (int64_t)p.parts * a.Hkv;
+  const int64_t blocks = (int64_t)p.parts * a.H;
   if (!grid_fits(blocks, NB * 64)) return DSP_ERR_SHAPE;
   kernel<<<dim3((uint32_t)blocks), NB * 64, lds, s>>>(p);
   if (int st = last_launch_status()) return st;
+  if (!own) {
+    auto* dkv = relpos_bwd_short_dkv_kernel<T, DC, NB, MINW>;
+    const size_t dkv_lds = (size_t)2 * 32 * NB * (row + 4) + shared_tables(a);
+    if (int st = lds_limit(dkv, dkv_lds)) return st;
+    const int64_t per_cu = std::min<int64_t>(8 / NB, 160 * 1024 / dkv_lds);
+    const int64_t want = (256 * per_cu + a.Hkv - 1) / a.Hkv;
+    const int64_t parts = (std::min(a.B * a.X, want) + 7) / 8 * 8;
+    if (!grid_fits(parts * a.Hkv, NB * 64)) return DSP_ERR_SHAPE;
+    dkv<<<dim3((uint32_t)(parts * a.Hkv)), NB * 64, dkv_lds, s>>>(p, (uint32_t)parts);
+    if (int st = last_launch_status()) return st;
+  }
   return bias_grad<T>(p, a, s);
 }
 

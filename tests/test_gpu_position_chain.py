@@ -140,6 +140,11 @@ MANY = [
     (1, 130, 80, 100, 2, 2, 96, False, None, None, True),
     (2, 700, 33, 33, 3, 3, 16, False, [0, 9], [33, 20], True),
     (2, 900, 20, 28, 3, 3, 72, True, [8, 3], None, True),
+    (2, 300, 33, 40, 6, 2, 64, True, [7, -5], [40, 31], True),
+    (2, 700, 3, 3, 8, 2, 128, True, None, [3, 2], True),
+    (3, 50, 64, 50, 4, 1, 24, False, [0, -70, 70], [50, 0, 1], True),
+    (2, 130, 32, 30, 8, 4, 72, False, None, None, True),
+    (1, 3, 2, 64, 5, 1, 96, True, [60], None, True),
     (3, 120, 64, 64, 2, 2, 128, False, [0, -70, 70], [64, 0, 1], True),
     (2, 900, 3, 75, 4, 2, 64, True, [72, 40], [75, 43], False),
     (1, 1700, 1, 150, 4, 2, 72, False, None, None, False),
@@ -155,6 +160,14 @@ MANY = [
 def test_many_units(torch, dtype, B, X, Lq, Lk, H, Hkv, D, causal, q_pos, kv_len, grads):
     c = ru.case(B, X, Lq, Lk, H, Hkv, D, 25, 9, dtype, seed=X)
     _check(torch, c, dtype, f"relpos X{X} {Lq}x{Lk} D{D}", causal=causal, q_pos=q_pos, kv_len=kv_len, grads=grads)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_short_units_with_long_tables(torch, dtype):
+    """Groups whose tables are past what the short units' kernel keeps."""
+    for M, H, Hkv in ((1024, 8, 2), (1024, 2, 2), (900, 4, 2)):
+        c = ru.case(2, 5, 20, 30, H, Hkv, 64, M, 30, dtype, seed=M)
+        _check(torch, c, dtype, f"relpos M{M} H{H}/{Hkv}", q_pos=[0, 950])
 
 
 def test_two_streams_at_once(torch):
