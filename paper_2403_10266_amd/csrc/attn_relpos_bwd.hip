@@ -915,11 +915,15 @@ int start_short(BwdParams& p, const RelposArgs& a, hipStream_t s) {
 
 template <typename T, int DC, int NW>
 int start_dq(BwdParams& p, const RelposArgs& a, hipStream_t s) {
-  constexpr int KB = sizeof(T) == 2 ? 64 : 32;
+  // 32 keys a tile and registers for two waves per SIMD (three where the heads allow it)
+  // against 64 keys: 32 heads of 2000 x 64 causal 354 -> 323 us (with dK and dV), heads of
+  // 128 600 -> 481, 8 x 16 units of 4096 x 72 3153 and 3171.  fp32 up to 96 columns is
+  // faster with two waves and some spills as well: 500 x 72 484 -> 447.
+  constexpr int KB = 32, MINW = sizeof(T) == 2 || DC <= 96 ? 2 : 1;
   const size_t n_tab = 2 * ((size_t)p.bias.M + kEdge) + 1;
   p.n_blk = (uint32_t)((a.Lq + 32 * NW - 1) / (32 * NW));
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T) + (size_t)NW * kDiag * 4 + n_tab * 4 * (1 + NW);
-  auto* kernel = relpos_bwd_dq_kernel<T, DC, NW, KB, sizeof(T) == 2 && DC <= 96 ? 2 : 1>;
+  auto* kernel = relpos_bwd_dq_kernel<T, DC, NW, KB, MINW>;
   if (int st = lds_limit(kernel, lds)) return st;
   kernel<<<dim3(p.H * p.parts), NW * 64, lds, s>>>(p);
   return last_launch_status();
