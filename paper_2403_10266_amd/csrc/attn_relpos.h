@@ -312,6 +312,8 @@ __device__ __forceinline__ void clear_pad(T* lds, int rows, int D, int tid, int 
 // a row's cache lines).  Chunk c goes to XCD c % 8, so that sequences of different
 // lengths spread over all of them.  A chunk's blocks follow each other; where the
 // blocks differ in cost (causal masks) every chunk's most costly ones come first.
+// Whole token rows against single heads: 1350 x 16 units of 49 x 72 158 and 181 us,
+// 400 x 16 of 100 145 and 156, 64 x 16 of 300 the same.
 struct Order {
   uint32_t n_chunks, per_xcd;   // chunks in all, and (rounded up) of an XCD
   uint32_t heads, blocks;       // of a chunk: heads, blocks of each head

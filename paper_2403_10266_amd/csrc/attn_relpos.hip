@@ -22,6 +22,13 @@
 // Few queries against many keys (a new token against a cache): the queries of a
 // key/value head's group share one block of 32 columns, and the keys are cut among
 // work-groups, whose unnormalised sums a second kernel joins.
+//
+// Measured in bf16, 16 heads of 72: 8 x 16 units of 4096 760-890 us (813-695 TFLOP/s;
+// bound by the matrix cores, busy 38%, and the exponentials and conversions beside
+// them); 1350 x 16 units of 49 158 us (5.2 TB/s, memory); 1024 x 16 units of 32 66-71 us
+// (4.3-4.6 TB/s, memory); a token against 4 caches of up to 50000 keys of 8 heads of 64
+// 38 us and 4 for the join (5.3 TB/s while it reads), against 2048 caches of up to 120
+// keys 51 us (4.8 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -559,9 +566,11 @@ struct Choice {
   int64_t n_split, split_keys;
 };
 
-// The few-queries form where a group's queries fit the 32 columns of a block.  Its keys
-// are cut while there are fewer work-groups than 8 for each CU (lengths differ, so more
-// than the chip holds at once), into pieces of at least 256 keys.
+// The few-queries form where a group's queries fit the 32 columns of a block (16384
+// units of 32 queries 66 us, 92 by the form for many; 8192 units of one token 62 and 542).
+// Its keys are cut while there are fewer work-groups than 8 for each CU (lengths differ,
+// so more than the chip holds at once; 4, 8 and 16 are within 4% of each other), into
+// pieces of at least 256 keys.
 Choice choose(const RelposArgs& a) {
   Choice c = {};
   const int64_t grp = a.H / a.Hkv;
@@ -626,14 +635,19 @@ int start_few(FwdParams& p, const RelposArgs& a, hipStream_t s) {
 template <typename T, int DC>
 int start(FwdParams& p, const RelposArgs& a, bool few, hipStream_t s) {
   if (few) {
-    // a wave per unit where the units alone fill the chip
-    const bool full = a.B * a.X * a.Hkv >= 256 * 12;
+    // One wave and one tile where there is one (1600 units of 32 queries and keys 11 us,
+    // four waves 21); a wave per unit, without the join, where the units alone fill the
+    // chip, 12 waves to a CU, and their keys are few (8192 units of 120 keys 62 us
+    // against 107 with four waves, 3200 of 200 39 against 47, of 400 78 and 77, of 2000
+    // 372 and 322); two tiles at once (2400 units of 64 keys 19 against 27).
+    const bool full = a.B * a.X * a.Hkv >= 256 * 12 && a.Lk <= 384;
     if (a.Lk <= 32) return start_few<T, DC, 1, true>(p, a, s);
     if (full) return start_few<T, DC, 1, false>(p, a, s);
     if (a.Lk <= 64) return start_few<T, DC, 2, true>(p, a, s);
     return start_few<T, DC, 4, false>(p, a, s);
   }
   constexpr bool B16 = sizeof(T) == 2;
+  // one tile of keys (and of queries): 21600 units of 49 158 us, by the loop below 360
   if (a.Lq <= 64 && a.Lk <= 64) return start_many<T, DC, 2, 1, 64, 1, B16 ? (DC <= 80 ? 3 : 2) : 1>(p, a, s);
   // Long rows.  Heads of at most 64 columns: 4 waves of 32 queries, 3 of such work-groups
   // to a CU (8 x 16 units of 4096 x 64: 627 us; 8 waves of 64 queries 630, and 81 instead
