@@ -854,8 +854,8 @@ constexpr int kDqWaves = 4;   // of a work-group of the dQ kernel, 32 queries ea
 // LDS of the short-unit kernel, and the blocks of 32 it takes the call with (0: not at
 // all): at most 64 queries and keys (fp32 up to 64 wide: a wider one's rows and sums do
 // not fit the registers); where heads share keys, tables of a group of 32 KB at most.
-// Against the kernels for long units: 1350 x 16 units of 49 x 72 387 us and 1390; heads
-// that share keys, 2000 x 16 over 4 of 49 x 72, 482 and 1332.
+// Against the kernels for long units: 1350 x 16 units of 49 x 72 403 us and 1227 in all;
+// heads that share keys, 2000 x 16 over 4 of 49 x 72, 472 and 1326.
 size_t short_lds(const RelposArgs& a, int nb, int row_bytes) {
   const size_t n_tab = 2 * ((size_t)a.max_dist + kEdge) + 1;
   return (size_t)4 * 32 * nb * row_bytes + (size_t)2 * 32 * nb * 4 + (n_tab * (1 + nb) + 2 * 64 * nb) * 4;
