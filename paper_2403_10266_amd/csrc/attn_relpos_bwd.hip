@@ -1,6 +1,6 @@
 // Gradient of attention with a learned relative position bias.  With
 //   z_ij = scale q_i . k_j + bias[bucket(j - i - q_pos)][h],  P = softmax(z),
-//   Delta_i = sum_d dO_id O_id,  dZ = P (dO V^T - Delta):
+//   Delta_i = sum_j P_ij dP_ij = sum_d dO_id O_id,  dZ = P (dP - Delta),  dP = dO V^T:
 //   dV = P^T dO,  dQ = scale dZ K,  dK = scale dZ^T Q,
 //   dbias[t][h] = sum of dZ_ij over every (b, x, i, j) whose distance has bucket t.
 // P is recomputed from the forward's row log-sum-exp.  Two kernels, both deterministic:
@@ -17,9 +17,8 @@
 // into buckets.
 //
 // P and dZ are rounded to bf16 for the products that take them as operands (the matrix
-// cores' type; their sums are fp32), dbias sums dZ before that rounding.  Delta comes from
-// o as the forward stored it, so it carries o's rounding, except for units of at most 64
-// positions, where it is formed from P and dP.
+// cores' type; their sums are fp32), dbias sums dZ before that rounding.  Delta is formed
+// from P and dP; only in fp32 and for units past 64 positions from the stored o.
 //
 // Measured in bf16: 32 heads of 64 over 8, 4 causal sequences of 2000, 1334, 667 and 0:
 // dQ 121 us, dK and dV 227, dbias 6 (matrix cores busy 27% and 25%: a wave's chain of
@@ -150,12 +149,16 @@ __device__ __forceinline__ void fold_sums(const BwdParams& p, float* acc, int n_
 }
 
 // ---------------------------------------------------------------------------
-// dQ, Delta and the sums of dZ by distance: 32 queries of one head per wave.
+// dQ, Delta and the sums of dZ by distance: 32 queries of one head per wave.  In bf16 the
+// keys pass twice, first for Delta_i = sum_j P_ij dP_ij.  Taken from o, Delta would carry
+// the rounding of o, and a bucket's sum, whose terms cancel (each row of dZ adds up to
+// nothing), that rounding many times over: 5e-3 of dbias at 384 causal positions.
 template <typename T, int DC, int NW, int KB, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams p) {
   using G = Geo<T, DC>;
   using M = Mx<T>;
   constexpr int NT = NW * 64, QB = NW * 32, NKT = KB / 32, TILE = KB * G::P;
+  constexpr bool TWICE = sizeof(T) == 2;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   T* lds = reinterpret_cast<T*>(smem);   // [2][K, V][KB][P]
   const int32_t near = p.bias.M + kEdge, n_tab = 2 * near + 1;
@@ -220,20 +223,20 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
     row_frags<T, DC>(on ? static_cast<const T*>(p.q) + q_at + (int64_t)row * p.qs[2] : nullptr, g, D, p.vec, qf);
     row_frags<T, DC>(on ? static_cast<const T*>(p.dout) + o_at + (int64_t)row * p.os[2] : nullptr, g, D, p.vec, df);
     float delta = 0.0f;
-    {
+    if constexpr (!TWICE) {
       typename M::frag of[G::NS];
       row_frags<T, DC>(on ? static_cast<const T*>(p.o) + o_at + (int64_t)row * p.os[2] : nullptr, g, D, p.vec, of);
 #pragma unroll
       for (int s = 0; s < G::NS; ++s)
 #pragma unroll
         for (int e = 0; e < G::E; ++e) delta += (float)df[s][e] * (float)of[s][e];
+      delta += swap_halves(delta);
     }
-    delta += swap_halves(delta);
     const uint64_t stat = ((uint64_t)bx * p.H + h) * p.Lq + row;
     // a row without keys, or past the end: P = exp2(-inf) = 0
     const float l = on ? p.lse[stat] : -INFINITY;
     const float lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
-    if (on && g == 0) p.delta[stat] = delta;
+    if (on && g == 0 && (!TWICE || k1 == 0)) p.delta[stat] = delta;
 
     ColAcc<T, DC> dq;
     dq.zero();
@@ -242,10 +245,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
     __syncthreads();
     const uint32_t n_it = (k1 + KB - 1) / KB;
     const int32_t wq = q0 + 32 * wave;
-    for (uint32_t it = 0; it < n_it; ++it) {
-      const uint32_t kb = it * KB;
-      const bool more = it + 1 < n_it;
-      if (more) fetch(kb + KB);
+    const uint32_t n_all = TWICE ? 2 * n_it : n_it;
+    for (uint32_t it = 0; it < n_all; ++it) {
+      const bool sums = TWICE && it < n_it;   // of Delta
+      const uint32_t kb = (it < n_it ? it : it - n_it) * KB;
+      const bool more = it + 1 < n_all;
+      if (more) fetch((it + 1 < n_it ? it + 1 : it + 1 - n_it) * KB);
       const T* kl = lds + (it & 1) * 2 * TILE;
       const T* vl = kl + TILE;
 #pragma unroll
@@ -277,6 +282,11 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
           for (int r = 0; r < 16; ++r)
             if (8 * (r / 4) + r % 4 >= stop) s[r] = -INFINITY;
         }
+        if (sums) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) delta += __builtin_amdgcn_exp2f(s[r]) * dp[r];
+          continue;
+        }
         ColB<T> z;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -293,6 +303,10 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
           add_diagonals(mine + d0, room + wave * kDiag, dp, lane);
         }
         dq.add(kl, 32 * kt, lane, z);
+      }
+      if (TWICE && it + 1 == n_it) {
+        delta += swap_halves(delta);
+        if (on && g == 0) p.delta[stat] = delta;
       }
       if (more) stash((it + 1) & 1);
       __syncthreads();

@@ -391,3 +391,16 @@ def test_no_units(torch):
         *_, db = dsp.dsp_attn_relpos_bwd(q, k, k, q, q, lse, 2, 2, bias, bk, dbias=z(4, 2) + 9)
         torch.cuda.synchronize()
         assert o.shape == q.shape and not db.any()
+
+
+@pytest.mark.parametrize("L,Lk,M,causal", [(384, 384, 16, True), (700, 116, 200, False)])
+def test_the_bias_gradient_is_rounded_once(torch, L, Lk, M, causal):
+    """The rows of dZ add up to nothing, so the sums of long buckets cancel: in bf16 they
+    still carry the rounding of the result, at most 2^-8 of it, and fp32 errors (2^-12)
+    alone."""
+    import paper_2403_10266_amd as dsp
+    c = ru.case(1, 4, L, Lk, 4, 4, 40, M, 8, "bf16", seed=28)
+    c["buckets"] = dsp.dsp_relpos_buckets(M, 8, not causal).numpy()
+    got = host(_run(torch, c, "bf16", causal=causal)["dbias"])
+    want = ru.wanted(c, "bf16", causal)["dbias"][0]
+    assert np.linalg.norm(got - want) <= (2.0 ** -8 + 2.0 ** -12) * np.linalg.norm(want)
