@@ -236,64 +236,78 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
     // a row without keys, or past the end: P = exp2(-inf) = 0
     const float l = on ? p.lse[stat] : -INFINITY;
     const float lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
-    if (on && g == 0 && (!TWICE || k1 == 0)) p.delta[stat] = delta;
-
-    ColAcc<T, DC> dq;
-    dq.zero();
     __syncthreads();   // the buffers, the table and the sums are free and set
     if (k1) stash(0);
     __syncthreads();
     const uint32_t n_it = (k1 + KB - 1) / KB;
     const int32_t wq = q0 + 32 * wave;
-    const uint32_t n_all = TWICE ? 2 * n_it : n_it;
-    for (uint32_t it = 0; it < n_all; ++it) {
-      const bool sums = TWICE && it < n_it;   // of Delta
-      const uint32_t kb = (it < n_it ? it : it - n_it) * KB;
-      const bool more = it + 1 < n_all;
-      if (more) fetch((it + 1 < n_it ? it + 1 : it + 1 - n_it) * KB);
-      const T* kl = lds + (it & 1) * 2 * TILE;
+    // S and dP of one block of 32 keys, S made the exponents of P; false: nothing to do
+    auto block = [&](const T* kl, uint32_t kb, int kt, floatx16& s, floatx16& dp) {
       const T* vl = kl + TILE;
+      const int32_t key0 = (int32_t)kb + 32 * kt, d0 = key0 - wq;
+      if (key0 >= (int32_t)k1 || (p.causal && d0 > 31)) return false;
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        const int32_t key0 = (int32_t)kb + 32 * kt, d0 = key0 - wq;
-        if (key0 >= (int32_t)k1 || (p.causal && d0 > 31)) continue;
-        floatx16 s, dp;
+      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+      for (int st = 0; st < G::NS; ++st) {
+        const int at = (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g;
+        s = M::mma(*reinterpret_cast<const typename M::frag*>(kl + at), qf[st], s);
+        dp = M::mma(*reinterpret_cast<const typename M::frag*>(vl + at), df[st], dp);
+      }
+      if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
+        const float t = (d0 < 0 ? left : right) - lse2;
 #pragma unroll
-        for (int st = 0; st < G::NS; ++st) {
-          const int at = (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g;
-          s = M::mma(*reinterpret_cast<const typename M::frag*>(kl + at), qf[st], s);
-          dp = M::mma(*reinterpret_cast<const typename M::frag*>(vl + at), df[st], dp);
-        }
-        const bool far = d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M;
-        if (far) {
-          const float t = (d0 < 0 ? left : right) - lse2;
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, t);
+      } else {
+        const float* tb = tab + near + d0 + 4 * g - l32;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, t);
-        } else {
-          const float* tb = tab + near + d0 + 4 * g - l32;
+        for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, tb[8 * (r / 4) + r % 4] - lse2);
+      }
+      if ((p.causal && d0 + 31 > 0) || key0 + 32 > (int32_t)k1) {
+        const int32_t stop = (p.causal ? min((int32_t)k1, wq + l32 + 1) : (int32_t)k1) - key0 - 4 * g;
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, tb[8 * (r / 4) + r % 4] - lse2);
-        }
-        if ((p.causal && d0 + 31 > 0) || key0 + 32 > (int32_t)k1) {
-          const int32_t stop = (p.causal ? min((int32_t)k1, wq + l32 + 1) : (int32_t)k1) - key0 - 4 * g;
+        for (int r = 0; r < 16; ++r)
+          if (8 * (r / 4) + r % 4 >= stop) s[r] = -INFINITY;
+      }
+      return true;
+    };
+    if constexpr (TWICE) {
+      for (uint32_t it = 0; it < n_it; ++it) {
+        fetch(it + 1 < n_it ? (it + 1) * KB : 0);
+        const T* kl = lds + (it & 1) * 2 * TILE;
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (8 * (r / 4) + r % 4 >= stop) s[r] = -INFINITY;
-        }
-        if (sums) {
+        for (int kt = 0; kt < NKT; ++kt) {
+          floatx16 s, dp;
+          if (!block(kl, it * KB, kt, s, dp)) continue;
 #pragma unroll
           for (int r = 0; r < 16; ++r) delta += __builtin_amdgcn_exp2f(s[r]) * dp[r];
-          continue;
         }
+        stash((it + 1) & 1);
+        __syncthreads();
+      }
+      delta += swap_halves(delta);
+    }
+    if (on && g == 0) p.delta[stat] = delta;
+    ColAcc<T, DC> dq;
+    dq.zero();
+    const uint32_t odd = TWICE ? n_it & 1 : 0;   // the buffer of the first tile
+    for (uint32_t it = 0; it < n_it; ++it) {
+      const uint32_t kb = it * KB;
+      const bool more = it + 1 < n_it;
+      if (more) fetch(kb + KB);
+      const T* kl = lds + ((it + odd) & 1) * 2 * TILE;
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        floatx16 s, dp;
+        if (!block(kl, kb, kt, s, dp)) continue;
+        const int32_t d0 = (int32_t)kb + 32 * kt - wq;
         ColB<T> z;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           dp[r] = __builtin_amdgcn_exp2f(s[r]) * (dp[r] - delta);
           z.set(r, dp[r]);
         }
-        if (far) {
+        if (d0 + 31 <= -p.bias.M || d0 - 31 >= p.bias.M) {
           float v = 0.0f;
 #pragma unroll
           for (int r = 0; r < 16; ++r) v += dp[r];
@@ -304,11 +318,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
         }
         dq.add(kl, 32 * kt, lane, z);
       }
-      if (TWICE && it + 1 == n_it) {
-        delta += swap_halves(delta);
-        if (on && g == 0) p.delta[stat] = delta;
-      }
-      if (more) stash((it + 1) & 1);
+      if (more) stash((it + 1 + odd) & 1);
       __syncthreads();
     }
     dq.scale(p.scale, lane);
