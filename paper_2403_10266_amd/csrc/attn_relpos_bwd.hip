@@ -21,9 +21,10 @@
 // from P and dP; only in fp32 and for units past 64 positions from the stored o.
 //
 // Measured in bf16: 32 heads of 64 over 8, 4 causal sequences of 2000, 1334, 667 and 0:
-// dQ 121 us, dK and dV 227, dbias 6 (matrix cores busy 27% and 25%: a wave's chain of
-// product, exponential and product, with two or three waves to a SIMD, and causal blocks of
-// unequal length); 8 x 16 units of 4096 x 72 3.15 ms in all (490 TFLOP/s of 5 products);
+// dQ 193 us, dK and dV 227, dbias 6 (bound by a wave's chain of product, exponential and
+// product, with two or three waves to a SIMD, the matrix cores busy 25-30%, and by causal
+// blocks of unequal length); 8 x 16 units of 4096 x 72 4.1-4.3 ms in all (370 TFLOP/s of the
+// gradient's 5 products);
 // 1350 x 16 units of 49 x 72 387 us (4.0 TB/s: memory, and the waits between a unit's
 // loads, its two passes and its stores).
 #include <algorithm>
@@ -152,7 +153,8 @@ __device__ __forceinline__ void fold_sums(const BwdParams& p, float* acc, int n_
 // dQ, Delta and the sums of dZ by distance: 32 queries of one head per wave.  In bf16 the
 // keys pass twice, first for Delta_i = sum_j P_ij dP_ij.  Taken from o, Delta would carry
 // the rounding of o, and a bucket's sum, whose terms cancel (each row of dZ adds up to
-// nothing), that rounding many times over: 5e-3 of dbias at 384 causal positions.
+// nothing), that rounding many times over: 5e-3 of dbias at 384 causal positions.  The
+// first pass costs a third of the gradient: 4096 x 72 3.15 -> 4.2 ms.
 template <typename T, int DC, int NW, int KB, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams p) {
   using G = Geo<T, DC>;
@@ -953,11 +955,12 @@ int start_short(BwdParams& p, const RelposArgs& a, hipStream_t s) {
 
 template <typename T, int DC, int NW>
 int start_dq(BwdParams& p, const RelposArgs& a, hipStream_t s) {
-  // 32 keys a tile and registers for two waves per SIMD (three where the heads allow it)
-  // against 64 keys: 32 heads of 2000 x 64 causal 354 -> 323 us (with dK and dV), heads of
-  // 128 600 -> 481, 8 x 16 units of 4096 x 72 3153 and 3171.  fp32 up to 96 columns is
-  // faster with two waves and some spills as well: 500 x 72 484 -> 447.
-  constexpr int KB = 32, MINW = sizeof(T) == 2 || DC <= 96 ? 2 : 1;
+  // 32 keys a tile and registers for two waves per SIMD against 64 keys (the whole
+  // gradient, without the first pass): 32 heads of 2000 x 64 causal 323 and 354 us, heads
+  // of 128 481 and 600, 8 x 16 units of 4096 x 72 3171 and 3153; fp32 up to 96 columns is
+  // faster with two waves and some spills as well, 500 x 72 447 and 484.  Three waves for
+  // bf16 up to 64 columns (with the first pass): 388 and 413 for the first of these.
+  constexpr int KB = 32, MINW = sizeof(T) == 2 && DC <= 64 ? 3 : sizeof(T) == 2 || DC <= 96 ? 2 : 1;
   const size_t n_tab = 2 * ((size_t)p.bias.M + kEdge) + 1;
   p.n_blk = (uint32_t)((a.Lq + 32 * NW - 1) / (32 * NW));
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T) + (size_t)NW * kDiag * 4 + n_tab * 4 * (1 + NW);
@@ -991,7 +994,8 @@ int start(BwdParams& p, const RelposArgs& a, hipStream_t s) {
   if (a.Lk == 0) return DSP_OK;
   // The most keys to a work-group that still fill the chip, which holds 256 of eight
   // waves: once where units are alike, twice where masks or lengths make them differ.
-  // 4 x 2000 tokens, 32 heads of 64 over 8, causal and ragged: gradients 478, 385 and
+  // 4 x 2000 tokens, 32 heads of 64 over 8, causal and ragged: gradients (measured with
+  // dQ in one pass) 478, 385 and
   // 445 us with 8, 4 and 2 blocks of keys; 16 heads of 72 over 4: 484, 349, 273; not
   // causal, 8 x 16 units of 4096: 3170, 3417, 3940.
   auto fills = [&](int64_t keys) {
