@@ -384,7 +384,9 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
  *          or NULL (Lk).  Keys and values past it are never used, whatever they
  *          hold; the others must be finite.
  * flags:   DSP_RELPOS_CAUSAL keeps the keys j <= i + q_pos only.
- * A query without keys (kv_len 0, or none before it) gives o = 0 and lse = -inf.
+ * A query without keys (kv_len 0, or none before it) gives o = 0 and lse = -inf.  A
+ * query that is not finite makes its own row of o and its lse NaN; a unit's gradients
+ * are NaN where a query or a row of dout of theirs is not finite, no other unit's.
  * lse:     fp32 [B * X * H][Lq], the row log-sum-exp of s, or NULL.
  * dtype:   DSP_BF16 (fp32 scores, softmax and accumulation; probabilities are
  *          rounded to bf16 for the product with v), D a multiple of 8 up to 128,

@@ -37,6 +37,10 @@
 namespace dsp {
 namespace {
 
+// Whether a row's sum says that it has no keys: exactly 0.  By its bits, since a query
+// that is not finite has a NaN there, which this file's comparisons may take either way.
+__device__ __forceinline__ bool no_keys(float sum) { return __builtin_bit_cast(uint32_t, sum) == 0u; }
+
 struct FwdParams {
   const void* q;
   const void* k;
@@ -330,13 +334,13 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
     const float l = sm.sum[j] + swap_halves(sm.sum[j]);
-    sm.o[j].scale(l > 0.0f ? 1.0f / l : 0.0f, lane);
+    sm.o[j].scale(no_keys(l) ? 0.0f : 1.0f / l, lane);
     const uint32_t c0 = 32 * (wave * QT + j);
     auto row = [&](int n) -> T* { return c0 + n < nq ? og + (int64_t)(qb * QB + c0 + n) * p.os[2] : nullptr; };
     if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, sm.o[j], lane, D, row);
     else store_rows<T, DC>(sm.o[j], lane, D, false, row);
     if (p.lse && g == 0 && c0 + l32 < nq)
-      p.lse[((uint64_t)bx * p.H + h) * p.Lq + qb * QB + c0 + l32] = l > 0.0f ? kLn2 * (sm.ref[j] + log2f(l)) : -INFINITY;
+      p.lse[((uint64_t)bx * p.H + h) * p.Lq + qb * QB + c0 + l32] = no_keys(l) ? -INFINITY : kLn2 * (sm.ref[j] + log2f(l));
   }
 }
 
@@ -446,7 +450,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
 
   T* og = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1];
   if constexpr (NW == 1) {
-    sm.o[0].scale(l > 0.0f ? 1.0f / l : 0.0f, lane);
+    sm.o[0].scale(no_keys(l) ? 0.0f : 1.0f / l, lane);
     auto row = [&](int n) -> T* {
       const uint32_t hh = (uint32_t)n / p.Lq;
       return (uint32_t)n < p.cols ? og + at_row(hh, n - hh * p.Lq, p.os[2]) : nullptr;
@@ -454,7 +458,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
     if (p.vec) store_rows_lds<T, DC>(vl, sm.o[0], lane, D, row);
     else store_rows<T, DC>(sm.o[0], lane, D, false, row);
     if (p.lse && g == 0 && (uint32_t)l32 < p.cols)
-      p.lse[((uint64_t)bx * p.H + h0 + ch) * p.Lq + cq] = l > 0.0f ? kLn2 * (sm.ref[0] + log2f(l)) : -INFINITY;
+      p.lse[((uint64_t)bx * p.H + h0 + ch) * p.Lq + cq] = no_keys(l) ? -INFINITY : kLn2 * (sm.ref[0] + log2f(l));
   } else {
     // the waves' columns meet at the largest of their references, and are added in
     // the waves' order; the tiles and the table are done with
@@ -493,7 +497,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
       } else {
         const float s = ms[(2 * NW + 1) * 32 + col];
         const uint32_t hh = col / p.Lq;
-        og[at_row(hh, col - hh * p.Lq, p.os[2]) + d] = (T)(s > 0.0f ? v / s : 0.0f);
+        og[at_row(hh, col - hh * p.Lq, p.os[2]) + d] = (T)(no_keys(s) ? 0.0f : v / s);
       }
     }
     if (threadIdx.x < p.cols) {
@@ -502,7 +506,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
       else if (p.lse) {
         const uint32_t hh = threadIdx.x / p.Lq;
         p.lse[((uint64_t)bx * p.H + h0 + hh) * p.Lq + threadIdx.x - hh * p.Lq] =
-            s > 0.0f ? kLn2 * (m + log2f(s)) : -INFINITY;
+            no_keys(s) ? -INFINITY : kLn2 * (m + log2f(s));
       }
     }
   }
@@ -557,8 +561,8 @@ __global__ __launch_bounds__(256) void relpos_join_kernel(FwdParams p) {
   const uint32_t kvh = p.H / p.grp, bx = unit / kvh, hh = col / p.Lq, i = col - hh * p.Lq;
   const uint32_t h = unit % kvh * p.grp + hh, b = bx / p.X, x = bx % p.X;
   static_cast<T*>(p.o)[(int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)i * p.os[2] + (int64_t)h * p.D + d] =
-      (T)(l > 0.0f ? a / l : 0.0f);
-  if (p.lse && d == 0) p.lse[((uint64_t)bx * p.H + h) * p.Lq + i] = l > 0.0f ? kLn2 * (top + log2f(l)) : -INFINITY;
+      (T)(no_keys(l) ? 0.0f : a / l);
+  if (p.lse && d == 0) p.lse[((uint64_t)bx * p.H + h) * p.Lq + i] = no_keys(l) ? -INFINITY : kLn2 * (top + log2f(l));
 }
 
 struct Choice {

@@ -67,3 +67,45 @@ def test_other_units_keep_their_bits(torch, dtype, X, Lq, Lk, H, Hkv, D):
             free[0 if name == "dbias" else x, h if heads == H else h // grp] = False
         assert same[free].all(), (name, (free & ~same).nonzero()[:5].tolist())
     assert bad["dq"].view(X, Lq, H, D)[0, 3, 0].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("X,Lq,Lk,H,Hkv,D", [
+    (2, 200, 200, 2, 2, 72), (16, 2000, 200, 16, 16, 72), (2, 200, 200, 2, 2, 64), (2, 50, 50, 2, 2, 72),
+    (1, 1, 900, 4, 4, 72), (2, 3, 100, 8, 2, 64), (2, 2, 20, 4, 2, 72), (1, 2, 60, 2, 2, 40), (3000, 1, 120, 4, 4, 72),
+])
+def test_a_query_that_is_not_finite_shows(torch, dtype, X, Lq, Lk, H, Hkv, D):
+    """Its row is NaN, its log-sum-exp too (only a row without keys is 0 with -inf), its
+    gradient and what it adds to the gradients of its keys as well; other rows stay.
+    Those of its wave may be summed from another reference: both results are off by at
+    most u of the largest value for P and u for the result, u = 2^-8 in bf16; in fp32 by
+    3 (D + 16) 2^-24 (1 + S), S < 60 the largest score: 2^-9 of the largest value."""
+    import paper_2403_10266_amd as dsp
+    tt = torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(X + D)
+    r = lambda *s: torch.randn(*s, generator=g, device="cuda").to(tt)  # noqa: E731
+    q, do = r(1, X, Lq, H * D), r(1, X, Lq, H * D)
+    k, v = r(1, X, Lk, Hkv * D), r(1, X, Lk, Hkv * D)
+    bias, bk = r(8, H), dsp.dsp_relpos_buckets(16, 8).cuda()
+    clean, lse0 = dsp.dsp_attn_relpos(q, k, v, H, Hkv, bias, bk, with_lse=True)
+    for value in (float("nan"), float("inf")):
+        q2 = q.clone()
+        q2[0, 0, Lq - 1, D + 3] = value                         # head 1
+        o, lse = dsp.dsp_attn_relpos(q2, k, v, H, Hkv, bias, bk, with_lse=True)
+        dq, dk, dv, _ = dsp.dsp_attn_relpos_bwd(q2, k, v, o, do, lse, H, Hkv, bias, bk)
+        torch.cuda.synchronize()
+        assert o[0, 0, Lq - 1, D:2 * D].isnan().all() and lse[0, 0, 1, Lq - 1].isnan(), value
+        assert dq[0, 0, Lq - 1, D:2 * D].isnan().any(), value
+        e = 1 // (H // Hkv)                                     # the keys of head 1
+        assert all(t[0, 0, :, e * D:(e + 1) * D].isnan().any() for t in (dk, dv)), value
+        free = torch.ones(1, X, Lq, H, dtype=torch.bool, device="cuda")
+        free[0, 0, Lq - 1, 1] = False
+        a, b = (t.float().view(1, X, Lq, H, D)[free] for t in (clean, o))
+        most = (4 * 2.0 ** -8 if dtype == "bf16" else 2.0 ** -9) * float(v.abs().max())
+        assert (a - b).abs().max() <= most, value
+        a, b = (t.transpose(2, 3)[free] for t in (lse0, lse))
+        assert (a - b).abs().max() <= 2.0 ** -9, value
+        k0 = torch.zeros(1, dtype=torch.int32, device="cuda")
+        o, lse = dsp.dsp_attn_relpos(q2, k, v, H, Hkv, bias, bk, kv_len=k0, with_lse=True)
+        torch.cuda.synchronize()
+        assert not o.any() and lse.isneginf().all()
