@@ -402,7 +402,9 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
  * strides).  Deterministic: no sum depends on timing.  Rows of dk and dv past kv_len
  * are 0, as is dbias where bias masks.  workspace:
  * dsp_attn_relpos_bwd_workspace_bytes(...) bytes, 16-byte aligned.  dq, dk and dv
- * may be columns of one buffer; other overlaps are DSP_ERR_ARG, as are broadcast keys.
+ * may be columns of one buffer; broadcast keys are DSP_ERR_ARG.
+ * In both calls every output, lse, dbias and the workspace among them, lies apart from
+ * everything else that the call reads or writes (DSP_ERR_ARG); gaps between rows are free.
  *
  * dsp_relpos_buckets -- fills buckets[2 * max_dist + 1] in HOST memory: with
  * n = n_buckets (bidirectional: half of them for each direction, keys after the

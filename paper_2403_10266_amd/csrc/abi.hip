@@ -5,6 +5,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <utility>
 
@@ -334,6 +335,46 @@ bool same_rows(const void* a, const int64_t* sa, const void* b, const int64_t* s
   return a == b;
 }
 
+// A block of n bytes shares none with the rows of (B, X, L): it is apart from their span or
+// lies in one of the gaps between them.  Strides that do not nest leave no gaps to rely on.
+bool block_apart(const void* block, int64_t n, const void* rows, const int64_t* st, int64_t w, int64_t L, int64_t B,
+                 int64_t X, int es) {
+  if (n <= 0 || w <= 0 || L <= 0) return true;
+  int64_t e[3] = {B, X, L}, s[3] = {st[0], st[1], st[2]}, span = w * es;
+  for (int i = 0; i < 3; ++i) {
+    for (int j = i + 1; j < 3; ++j)
+      if (s[j] > s[i]) { std::swap(s[i], s[j]); std::swap(e[i], e[j]); }
+    span += (e[i] - 1) * s[i] * es;
+  }
+  if (!overlap(block, (size_t)n, rows, (size_t)span)) return true;
+  int64_t from = (intptr_t)block - (intptr_t)rows;
+  for (int i = 0; i < 3; ++i) {   // from the largest stride down: which of its pieces the block starts in
+    if (e[i] <= 1) continue;
+    const int64_t step = s[i] * es;
+    span -= (e[i] - 1) * step;    // of one piece
+    if (from < 0 || step < span) return false;
+    const int64_t at = std::min(from / step, e[i] - 1);
+    from -= at * step;
+    if (at < e[i] - 1 && from + n > step) return false;   // it reaches the next piece
+    if (from >= span) return true;
+  }
+  return false;
+}
+
+// What a call reads or writes: rows of the (B, X, L) grid (elements of es bytes), or a block.
+struct Mem {
+  const void* p;
+  const int64_t* st;   // rows: strides; a block: null
+  int64_t w, L;        // rows: their width and number; a block: its bytes
+};
+Mem mem_block(const void* p, int64_t bytes) { return {p, nullptr, p ? bytes : 0, 0}; }
+bool apart(const Mem& a, const Mem& b, int64_t B, int64_t X, int es) {
+  if (a.st && b.st) return rows_apart(a.p, a.st, a.w, a.L, b.p, b.st, b.w, b.L, B, X, es);
+  if (a.st) return block_apart(b.p, b.w, a.p, a.st, a.w, a.L, B, X, es);
+  if (b.st) return block_apart(a.p, a.w, b.p, b.st, b.w, b.L, B, X, es);
+  return !overlap(a.p, (size_t)a.w, b.p, (size_t)b.w);
+}
+
 int qk_norm_impl(QkNormArgs& a, bool bwd, int flags, int H, int Hkv, const int64_t* const (&xs)[2],
                  const int64_t* const (&ds)[2], const int64_t* const (&ys)[2], void* workspace, size_t ws_bytes,
                  int dtype, void* stream) {
@@ -460,31 +501,34 @@ int relpos_impl(RelposArgs& a, bool bwd, int flags, void* workspace, size_t ws_b
   for (const int64_t* st : {a.q_strides, a.kv_strides, a.o_strides})
     if (st[2] >= far) return DSP_ERR_SHAPE;
   auto disjoint = [&](int64_t L, const int64_t* st, int64_t w) { return rows_disjoint(a.B, a.X, L, st, w); };
-  const int64_t B = a.B, X = a.X;
-  auto apart = [&](const void* p, const int64_t* sp, int64_t wp, int64_t Lp, const void* r, const int64_t* sr,
-                   int64_t wr, int64_t Lr) { return rows_apart(p, sp, wp, Lp, r, sr, wr, Lr, B, X, es); };
   const int64_t Lq = no_q ? 0 : a.Lq, Lk = no_k ? 0 : a.Lk;
   const int64_t *sq = a.q_strides, *sk = a.kv_strides, *so = a.o_strides;
-  if (!bwd) {
-    if (!disjoint(a.Lq, so, wq)) return DSP_ERR_ARG;
-    if (!apart(a.o, so, wq, Lq, a.q, sq, wq, Lq) || !apart(a.o, so, wq, Lq, a.k, sk, wk, Lk) ||
-        !apart(a.o, so, wq, Lq, a.v, sk, wk, Lk))
-      return DSP_ERR_ARG;
-  } else {
-    if ((!no_q && !disjoint(a.Lq, sq, wq)) || (!no_k && !disjoint(a.Lk, sk, wk))) return DSP_ERR_ARG;
-    struct Rows { const void* p; const int64_t* st; int64_t w, L; };
-    const Rows in[] = {{a.q, sq, wq, Lq}, {a.k, sk, wk, Lk}, {a.v, sk, wk, Lk}, {a.o, so, wq, Lq}, {a.dout, so, wq, Lq}};
-    const Rows out[] = {{a.dq, sq, wq, Lq}, {a.dk, sk, wk, Lk}, {a.dv, sk, wk, Lk}};
-    for (int i = 0; i < 3; ++i) {
-      for (const Rows& r : in)
-        if (!apart(out[i].p, out[i].st, out[i].w, out[i].L, r.p, r.st, r.w, r.L)) return DSP_ERR_ARG;
-      for (int j = 0; j < i; ++j)
-        if (!apart(out[i].p, out[i].st, out[i].w, out[i].L, out[j].p, out[j].st, out[j].w, out[j].L)) return DSP_ERR_ARG;
-    }
-    if (overlap(a.dbias, (size_t)a.n_buckets * a.H * es, a.bias, (size_t)a.n_buckets * a.H * es)) return DSP_ERR_ARG;
-  }
+  if (!bwd && !disjoint(a.Lq, so, wq)) return DSP_ERR_ARG;
+  if (bwd && ((!no_q && !disjoint(a.Lq, sq, wq)) || (!no_k && !disjoint(a.Lk, sk, wk)))) return DSP_ERR_ARG;
+  // every output is apart from every input and from the other outputs
+  const Mem q = {a.q, sq, wq, Lq}, k = {a.k, sk, wk, Lk}, v = {a.v, sk, wk, Lk}, o = {a.o, so, wq, Lq};
+  const Mem dout = {a.dout, so, wq, Lq}, dq = {a.dq, sq, wq, Lq}, dk = {a.dk, sk, wk, Lk}, dv = {a.dv, sk, wk, Lk};
+  const Mem lse = mem_block(a.lse, a.B * a.X * a.H * Lq * 4), none = {};
+  const int64_t table = (int64_t)a.n_buckets * a.H * es;
+  const Mem bias = mem_block(a.bias, table), buckets = mem_block(a.buckets, (2 * (int64_t)a.max_dist + 1) * 4);
+  const Mem q_pos = mem_block(a.q_pos, a.B * 4), kv_len = mem_block(a.kv_len, a.B * 4);
+  const Mem fwd_in[] = {q, k, v, bias, buckets, q_pos, kv_len, none, none, none};
+  const Mem bwd_in[] = {q, k, v, bias, buckets, q_pos, kv_len, o, dout, lse};
+  const Mem fwd_out[] = {o, lse, none, none}, bwd_out[] = {dq, dk, dv, mem_block(a.dbias, table)};
+  const auto& in = bwd ? bwd_in : fwd_in;
+  const auto& out = bwd ? bwd_out : fwd_out;
+  auto clear = [&](const Mem& m, int others) {
+    for (const Mem& i : in)
+      if (!apart(m, i, a.B, a.X, es)) return false;
+    for (int j = 0; j < others; ++j)
+      if (!apart(m, out[j], a.B, a.X, es)) return false;
+    return true;
+  };
+  for (int i = 0; i < 4; ++i)
+    if (!clear(out[i], i)) return DSP_ERR_ARG;
   const size_t need = bwd ? attn_relpos_bwd_workspace_bytes(a) : attn_relpos_workspace_bytes(a);
   if (need && (!workspace || ws_bytes < need || !aligned(workspace, 16))) return DSP_ERR_WORKSPACE;
+  if (need && !clear(mem_block(workspace, (int64_t)need), 4)) return DSP_ERR_ARG;
   a.workspace = static_cast<float*>(workspace);
   a.scale = scale > 0.0f ? scale : (float)(1.0 / sqrt((double)a.D));
   a.causal = flags & DSP_RELPOS_CAUSAL;
