@@ -344,6 +344,8 @@ int dsp_attn_general_bwd(const void* q, const void* k, const void* v, const void
  *   dgq, dgk: fp32 [D], or NULL.  workspace: at least
  *   dsp_qk_norm_rope_bwd_workspace_bytes(B, X, L, H, Hkv, D) bytes, 16-byte
  *   aligned, needed when dgq or dgk is given.  Deterministic.
+ * Outputs and the workspace lie apart from gains, tables and positions too, and from one
+ * another (DSP_ERR_ARG); gaps between rows are free.
  * Errors: DSP_ERR_NULL, DSP_ERR_SHAPE (a size < 0, D outside 1 .. 256, no heads,
  *   rot odd or past D, P < 1 or (pos NULL) P < L with rot > 0, 2^31 rows of
  *   B X L heads or more), DSP_ERR_DTYPE, DSP_ERR_ALIGN (off an element),

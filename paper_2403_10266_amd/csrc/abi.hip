@@ -414,25 +414,35 @@ int qk_norm_impl(QkNormArgs& a, bool bwd, int flags, int H, int Hkv, const int64
   if (!tokens) return gains ? launch_qk_norm(a, bwd, nullptr, s) : DSP_OK;  // no rows: dg is a sum of nothing
   if (a.rot && (!a.cos || !a.sin)) return DSP_ERR_NULL;
   if (!aligned(a.cos, 4) || !aligned(a.sin, 4) || !aligned(a.pos, 4)) return DSP_ERR_ALIGN;
-  for (int i = 0; i < 2; ++i) {  // an output is apart from everything else, or in place of its own input
+  // An output is apart from everything else, or in place of its own input.
+  Mem in[9], out[4];
+  for (int i = 0; i < 2; ++i) {
     const QkNormSide& d = a.side[i];
-    if (!heads[i]) continue;
-    const int64_t w = (int64_t)heads[i] * a.D;
-    for (int j = 0; j < 2; ++j) {
-      const QkNormSide& o = a.side[j];
-      if (!heads[j]) continue;
-      const int64_t ow = (int64_t)heads[j] * a.D;
-      auto clear = [&](const void* ptr, const int64_t* st) {
-        return (i == j && same_rows(d.y, d.y_strides, ptr, st, a.B, a.X, a.L)) ||
-               rows_apart(d.y, d.y_strides, w, a.L, ptr, st, ow, a.L, a.B, a.X, es);
-      };
-      if (!clear(o.x, o.x_strides) || (bwd && !clear(o.dy, o.dy_strides))) return DSP_ERR_ARG;
-      if (i != j && !rows_apart(d.y, d.y_strides, w, a.L, o.y, o.y_strides, ow, a.L, a.B, a.X, es)) return DSP_ERR_ARG;
-    }
+    const int64_t w = heads[i] ? (int64_t)heads[i] * a.D : 0, gain = heads[i] ? a.D : 0;
+    in[i] = {d.x, d.x_strides, w, a.L};
+    in[2 + i] = {d.dy, d.dy_strides, bwd ? w : 0, a.L};
+    in[4 + i] = mem_block(d.gain, gain * es);
+    out[i] = {d.y, d.y_strides, w, a.L};
+    out[2 + i] = mem_block(d.dgain, gain * 4);
   }
+  in[6] = mem_block(a.cos, a.rot ? a.P * a.rot / 2 * 4 : 0);
+  in[7] = mem_block(a.sin, a.rot ? a.P * a.rot / 2 * 4 : 0);
+  in[8] = mem_block(a.pos, a.rot ? a.B * a.L * 4 : 0);
+  auto clear = [&](const Mem& m, int i, int others) {
+    for (int j = 0; j < 9; ++j) {
+      const bool own = i < 2 && j < 4 && j % 2 == i && same_rows(m.p, m.st, in[j].p, in[j].st, a.B, a.X, a.L);
+      if (!own && !apart(m, in[j], a.B, a.X, es)) return false;
+    }
+    for (int j = 0; j < others; ++j)
+      if (!apart(m, out[j], a.B, a.X, es)) return false;
+    return true;
+  };
+  for (int i = 0; i < 4; ++i)
+    if (!clear(out[i], i, i)) return DSP_ERR_ARG;
   if (gains) {
     const size_t need = qk_norm_workspace_bytes(tokens, H, Hkv, a.D);
     if (!workspace || ws_bytes < need || !aligned(workspace, 16)) return DSP_ERR_WORKSPACE;
+    if (!clear(mem_block(workspace, (int64_t)need), 4, 4)) return DSP_ERR_ARG;
   }
   a.half = !(flags & DSP_ROPE_ADJACENT);
   a.bf16 = dtype == DSP_BF16;

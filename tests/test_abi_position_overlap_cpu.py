@@ -3,7 +3,7 @@ refused, without a GPU: every call here fails validation."""
 import pytest
 
 import paper_2403_10266_amd as dsp
-from tests.test_abi_position_cpu import A, BF, F32, _relpos, _st
+from tests.test_abi_position_cpu import A, BF, F32, _norm, _relpos, _st
 
 
 @pytest.fixture(scope="module")
@@ -82,3 +82,41 @@ def test_blocks_beside_rows_that_share_memory(lib):
                            (A[1] + 2 * span, dsp.DSP_ERR_WORKSPACE), (A[1] - 4 * 15, dsp.DSP_ERR_ARG),
                            (A[1] - 4 * 16, dsp.DSP_ERR_WORKSPACE)):      # 2 x 8 floats
             assert _relpos(lib, **kw, lse=at) == status, (span, at - A[1])
+
+
+def test_norm_outputs_over_gains_and_tables(lib):
+    for bwd in (False, True):
+        for n in ("yq", "yk"):
+            for at in (A[4], A[5], A[6], A[7], A[13], A[6] - 64, A[7] + 4 * 5 * 36 - 4):
+                assert _norm(lib, bwd, pos=A[13], **{n: at}) == dsp.DSP_ERR_ARG, (bwd, n, hex(at))
+
+
+def test_norm_gain_gradients_over_something(lib):
+    for n in ("dgq", "dgk"):
+        for at in (A[0], A[1], A[2], A[3], A[4], A[5], A[6], A[7], A[8], A[9], A[13], A[0] - 4 * 71,
+                   A[1] + 2 * (2 * 15 * 144) - 4):
+            assert _norm(lib, True, pos=A[13], **{n: at}) == dsp.DSP_ERR_ARG, (n, hex(at))
+    assert _norm(lib, True, dgk=A[10] + 4 * 71) == dsp.DSP_ERR_ARG
+    assert _norm(lib, True, dgk=A[10] + 4 * 72, ws=None) == dsp.DSP_ERR_WORKSPACE
+
+
+def test_norm_workspace_over_something(lib):
+    need = lib.dsp_qk_norm_rope_bwd_workspace_bytes(2, 3, 5, 4, 2, 72)
+    for at in (*(A[i] for i in range(12)), A[13], A[3] - need + 16):
+        assert _norm(lib, True, pos=A[13], ws=at) == dsp.DSP_ERR_ARG, hex(at)
+
+
+def test_norm_blocks_between_rows(lib):
+    """Gains' gradients in a gap between the rows of q and its gradient are apart."""
+    wide = _st(20000, 6000, 904)
+    gap = A[0] + 2 * (6000 + 904 + 288)
+    for at, status in ((gap, dsp.DSP_ERR_WORKSPACE), (gap - 4, dsp.DSP_ERR_ARG), (gap + 2 * 616 - 288, dsp.DSP_ERR_WORKSPACE),
+                       (gap + 2 * 616 - 284, dsp.DSP_ERR_ARG)):
+        assert _norm(lib, True, qs=wide, dgq=at, ws=None) == status, at - gap
+
+
+def test_norm_without_rotation_or_a_side(lib):
+    """Tables without rotation, and an absent side's arguments, are not looked at."""
+    assert _norm(lib, True, rot=0, dgq=A[6], ws=None) == dsp.DSP_ERR_WORKSPACE
+    assert _norm(lib, True, Hkv=0, dgq=A[5], ws=None) == dsp.DSP_ERR_WORKSPACE
+    assert _norm(lib, True, H=0, dgk=A[4], ws=None) == dsp.DSP_ERR_WORKSPACE
