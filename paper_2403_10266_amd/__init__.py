@@ -731,11 +731,36 @@ def dsp_attn_relpos(q, k, v, H: int, Hkv: int, bias, buckets, causal: bool = Fal
     return (out, lse) if lse is not None else out
 
 
+def _relpos_grads(w, q, k, v, dq, dk, dv):
+    """The gradients given, and new ones laid out like their inputs for the others; for
+    columns of packed rows ([Q | K | V]) without any, the columns of one new buffer."""
+    torch = _torch()
+    ins, grads = (q, k, v), [dq, dk, dv]
+    for i, (name, t) in enumerate(zip("qkv", ins)):
+        if grads[i] is None:
+            if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+                raise ValueError(f"{w}: {name} broadcasts, so its rows have no gradient of their own; pass a copy")
+            if t.is_contiguous():
+                grads[i] = torch.empty_like(t)
+    if all(g is None for g in grads) and q.shape[:3] == k.shape[:3] and q.stride() == k.stride() \
+            and len({t.untyped_storage().data_ptr() for t in ins}) == 1:
+        pitch = min((s for n, s in zip(q.shape[:3], q.stride()) if n > 1), default=0)
+        first = min(t.storage_offset() for t in ins)
+        cols = [(t.storage_offset() - first, t.storage_offset() - first + t.shape[3]) for t in ins]
+        order = sorted(cols)
+        if order[2][1] <= pitch and all(a[1] <= b[0] for a, b in zip(order, order[1:])):
+            row = torch.empty_strided((*q.shape[:3], order[2][1]), q.stride(), dtype=q.dtype, device=q.device)
+            return [row[..., a:b] for a, b in cols]
+    return [torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device) if g is None else g
+            for t, g in zip(ins, grads)]
+
+
 def dsp_attn_relpos_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, bias, buckets, causal: bool = False, q_pos=None,
                         kv_len=None, dq=None, dk=None, dv=None, dbias=None, scale: float = 0.0, workspace=None,
                         stream=None):
     """Gradients of dsp_attn_relpos, given its o and lse and the gradient dout (o's
-    strides): (dq like q, dk and dv like k and v, dbias like bias)."""
+    strides): (dq like q, dk and dv like k and v, dbias like bias), each with its input's
+    strides.  New ones for columns of a packed projection are columns of one buffer."""
     torch = _torch()
     w = "dsp_attn_relpos_bwd"
     B, X, Lq, Lk, C, D = _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len)
@@ -745,9 +770,7 @@ def dsp_attn_relpos_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, bias, buckets, 
         raise ValueError(f"{w}: dout must have the strides of o")
     _check(w, "lse", lse, dtype=torch.float32, numel=B * X * H * Lq, like=q)
     with _on_device(q, stream) as s:
-        dq = torch.empty_like(q) if dq is None else dq
-        dk = torch.empty_like(k) if dk is None else dk
-        dv = torch.empty_like(v) if dv is None else dv
+        dq, dk, dv = _relpos_grads(w, q, k, v, dq, dk, dv)
         _check(w, "dq", dq, dtype=q.dtype, shape=q.shape, strides=q.stride(), contiguous=False, like=q)
         _check(w, "dk", dk, dtype=q.dtype, shape=k.shape, strides=k.stride(), contiguous=False, like=q)
         _check(w, "dv", dv, dtype=q.dtype, shape=k.shape, strides=k.stride(), contiguous=False, like=q)
