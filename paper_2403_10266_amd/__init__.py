@@ -594,16 +594,22 @@ def dsp_layernorm(x, eps: float = 1e-6, out=None, out_dtype=None, stream=None):
     return out
 
 
+def _same_layout(a, b) -> bool:
+    """Whether a and b, of one shape, have the same strides where a dimension has more than
+    one element (the others' say nothing)."""
+    return a.stride() == b.stride() or a.numel() == 0 or all(
+        n < 2 or s == t for n, s, t in zip(a.shape, a.stride(), b.stride()))
+
+
 def _st3(t):
     return (ctypes.c_int64 * 3)(*t.stride()[:3])
 
 
-def _general_views(w, q, k, v, H, Hkv):
+def _general_views(w, q, k, v, H, Hkv, same=lambda a, b: a.stride() == b.stride()):
     for name, t in (("q", q), ("k", k), ("v", v)):
         _check(w, name, t, contiguous=False, like=q, dtype=q.dtype)
     _float_dtype(w, q)
-    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or q.stride(3) != 1 \
-            or k.stride(3) != 1:
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape or not same(k, v) or q.stride(3) != 1 or k.stride(3) != 1:
         raise ValueError(f"{w}: q [B, X, Lq, C] and k, v [B, X, Lk, Ckv] views of one layout")
     B, X, Lq, C = q.shape
     if H < 1 or Hkv < 1 or C % H or tuple(k.shape[:2]) != (B, X):
@@ -677,7 +683,7 @@ def dsp_relpos_buckets(max_dist: int, n_buckets: int, bidirectional: bool = True
 
 def _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len):
     torch = _torch()
-    dims = _general_views(w, q, k, v, H, Hkv)
+    dims = _general_views(w, q, k, v, H, Hkv, _same_layout)
     dev = q.get_device()
     if not (_as(bias, q.dtype, (bias.shape[0] if bias is not None and bias.dim() else 0, H), dev)
             and bias.shape[0] > 0 and bias.is_contiguous()):
@@ -742,7 +748,7 @@ def _relpos_grads(w, q, k, v, dq, dk, dv):
                 raise ValueError(f"{w}: {name} broadcasts, so its rows have no gradient of their own; pass a copy")
             if t.is_contiguous():
                 grads[i] = torch.empty_like(t)
-    if all(g is None for g in grads) and q.shape[:3] == k.shape[:3] and q.stride() == k.stride() \
+    if all(g is None for g in grads) and q.shape[:3] == k.shape[:3] and _same_layout(q[..., :1], k[..., :1]) \
             and len({t.untyped_storage().data_ptr() for t in ins}) == 1:
         pitch = min((s for n, s in zip(q.shape[:3], q.stride()) if n > 1), default=0)
         first = min(t.storage_offset() for t in ins)
@@ -766,14 +772,15 @@ def dsp_attn_relpos_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, bias, buckets, 
     B, X, Lq, Lk, C, D = _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len)
     _like_view(w, o, q, "o")
     _like_view(w, dout, q, "dout")
-    if dout.stride() != o.stride():
+    if not _same_layout(dout, o):
         raise ValueError(f"{w}: dout must have the strides of o")
     _check(w, "lse", lse, dtype=torch.float32, numel=B * X * H * Lq, like=q)
     with _on_device(q, stream) as s:
         dq, dk, dv = _relpos_grads(w, q, k, v, dq, dk, dv)
-        _check(w, "dq", dq, dtype=q.dtype, shape=q.shape, strides=q.stride(), contiguous=False, like=q)
-        _check(w, "dk", dk, dtype=q.dtype, shape=k.shape, strides=k.stride(), contiguous=False, like=q)
-        _check(w, "dv", dv, dtype=q.dtype, shape=k.shape, strides=k.stride(), contiguous=False, like=q)
+        for name, g, x in (("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+            _check(w, name, g, dtype=q.dtype, shape=x.shape, contiguous=False, like=q)
+            if not _same_layout(g, x):
+                raise ValueError(f"{w}: {name} must have the strides of its input, {x.stride()}, got {g.stride()}")
         dbias = torch.empty_like(bias) if dbias is None else dbias
         _check(w, "dbias", dbias, dtype=q.dtype, shape=bias.shape, like=q)
         dt, M = _dtype_code(q), buckets.numel() // 2

@@ -89,3 +89,24 @@ def test_broadcast_inputs_have_no_gradient(torch):
     for args, name in (((one(q), k, v), "q"), ((q, one(k), one(v)), "k")):
         with pytest.raises(ValueError, match=f"{name} broadcasts"):
             _both(torch, c, *args, lambda o: dev(c["do"], "bf16"))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,X,L", [(1, 3, 45), (2, 1, 45), (1, 1, 70), (1, 1, 1)])
+def test_strides_of_single_elements_say_nothing(torch, dtype, B, X, L):
+    """v, dout and the gradients with other strides in dimensions of one element than k,
+    o and the inputs."""
+    c = _case(torch, dtype, B=B, X=X, L=L, seed=3)
+
+    def odd(t):
+        st = [s if n > 1 else 8 * (i + 3) * t.shape[3] for i, (n, s) in enumerate(zip(t.shape[:3], t.stride()))]
+        return torch.empty(t.numel(), dtype=t.dtype, device="cuda").as_strided(t.shape, (*st, 1)).copy_(t)
+
+    q, k, v, do = (dev(c[n], dtype) for n in ("q", "k", "v", "do"))
+    for a, b, d, g in ((k, odd(v), do, None), (k, v, odd(do), None), (k, v, do, odd), (odd(k), odd(v), odd(do), odd)):
+        kw = {} if g is None else dict(dq=g(q), dk=g(k), dv=g(v))
+        _held(c, _both(torch, c, q, a, b, lambda o: d, **kw), dtype)
+    with pytest.raises(ValueError, match="strides"):
+        wide = torch.zeros(2, 3, 45, 192, dtype=q.dtype, device="cuda")[..., :96]
+        c = _case(torch, dtype)
+        _both(torch, c, *(dev(c[n], dtype) for n in "qkv"), lambda o: wide)
