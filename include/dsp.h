@@ -372,7 +372,8 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
  *     o_i = softmax over j (s_i) v,
  * on the units, heads and layouts of dsp_attn_general (Hkv key/value heads shared
  * by H / Hkv query heads each, lengths Lq and Lk, any strides, 0 to broadcast keys
- * and values).
+ * and values; k and v have one layout, not one buffer: values may stay in a packed
+ * projection while normalised keys lie in another buffer of its strides).
  * bias:    [n_buckets][H] of dtype.  A value of -1e30 or less (-inf, or the type's
  *          lowest) takes the keys of its distances out.
  * buckets: DEVICE int32 [2 * max_dist + 1], the bucket of each distance

@@ -110,3 +110,41 @@ def test_strides_of_single_elements_say_nothing(torch, dtype, B, X, L):
         wide = torch.zeros(2, 3, 45, 192, dtype=q.dtype, device="cuda")[..., :96]
         c = _case(torch, dtype)
         _both(torch, c, *(dev(c[n], dtype) for n in "qkv"), lambda o: wide)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [45, 150])
+def test_a_training_step_without_copies(torch, dtype, L):
+    """The raw projection [Q | K | V] stays for the norm's gradient: the norm writes into
+    the columns of a second buffer of its layout, the values are read where they are, and
+    the gradients meet in one packed buffer, the norm's in place.  The bits of the step
+    on contiguous copies."""
+    import paper_2403_10266_amd as dsp
+    B, X, H, D = 2, 3, 4, 24
+    C = H * D
+    c = _case(torch, dtype, L=L, seed=5)
+    raw = torch.cat([dev(c[n], dtype) for n in "qkv"], -1)
+    do = dev(c["do"], dtype)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    gq, gk = ((1 + 0.1 * torch.randn(D, generator=g, device="cuda")).to(raw.dtype) for _ in range(2))
+    ang = torch.arange(float(L))[:, None] * 100.0 ** (-torch.arange(D // 2) / 12)
+    norm = dict(gq=gq, gk=gk, cos=ang.cos().cuda(), sin=ang.sin().cuda())
+    bias, bk = dev(c["bias"], dtype), torch.from_numpy(c["buckets"]).cuda()
+
+    rq, rk, v = raw.split(C, dim=-1)
+    q, k, _ = torch.empty_like(raw).split(C, dim=-1)
+    dsp.dsp_qk_norm_rope(rq, rk, H, H, out_q=q, out_k=k, **norm)
+    o, lse = dsp.dsp_attn_relpos(q, k, v, H, H, bias, bk, causal=True, with_lse=True)
+    grad = torch.empty_like(raw)
+    dq, dk, dv = grad.split(C, dim=-1)
+    *_, db = dsp.dsp_attn_relpos_bwd(q, k, v, o, do, lse, H, H, bias, bk, causal=True, dq=dq, dk=dk, dv=dv)
+    _, _, dgq, dgk = dsp.dsp_qk_norm_rope_bwd(rq, rk, dq, dk, H, H, dq=dq, dk=dk, **norm)
+
+    cq, ck, cv = (t.contiguous() for t in (rq, rk, v))
+    yq, yk = dsp.dsp_qk_norm_rope(cq, ck, H, H, **norm)
+    o2, lse2 = dsp.dsp_attn_relpos(yq, yk, cv, H, H, bias, bk, causal=True, with_lse=True)
+    aq, ak, av, db2 = dsp.dsp_attn_relpos_bwd(yq, yk, cv, o2, do, lse2, H, H, bias, bk, causal=True)
+    nq, nk, dgq2, dgk2 = dsp.dsp_qk_norm_rope_bwd(cq, ck, aq, ak, H, H, **norm)
+    torch.cuda.synchronize()
+    for a, b in ((o, o2), (lse, lse2), (dq, nq), (dk, nk), (dv, av), (db, db2), (dgq, dgq2), (dgk, dgk2)):
+        assert torch.equal(a, b)
