@@ -209,13 +209,13 @@ __device__ __forceinline__ void store_rows(const ColAcc<T, DC>& a, int lane, int
 
 // The same through LDS: `so` holds 32 rows of pitch P for this wave alone, and the rows
 // leave as whole 16-byte chunks, consecutive lanes along a row (from the accumulators
-// a store would write 8 or 16 bytes of 32 rows each).  Columns past D stay as they are:
-// where `so` is a tile's rows they are its padding, cleared once, and a sum there is not 0
-// but NaN where an operand was not finite.
+// a store would write 8 or 16 bytes of 32 rows each).  cols: the columns written there,
+// all (DP) where the rows are done with, D where a later tile takes them: past D lies its
+// padding, cleared once, and a sum there is not 0 but NaN where an operand was not finite.
 template <typename T, int DC, typename F>
-__device__ __forceinline__ void store_rows_lds(T* so, const ColAcc<T, DC>& a, int lane, int D, F row_of) {
+__device__ __forceinline__ void store_rows_lds(T* so, const ColAcc<T, DC>& a, int lane, int D, int cols, F row_of) {
   using G = Geo<T, DC>;
-  store_rows<T, DC>(a, lane, D, true, [&](int n) { return so + n * G::P; });
+  store_rows<T, DC>(a, lane, cols, true, [&](int n) { return so + n * G::P; });
   const int ch = D / G::E;   // whole chunks: the callers' rows are aligned
   int row = lane / ch, col = lane - row * ch;
   const int dr = 64 / ch, dc = 64 - dr * ch;

@@ -337,7 +337,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_fwd_kernel(FwdParams p) 
     sm.o[j].scale(no_keys(l) ? 0.0f : 1.0f / l, lane);
     const uint32_t c0 = 32 * (wave * QT + j);
     auto row = [&](int n) -> T* { return c0 + n < nq ? og + (int64_t)(qb * QB + c0 + n) * p.os[2] : nullptr; };
-    if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, sm.o[j], lane, D, row);
+    if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, sm.o[j], lane, D, G::DP, row);
     else store_rows<T, DC>(sm.o[j], lane, D, false, row);
     if (p.lse && g == 0 && c0 + l32 < nq)
       p.lse[((uint64_t)bx * p.H + h) * p.Lq + qb * QB + c0 + l32] = no_keys(l) ? -INFINITY : kLn2 * (sm.ref[j] + log2f(l));
@@ -455,7 +455,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_few_kernel(FwdParams p) 
       const uint32_t hh = (uint32_t)n / p.Lq;
       return (uint32_t)n < p.cols ? og + at_row(hh, n - hh * p.Lq, p.os[2]) : nullptr;
     };
-    if (p.vec) store_rows_lds<T, DC>(vl, sm.o[0], lane, D, row);
+    if (p.vec) store_rows_lds<T, DC>(vl, sm.o[0], lane, D, G::DP, row);
     else store_rows<T, DC>(sm.o[0], lane, D, false, row);
     if (p.lse && g == 0 && (uint32_t)l32 < p.cols)
       p.lse[((uint64_t)bx * p.H + h0 + ch) * p.Lq + cq] = no_keys(l) ? -INFINITY : kLn2 * (sm.ref[0] + log2f(l));

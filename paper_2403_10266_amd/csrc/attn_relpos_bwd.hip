@@ -329,7 +329,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void relpos_bwd_dq_kernel(BwdParams 
       const uint32_t r = blk * QB + 32 * wave + n;
       return r < p.Lq ? out + (int64_t)r * p.qs[2] : nullptr;
     };
-    if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, dq, lane, D, q_out);   // this wave's rows of the tiles
+    if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, dq, lane, D, D, q_out);   // this wave's rows of the tiles
     else store_rows<T, DC>(dq, lane, D, false, q_out);
   }
 
@@ -499,8 +499,8 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void relpos_bwd_dkv_kernel(BwdP
       T* so = lds + wave * 32 * G::P;   // the tiles are done with
       static_assert(KW * 32 <= 4 * QB, "rows to write through");
       __syncthreads();
-      store_rows_lds<T, DC>(so, dk, lane, D, [&](int n) { return row(out[0], n); });
-      store_rows_lds<T, DC>(so, dv, lane, D, [&](int n) { return row(out[1], n); });
+      store_rows_lds<T, DC>(so, dk, lane, D, G::DP, [&](int n) { return row(out[0], n); });
+      store_rows_lds<T, DC>(so, dv, lane, D, G::DP, [&](int n) { return row(out[1], n); });
     } else {
       store_rows<T, DC>(dk, lane, D, false, [&](int n) { return row(out[0], n); });
       store_rows<T, DC>(dv, lane, D, false, [&](int n) { return row(out[1], n); });
@@ -583,8 +583,8 @@ __device__ __forceinline__ void short_store(const BwdParams& p, T* kl, T* vl, in
     };
   };
   if (p.vec) {
-    store_rows_lds<T, DC>(kl + 32 * wave * G::P, dk, lane, D, out(p.dk));
-    store_rows_lds<T, DC>(vl + 32 * wave * G::P, dv, lane, D, out(p.dv));
+    store_rows_lds<T, DC>(kl + 32 * wave * G::P, dk, lane, D, D, out(p.dk));
+    store_rows_lds<T, DC>(vl + 32 * wave * G::P, dv, lane, D, D, out(p.dv));
   } else {
     store_rows<T, DC>(dk, lane, D, false, out(p.dk));
     store_rows<T, DC>(dv, lane, D, false, out(p.dv));
@@ -781,7 +781,7 @@ __global__ __launch_bounds__(NB * 64, MINW) void relpos_bwd_short_kernel(BwdPara
       const uint32_t r = 32 * wave + n;
       return r < p.Lq ? static_cast<T*>(p.dq) + q_at + (int64_t)r * p.qs[2] : nullptr;
     };
-    if (p.vec) store_rows_lds<T, DC>(kl + 32 * wave * G::P, dq, lane, D, q_out);
+    if (p.vec) store_rows_lds<T, DC>(kl + 32 * wave * G::P, dq, lane, D, D, q_out);
     else store_rows<T, DC>(dq, lane, D, false, q_out);
     if constexpr (OWN) {
       ColAcc<T, DC> dk, dv;
