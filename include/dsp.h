@@ -340,7 +340,9 @@ int dsp_attn_general_bwd(const void* q, const void* k, const void* v, const void
  * dsp_qk_norm_rope_bwd -- its gradient: with dn the turn back of dy and w = g dn,
  *     dg = sum over tokens and heads of dn * u * r,  r = 1/sqrt(mean(u^2) + eps),
  *     du = r (w - u r^2 mean(w u)).
- *   dq and dk may be in place of dyq and dyk, or of q and k (equal strides).
+ *   dq and dk may be in place of dyq and dyk, or of q and k (equal strides).  A token
+ *   whose position has no row makes its rows of them and the sums dg NaN, whatever its dy:
+ *   padding takes any row of the table.
  *   dgq, dgk: fp32 [D], or NULL.  workspace: at least
  *   dsp_qk_norm_rope_bwd_workspace_bytes(B, X, L, H, Hkv, D) bytes, 16-byte
  *   aligned, needed when dgq or dgk is given.  Deterministic.
@@ -387,6 +389,7 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
  *          or NULL (Lk).  Keys and values past it are never used, whatever they
  *          hold; the others must be finite.
  * flags:   DSP_RELPOS_CAUSAL keeps the keys j <= i + q_pos only.
+ * scale:   softmax scale; scale <= 0 selects 1/sqrt(D).
  * A query without keys (kv_len 0, or none before it) gives o = 0 and lse = -inf.  A
  * query that is not finite makes its own row of o and its lse NaN; a unit's gradients
  * are NaN where a query or a row of dout of theirs is not finite, no other unit's.
@@ -402,7 +405,8 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
  *
  * dsp_attn_relpos_bwd -- the gradients dq, dk, dv (strides of q and k) and
  * dbias [n_buckets][H] of dtype, from the forward's o and lse and from dout (o's
- * strides).  Deterministic: no sum depends on timing.  Rows of dk and dv past kv_len
+ * strides; DSP_BF16 takes o's address but none of its values).  Deterministic: no sum
+ * depends on timing.  Rows of dk and dv past kv_len
  * are 0, as is dbias where bias masks.  workspace:
  * dsp_attn_relpos_bwd_workspace_bytes(...) bytes, 16-byte aligned.  dq, dk and dv
  * may be columns of one buffer; broadcast keys are DSP_ERR_ARG.

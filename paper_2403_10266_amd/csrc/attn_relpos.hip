@@ -23,12 +23,14 @@
 // key/value head's group share one block of 32 columns, and the keys are cut among
 // work-groups, whose unnormalised sums a second kernel joins.
 //
-// Measured in bf16, 16 heads of 72: 8 x 16 units of 4096 760-890 us (813-695 TFLOP/s;
-// bound by the matrix cores, busy 38%, and the exponentials and conversions beside
-// them); 1350 x 16 units of 49 158 us (5.2 TB/s, memory); 1024 x 16 units of 32 66-71 us
-// (4.3-4.6 TB/s, memory); a token against 4 caches of up to 50000 keys of 8 heads of 64
-// 38 us and 4 for the join (5.3 TB/s while it reads), against 2048 caches of up to 120
-// keys 51 us (4.8 TB/s).
+// Measured in bf16, 16 heads of 72: 8 x 16 units of 4096 750-860 us with the box's clock
+// (825-720 TFLOP/s): the matrix cores are busy 38%, the vector units 30%, waits take 30%;
+// whether the reference moves is asked between a tile's exponentials and its second
+// product, so none of the one runs under the other.  The plain attention, which multiplies
+// first and corrects afterwards, takes 600-640 us.  1350 x 16 units of 49: 159-175 us (3.8-3.5
+// TB/s; the plain attention 120); 1024 x 16 units of 32 66-71 us (4.3-4.6 TB/s, memory); a
+// token against 4 caches of up to 50000 keys of 8 heads of 64 38 us and 4 for the join (5.3
+// TB/s while it reads), against 2048 caches of up to 120 keys 50 us (4.9 TB/s).
 #include <algorithm>
 #include <type_traits>
 

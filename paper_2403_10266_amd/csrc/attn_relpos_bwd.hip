@@ -21,12 +21,13 @@
 // from P and dP; only in fp32 and for units past 64 positions from the stored o.
 //
 // Measured in bf16: 32 heads of 64 over 8, 4 causal sequences of 2000, 1334, 667 and 0:
-// dQ 193 us, dK and dV 227, dbias 6 (bound by a wave's chain of product, exponential and
-// product, with two or three waves to a SIMD, the matrix cores busy 25-30%, and by causal
-// blocks of unequal length); 8 x 16 units of 4096 x 72 4.1-4.3 ms in all (370 TFLOP/s of the
-// gradient's 5 products);
-// 1350 x 16 units of 49 x 72 387 us (4.0 TB/s: memory, and the waits between a unit's
-// loads, its two passes and its stores).
+// dQ 189 us, dK and dV 215, dbias 6 (bound by a wave's chain of product, exponential and
+// product, with two or three waves to a SIMD, the matrix cores busy 25-27%, waits 48%, and by
+// causal blocks of unequal length); 8 x 16 units of 4096 x 72 4.1-4.3 ms in all (370 TFLOP/s
+// of the gradient's 5 products; the plain gradient 2.3 ms); 1350 x 16 units of 49 x 72
+// 367-390 us: seven passes over rows, 1.07 GB (by the counters 1.16), 2.7-2.9 TB/s, so not
+// memory but a unit's chain of loads, two passes and stores, with three work-groups to a CU
+// and nothing of the next unit on its way (waits 46%).
 #include <algorithm>
 #include <type_traits>
 
@@ -880,8 +881,8 @@ constexpr int kDqWaves = 4;   // of a work-group of the dQ kernel, 32 queries ea
 // LDS of the short-unit kernel, and the blocks of 32 it takes the call with (0: not at
 // all): at most 64 queries and keys (fp32 up to 64 wide: a wider one's rows and sums do
 // not fit the registers); where heads share keys, tables of a group of 32 KB at most.
-// Against the kernels for long units: 1350 x 16 units of 49 x 72 403 us and 1227 in all;
-// heads that share keys, 2000 x 16 over 4 of 49 x 72, 472 and 1326.
+// Against the kernels for long units: 1350 x 16 units of 49 x 72 367-406 us and 1303 in all;
+// heads that share keys, 2000 x 16 over 4 of 49 x 72, 467 and 1404.
 size_t short_lds(const RelposArgs& a, int nb, int row_bytes) {
   const size_t n_tab = 2 * ((size_t)a.max_dist + kEdge) + 1;
   return (size_t)4 * 32 * nb * row_bytes + (size_t)2 * 32 * nb * 4 + (n_tab * (1 + nb) + 2 * 64 * nb) * 4;
@@ -955,11 +956,12 @@ int start_short(BwdParams& p, const RelposArgs& a, hipStream_t s) {
 
 template <typename T, int DC, int NW>
 int start_dq(BwdParams& p, const RelposArgs& a, hipStream_t s) {
-  // 32 keys a tile and registers for two waves per SIMD against 64 keys (the whole
-  // gradient, without the first pass): 32 heads of 2000 x 64 causal 323 and 354 us, heads
-  // of 128 481 and 600, 8 x 16 units of 4096 x 72 3171 and 3153; fp32 up to 96 columns is
-  // faster with two waves and some spills as well, 500 x 72 447 and 484.  Three waves for
-  // bf16 up to 64 columns (with the first pass): 388 and 413 for the first of these.
+  // 32 keys a tile and registers for two waves per SIMD against 64 keys, the whole
+  // gradient: 32 heads of 2000 x 128 causal 787 and 1308 us, 16 of 72 321 and 314, 8 x 16
+  // units of 4096 x 72 4200 and 4150.  Three waves for bf16 up to 64 columns: 32 heads of
+  // 2000 x 64 causal 388 with 32 keys, 557 with 64, and 410 with two waves and either.  fp32
+  // up to 96 columns with two waves and some spills is within 10% of one wave either way: 8 x
+  // 16 units of 700 x 64 639 and 694, of 300 x 96 314 and 330, of 700 x 72 1020 and 938.
   constexpr int KB = 32, MINW = sizeof(T) == 2 && DC <= 64 ? 3 : sizeof(T) == 2 || DC <= 96 ? 2 : 1;
   const size_t n_tab = 2 * ((size_t)p.bias.M + kEdge) + 1;
   p.n_blk = (uint32_t)((a.Lq + 32 * NW - 1) / (32 * NW));
@@ -993,11 +995,12 @@ int start(BwdParams& p, const RelposArgs& a, hipStream_t s) {
   if (int st = bias_grad<T>(p, a, s)) return st;
   if (a.Lk == 0) return DSP_OK;
   // The most keys to a work-group that still fill the chip, which holds 256 of eight
-  // waves: once where units are alike, twice where masks or lengths make them differ.
-  // 4 x 2000 tokens, 32 heads of 64 over 8, causal and ragged: gradients (measured with
-  // dQ in one pass) 478, 385 and
-  // 445 us with 8, 4 and 2 blocks of keys; 16 heads of 72 over 4: 484, 349, 273; not
-  // causal, 8 x 16 units of 4096: 3170, 3417, 3940.
+  // waves: once where units are alike, twice where masks or lengths may make them differ
+  // (lengths lie on the device, so any that are given count).  Whole gradients with 8, 4 and
+  // 2 blocks of keys: 4 x 2000 tokens, causal and ragged, 32 heads of 64 over 8 (256, 512 and
+  // 1024 work-groups) 536, 417 and 463 us, 16 of 72 over 4 (half as many) 523, 395 and 323;
+  // 64 units of 200, 16 heads of 72 over 4, not causal (256, 512, 1024) 205, 268 and 256, 16 x
+  // 32 of 400 x 64 (1024 ..) 272, 325 and 373, 8 x 16 of 4096 x 72 4188, 4448 and 4950.
   auto fills = [&](int64_t keys) {
     return a.B * a.X * a.Hkv * ((a.Lk + keys - 1) / keys) >= (a.causal || a.kv_len ? 512 : 256);
   };

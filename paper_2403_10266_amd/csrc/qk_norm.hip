@@ -17,9 +17,9 @@
 // run, pairs (i, i + rot/2) in two runs of 8 bytes, one of each half, so no lane
 // needs another's elements.  A lane keeps its gains in registers and, for the
 // gradient, its share of dg; the lanes' shares are added in a fixed order.
-// Measured: 129600 tokens of 32 + 32 heads of 64 in bf16 410 us (5.2 TB/s, what a copy
-// reaches), 32 x 1024 tokens of 16 + 16 of 72 73 us (4.1 TB/s), gradients of 13600 tokens of
-// those 45 us and 4 for the gains (4.2 TB/s).
+// Measured: 129600 tokens of 32 + 32 heads of 64 in bf16 400-410 us (5.3-5.2 TB/s, what a copy
+// reaches), 32 x 1024 tokens of 16 + 16 of 72 71-73 us (4.3-4.1 TB/s; in fp32 136, 4.4),
+// gradients of 13600 tokens of those 43-45 us and 4 for the gains (4.4-4.2 TB/s).
 // Where the width, the rotation or an offset asks for it, a chunk is 8 or 4 bytes; what
 // has no such chunk either takes a wave per row, element by element.
 #include <hip/hip_runtime.h>
