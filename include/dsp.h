@@ -347,7 +347,7 @@ int dsp_attn_general_bwd(const void* q, const void* k, const void* v, const void
  *   dsp_qk_norm_rope_bwd_workspace_bytes(B, X, L, H, Hkv, D) bytes, 16-byte
  *   aligned, needed when dgq or dgk is given.  Deterministic.
  * Outputs and the workspace lie apart from gains, tables and positions too, and from one
- * another (DSP_ERR_ARG); gaps between rows are free.
+ * another (DSP_ERR_ARG); dgq, dgk and the workspace may lie in gaps between rows.
  * Errors: DSP_ERR_NULL, DSP_ERR_SHAPE (a size < 0, D outside 1 .. 256, no heads,
  *   rot odd or past D, P < 1 or (pos NULL) P < L with rot > 0, 2^31 rows of
  *   B X L heads or more), DSP_ERR_DTYPE, DSP_ERR_ALIGN (off an element),
@@ -411,7 +411,8 @@ int dsp_qk_norm_rope_bwd(const void* q, const void* k, const void* dyq, const vo
  * dsp_attn_relpos_bwd_workspace_bytes(...) bytes, 16-byte aligned.  dq, dk and dv
  * may be columns of one buffer; broadcast keys are DSP_ERR_ARG.
  * In both calls every output, lse, dbias and the workspace among them, lies apart from
- * everything else that the call reads or writes (DSP_ERR_ARG); gaps between rows are free.
+ * everything else that the call reads or writes (DSP_ERR_ARG); lse, dbias and the
+ * workspace may lie in gaps between rows.
  *
  * dsp_relpos_buckets -- fills buckets[2 * max_dist + 1] in HOST memory: with
  * n = n_buckets (bidirectional: half of them for each direction, keys after the

@@ -23,7 +23,7 @@
 // key/value head's group share one block of 32 columns, and the keys are cut among
 // work-groups, whose unnormalised sums a second kernel joins.
 //
-// Measured in bf16, 16 heads of 72: 8 x 16 units of 4096 750-860 us with the box's clock
+// Measured in bf16, 16 heads of 72: 8 x 16 units of 4096 750-860 us with the card's clock
 // (825-720 TFLOP/s): the matrix cores are busy 38%, the vector units 30%, waits take 30%;
 // whether the reference moves is asked between a tile's exponentials and its second
 // product, so none of the one runs under the other.  The plain attention, which multiplies
