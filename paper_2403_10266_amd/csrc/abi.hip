@@ -9,6 +9,7 @@
 #include <mutex>
 #include <utility>
 
+#include "abi_checks.h"
 #include "dsp_internal.h"
 
 using namespace dsp;
@@ -16,23 +17,6 @@ using namespace dsp;
 namespace {
 
 constexpr int kVersion = 1 * 10000 + 0 * 100 + 0;
-
-bool valid_dtype(int dt) { return dt == DSP_F32 || dt == DSP_BF16; }
-int elem_size(int dt) { return dt == DSP_F32 ? 4 : 2; }
-bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
-hipStream_t as_stream(void* s) { return static_cast<hipStream_t>(s); }
-
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-  return na && nb && pa < pb + nb && pb < pa + na;
-}
-
-bool mul_ok(int64_t a, int64_t b, int64_t* out) {
-  if (a < 0 || b < 0) return false;
-  if (a != 0 && b > INT64_MAX / a) return false;
-  *out = a * b;
-  return true;
-}
 
 // Sequence tensors [B, S_1, .., S_K, C] with K = 2 or 3: checks ndim and the
 // sizes, and returns the element count (via *elems) and the row strides of
@@ -124,24 +108,6 @@ int switch_impl(const void* x, void* y, const int64_t* shape, int ndim, int from
   hipStream_t s = as_stream(stream);
   if (use_rows) return launch_switch_rows(x, y, B, D1, D2, row_bytes, from_dim, to_dim, n_chunks, s);
   return launch_switch_tiles(x, y, B, D1, D2, C, elem_size(dtype), from_dim, to_dim, n_chunks, s);
-}
-
-// Rows of a (B, X, L) grid with element strides st = {b, x, l}, each `width`
-// elements wide, do not overlap when, taking the dimensions of extent > 1 by
-// increasing stride, every stride is at least the span of the smaller ones.
-bool rows_disjoint(int64_t B, int64_t X, int64_t L, const int64_t* st, int64_t width) {
-  int64_t e[3] = {B, X, L}, s[3] = {st[0], st[1], st[2]};
-  for (int i = 0; i < 3; ++i)
-    for (int j = i + 1; j < 3; ++j)
-      if (s[j] < s[i]) { std::swap(s[i], s[j]); std::swap(e[i], e[j]); }
-  int64_t span = width;
-  for (int i = 0; i < 3; ++i) {
-    if (e[i] <= 1) continue;
-    if (s[i] < span) return false;
-    if (!mul_ok(s[i], e[i] - 1, &span) || span > INT64_MAX - width) return false;
-    span += width;
-  }
-  return true;
 }
 
 // Attention over general layouts: queries (B, X, Lq) of H heads with q_st,
@@ -293,86 +259,6 @@ int attn_impl(const void* q, const void* k, const void* v, void* o, int64_t B, i
     return DSP_ERR_SHAPE;
   const int64_t in_st[3] = {bl_in, xl_in, ld_in}, out_st[3] = {bl_out, xl_out, ld_out};
   return attn_impl_strided(q, k, v, o, B, X, L, H, D, in_st, out_st, scale, dtype, stream);
-}
-
-// offsets_ok with room to spare: sums of the terms in bytes stay below 2^63
-bool spans_ok(int64_t B, int64_t X, int64_t L, const int64_t* st) {
-  const int64_t n[3] = {B, X, L};
-  for (int i = 0; i < 3; ++i) {
-    int64_t t;
-    if (st[i] < 0 || !mul_ok(n[i] - 1, st[i], &t) || t > (int64_t(1) << 58)) return false;
-  }
-  return true;
-}
-
-// Two row tensors of (B, X, La) and (B, X, Lb) rows share no element: their spans
-// are apart, or they have one grid and layout and lie in different columns of its rows.
-bool rows_apart(const void* a, const int64_t* sa, int64_t wa, int64_t La, const void* b, const int64_t* sb, int64_t wb,
-                int64_t Lb, int64_t B, int64_t X, int es) {
-  auto span = [&](const int64_t* st, int64_t w, int64_t L) {
-    return (size_t)((B - 1) * st[0] + (X - 1) * st[1] + (L - 1) * st[2] + w) * es;
-  };
-  if (!wa || !wb || !La || !Lb || !overlap(a, span(sa, wa, La), b, span(sb, wb, Lb))) return true;
-  if (La != Lb) return false;
-  const int64_t L = La;
-  const int64_t ext[3] = {B, X, L};
-  int64_t pitch = INT64_MAX;
-  for (int i = 0; i < 3; ++i) {
-    if (ext[i] <= 1) continue;
-    if (sa[i] != sb[i] || sa[i] == 0) return false;
-    pitch = sa[i] < pitch ? sa[i] : pitch;
-    for (int j = 0; j < 3; ++j)   // whole pitches: a larger stride starts after the smaller one's rows
-      if (j != i && ext[j] > 1 && sa[j] >= sa[i] && sa[j] / sa[i] < ext[i]) return false;
-  }
-  const int64_t off = ((intptr_t)b - (intptr_t)a) / es;
-  if (((intptr_t)b - (intptr_t)a) % es) return false;
-  return off >= 0 ? off >= wa && off <= pitch - wb : -off >= wb && -off <= pitch - wa;
-}
-bool same_rows(const void* a, const int64_t* sa, const void* b, const int64_t* sb, int64_t B, int64_t X, int64_t L) {
-  const int64_t ext[3] = {B, X, L};
-  for (int i = 0; i < 3; ++i)
-    if (ext[i] > 1 && sa[i] != sb[i]) return false;
-  return a == b;
-}
-
-// A block of n bytes shares none with the rows of (B, X, L): it is apart from their span or
-// lies in one of the gaps between them.  Strides that do not nest leave no gaps to rely on.
-bool block_apart(const void* block, int64_t n, const void* rows, const int64_t* st, int64_t w, int64_t L, int64_t B,
-                 int64_t X, int es) {
-  if (n <= 0 || w <= 0 || L <= 0) return true;
-  int64_t e[3] = {B, X, L}, s[3] = {st[0], st[1], st[2]}, span = w * es;
-  for (int i = 0; i < 3; ++i) {
-    for (int j = i + 1; j < 3; ++j)
-      if (s[j] > s[i]) { std::swap(s[i], s[j]); std::swap(e[i], e[j]); }
-    span += (e[i] - 1) * s[i] * es;
-  }
-  if (!overlap(block, (size_t)n, rows, (size_t)span)) return true;
-  int64_t from = (intptr_t)block - (intptr_t)rows;
-  for (int i = 0; i < 3; ++i) {   // from the largest stride down: which of its pieces the block starts in
-    if (e[i] <= 1) continue;
-    const int64_t step = s[i] * es;
-    span -= (e[i] - 1) * step;    // of one piece
-    if (from < 0 || step < span) return false;
-    const int64_t at = std::min(from / step, e[i] - 1);
-    from -= at * step;
-    if (at < e[i] - 1 && from + n > step) return false;   // it reaches the next piece
-    if (from >= span) return true;
-  }
-  return false;
-}
-
-// What a call reads or writes: rows of the (B, X, L) grid (elements of es bytes), or a block.
-struct Mem {
-  const void* p;
-  const int64_t* st;   // rows: strides; a block: null
-  int64_t w, L;        // rows: their width and number; a block: its bytes
-};
-Mem mem_block(const void* p, int64_t bytes) { return {p, nullptr, p ? bytes : 0, 0}; }
-bool apart(const Mem& a, const Mem& b, int64_t B, int64_t X, int es) {
-  if (a.st && b.st) return rows_apart(a.p, a.st, a.w, a.L, b.p, b.st, b.w, b.L, B, X, es);
-  if (a.st) return block_apart(b.p, b.w, a.p, a.st, a.w, a.L, B, X, es);
-  if (b.st) return block_apart(a.p, a.w, b.p, b.st, b.w, b.L, B, X, es);
-  return !overlap(a.p, (size_t)a.w, b.p, (size_t)b.w);
 }
 
 int qk_norm_impl(QkNormArgs& a, bool bwd, int flags, int H, int Hkv, const int64_t* const (&xs)[2],
