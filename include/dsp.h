@@ -52,7 +52,8 @@ typedef enum {
   DSP_ERR_ARG = 8        /* any other invalid argument (flags, eps, ...) */
 } dsp_status_t;
 
-typedef enum { DSP_F32 = 0, DSP_BF16 = 1 } dsp_dtype_t;
+/* DSP_E4M3: caches of dsp_kv_append and dsp_attn_paged only. */
+typedef enum { DSP_F32 = 0, DSP_BF16 = 1, DSP_E4M3 = 2 } dsp_dtype_t;
 
 /* Human-readable name of a status code (static string, never NULL). */
 const char* dsp_status_str(int status);
@@ -442,6 +443,122 @@ int dsp_attn_relpos_bwd(const void* q, const void* k, const void* v, const void*
                         const int32_t* kv_len, int flags, void* workspace, size_t ws_bytes, int64_t B, int64_t X,
                         int64_t Lq, int64_t Lk, int H, int Hkv, int D, const int64_t* q_strides,
                         const int64_t* kv_strides, const int64_t* o_strides, float scale, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * dsp_attn_window -- attention with a window to either side of a query and first
+ * tokens that stay visible (sinks), on the units, heads and layouts of
+ * dsp_attn_general (any strides, 0 to broadcast keys and values; k and v have one
+ * layout, not one buffer).  The query i of sequence b, at position p = i + q_pos[b],
+ * sees the keys j < kv_len[b] with
+ *     j <= p + right  (right < 0: no bound; 0: causal)  and
+ *     j >= p - left   (left < 0: no bound)  or  j < sinks,
+ * and o_i = softmax over those j (scale * q_i . k_j) v.
+ * q_pos:   DEVICE int32 [B], the key index of each sequence's first query, or NULL (0).
+ * kv_len:  DEVICE int32 [B], the keys that each sequence has, 0 .. Lk (clamped),
+ *          or NULL (Lk).
+ * A query that sees nothing gives o = 0 and lse = -inf.  Keys and values that no query
+ * of their sequence sees are never used, whatever they hold; a key or value that is not
+ * finite may make every query of its unit NaN, and a query that is not finite its own row.
+ * lse:     fp32 [B * X * H][Lq], the row log-sum-exp of the scaled scores, or NULL.
+ * scale:   softmax scale; scale <= 0 selects 1/sqrt(D).
+ * dtype:   DSP_BF16 (fp32 scores, softmax and accumulation; probabilities are rounded to
+ *          bf16 for the product with v), D a multiple of 8 up to 128, 16-byte aligned
+ *          tensors and strides multiples of 8; or DSP_F32, any D up to 128.  Lq and Lk
+ *          below 2^30, Lq * H / Hkv below 2^31, and 64 rows of each tensor within 2^31 bytes.
+ * workspace: dsp_attn_window_workspace_bytes(...) bytes, 16-byte aligned (0 except for a
+ *          few queries against many keys: there the keys are cut among work-groups, whose
+ *          sums are joined).  Calls that may run at once, captured ones among them, have
+ *          workspaces of their own.
+ *
+ * dsp_attn_window_bwd -- the gradients dq, dk, dv (strides of q and k) from the forward's
+ * o and lse and from dout (o's strides).  Deterministic.  Rows of dk and dv that no query
+ * sees are 0, as are rows of dq that see nothing.  workspace:
+ * dsp_attn_window_bwd_workspace_bytes(...) bytes, 16-byte aligned.  dq, dk and dv may be
+ * columns of one buffer; broadcast keys are DSP_ERR_ARG.
+ * In both calls every output and the workspace lies apart from everything else that the
+ * call reads or writes (DSP_ERR_ARG); lse and the workspace may lie in gaps between rows.
+ * Errors: DSP_ERR_NULL, DSP_ERR_SHAPE (sizes < 0 or unsupported, H % Hkv),
+ *   DSP_ERR_DTYPE, DSP_ERR_ALIGN, DSP_ERR_ARG (scale not finite, sinks < 0, overlapping
+ *   outputs), DSP_ERR_WORKSPACE, DSP_ERR_HIP.  An empty input launches nothing and may
+ *   come with NULL pointers (the gradient of no queries writes 0 into dk and dv).
+ * ------------------------------------------------------------------------ */
+size_t dsp_attn_window_workspace_bytes(int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D, int left,
+                                       int right, int sinks, int dtype);
+int dsp_attn_window(const void* q, const void* k, const void* v, void* o, float* lse, const int32_t* q_pos,
+                    const int32_t* kv_len, int left, int right, int sinks, void* workspace, size_t ws_bytes, int64_t B,
+                    int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D, const int64_t* q_strides,
+                    const int64_t* kv_strides, const int64_t* o_strides, float scale, int dtype, void* stream);
+size_t dsp_attn_window_bwd_workspace_bytes(int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D, int left,
+                                           int right, int sinks, int dtype);
+int dsp_attn_window_bwd(const void* q, const void* k, const void* v, const void* o, const void* dout, const float* lse,
+                        void* dq, void* dk, void* dv, const int32_t* q_pos, const int32_t* kv_len, int left, int right,
+                        int sinks, void* workspace, size_t ws_bytes, int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H,
+                        int Hkv, int D, const int64_t* q_strides, const int64_t* kv_strides, const int64_t* o_strides,
+                        float scale, int dtype, void* stream);
+
+/* ------------------------------------------------------------------------
+ * A paged cache of keys and values: n_pages pages of `page` slots (a power of two, 16 ..
+ * 1024), element (page, slot, head h, d) at page*cache_strides[0] + slot*cache_strides[1]
+ * + h*cache_strides[2] + d of k_cache and of v_cache (one layout; the two may interleave
+ * in one buffer).  Position j of sequence n lies in slot j % page of page
+ * table[n][j / page].
+ * table:    DEVICE int32 [N][max_pages].  An entry outside 0 .. n_pages - 1 is no page:
+ *           its keys are not seen and tokens for it are dropped (a page given back, or not
+ *           yet needed).  Nothing outside the caches is read or written.
+ * q_start:  DEVICE int32 [N + 1], rising: rows q_start[n] .. q_start[n + 1] - 1 of the T
+ *           packed rows are sequence n's new tokens.  Values outside 0 .. T are clamped.
+ * kv_len:   DEVICE int32 [N], the positions of each sequence, the new tokens being the
+ *           last of them: its row i is position kv_len[n] - (q_start[n+1] - q_start[n]) + i.
+ * cache_dtype: dtype, or DSP_E4M3 where dtype is DSP_BF16: 8-bit codes (3 bits of mantissa,
+ *           4 of exponent, no infinity) times k_scale[page][h] and v_scale[page][h] (DEVICE
+ *           fp32 [n_pages][Hkv], powers of two; NULL otherwise).
+ *
+ * dsp_kv_append -- writes the new keys and values (k, v: T rows of Hkv heads, k_stride and
+ * v_stride elements apart) into the cache, the first `rot` elements of each key turned by
+ * its position as in dsp_qk_norm_rope (cos, sin, P, rot, flags; pos: DEVICE int32 [T], the
+ * table's row of each token, or NULL: its position; a position without a row gives NaN in
+ * the elements that turn), and, for H > 0, the queries q turned the same way into yq (T
+ * rows; in place allowed with equal strides).
+ *   DSP_E4M3: a page's scale for a head is the least power of two s, at least 2^-64, with
+ *   |x| <= 448 s for every token that the page was given since its slot 0 was written;
+ *   where new tokens make it grow, the slots before them are rounded again.  Elements that
+ *   are not finite are held as NaN and do not count.  A page whose slot 0 is not among the
+ *   new tokens must hold what earlier calls wrote (or scale 0: nothing).
+ *   Slots other than the new tokens' (8 bits: and those before them in the page) and rows of
+ *   no sequence are left as they were.  A page that is written belongs to one sequence.
+ *   D up to 256 at any alignment of an element; 16-byte aligned tensors and tables, with
+ *   D and rot multiples of 8, are fastest.
+ *
+ * dsp_attn_paged -- attention of the new tokens (q, o: T rows of H heads, q_stride and
+ * o_stride elements apart) over their sequences' cached positions, with the visibility,
+ * scale and precision of dsp_attn_window (left -1, right 0: causal without a window).
+ * max_q:    no sequence has more new tokens (rows past it are left as they were); with
+ *           max_q * H / Hkv <= 32 the keys are cut among work-groups.
+ * lse:      fp32 [T][H], or NULL.
+ * Rows of no sequence are left as they were.  DSP_BF16: D a multiple of 8 up to 128,
+ * 16-byte aligned q and o and bf16 caches (8-byte for DSP_E4M3) with strides multiples of 8;
+ * DSP_F32: any D up to 128.  workspace: dsp_attn_paged_workspace_bytes(...) bytes,
+ * 16-byte aligned, of each call's own.
+ *
+ * Outputs lie apart from everything that the call reads and from one another (DSP_ERR_ARG;
+ * the caches: from first element to last).  N <= 2^20, T * H and max_pages * page below
+ * 2^30, 64 slots of a page within 2^31 bytes.
+ * Errors: DSP_ERR_NULL, DSP_ERR_SHAPE, DSP_ERR_DTYPE, DSP_ERR_ALIGN, DSP_ERR_ARG,
+ *   DSP_ERR_WORKSPACE, DSP_ERR_HIP.  No sequences or no rows launch nothing.
+ * ------------------------------------------------------------------------ */
+int dsp_kv_append(const void* k, const void* v, const void* q, void* yq, void* k_cache, void* v_cache, float* k_scale,
+                  float* v_scale, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, const float* cos,
+                  const float* sin, const int32_t* pos, int64_t P, int rot, int flags, int64_t N, int64_t T,
+                  int64_t n_pages, int64_t max_pages, int page, int H, int Hkv, int D, int64_t k_stride, int64_t v_stride,
+                  int64_t q_stride, int64_t yq_stride, const int64_t* cache_strides, int cache_dtype, int dtype,
+                  void* stream);
+size_t dsp_attn_paged_workspace_bytes(int64_t N, int64_t T, int64_t max_q, int64_t n_pages, int64_t max_pages, int page,
+                                      int H, int Hkv, int D, int left, int right, int sinks, int dtype);
+int dsp_attn_paged(const void* q, const void* k_cache, const void* v_cache, void* o, float* lse, const float* k_scale,
+                   const float* v_scale, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, int left,
+                   int right, int sinks, void* workspace, size_t ws_bytes, int64_t N, int64_t T, int64_t max_q,
+                   int64_t n_pages, int64_t max_pages, int page, int H, int Hkv, int D, int64_t q_stride,
+                   const int64_t* cache_strides, int64_t o_stride, float scale, int cache_dtype, int dtype, void* stream);
 
 /* ------------------------------------------------------------------------
  * dsp_layernorm -- per-row normalisation over C (Eq. 4, 6):

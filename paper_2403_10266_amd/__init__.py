@@ -11,7 +11,7 @@ binding's functions raises.
 Entry points (see ``include/dsp.h`` for the exact contracts):
 ``dsp_switch``, ``dsp_exchange_unpack``, ``dsp_split``, ``dsp_gather``,
 ``dsp_spatial_attn``, ``dsp_temporal_attn``, ``dsp_attn_strided``,
-``dsp_attn_fwd_lse``, ``dsp_attn_bwd``, ``dsp_attn_general``, ``dsp_attn_general_bwd``, ``dsp_attn_relpos``, ``dsp_attn_relpos_bwd``, ``dsp_relpos_buckets``, ``dsp_qk_norm_rope``, ``dsp_qk_norm_rope_bwd``, ``dsp_layernorm_bwd``, ``dsp_linear_bwd_data``, ``dsp_linear_bwd_weight``,
+``dsp_attn_fwd_lse``, ``dsp_attn_bwd``, ``dsp_attn_general``, ``dsp_attn_general_bwd``, ``dsp_attn_relpos``, ``dsp_attn_relpos_bwd``, ``dsp_relpos_buckets``, ``dsp_attn_window``, ``dsp_attn_window_bwd``, ``dsp_kv_append``, ``dsp_attn_paged``, ``dsp_qk_norm_rope``, ``dsp_qk_norm_rope_bwd``, ``dsp_layernorm_bwd``, ``dsp_linear_bwd_data``, ``dsp_linear_bwd_weight``,
 ``dsp_layernorm``, ``dsp_linear``, ``dsp_st_block_forward``.
 """
 from __future__ import annotations
@@ -26,7 +26,7 @@ LIB_PATH = _PKG / "libdsp.so"
 # status codes and enums of include/dsp.h
 DSP_OK, DSP_ERR_NULL, DSP_ERR_DIM, DSP_ERR_SHAPE, DSP_ERR_DTYPE, DSP_ERR_ALIGN, DSP_ERR_HIP, \
     DSP_ERR_WORKSPACE, DSP_ERR_ARG = range(9)
-DSP_F32, DSP_BF16 = 0, 1
+DSP_F32, DSP_BF16, DSP_E4M3 = 0, 1, 2
 DSP_EPI_NONE, DSP_EPI_GELU, DSP_EPI_RESID, DSP_EPI_F32, DSP_EPI_RELU = 0, 1, 2, 3, 4
 DSP_BLOCK_NO_MLP_LN, DSP_BLOCK_ATTN_ONLY, DSP_BLOCK_POST_LN, DSP_BLOCK_RELU = 1, 2, 4, 8
 DSP_ROPE_ADJACENT = 1
@@ -86,6 +86,17 @@ _SIGNATURES = {
     "dsp_qk_norm_rope_bwd_workspace_bytes": (_SZ, [_I64, _I64, _I64, _I, _I, _I]),
     "dsp_qk_norm_rope_bwd": (_I, [_P] * 13 + [_I64, _I, _I, _P, _SZ, _I64, _I64, _I64, _I, _I, _I]
                              + [_c.POINTER(_I64)] * 6 + [_F, _I, _P]),
+    "dsp_attn_window_workspace_bytes": (_SZ, [_I64] * 4 + [_I] * 7),
+    "dsp_attn_window": (_I, [_P] * 7 + [_I] * 3 + [_P, _SZ] + [_I64] * 4 + [_I] * 3 + [_c.POINTER(_I64)] * 3
+                        + [_F, _I, _P]),
+    "dsp_attn_window_bwd_workspace_bytes": (_SZ, [_I64] * 4 + [_I] * 7),
+    "dsp_attn_window_bwd": (_I, [_P] * 11 + [_I] * 3 + [_P, _SZ] + [_I64] * 4 + [_I] * 3 + [_c.POINTER(_I64)] * 3
+                            + [_F, _I, _P]),
+    "dsp_kv_append": (_I, [_P] * 14 + [_I64, _I, _I] + [_I64] * 4 + [_I] * 4 + [_I64] * 4
+                      + [_c.POINTER(_I64), _I, _I, _P]),
+    "dsp_attn_paged_workspace_bytes": (_SZ, [_I64] * 5 + [_I] * 8),
+    "dsp_attn_paged": (_I, [_P] * 10 + [_I] * 3 + [_P, _SZ] + [_I64] * 5 + [_I] * 4
+                       + [_I64, _c.POINTER(_I64), _I64, _F, _I, _I, _P]),
     "dsp_layernorm": (_I, [_P, _I, _P, _I, _I64, _I, _F, _P]),
     "dsp_attn_general": (_I, [_P, _P, _P, _P, _P, _I64, _I64, _I64, _I64, _I, _I, _I, _c.POINTER(_I64),
                               _c.POINTER(_I64), _c.POINTER(_I64), _F, _I, _P]),
@@ -693,10 +704,16 @@ def _relpos_args(w, q, k, v, H, Hkv, bias, buckets, q_pos, kv_len):
             and buckets.is_contiguous()):
         _check(w, "buckets", buckets, dtype=torch.int32, like=q)
         raise ValueError(f"{w}: buckets must be [2 * max_dist + 1]")
-    for name, t in (("q_pos", q_pos), ("kv_len", kv_len)):
-        if t is not None and not (_as(t, torch.int32, dims[:1], dev) and t.is_contiguous()):
-            _check(w, name, t, dtype=torch.int32, shape=dims[:1], like=q)
+    _lengths(w, q, dims[:1], q_pos=q_pos, kv_len=kv_len)
     return dims
+
+
+def _lengths(w, like, shape, **given):
+    """int32 tensors of one shape on like's device, or None."""
+    torch = _torch()
+    for name, t in given.items():
+        if t is not None and not (_as(t, torch.int32, shape, like.get_device()) and t.is_contiguous()):
+            _check(w, name, t, dtype=torch.int32, shape=shape, like=like)
 
 
 def _workspace(w, need, workspace, like):
@@ -793,6 +810,203 @@ def dsp_attn_relpos_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, bias, buckets, 
             _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv, D, _I3(*q.stride()[:3]), _I3(*k.stride()[:3]),
             _I3(*o.stride()[:3]), scale, dt, s), w)
     return dq, dk, dv, dbias
+
+
+def _window(w, left, right, sinks):
+    """The window's three numbers as the C entry points take them."""
+    if sinks < 0:
+        raise ValueError(f"{w}: sinks must not be negative")
+    most = 2 ** 31 - 1
+    return min(max(int(left), -1), most), min(max(int(right), -1), most), min(int(sinks), most)
+
+
+def dsp_attn_window(q, k, v, H: int, Hkv: int, left: int = -1, right: int = -1, sinks: int = 0, q_pos=None, kv_len=None,
+                    out=None, lse=None, with_lse: bool = False, scale: float = 0.0, workspace=None, stream=None):
+    """Attention with a window (see dsp.h) over dim 2 of 4-D views q [B, X, Lq, H*D], k
+    and v [B, X, Lk, Hkv*D]: a query at position p (its place, plus ``q_pos`` of its
+    sequence) sees the keys from p - left to p + right (negative: no bound) and the first
+    ``sinks`` ones before them, inside ``kv_len`` (int32 [B], default Lk).  Returns out
+    [B, X, Lq, H*D] (and lse [B, X, H, Lq] fp32 when with_lse or lse is given)."""
+    torch = _torch()
+    w = "dsp_attn_window"
+    B, X, Lq, Lk, C, D = _general_views(w, q, k, v, H, Hkv, _same_layout)
+    _lengths(w, q, (B,), q_pos=q_pos, kv_len=kv_len)
+    win = _window(w, left, right, sinks)
+    with _on_device(q, stream) as s:
+        if out is None:
+            out = torch.empty((B, X, Lq, C), dtype=q.dtype, device=q.device)
+        _like_view(w, out, q, "out")
+        if with_lse and lse is None:
+            lse = torch.empty((B, X, H, Lq), dtype=torch.float32, device=q.device)
+        if lse is not None:
+            _check(w, "lse", lse, dtype=torch.float32, numel=B * X * H * Lq, like=q)
+        dt = _dtype_code(q)
+        L = lib()
+        ws = _workspace(w, L.dsp_attn_window_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, *win, dt), workspace, q)
+        _check_status(L.dsp_attn_window(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _at(lse), _at(q_pos), _at(kv_len), *win, _at(ws),
+            _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv, D, _I3(*q.stride()[:3]), _I3(*k.stride()[:3]),
+            _I3(*out.stride()[:3]), scale, dt, s), w)
+    return (out, lse) if lse is not None else out
+
+
+def dsp_attn_window_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, left: int = -1, right: int = -1, sinks: int = 0,
+                        q_pos=None, kv_len=None, dq=None, dk=None, dv=None, scale: float = 0.0, workspace=None,
+                        stream=None):
+    """Gradients of dsp_attn_window, given its o and lse and the gradient dout (o's
+    strides): (dq like q, dk and dv like k and v), each with its input's strides.  New ones
+    for columns of a packed projection are columns of one buffer."""
+    torch = _torch()
+    w = "dsp_attn_window_bwd"
+    B, X, Lq, Lk, C, D = _general_views(w, q, k, v, H, Hkv, _same_layout)
+    _lengths(w, q, (B,), q_pos=q_pos, kv_len=kv_len)
+    win = _window(w, left, right, sinks)
+    _like_view(w, o, q, "o")
+    _like_view(w, dout, q, "dout")
+    if not _same_layout(dout, o):
+        raise ValueError(f"{w}: dout must have the strides of o")
+    _check(w, "lse", lse, dtype=torch.float32, numel=B * X * H * Lq, like=q)
+    with _on_device(q, stream) as s:
+        dq, dk, dv = _relpos_grads(w, q, k, v, dq, dk, dv)
+        for name, g, x in (("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
+            _check(w, name, g, dtype=q.dtype, shape=x.shape, contiguous=False, like=q)
+            if not _same_layout(g, x):
+                raise ValueError(f"{w}: {name} must have the strides of its input, {x.stride()}, got {g.stride()}")
+        dt = _dtype_code(q)
+        L = lib()
+        ws = _workspace(w, L.dsp_attn_window_bwd_workspace_bytes(B, X, Lq, Lk, H, Hkv, D, *win, dt), workspace, q)
+        _check_status(L.dsp_attn_window_bwd(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), dout.data_ptr(), lse.data_ptr(), dq.data_ptr(),
+            dk.data_ptr(), dv.data_ptr(), _at(q_pos), _at(kv_len), *win, _at(ws),
+            _nbytes(ws) if ws is not None else 0, B, X, Lq, Lk, H, Hkv, D, _I3(*q.stride()[:3]), _I3(*k.stride()[:3]),
+            _I3(*o.stride()[:3]), scale, dt, s), w)
+    return dq, dk, dv
+
+
+def _rows2(w, name, t, dt, shape, like):
+    """Packed rows: a 2-D view with a unit last stride."""
+    if not (_as(t, dt, shape, like.get_device()) and t.stride(1) == 1):
+        _check(w, name, t, dtype=dt, shape=shape, contiguous=False, like=like)
+        raise ValueError(f"{w}: {name} must have a unit last stride")
+    return t
+
+
+def _paged_args(w, like, k_cache, v_cache, table, q_start, kv_len, k_scale, v_scale):
+    """Checks what the calls on a paged cache share; returns (N, n_pages, max_pages, page, Hkv, D, cache dtype)."""
+    torch = _torch()
+    dt, f8, dev = _float_dtype(w, like), torch.float8_e4m3fn, like.get_device()
+    for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
+        _check(w, name, c, contiguous=False, like=like)
+        if c.dtype not in (dt, f8) or (c.dtype == f8 and dt != torch.bfloat16):
+            raise ValueError(f"{w}: {name} must be {dt}" + (" or float8_e4m3fn" if dt == torch.bfloat16 else "")
+                             + f", got {c.dtype}")
+        if c.dim() != 4 or c.stride(3) != 1:
+            raise ValueError(f"{w}: {name} must be a view [pages, page, Hkv, D] with a unit last stride")
+    if k_cache.dtype != v_cache.dtype or k_cache.shape != v_cache.shape or not _same_layout(k_cache, v_cache):
+        raise ValueError(f"{w}: k_cache and v_cache must have one type, shape and layout")
+    n_pages, page, Hkv, D = k_cache.shape
+    e4m3 = k_cache.dtype == f8
+    for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if (t is not None) != e4m3:
+            raise ValueError(f"{w}: {name} comes with float8_e4m3fn caches, and only with them")
+        if e4m3 and not (_as(t, torch.float32, (n_pages, Hkv), dev) and t.is_contiguous()):
+            _check(w, name, t, dtype=torch.float32, shape=(n_pages, Hkv), like=like)
+    if table is None or table.dim() != 2 or kv_len is None or q_start is None:
+        raise ValueError(f"{w}: table [N, max_pages], q_start [N + 1] and kv_len [N] are required")
+    N = table.shape[0]
+    _lengths(w, like, tuple(table.shape), table=table)
+    _lengths(w, like, (N + 1,), q_start=q_start)
+    _lengths(w, like, (N,), kv_len=kv_len)
+    return N, n_pages, table.shape[1], page, Hkv, D, DSP_E4M3 if e4m3 else _dtype_code(like)
+
+
+def dsp_kv_append(k, v, k_cache, v_cache, table, q_start, kv_len, k_scale=None, v_scale=None, cos=None, sin=None,
+                  pos=None, interleaved: bool = False, q=None, out_q=None, stream=None):
+    """Writes new keys and values, packed rows k and v [T, Hkv*D], into a paged cache (see
+    dsp.h): ``k_cache`` and ``v_cache`` views [pages, page, Hkv, D] of one layout (any
+    strides, a unit last one) in k's dtype or float8_e4m3fn, the latter with ``k_scale``
+    and ``v_scale`` float32 [pages, Hkv].  ``table`` int32 [N, max_pages], ``q_start``
+    int32 [N + 1] (each sequence's rows), ``kv_len`` int32 [N] (its positions, the new
+    ones included).  With ``cos``, ``sin`` float32 [P, rot/2] keys turn by their position,
+    or by ``pos`` int32 [T]; with ``q`` [T, H*D] the queries turn too, into ``out_q`` (new,
+    or given; q itself: in place), which is returned (None without q).  Rows of no
+    sequence are left as they were."""
+    torch = _torch()
+    w = "dsp_kv_append"
+    _check(w, "k", k, contiguous=False)
+    N, n_pages, max_pages, page, Hkv, D, cdt = _paged_args(w, k, k_cache, v_cache, table, q_start, kv_len, k_scale, v_scale)
+    if k.dim() != 2:
+        raise ValueError(f"{w}: k and v must be packed rows [T, Hkv * D]")
+    T, dt = k.shape[0], k.dtype
+    _rows2(w, "k", k, dt, (T, Hkv * D), k)
+    _rows2(w, "v", v, dt, (T, Hkv * D), k)
+    H = 0
+    if q is not None:
+        _check(w, "q", q, dtype=dt, contiguous=False, like=k)
+        if q.dim() != 2 or q.shape[0] != T or q.shape[1] % D or q.shape[1] == 0:
+            raise ValueError(f"{w}: q must be packed rows [T, H * D]")
+        H = q.shape[1] // D
+        _rows2(w, "q", q, dt, (T, H * D), k)
+    elif out_q is not None:
+        raise ValueError(f"{w}: out_q without q")
+    if (cos is None) != (sin is None):
+        raise ValueError(f"{w}: cos and sin come together")
+    P = rot = 0
+    if cos is not None:
+        if cos.dim() != 2:
+            raise ValueError(f"{w}: cos must be [P, rot / 2]")
+        for name, t in (("cos", cos), ("sin", sin)):
+            if not (_as(t, torch.float32, cos.shape, k.get_device()) and t.is_contiguous()):
+                _check(w, name, t, dtype=torch.float32, shape=cos.shape, like=k)
+        P, rot = cos.shape[0], 2 * cos.shape[1]
+    _lengths(w, k, (T,), pos=pos)
+    with _on_device(k, stream) as s:
+        if q is not None:
+            out_q = torch.empty((T, H * D), dtype=dt, device=k.device) if out_q is None else out_q
+            _rows2(w, "out_q", out_q, dt, (T, H * D), k)
+        _check_status(lib().dsp_kv_append(
+            k.data_ptr(), v.data_ptr(), _at(q), _at(out_q), k_cache.data_ptr(), v_cache.data_ptr(), _at(k_scale),
+            _at(v_scale), table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), _at(cos), _at(sin), _at(pos), P, rot,
+            DSP_ROPE_ADJACENT if interleaved else 0, N, T, n_pages, max_pages, page, H, Hkv, D, k.stride(0), v.stride(0),
+            q.stride(0) if H else 0, out_q.stride(0) if H else 0, _I3(*k_cache.stride()[:3]), cdt, _dtype_code(k), s), w)
+    return out_q
+
+
+def dsp_attn_paged(q, k_cache, v_cache, table, q_start, kv_len, H: int, max_q: int | None = None, left: int = -1,
+                   right: int = 0, sinks: int = 0, k_scale=None, v_scale=None, out=None, lse=None, with_lse: bool = False,
+                   scale: float = 0.0, workspace=None, stream=None):
+    """Attention of new tokens, packed rows q [T, H*D], over their sequences' positions in a
+    paged cache (see dsp_kv_append and dsp.h), with the window of dsp_attn_window.
+    ``max_q``: the most new tokens of one sequence (default T); a small one, as in
+    generation, lets the keys be cut among work-groups.  Returns out [T, H*D] (and lse
+    [T, H] fp32 when with_lse or lse is given); rows of no sequence are left as they were
+    (in a new tensor: whatever it holds)."""
+    torch = _torch()
+    w = "dsp_attn_paged"
+    _check(w, "q", q, contiguous=False)
+    N, n_pages, max_pages, page, Hkv, D, cdt = _paged_args(w, q, k_cache, v_cache, table, q_start, kv_len, k_scale, v_scale)
+    if H < 1 or H % Hkv or q.dim() != 2:
+        raise ValueError(f"{w}: q must be packed rows [T, H * D], H a multiple of the cache's heads")
+    T, dt = q.shape[0], q.dtype
+    _rows2(w, "q", q, dt, (T, H * D), q)
+    win = _window(w, left, right, sinks)
+    max_q = T if max_q is None else int(max_q)
+    with _on_device(q, stream) as s:
+        out = torch.empty((T, H * D), dtype=dt, device=q.device) if out is None else out
+        _rows2(w, "out", out, dt, (T, H * D), q)
+        if with_lse and lse is None:
+            lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
+        if lse is not None:
+            _check(w, "lse", lse, dtype=torch.float32, shape=(T, H), like=q)
+        L, code = lib(), _dtype_code(q)
+        ws = _workspace(w, L.dsp_attn_paged_workspace_bytes(N, T, max_q, n_pages, max_pages, page, H, Hkv, D, *win, code),
+                        workspace, q)
+        _check_status(L.dsp_attn_paged(
+            q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), out.data_ptr(), _at(lse), _at(k_scale), _at(v_scale),
+            table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), *win, _at(ws), _nbytes(ws) if ws is not None else 0,
+            N, T, max_q, n_pages, max_pages, page, H, Hkv, D, q.stride(0), _I3(*k_cache.stride()[:3]), out.stride(0),
+            scale, cdt, code, s), w)
+    return (out, lse) if lse is not None else out
 
 
 def _norm_rope_args(w, q, k, H, Hkv, gq, gk, cos, sin, pos):

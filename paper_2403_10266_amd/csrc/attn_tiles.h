@@ -337,8 +337,8 @@ struct Place {
   uint32_t bx, h, block;   // block 0 is the most costly
   bool any;                // the grid is rounded up: nothing to do
 };
-__device__ __forceinline__ Place place(const Order& o) {
-  const uint32_t xcd = blockIdx.x & 7u, j = blockIdx.x >> 3;
+__device__ __forceinline__ Place place(const Order& o, uint32_t i = blockIdx.x) {
+  const uint32_t xcd = i & 7u, j = i >> 3;
   Place p;
   uint32_t local, head;
   if (o.costly_first) {

@@ -1,0 +1,508 @@
+// Gradient of attention with a window and first tokens that stay visible.  With
+//   z_ij = scale q_i . k_j over the keys j that query i sees,  P = softmax(z),
+//   Delta_i = sum_d dO_id O_id,  dZ = P (dP - Delta),  dP = dO V^T:
+//   dV = P^T dO,  dQ = scale dZ K,  dK = scale dZ^T Q.
+// P is recomputed from the forward's row log-sum-exp.  Two kernels, both deterministic:
+// the first owns blocks of (query, head) columns of a key/value head's group and visits
+// the keys that they see (dQ, Delta), the second owns blocks of keys and visits the
+// queries that see them, head by head of the group (dK, dV).
+//
+// A first token that stays visible is seen by every later query, so its block of keys has
+// a window's queries many times over.  Those queries are cut into parts, work-groups of
+// about a window's work whose fp32 sums a third kernel adds in order.
+//
+// P and dZ are rounded to bf16 for the products that take them as operands (the matrix
+// cores' type; their sums are fp32).
+#include <algorithm>
+
+#include "attn_window.h"
+
+namespace dsp {
+namespace {
+
+struct BwdParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* o;
+  const void* dout;
+  const float* lse;
+  void* dq;
+  void* dk;
+  void* dv;
+  float* delta;      // [B X H][Lq]
+  float* part;       // sinks: [unit and head][block][part][dK, dV][keys][D]
+  const int32_t* q_pos;
+  const int32_t* kv_len;
+  int64_t qs[3], ks[3], os[3];
+  Window win;
+  uint32_t X, H, Hkv, grp, Lq, Lk, D;
+  Order order;
+  uint32_t parts, sink_blocks;   // parts of the first blocks of keys (0: they are like the others)
+  uint32_t sink_groups;          // work-groups for them, the first of the grid
+  float c, scale;
+  bool vec;
+};
+
+__device__ __forceinline__ int64_t bx_at(const BwdParams& p, uint32_t bx, const int64_t* st) {
+  return (int64_t)(bx / p.X) * st[0] + (int64_t)(bx % p.X) * st[1];
+}
+
+// dQ and Delta: 32 columns per wave, keys on the rows of the products.
+template <typename T, int DC, int NW, int KB, int MINW>
+__global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  using R = Rows16<T, T, DC>;
+  constexpr int NT = NW * 64, CB = NW * 32, NKT = KB / 32, GR = KB / 16, TILE = KB * G::P;
+  constexpr int NL = 2 * GR / NW;
+  static_assert(2 * GR % NW == 0 && NW <= 4 * NKT, "every wave loads the same; the output rows fit the tiles");
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* lds = reinterpret_cast<T*>(smem);   // [2][K, V][KB][P]
+
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place pl = place(p.order);
+  if (!pl.any) return;
+  const uint32_t bx = pl.bx, e = pl.h, blk = p.order.blocks - 1 - pl.block, b = bx / p.X;
+  const uint32_t cols = p.Lq * p.grp, c0 = blk * CB;
+  const int D = (int)p.D;
+  const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D;
+  const T* kg = static_cast<const T*>(p.k) + k_at;
+  const T* vg = static_cast<const T*>(p.v) + k_at;
+  const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
+  const int64_t p0 = position(p.q_pos, b);
+  auto seen_by = [&](uint32_t c) { return seen(p.win, p0 + min(c, cols - 1) / p.grp, len); };
+  const Seen first = seen_by(c0), last = seen_by(c0 + CB - 1);
+  const Tiles<KB> tiles(first, last);
+
+  const uint32_t row_bytes = (uint32_t)p.ks[2] * (uint32_t)sizeof(T);
+  const typename R::Map map = R::map(D, row_bytes, lane);
+  R rows[NL];
+  auto fetch = [&](int32_t t) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int li = wave + i * NW;
+      const int32_t key0 = tiles.key0(t) + 16 * (li % GR);
+      rows[i].fetch(map, (li < GR ? kg : vg) + (int64_t)key0 * p.ks[2], row_bytes, D, p.vec, [&](int r) {
+        const int32_t j = key0 + r;
+        return j < last.sink || (j >= first.lo && j < last.hi);
+      });
+    }
+  };
+  auto stash = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int li = wave + i * NW;
+      rows[i].stash(map, lds + buf * 2 * TILE + (li < GR ? 0 : TILE) + 16 * (li % GR) * G::P, 1.0f);
+    }
+  };
+  if (tiles.n) fetch(0);
+  const uint32_t c = c0 + 32 * wave + l32, cc = min(c, cols - 1), qi = cc / p.grp, qh = e * p.grp + cc - qi * p.grp;
+  const bool on = c < cols;
+  const int64_t q_at = bx_at(p, bx, p.qs), o_at = bx_at(p, bx, p.os);
+  auto at = [&](const void* base, int64_t from, int64_t row) {
+    return on ? static_cast<const T*>(base) + from + (int64_t)qi * row + (int64_t)qh * D : nullptr;
+  };
+  typename M::frag qf[G::NS], df[G::NS];
+  row_frags<T, DC>(at(p.q, q_at, p.qs[2]), g, D, p.vec, qf);
+  row_frags<T, DC>(at(p.dout, o_at, p.os[2]), g, D, p.vec, df);
+  float delta = 0.0f;
+  {
+    typename M::frag of[G::NS];
+    row_frags<T, DC>(at(p.o, o_at, p.os[2]), g, D, p.vec, of);
+#pragma unroll
+    for (int s = 0; s < G::NS; ++s)
+#pragma unroll
+      for (int k = 0; k < G::E; ++k) delta += (float)df[s][k] * (float)of[s][k];
+    delta += swap_halves(delta);
+  }
+  const uint64_t stat = ((uint64_t)bx * p.H + qh) * p.Lq + qi;
+  // a row that sees nothing, or past the end: P = exp2(-inf) = 0
+  const float l = on ? p.lse[stat] : -INFINITY;
+  const float lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
+  if (on && g == 0) p.delta[stat] = delta;
+  const Seen col = seen(p.win, p0 + qi, len);
+  const Seen wf = seen_by(c0 + 32 * wave), wl = seen_by(c0 + 32 * wave + 31);
+  const bool wave_on = c0 + 32 * wave < cols;
+  clear_pad<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
+  if (tiles.n) stash(0);
+  __syncthreads();
+
+  ColAcc<T, DC> dq;
+  dq.zero();
+  for (int32_t it = 0; it < tiles.n; ++it) {
+    const bool more = it + 1 < tiles.n;
+    if (more) fetch(it + 1);
+    const T* kl = lds + (it & 1) * 2 * TILE;
+    const T* vl = kl + TILE;
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt) {
+      const int32_t key0 = tiles.key0(it) + 32 * kt;
+      if (!wave_on || (key0 >= wl.sink && (key0 + 32 <= wf.lo || key0 >= wl.hi))) continue;
+      floatx16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+#pragma unroll
+      for (int st = 0; st < G::NS; ++st) {
+        const int a = (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g;
+        s = M::mma(*reinterpret_cast<const typename M::frag*>(kl + a), qf[st], s);
+        dp = M::mma(*reinterpret_cast<const typename M::frag*>(vl + a), df[st], dp);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, -lse2);
+      if (!(key0 + 32 <= wf.sink || (key0 >= wl.lo && key0 + 32 <= wf.hi))) {
+        const int32_t j = key0 + 4 * g;
+        const uint32_t from = (uint32_t)(j - col.lo), width = (uint32_t)max(col.hi - col.lo, 0);
+        const int32_t left = col.sink - j;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int k = 8 * (r / 4) + r % 4;
+          if (!(from + k < width || k < left)) s[r] = -INFINITY;
+        }
+      }
+      ColB<T> z;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z.set(r, __builtin_amdgcn_exp2f(s[r]) * (dp[r] - delta));
+      dq.add(kl, 32 * kt, lane, z);
+    }
+    if (more) stash((it + 1) & 1);
+    __syncthreads();
+  }
+  dq.scale(p.scale, lane);
+  T* out = static_cast<T*>(p.dq) + q_at + (int64_t)e * p.grp * D;
+  auto row = [&](int n) -> T* {
+    const uint32_t k = c0 + 32 * wave + n, i = k / p.grp;
+    return k < cols ? out + (int64_t)i * p.qs[2] + (int64_t)(k - i * p.grp) * D : nullptr;
+  };
+  if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, dq, lane, D, G::DP, row);
+  else store_rows<T, DC>(dq, lane, D, false, row);
+}
+
+// The queries that see key j: first <= i < end.
+struct SeenBy {
+  int32_t first, end;
+};
+__device__ __forceinline__ SeenBy seen_by(const Window& w, int64_t p0, int32_t n, int32_t len, int64_t j) {
+  auto clamp = [n](int64_t v) { return (int32_t)(v < 0 ? 0 : v > n ? n : v); };
+  SeenBy s;
+  s.first = w.right < 0 ? 0 : clamp(j - w.right - p0);
+  s.end = j >= len ? 0 : w.left < 0 || j < w.sinks ? n : clamp(j + w.left - p0 + 1);
+  return s;
+}
+
+// dK and dV, over the queries of every head of the key/value head's group, in tiles of
+// 32 QT: KW blocks of 32 keys, each tile's queries shared out among QS waves for each,
+// whose sums are joined at the end.
+template <typename T, int DC, int KW, int QS, int QT, int MINW>
+__global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  constexpr int NT = KW * QS * 64, QB = 32 * QT, TILE = QB * G::P, KEYS = 32 * KW;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* lds = reinterpret_cast<T*>(smem);                            // [2][Q, dO][QB][P]
+  float* stat = reinterpret_cast<float*>(lds + 4 * TILE);         // [2][lse2, Delta][QB]
+
+  const int lane0 = threadIdx.x & 63, lane = lane0, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kw = wave / QS, qs = wave % QS;
+  uint32_t blk, bx, e, part = 0;
+  const bool sink = blockIdx.x < p.sink_groups;
+  if (sink) {
+    const uint32_t u = blockIdx.x / p.parts, ub = u / p.sink_blocks;
+    part = blockIdx.x - u * p.parts;
+    blk = u - ub * p.sink_blocks;
+    bx = ub / p.Hkv;
+    e = ub - bx * p.Hkv;
+  } else {
+    const Place pl = place(p.order, blockIdx.x - p.sink_groups);
+    if (!pl.any || (p.parts && pl.block < p.sink_blocks)) return;
+    blk = pl.block, bx = pl.bx, e = pl.h;
+  }
+  const uint32_t b = bx / p.X;
+  const int D = (int)p.D;
+  const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D;
+  const int64_t q_bx = bx_at(p, bx, p.qs), o_bx = bx_at(p, bx, p.os);
+  const int32_t first_key = (int32_t)(blk * KEYS), key = first_key + 32 * kw + l32;
+  const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
+  const int64_t p0 = position(p.q_pos, b);
+  const SeenBy mine = seen_by(p.win, p0, (int32_t)p.Lq, len, key);
+  // of the wave's keys: the tiles that any is seen from, and those that all are
+  int32_t any0 = mine.first < mine.end ? mine.first : INT32_MAX, any1 = mine.end, all0 = mine.first, all1 = mine.end;
+#pragma unroll
+  for (int off = 16; off; off >>= 1) {
+    any0 = min(any0, __shfl_xor(any0, off));
+    any1 = max(any1, __shfl_xor(any1, off));
+    all0 = max(all0, __shfl_xor(all0, off));
+    all1 = min(all1, __shfl_xor(all1, off));
+  }
+  any0 = __builtin_amdgcn_readfirstlane(any0), any1 = __builtin_amdgcn_readfirstlane(any1);
+  all0 = __builtin_amdgcn_readfirstlane(all0), all1 = __builtin_amdgcn_readfirstlane(all1);
+  typename M::frag kf[G::NS], vf[G::NS];
+  const bool there = mine.first < mine.end;   // a key that nothing sees may hold anything
+  row_frags<T, DC>(there ? static_cast<const T*>(p.k) + k_at + (int64_t)key * p.ks[2] : nullptr, g, D, p.vec, kf);
+  row_frags<T, DC>(there ? static_cast<const T*>(p.v) + k_at + (int64_t)key * p.ks[2] : nullptr, g, D, p.vec, vf);
+
+  const uint32_t q_row = (uint32_t)p.qs[2] * (uint32_t)sizeof(T), o_row = (uint32_t)p.os[2] * (uint32_t)sizeof(T);
+  using TileT = Tile<T, DC, QB, NT>;
+  const typename TileT::Map mq = TileT::map(D, q_row, threadIdx.x), mo = TileT::map(D, o_row, threadIdx.x);
+  TileT tq, to;
+  static_assert(NT >= 2 * QB, "a statistic for each thread");
+  float pre = 0.0f;
+  clear_pad<T, DC>(lds, 4 * QB, D, threadIdx.x, NT);
+
+  ColAcc<T, DC> dk, dv;
+  dk.zero();
+  dv.zero();
+  // the tiles of queries that see the work-group's keys, head after head
+  const int32_t key_end = min(first_key + KEYS, len);
+  const SeenBy lowest = seen_by(p.win, p0, (int32_t)p.Lq, len, first_key);
+  const SeenBy highest = seen_by(p.win, p0, (int32_t)p.Lq, len, (int64_t)key_end - 1);
+  const int32_t q_end = first_key < key_end ? max(lowest.end, highest.end) : 0;
+  const uint32_t it0 = (uint32_t)lowest.first / QB, n_it = q_end > lowest.first ? ((uint32_t)q_end + QB - 1) / QB - it0 : 0;
+  uint32_t step = 0, steps = n_it * p.grp;
+  if (sink) {
+    const uint32_t per = (steps + p.parts - 1) / p.parts;
+    step = min(part * per, steps);
+    steps = min(step + per, steps);
+  }
+  uint32_t hh = n_it ? step / n_it : 0, it = step - hh * n_it;   // the step to fetch
+  auto fetch = [&]() {
+    const uint32_t h = e * p.grp + hh, q0 = (it0 + it) * QB, rows = min(p.Lq - q0, (uint32_t)QB);
+    tq.fetch(mq, static_cast<const T*>(p.q) + q_bx + (int64_t)h * D + (int64_t)q0 * p.qs[2], rows, q_row, D, p.vec);
+    to.fetch(mo, static_cast<const T*>(p.dout) + o_bx + (int64_t)h * D + (int64_t)q0 * p.os[2], rows, o_row, D, p.vec);
+    if (threadIdx.x < 2 * QB) {
+      const uint32_t i = threadIdx.x % QB;
+      const bool is_delta = threadIdx.x >= QB;
+      const uint64_t at = ((uint64_t)bx * p.H + h) * p.Lq + q0 + i;
+      const float l = i < rows ? (is_delta ? p.delta : p.lse)[at] : is_delta ? 0.0f : -INFINITY;
+      pre = is_delta ? l : l == -INFINITY ? INFINITY : l * kLog2e;
+    }
+  };
+  auto stash = [&](int buf) {
+    tq.stash(mq, lds + buf * 2 * TILE);
+    to.stash(mo, lds + buf * 2 * TILE + TILE);
+    if (threadIdx.x < 2 * QB) stat[buf * 2 * QB + threadIdx.x] = pre;
+  };
+  if (step < steps) {
+    fetch();
+    stash(0);
+  }
+  __syncthreads();
+  for (int buf = 0; step < steps; ++step, buf ^= 1) {
+    const int32_t qt0 = (int32_t)((it0 + it) * QB);   // the tile's first query
+    const bool more = step + 1 < steps;
+    if (++it == n_it) it = 0, ++hh;
+    if (more) fetch();
+    int lane = lane0;
+    asm volatile("" : "+v"(lane));   // addresses made of it are cheaper to form again than to keep
+    const int l32 = lane & 31, g = lane >> 5;
+    const T* ql = lds + buf * 2 * TILE;
+    const T* ol = ql + TILE;
+    const float* sl = stat + buf * 2 * QB;
+#pragma unroll
+    for (int i = 0; i < QT / QS; ++i) {
+      const int sub = i * QS + qs;
+      const int32_t q0 = qt0 + 32 * sub;
+      if (q0 >= any1 || q0 + 32 <= any0) continue;
+      floatx16 s, dp;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
+#pragma unroll
+      for (int st = 0; st < G::NS; ++st) {
+        const int a = (32 * sub + l32) * G::P + 2 * G::E * st + G::E * g;
+        s = M::mma(*reinterpret_cast<const typename M::frag*>(ql + a), kf[st], s);
+        dp = M::mma(*reinterpret_cast<const typename M::frag*>(ol + a), vf[st], dp);
+      }
+      // lane (n + 32 g): key n, queries 8 (r / 4) + 4 g + r % 4
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const floatx4 l = *reinterpret_cast<const floatx4*>(sl + 32 * sub + 8 * q + 4 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[4 * q + j] = fmaf(s[4 * q + j], p.c, -l[j]);
+      }
+      if (q0 < all0 || q0 + 32 > all1) {
+        const uint32_t from = (uint32_t)(q0 + 4 * g - mine.first), width = (uint32_t)max(mine.end - mine.first, 0);
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (!(from + 8 * (r / 4) + r % 4 < width)) s[r] = -INFINITY;
+      }
+      ColB<T> pb, zb;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const floatx4 dl = *reinterpret_cast<const floatx4*>(sl + QB + 32 * sub + 8 * q + 4 * g);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float e = __builtin_amdgcn_exp2f(s[4 * q + j]);
+          pb.set(4 * q + j, e);
+          zb.set(4 * q + j, e * (dp[4 * q + j] - dl[j]));
+        }
+      }
+      dv.add(ol, 32 * sub, lane, pb);
+      dk.add(ql, 32 * sub, lane, zb);
+    }
+    if (more) stash(buf ^ 1);
+    __syncthreads();
+  }
+  dk.scale(p.scale, lane);
+  T* const out[2] = {static_cast<T*>(p.dk) + k_at, static_cast<T*>(p.dv) + k_at};
+  float* const sums_at = p.part + ((((uint64_t)bx * p.Hkv + e) * p.sink_blocks + blk) * p.parts + part) * 2 * KEYS * p.D;
+  if constexpr (QS == 1) {
+    const uint32_t k0 = first_key + 32 * kw;
+    auto row = [&](T* base, int n) -> T* { return k0 + n < p.Lk ? base + (int64_t)(k0 + n) * p.ks[2] : nullptr; };
+    auto part_row = [&](int which, int n) -> float* { return sums_at + ((uint64_t)which * KEYS + 32 * kw + n) * p.D; };
+    if (sink) {
+      const bool vec4 = p.D % 4 == 0;
+      store_rows<T, DC>(dk, lane, D, vec4, [&](int n) { return part_row(0, n); });
+      store_rows<T, DC>(dv, lane, D, vec4, [&](int n) { return part_row(1, n); });
+    } else if (p.vec) {
+      T* so = lds + wave * 32 * G::P;   // the tiles are done with
+      static_assert(KW * 32 <= 4 * QB, "rows to write through");
+      store_rows_lds<T, DC>(so, dk, lane, D, G::DP, [&](int n) { return row(out[0], n); });
+      store_rows_lds<T, DC>(so, dv, lane, D, G::DP, [&](int n) { return row(out[1], n); });
+    } else {
+      store_rows<T, DC>(dk, lane, D, false, [&](int n) { return row(out[0], n); });
+      store_rows<T, DC>(dv, lane, D, false, [&](int n) { return row(out[1], n); });
+    }
+  } else {
+    // the QS waves' sums of a key, added in order
+    float* sums = reinterpret_cast<float*>(smem);   // [QS][KEYS][DP]
+    constexpr int W = G::DP, ROWS = KEYS;
+    static_assert((size_t)QS * ROWS * W * 4 <= (size_t)4 * TILE * sizeof(T), "the sums fit the tiles");
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+      __syncthreads();
+      store_rows<T, DC>(which ? dv : dk, lane, W, true, [&](int n) { return sums + (qs * ROWS + kw * 32 + n) * W; });
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < ROWS * W / 4; i += NT) {
+        const uint32_t n = i / (W / 4), d = i % (W / 4) * 4;
+        floatx4 v = *reinterpret_cast<const floatx4*>(sums + n * W + d);
+#pragma unroll
+        for (int q = 1; q < QS; ++q) v += *reinterpret_cast<const floatx4*>(sums + (q * ROWS + n) * W + d);
+        if (sink)
+          store4(sums_at + ((uint64_t)which * KEYS + n) * p.D, (int)d, D, p.D % 4 == 0, v[0], v[1], v[2], v[3]);
+        else if (first_key + n < p.Lk)
+          store4(out[which] + (int64_t)(first_key + n) * p.ks[2], (int)d, D, p.vec, v[0], v[1], v[2], v[3]);
+      }
+    }
+  }
+}
+
+// dK and dV of the first blocks of keys: their parts added in order.
+template <typename T>
+__global__ __launch_bounds__(256) void window_bwd_sink_kernel(BwdParams p, uint32_t keys) {
+  const uint32_t ub = blockIdx.x / p.sink_blocks, blk = blockIdx.x - ub * p.sink_blocks;
+  const uint32_t bx = ub / p.Hkv, e = ub - bx * p.Hkv, n = keys * p.D;
+  const float* from = p.part + (uint64_t)blockIdx.x * p.parts * 2 * n;
+  const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * p.D;
+  for (uint32_t i = blockIdx.y * 256 + threadIdx.x; i < 2 * n; i += gridDim.y * 256) {
+    float v = 0.0f;
+#pragma unroll 8
+    for (uint32_t s = 0; s < p.parts; ++s) v += from[(uint64_t)s * 2 * n + i];
+    const uint32_t which = i >= n, at = i - which * n, key = at / p.D, d = at - key * p.D, j = blk * keys + key;
+    if (j < p.Lk) (static_cast<T*>(which ? p.dv : p.dk) + k_at)[(int64_t)j * p.ks[2] + d] = (T)v;
+  }
+}
+
+template <typename K>
+int lds_limit(K* kernel, size_t lds) {
+  if (lds <= 64 * 1024) return DSP_OK;
+  return hip_status(
+      hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+}
+
+constexpr int kDkvKeys = 128;   // of a work-group
+// Parts of the first keys' queries: about a window's work each, where that is less than a
+// half of all.
+struct Sinks {
+  int64_t blocks, parts;
+};
+Sinks sinks_of(const WindowArgs& a) {
+  Sinks s = {0, 0};
+  if (a.win.sinks == 0 || a.win.left < 0 || a.Lq == 0 || a.Lk == 0) return s;
+  const int64_t band = (int64_t)a.win.left + (a.win.right < 0 ? a.Lq : a.win.right) + kDkvKeys + 64;
+  const int64_t parts = std::min<int64_t>(a.Lq / std::max<int64_t>(band, 256), 64);
+  if (parts < 2) return s;
+  s.blocks = (std::min<int64_t>(a.win.sinks, a.Lk) + kDkvKeys - 1) / kDkvKeys;
+  s.parts = parts;
+  return s;
+}
+
+template <typename T, int DC>
+int start_dq(BwdParams& p, const WindowArgs& a, hipStream_t s) {
+  constexpr int NW = 4, CB = 32 * NW, KB = 32, MINW = sizeof(T) == 2 && DC <= 64 ? 3 : sizeof(T) == 2 || DC <= 96 ? 2 : 1;
+  p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
+  const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T);
+  auto* kernel = window_bwd_dq_kernel<T, DC, NW, KB, MINW>;
+  if (!grid_fits(order_blocks(p.order), NW * 64)) return DSP_ERR_SHAPE;
+  if (int st = lds_limit(kernel, lds)) return st;
+  kernel<<<dim3((uint32_t)order_blocks(p.order)), NW * 64, lds, s>>>(p);
+  return last_launch_status();
+}
+
+template <typename T, int DC, int KW, int QS, int QT, int MINW>
+int start_dkv(BwdParams& p, const WindowArgs& a, hipStream_t s) {
+  static_assert(32 * KW == kDkvKeys, "the sinks' workspace");
+  constexpr int QB = 32 * QT;
+  p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lk + 32 * KW - 1) / (32 * KW), a.win.right >= 0 && a.win.left < 0);
+  const Sinks sk = sinks_of(a);
+  p.parts = (uint32_t)sk.parts, p.sink_blocks = (uint32_t)sk.blocks;
+  const int64_t first = a.B * a.X * a.Hkv * sk.blocks * sk.parts, blocks = first + order_blocks(p.order);
+  if (!grid_fits(blocks, KW * QS * 64)) return DSP_ERR_SHAPE;
+  p.sink_groups = (uint32_t)first;
+  const size_t lds = (size_t)4 * QB * Geo<T, DC>::P * sizeof(T) + (size_t)4 * QB * 4;
+  auto* kernel = window_bwd_dkv_kernel<T, DC, KW, QS, QT, MINW>;
+  if (int st = lds_limit(kernel, lds)) return st;
+  kernel<<<dim3((uint32_t)blocks), KW * QS * 64, lds, s>>>(p);
+  if (int st = last_launch_status()) return st;
+  if (!sk.parts) return DSP_OK;
+  const int64_t ub = a.B * a.X * a.Hkv * sk.blocks;
+  window_bwd_sink_kernel<T><<<dim3((uint32_t)ub, 8), 256, 0, s>>>(p, 32 * KW);
+  return last_launch_status();
+}
+
+template <typename T, int DC>
+int start(BwdParams& p, const WindowArgs& a, hipStream_t s) {
+  if (a.Lq > 0)
+    if (int st = start_dq<T, DC>(p, a, s)) return st;
+  if (a.Lk == 0) return DSP_OK;
+  constexpr bool B16 = sizeof(T) == 2;
+  return start_dkv<T, DC, 4, 1, B16 ? 2 : 1, B16 && DC <= 80 ? 2 : 1>(p, a, s);
+}
+
+}  // namespace
+
+size_t attn_window_bwd_workspace_bytes(const WindowArgs& a) {
+  const int64_t stats = (a.B * a.X * a.H * a.Lq + 63) / 64 * 64;
+  const Sinks s = sinks_of(a);
+  return (size_t)(stats + a.B * a.X * a.Hkv * s.blocks * s.parts * 2 * kDkvKeys * a.D) * 4;
+}
+
+int launch_attn_window_bwd(const WindowArgs& a, hipStream_t s) {
+  BwdParams p = {};
+  p.q = a.q, p.k = a.k, p.v = a.v, p.o = a.o, p.dout = a.dout, p.lse = a.lse;
+  p.dq = a.dq, p.dk = a.dk, p.dv = a.dv;
+  p.delta = a.workspace;
+  p.part = a.workspace + (a.B * a.X * a.H * a.Lq + 63) / 64 * 64;
+  p.q_pos = a.q_pos, p.kv_len = a.kv_len;
+  for (int i = 0; i < 3; ++i) p.qs[i] = a.q_strides[i], p.ks[i] = a.kv_strides[i], p.os[i] = a.o_strides[i];
+  p.win = a.win;
+  p.X = (uint32_t)a.X, p.H = a.H, p.Hkv = a.Hkv, p.grp = a.H / a.Hkv, p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk;
+  p.D = a.D;
+  p.c = a.scale * kLog2e, p.scale = a.scale;
+  p.vec = a.vec;
+  if (a.bf16) {
+    if (a.D <= 32) return start<bf16, 32>(p, a, s);
+    if (a.D <= 48) return start<bf16, 48>(p, a, s);
+    if (a.D <= 64) return start<bf16, 64>(p, a, s);
+    if (a.D <= 80) return start<bf16, 80>(p, a, s);
+    if (a.D <= 96) return start<bf16, 96>(p, a, s);
+    return start<bf16, 128>(p, a, s);
+  }
+  if (a.D <= 32) return start<float, 32>(p, a, s);
+  if (a.D <= 64) return start<float, 64>(p, a, s);
+  if (a.D <= 96) return start<float, 96>(p, a, s);
+  return start<float, 128>(p, a, s);
+}
+
+}  // namespace dsp

@@ -1,0 +1,732 @@
+// Kernels of attention with a window and first tokens that stay visible, over rows of a
+// tensor (attn_window.hip) and over pages of a cache (attn_paged.hip):
+//   o_i = sum_j softmax_j(scale q_i . k_j) v_j  over the keys that query i sees.
+//
+// One pass over the keys with the running maximum and sum of the softmax; both products
+// on the matrix cores, computed transposed (keys on rows, queries on columns): a lane
+// owns one column, so the statistics are per-lane scalars and the probabilities are the
+// next product's operand as they stand.  Columns are the (query, head) pairs of one
+// key/value head's group, heads fastest: a tile of keys serves the whole group, and a
+// block of columns spans few positions, so that a narrow window leaves few keys.
+// Only the tiles that a block of columns sees are visited, and only those on the
+// window's edges are masked.
+//
+// Keys come in groups of 16 rows, each loaded by one wave, so that a group's page, its
+// place and its scale are scalars.  e4m3 rows become bf16 on their way into LDS, exactly
+// (the scales are powers of two); from there on there is one kernel for all caches.
+#pragma once
+
+#include <algorithm>
+
+#include "attn_window.h"
+
+namespace dsp {
+namespace {
+
+struct FwdParams {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;
+  float* part;       // split keys: the columns' references, sums and rows of each work-group
+  const int32_t* q_pos;
+  const int32_t* kv_len;
+  const int32_t* q_start;
+  const int32_t* table;
+  const float* k_scale;
+  const float* v_scale;
+  int64_t qs[3], ks[3], os[3];
+  Window win;
+  uint32_t X, H, Hkv, grp, Lq, Lk, D;
+  uint32_t N, T, n_pages, max_pages, shift;   // pages
+  Order order;       // many columns, rows of a tensor
+  uint32_t n_blk;    // many columns, pages: blocks in all
+  uint32_t few_cols; // many columns: units of at most so many are left to the other form
+  uint32_t pieces, n_split, cblk;   // few columns: units times splits, blocks of 32 columns
+  float c;           // scale * log2(e)
+  bool vec;
+};
+
+// A sequence (or a unit of B X) and one of its key/value heads.
+template <typename T, typename S, bool PAGED>
+struct Unit {
+  const T* q;        // column (query i, head hh of the group): q + i q_row + hh D
+  T* o;
+  float* lse;        // + i lse_i + hh lse_h
+  int64_t q_row, o_row, lse_i, lse_h;
+  int64_t p0;        // position of query 0
+  int32_t nq, len;
+  Source<S, PAGED> src;
+};
+template <typename T, typename S>
+__device__ __forceinline__ Unit<T, S, false> unit(const FwdParams& p, uint32_t bx, uint32_t e, Unit<T, S, false>*) {
+  Unit<T, S, false> u;
+  const uint32_t b = bx / p.X, x = bx - b * p.X, h0 = e * p.grp;
+  u.q = static_cast<const T*>(p.q) + (int64_t)b * p.qs[0] + (int64_t)x * p.qs[1] + (int64_t)h0 * p.D;
+  u.o = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)h0 * p.D;
+  u.lse = p.lse ? p.lse + ((uint64_t)bx * p.H + h0) * p.Lq : nullptr;
+  u.q_row = p.qs[2], u.o_row = p.os[2], u.lse_i = 1, u.lse_h = p.Lq;
+  u.p0 = position(p.q_pos, b);
+  u.nq = (int32_t)p.Lq;
+  u.len = (int32_t)length(p.kv_len, b, p.Lk);
+  const int64_t at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)e * p.D;
+  u.src.k = static_cast<const S*>(p.k) + at;
+  u.src.v = static_cast<const S*>(p.v) + at;
+  u.src.row = p.ks[2];
+  u.src.row_bytes = (uint32_t)p.ks[2] * (uint32_t)sizeof(S);
+  return u;
+}
+template <typename T, typename S>
+__device__ __forceinline__ Unit<T, S, true> unit(const FwdParams& p, uint32_t n, uint32_t e, Unit<T, S, true>*) {
+  Unit<T, S, true> u;
+  const Rows r = new_rows(p.q_start, n, p.T);
+  const uint32_t h0 = e * p.grp;
+  u.q = static_cast<const T*>(p.q) + (int64_t)r.first * p.qs[2] + (int64_t)h0 * p.D;
+  u.o = static_cast<T*>(p.o) + (int64_t)r.first * p.os[2] + (int64_t)h0 * p.D;
+  u.lse = p.lse ? p.lse + (uint64_t)r.first * p.H + h0 : nullptr;
+  u.q_row = p.qs[2], u.o_row = p.os[2], u.lse_i = p.H, u.lse_h = 1;
+  u.p0 = (int64_t)p.kv_len[n] - r.n;
+  u.nq = min(r.n, (int32_t)p.Lq);
+  u.len = (int32_t)length(p.kv_len, n, p.Lk);
+  u.src.k = static_cast<const S*>(p.k) + (int64_t)e * p.ks[2];
+  u.src.v = static_cast<const S*>(p.v) + (int64_t)e * p.ks[2];
+  u.src.table = p.table + (uint64_t)n * p.max_pages;
+  u.src.ks = p.k_scale ? p.k_scale + e : nullptr;
+  u.src.vs = p.v_scale ? p.v_scale + e : nullptr;
+  u.src.page = p.ks[0], u.src.row = p.ks[1];
+  u.src.row_bytes = (uint32_t)p.ks[1] * (uint32_t)sizeof(S);
+  u.src.n_pages = p.n_pages, u.src.n_heads = p.Hkv, u.src.shift = p.shift;
+  return u;
+}
+
+// The softmax of QT blocks of 32 columns over NKT blocks of 32 keys at a time.
+// LAZY: the subtracted reference follows the running maximum only when it has to (it is
+// the maximum of the first tile until a tile's probabilities sum to more than 2^16);
+// otherwise every tile takes its maxima (few keys, and passes that memory bounds).
+template <typename T, int DC, int QT, int NKT, bool LAZY>
+struct Softmax {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  static constexpr float kMove = 65536.0f;
+  ColAcc<T, DC> o[QT];
+  float ref[QT], sum[QT];   // exp2 units; the sum of this lane's keys
+  bool set;                 // every column that sees a key has a reference
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+      o[j].zero();
+      ref[j] = -INFINITY;
+      sum[j] = 0.0f;
+    }
+    set = false;
+  }
+
+  // Scores of the tile from key0 in exp2 units, less `minus`.  mask: some column does not
+  // see some key of it; gone: bits of its groups of 16 keys that are not there.
+  template <typename KF, typename Q>
+  static __device__ __forceinline__ void scores(floatx16 (&s)[NKT][QT], const KF& kf, const Q& qf, int32_t key0, bool mask,
+                                                uint32_t gone, float c, const Seen (&cols)[QT],
+                                                const float (&minus)[QT], int lane) {
+    const int g = lane >> 5;
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int j = 0; j < QT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][j][r] = 0.0f;
+#pragma unroll
+    for (int st = 0; st < G::NS; ++st)
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        const auto a = kf(kt, st);
+#pragma unroll
+        for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(a, qf[j][st], s[kt][j]);
+      }
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int j = 0; j < QT; ++j)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[kt][j][r] = fmaf(s[kt][j][r], c, -minus[j]);
+    if (mask) {
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+          const int32_t at = key0 + 32 * kt + 4 * g;
+          const uint32_t from = (uint32_t)(at - cols[j].lo), width = (uint32_t)max(cols[j].hi - cols[j].lo, 0);
+          const int32_t left = cols[j].sink - at;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int k = 8 * (r / 4) + r % 4;
+            const bool off = gone >> (2 * kt + r / 8) & 1;
+            if (off || !(from + k < width || k < left)) s[kt][j][r] = -INFINITY;
+          }
+        }
+    }
+  }
+
+  // One tile: kf(kt, st) the fragments of its keys, vl its values in LDS.
+  template <typename KF, typename Q>
+  __device__ __forceinline__ void step(const KF& kf, const T* vl, const Q& qf, int32_t key0, bool mask, uint32_t gone,
+                                       float c, const Seen (&cols)[QT], int lane) {
+    ColB<T> pf[NKT][QT];
+    float add[QT];
+    bool move = !LAZY || !set;
+    if (LAZY && set) {
+      floatx16 s[NKT][QT];
+      float by[QT];
+#pragma unroll
+      for (int j = 0; j < QT; ++j) by[j] = ref[j] == -INFINITY ? 0.0f : ref[j];   // a column that sees nothing
+      scores(s, kf, qf, key0, mask, gone, c, cols, by, lane);
+      move = probabilities(s, pf, add);
+    }
+    if (!LAZY || __any(move)) {
+      // the scores themselves, their maxima, and the sums moved to those
+      floatx16 s[NKT][QT];
+      float zero[QT];
+#pragma unroll
+      for (int j = 0; j < QT; ++j) zero[j] = 0.0f;
+      scores(s, kf, qf, key0, mask, gone, c, cols, zero, lane);
+      bool all = true;
+#pragma unroll
+      for (int j = 0; j < QT; ++j) {
+        float m = s[0][j][0];
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kt][j][r]);
+        m = fmaxf(fmaxf(m, swap_halves(m)), ref[j]);
+        const float f = ref[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[j] - m);
+        sum[j] *= f;
+        o[j].scale(f, lane);
+        ref[j] = m;
+        all &= m != -INFINITY || !sees_any(cols[j]);
+        const float by = m == -INFINITY ? 0.0f : m;   // nothing yet: every score is -inf
+#pragma unroll
+        for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][j][r] -= by;
+      }
+      set = __all(all);
+      probabilities(s, pf, add);
+    }
+#pragma unroll
+    for (int j = 0; j < QT; ++j) sum[j] += add[j];
+#pragma unroll
+    for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+      for (int j = 0; j < QT; ++j) o[j].add(vl, 32 * kt, lane, pf[kt][j]);
+  }
+  // exp2 of the scores, as operands and summed; whether some column's are too large
+  static __device__ __forceinline__ bool probabilities(const floatx16 (&s)[NKT][QT], ColB<T> (&pf)[NKT][QT],
+                                                       float (&add)[QT]) {
+    bool over = false;
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+      float a = 0.0f;
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float e = __builtin_amdgcn_exp2f(s[kt][j][r]);
+          a += e;
+          pf[kt][j].set(r, e);
+        }
+      add[j] = a;
+      over |= a > kMove;
+    }
+    return over;
+  }
+};
+
+// What a block of columns does with a tile of KB keys: nothing, or with a mask, or all of it.
+struct Edges {
+  Seen first, last;
+  __device__ __forceinline__ bool none(int32_t key0, int32_t n) const {
+    return key0 >= last.sink && (key0 + n <= first.lo || key0 >= last.hi);
+  }
+  __device__ __forceinline__ bool all(int32_t key0, int32_t n) const {
+    return key0 + n <= first.sink || (key0 >= last.lo && key0 + n <= first.hi);
+  }
+};
+// The queries of columns c0 .. c0 + n - 1 of a unit (those that it has), as Edges.
+template <typename U>
+__device__ __forceinline__ Edges edges(const Window& w, const U& u, uint32_t grp, uint32_t c0, uint32_t n) {
+  const uint32_t cols = (uint32_t)u.nq * grp, c1 = min(c0 + n, cols) - 1;
+  return {seen(w, u.p0 + c0 / grp, u.len), seen(w, u.p0 + c1 / grp, u.len)};
+}
+
+// Many columns: QT blocks of 32 per wave, the keys in LDS tiles that all waves share,
+// the next tile on its way in registers.
+template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int MINW>
+__global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  using U = Unit<T, S, PAGED>;
+  using R = Rows16<T, S, DC>;
+  constexpr int NT = NW * 64, CB = NW * 32 * QT, NKT = KB / 32, GR = KB / 16;
+  constexpr int TILE = KB * G::P;
+  constexpr int NL = (2 * GR + NW - 1) / NW;   // group loads of a wave: K's groups, then V's
+  static_assert(2 * GR % NW == 0, "every wave loads the same");
+  static_assert(NW <= 4 * NKT, "the output rows fit the tiles");
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* lds = reinterpret_cast<T*>(smem);                       // [2][K, V][KB][P]
+  uint32_t* gone = reinterpret_cast<uint32_t*>(lds + 4 * TILE);   // [2][GR]: pages that are not there
+
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t un, e, blk;
+  if constexpr (PAGED) {
+    e = blockIdx.x % p.Hkv;
+    const uint32_t w = p.n_blk - 1 - blockIdx.x / p.Hkv;   // a sequence's last blocks have the most keys
+    un = __builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, p.grp, CB, 1, w, lane));
+    const int32_t at = (int32_t)w - first_piece(p.q_start, un, p.T, p.grp, CB, 1);
+    if (at < 0) return;
+    blk = (uint32_t)at;
+  } else {
+    const Place pl = place(p.order);
+    if (!pl.any) return;
+    un = pl.bx, e = pl.h, blk = p.order.blocks - 1 - pl.block;
+  }
+  const U u = unit<T, S>(p, un, e, (U*)nullptr);
+  const uint32_t cols = (uint32_t)u.nq * p.grp, c0 = blk * CB;
+  if (c0 >= cols || cols <= p.few_cols) return;
+  const int D = (int)p.D;
+  const Edges we = edges(p.win, u, p.grp, c0, CB);           // of the work-group
+  const Tiles<KB> tiles(we.first, we.last);
+
+  const typename R::Map map = R::map(D, u.src.row_bytes, lane);
+  R rows[NL];
+  float scale[NL];
+  bool lost[NL];
+  int32_t id[NL];
+  auto ask = [&](int32_t t) {      // the pages of this wave's groups
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+      id[i] = u.src.page_of(tiles.key0(t) + 16 * ((wave + i * NW) % GR), t < tiles.n ? we.last.hi : 0);
+  };
+  auto fetch = [&](int32_t t) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int li = wave + i * NW;
+      const int32_t key0 = tiles.key0(t) + 16 * (li % GR);
+      const auto gp = u.src.group(key0, id[i]);
+      scale[i] = li < GR ? gp.ks : gp.vs;
+      lost[i] = gp.gone;
+      rows[i].fetch(map, li < GR ? gp.k : gp.v, u.src.row_bytes, D, p.vec, [&](int r) {
+        const int32_t j = key0 + r;
+        return !gp.gone && (j < we.last.sink || (j >= we.first.lo && j < we.last.hi));
+      });
+    }
+  };
+  auto stash = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int li = wave + i * NW;
+      rows[i].stash(map, lds + buf * 2 * TILE + (li < GR ? 0 : TILE) + 16 * (li % GR) * G::P, scale[i]);
+      if (PAGED && li < GR && lane == 0) gone[buf * GR + li] = lost[i];
+    }
+  };
+  if (tiles.n) {
+    ask(0);
+    fetch(0);
+    ask(1);
+  }
+  typename M::frag qf[QT][G::NS];
+  Seen col[QT];
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    const uint32_t c = c0 + 32 * (wave * QT + j) + l32, cc = min(c, cols - 1), i = cc / p.grp, hh = cc - i * p.grp;
+    row_frags<T, DC>(c < cols ? u.q + (int64_t)i * u.q_row + (int64_t)hh * D : nullptr, g, D, p.vec, qf[j]);
+    col[j] = seen(p.win, u.p0 + i, u.len);
+  }
+  const uint32_t w0 = c0 + 32 * QT * wave;
+  const bool on = w0 < cols;
+  const Edges ed = edges(p.win, u, p.grp, min(w0, cols - 1), 32 * QT);   // of the wave
+  clear_pad<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
+  if (tiles.n) stash(0);
+  Softmax<T, DC, QT, NKT, true> sm;
+  sm.init();
+  __syncthreads();
+  for (int32_t it = 0; it < tiles.n; ++it) {
+    const int32_t key0 = tiles.key0(it);
+    const bool more = it + 1 < tiles.n;
+    if (more) {
+      fetch(it + 1);
+      ask(it + 2);
+    }
+    const int buf = it & 1;
+    const T* kl = lds + buf * 2 * TILE;
+    if (on && !ed.none(key0, KB)) {
+      uint32_t lost_bits = 0;
+      if constexpr (PAGED) {
+#pragma unroll
+        for (int i = 0; i < GR; ++i) lost_bits |= gone[buf * GR + i] << i;
+        lost_bits = __builtin_amdgcn_readfirstlane(lost_bits);
+      }
+      sm.step(
+          [&](int kt, int st) {
+            return *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
+          },
+          kl + TILE, qf, key0, lost_bits || !ed.all(key0, KB), lost_bits, p.c, col, lane);
+    }
+    if (more) stash(buf ^ 1);
+    __syncthreads();
+  }
+
+#pragma unroll
+  for (int j = 0; j < QT; ++j) {
+    const float l = sm.sum[j] + swap_halves(sm.sum[j]);
+    sm.o[j].scale(l == 0.0f ? 0.0f : 1.0f / l, lane);
+    const uint32_t j0 = c0 + 32 * (wave * QT + j);
+    auto row = [&](int n) -> T* {
+      const uint32_t c = j0 + n, i = c / p.grp;
+      return c < cols ? u.o + (int64_t)i * u.o_row + (int64_t)(c - i * p.grp) * D : nullptr;
+    };
+    if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, sm.o[j], lane, D, G::DP, row);
+    else store_rows<T, DC>(sm.o[j], lane, D, false, row);
+    const uint32_t c = j0 + l32, i = c / p.grp;
+    if (u.lse && g == 0 && c < cols)
+      u.lse[(int64_t)i * u.lse_i + (int64_t)(c - i * p.grp) * u.lse_h] =
+          l == 0.0f ? -INFINITY : kLn2 * (sm.ref[j] + log2f(l));
+  }
+}
+
+// Few columns: a block of 32 of them, the keys' tiles of 32 cut among work-groups and,
+// inside one, among its waves, each with LDS rows of its own and no barrier until the
+// waves' sums are joined.  A pass over a cache is bound by memory: what counts is how
+// many waves a CU holds, that each has its next tile on its way, and that every load
+// runs along rows.
+constexpr int kMinTiles = 4;   // of a work-group's wave, where the keys are cut
+struct Cut {                   // tiles of each part, and parts that have any
+  int32_t per, used;
+};
+__device__ __forceinline__ Cut cut(int32_t n, uint32_t n_split, int waves) {
+  Cut c;
+  const int32_t even = (n + (int32_t)n_split - 1) / (int32_t)n_split;
+  c.per = (max(even, kMinTiles * waves) + waves - 1) / waves * waves;
+  c.used = max((n + c.per - 1) / c.per, 1);
+  return c;
+}
+
+template <typename T, typename S, bool PAGED, int DC, int NW, int MINW>
+__global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  using U = Unit<T, S, PAGED>;
+  using R = Rows16<T, S, DC>;
+  constexpr int TILE = 32 * G::P;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  T* kl = reinterpret_cast<T*>(smem) + wave * 2 * TILE;   // [NW][K, V][32][P]
+  T* vl = kl + TILE;
+
+  // an XCD takes the heads of a stretch of keys, which together read whole token rows
+  const uint32_t he = p.Hkv * p.cblk, j8 = blockIdx.x >> 3, piece = j8 / he * 8 + (blockIdx.x & 7u);
+  if (piece >= p.pieces) return;
+  const uint32_t ec = j8 % he, e = ec / p.cblk, cb = ec - e * p.cblk;
+  const uint32_t un = piece / p.n_split, split = piece - un * p.n_split;
+  const U u = unit<T, S>(p, un, e, (U*)nullptr);
+  const uint32_t cols = (uint32_t)u.nq * p.grp, c0 = 32 * cb;
+  if (c0 >= cols || cols > p.few_cols) return;
+  const uint32_t nc = min(cols - c0, 32u);
+  const int D = (int)p.D;
+  const Edges ed = edges(p.win, u, p.grp, c0, 32);
+  const Tiles<32> tiles(ed.first, ed.last);
+  const Cut part = cut(tiles.n, p.n_split, NW);
+  if ((int32_t)split >= part.used) return;
+  const int32_t t1 = min(tiles.n, ((int32_t)split + 1) * part.per);
+
+  const typename R::Map map = R::map(D, u.src.row_bytes, lane);
+  R rk[2], rv[2];
+  float ks[2], vs[2];
+  int32_t id[2];
+  uint32_t lost = 0;
+  auto ask = [&](int32_t t) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) id[i] = u.src.page_of(tiles.key0(t) + 16 * i, t < t1 ? ed.last.hi : 0);
+  };
+  auto fetch = [&](int32_t t) {
+    lost = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int32_t key0 = tiles.key0(t) + 16 * i;
+      const auto gp = u.src.group(key0, id[i]);
+      ks[i] = gp.ks, vs[i] = gp.vs;
+      lost |= (gp.gone ? 1u : 0u) << i;
+      auto on = [&](int r) {
+        const int32_t j = key0 + r;
+        return !gp.gone && (j < ed.last.sink || (j >= ed.first.lo && j < ed.last.hi));
+      };
+      rk[i].fetch(map, gp.k, u.src.row_bytes, D, p.vec, on);
+      rv[i].fetch(map, gp.v, u.src.row_bytes, D, p.vec, on);
+    }
+  };
+  const int32_t mine = (int32_t)split * part.per + wave;
+  if (mine < t1) {
+    ask(mine);
+    fetch(mine);
+    ask(mine + NW);
+  }
+  clear_pad<T, DC>(kl, 64, D, lane, 64);
+  const uint32_t c = c0 + min((uint32_t)l32, nc - 1), ci = c / p.grp, ch = c - ci * p.grp;
+  typename M::frag qf[1][G::NS];
+  row_frags<T, DC>((uint32_t)l32 < nc ? u.q + (int64_t)ci * u.q_row + (int64_t)ch * D : nullptr, g, D, p.vec, qf[0]);
+  const Seen col[1] = {seen(p.win, u.p0 + ci, u.len)};
+
+  Softmax<T, DC, 1, 1, false> sm;
+  sm.init();
+  for (int32_t t = mine; t < t1; t += NW) {
+    wave_order();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      rk[i].stash(map, kl + 16 * i * G::P, ks[i]);
+      rv[i].stash(map, vl + 16 * i * G::P, vs[i]);
+    }
+    const uint32_t was_lost = lost;
+    wave_order();
+    if (t + NW < t1) {
+      fetch(t + NW);
+      ask(t + 2 * NW);
+    }
+    const int32_t key0 = tiles.key0(t);
+    sm.step(
+        [&](int, int st) {
+          return *reinterpret_cast<const typename M::frag*>(kl + l32 * G::P + 2 * G::E * st + G::E * g);
+        },
+        vl, qf, key0, was_lost || !ed.all(key0, 32), was_lost, p.c, col, lane);
+  }
+  float l = sm.sum[0] + swap_halves(sm.sum[0]);
+
+  // the waves' columns meet at the largest of their references, and are added in the
+  // waves' order; the tiles are done with
+  auto out = [&](uint32_t n) {
+    const uint32_t k = c0 + n, i = k / p.grp;
+    return u.o + (int64_t)i * u.o_row + (int64_t)(k - i * p.grp) * D;
+  };
+  auto put_lse = [&](uint32_t n, float m, float s) {
+    const uint32_t k = c0 + n, i = k / p.grp;
+    if (u.lse)
+      u.lse[(int64_t)i * u.lse_i + (int64_t)(k - i * p.grp) * u.lse_h] = s == 0.0f ? -INFINITY : kLn2 * (m + log2f(s));
+  };
+  if constexpr (NW == 1) {
+    if (part.used == 1) {
+      sm.o[0].scale(l == 0.0f ? 0.0f : 1.0f / l, lane);
+      wave_order();
+      auto row = [&](int n) -> T* { return (uint32_t)n < nc ? out(n) : nullptr; };
+      if (p.vec) store_rows_lds<T, DC>(vl, sm.o[0], lane, D, G::DP, row);
+      else store_rows<T, DC>(sm.o[0], lane, D, false, row);
+      if (g == 0 && (uint32_t)l32 < nc) put_lse(l32, sm.ref[0], l);
+      return;
+    }
+  }
+  __syncthreads();
+  float* ms = reinterpret_cast<float*>(smem);   // [NW][32] references, [NW][32] sums, [2][32] joined
+  if (g == 0) {
+    ms[wave * 32 + l32] = sm.ref[0];
+    ms[(NW + wave) * 32 + l32] = l;
+  }
+  __syncthreads();
+  float top = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) top = fmaxf(top, ms[w * 32 + l32]);
+  const float base = top == -INFINITY ? 0.0f : top;
+  l = 0.0f;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) l += __builtin_amdgcn_exp2f(ms[w * 32 + l32] - base) * ms[(NW + w) * 32 + l32];
+  sm.o[0].scale(__builtin_amdgcn_exp2f(sm.ref[0] - base), lane);
+  float* rows = ms + (2 * NW + 2) * 32;   // [NW][nc][DP]
+  store_rows<T, DC>(sm.o[0], lane, G::DP, true, [&](int n) -> float* {
+    return (uint32_t)n < nc ? rows + (wave * nc + n) * G::DP : nullptr;
+  });
+  if (wave == 0 && g == 0) {
+    ms[2 * NW * 32 + l32] = top;
+    ms[(2 * NW + 1) * 32 + l32] = l;
+  }
+  __syncthreads();
+  // maxima, sums, rows of 32 columns
+  float* to = p.part + (((uint64_t)un * he + ec) * p.n_split + split) * 32 * (2 + p.D);
+  for (uint32_t i = threadIdx.x; i < nc * p.D; i += NW * 64) {
+    const uint32_t n = i / p.D, d = i - n * p.D;
+    float v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) v += rows[(w * nc + n) * G::DP + d];
+    const float s = ms[(2 * NW + 1) * 32 + n];
+    if (part.used > 1) to[64 + i] = v;
+    else out(n)[d] = (T)(s == 0.0f ? 0.0f : v / s);
+  }
+  if (threadIdx.x < nc) {
+    const float m = ms[2 * NW * 32 + threadIdx.x], s = ms[(2 * NW + 1) * 32 + threadIdx.x];
+    if (part.used > 1) to[threadIdx.x] = m, to[32 + threadIdx.x] = s;
+    else put_lse(threadIdx.x, m, s);
+  }
+}
+
+// Joins the parts of one column: with their references m_s, sums l_s and rows o_s,
+// o = sum 2^(m_s - m) o_s / sum 2^(m_s - m) l_s.  A work-group per column; 256 / DP groups
+// of threads take every such part, and their sums are added in order.
+constexpr int kMaxSplit = 512;
+template <typename T, typename S, bool PAGED, int DP>
+__global__ __launch_bounds__(256) void window_join_kernel(FwdParams p, int waves) {
+  constexpr int GR = 256 / DP;
+  __shared__ float f[kMaxSplit], red[256], m4[4];
+  using U = Unit<T, S, PAGED>;
+  const uint32_t he = p.Hkv * p.cblk, n = blockIdx.x & 31u, uec = blockIdx.x >> 5, un = uec / he, ec = uec - un * he;
+  const uint32_t e = ec / p.cblk, cb = ec - e * p.cblk;
+  const U u = unit<T, S>(p, un, e, (U*)nullptr);
+  const uint32_t cols = (uint32_t)u.nq * p.grp, c = 32 * cb + n;
+  if (c >= cols || cols > p.few_cols) return;
+  const Edges ed = edges(p.win, u, p.grp, 32 * cb, 32);
+  const Tiles<32> tiles(ed.first, ed.last);
+  const uint32_t used = (uint32_t)cut(tiles.n, p.n_split, waves).used;
+  if (used == 1) return;
+  const uint32_t stride = 32 * (2 + p.D);
+  const float* w = p.part + (uint64_t)uec * p.n_split * stride;
+  float m = -INFINITY;
+  for (uint32_t s = threadIdx.x; s < used; s += 256) {
+    f[s] = w[(uint64_t)s * stride + n];
+    m = fmaxf(m, f[s]);
+  }
+#pragma unroll
+  for (int off = 32; off; off >>= 1) m = fmaxf(m, __shfl_xor(m, off));
+  if ((threadIdx.x & 63) == 0) m4[threadIdx.x >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+  const float top = m == -INFINITY ? 0.0f : m;
+  for (uint32_t s = threadIdx.x; s < used; s += 256) f[s] = __builtin_amdgcn_exp2f(f[s] - top);   // no keys: 0
+  __syncthreads();
+  const uint32_t d = threadIdx.x % DP, gr = threadIdx.x / DP;
+  float a = 0.0f, l = 0.0f;
+  if (d < p.D) {
+#pragma unroll 4
+    for (uint32_t s = gr; s < used; s += GR) {
+      const float* ws = w + (uint64_t)s * stride;
+      l += f[s] * ws[32 + n];
+      a += f[s] * ws[64 + n * p.D + d];
+    }
+  }
+  red[threadIdx.x] = a;
+  __syncthreads();
+  if (gr == 0) {
+#pragma unroll
+    for (int i = 1; i < GR; ++i) a += red[i * DP + d];
+  }
+  __syncthreads();
+  red[threadIdx.x] = l;
+  __syncthreads();
+  if (gr || d >= p.D) return;
+#pragma unroll
+  for (int i = 1; i < GR; ++i) l += red[i * DP + d];
+  const uint32_t i = c / p.grp, hh = c - i * p.grp;
+  u.o[(int64_t)i * u.o_row + (int64_t)hh * p.D + d] = (T)(l == 0.0f ? 0.0f : a / l);
+  if (u.lse && d == 0)
+    u.lse[(int64_t)i * u.lse_i + (int64_t)hh * u.lse_h] = l == 0.0f ? -INFINITY : kLn2 * (top + log2f(l));
+}
+
+template <typename K>
+int launch(K* kernel, int64_t blocks, int threads, size_t lds, FwdParams& p, hipStream_t s) {
+  if (!grid_fits(blocks, threads)) return DSP_ERR_SHAPE;
+  if (lds > 64 * 1024) {
+    const hipError_t e =
+        hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return DSP_ERR_HIP;
+  }
+  kernel<<<dim3((uint32_t)blocks), threads, lds, s>>>(p);
+  return last_launch_status();
+}
+
+template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int MINW>
+int start_many(FwdParams& p, const WindowArgs& a, hipStream_t s) {
+  constexpr int CB = NW * 32 * QT;
+  int64_t blocks;
+  if (PAGED) {
+    p.n_blk = (uint32_t)(a.T * p.grp / CB + a.B);
+    blocks = (int64_t)p.n_blk * a.Hkv;
+  } else {
+    p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
+    blocks = order_blocks(p.order);
+  }
+  const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T) + 2 * (KB / 16) * 4;
+  return launch(window_fwd_kernel<T, S, PAGED, DC, NW, QT, KB, MINW>, blocks, NW * 64, lds, p, s);
+}
+
+template <typename T, typename S, bool PAGED, int DC, int NW>
+int start_few(FwdParams& p, const WindowArgs& a, hipStream_t s) {
+  constexpr int MINW = sizeof(T) == 4 ? 1 : DC <= 80 ? 3 : 2;
+  size_t lds = (size_t)NW * 2 * 32 * Geo<T, DC>::P * sizeof(T);
+  lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * 32 * Geo<T, DC>::DP) * 4);
+  const int64_t pieces = a.B * a.X * p.n_split;
+  p.pieces = (uint32_t)pieces;
+  int st = launch(window_few_kernel<T, S, PAGED, DC, NW, MINW>, (pieces + 7) / 8 * 8 * a.Hkv * p.cblk, NW * 64, lds, p, s);
+  if (st != DSP_OK || p.n_split == 1) return st;
+  const int64_t cols = a.B * a.X * a.Hkv * p.cblk * 32;   // few units: they are why the keys are split
+  if (!grid_fits(cols, 256)) return DSP_ERR_SHAPE;
+  if (a.D <= 64) window_join_kernel<T, S, PAGED, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
+  else window_join_kernel<T, S, PAGED, 128><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
+  return last_launch_status();
+}
+
+// How a call is cut: whether units of few columns have a launch of their own, and into
+// how many parts their keys go at most.
+struct Choice {
+  bool few, many;
+  int64_t cblk, n_split;
+};
+inline Choice choose(const WindowArgs& a) {
+  Choice c = {};
+  const int64_t grp = a.H / a.Hkv, cols = a.Lq * grp;
+  c.few = grp <= 32;
+  c.many = cols > 32;
+  if (c.many && !(a.page_shift && a.B > 1)) c.few = false;
+  c.cblk = 1;
+  c.n_split = 1;
+  if (!c.few) return c;
+  // keys that a block of columns can see
+  int64_t keys = a.Lk;
+  if (a.win.left >= 0 && a.win.right >= 0)
+    keys = std::min<int64_t>(keys, (int64_t)a.win.left + a.win.right + a.win.sinks + 64);
+  const int64_t units = std::max<int64_t>(a.B * a.X * a.Hkv, 1);
+  const int64_t n = std::min<int64_t>({(256 * 8 + units - 1) / units, keys / 256, kMaxSplit});
+  if (n > 1) c.n_split = n;
+  return c;
+}
+inline size_t part_bytes(const WindowArgs& a) {
+  const Choice c = choose(a);
+  return c.n_split > 1 ? (size_t)(a.B * a.X * a.Hkv * c.cblk * c.n_split) * 32 * (2 + (size_t)a.D) * 4 : 0;
+}
+
+template <typename T, typename S, bool PAGED, int DC>
+int start(FwdParams& p, const WindowArgs& a, const Choice& c, hipStream_t s) {
+  p.few_cols = c.few ? 32 : 0;
+  p.cblk = (uint32_t)c.cblk;
+  p.n_split = (uint32_t)c.n_split;
+  if (c.few) {
+    if (int st = start_few<T, S, PAGED, DC, 4>(p, a, s)) return st;
+  }
+  if (!c.many) return DSP_OK;
+  constexpr bool B16 = sizeof(T) == 2;
+  return start_many<T, S, PAGED, DC, 4, 1, B16 ? 64 : 32, B16 ? (DC <= 64 ? 3 : 2) : 1>(p, a, s);
+}
+
+inline FwdParams params(const WindowArgs& a) {
+  FwdParams p = {};
+  p.q = a.q, p.k = a.k, p.v = a.v, p.o = a.o, p.lse = a.lse, p.part = a.workspace;
+  p.q_pos = a.q_pos, p.kv_len = a.kv_len, p.q_start = a.q_start, p.table = a.table;
+  p.k_scale = a.k_scale, p.v_scale = a.v_scale;
+  for (int i = 0; i < 3; ++i) p.qs[i] = a.q_strides[i], p.ks[i] = a.kv_strides[i], p.os[i] = a.o_strides[i];
+  p.win = a.win;
+  p.X = (uint32_t)a.X, p.H = a.H, p.Hkv = a.Hkv, p.grp = a.H / a.Hkv, p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk;
+  p.D = a.D;
+  p.N = (uint32_t)a.B, p.T = (uint32_t)a.T, p.n_pages = (uint32_t)a.n_pages, p.max_pages = (uint32_t)a.max_pages;
+  p.shift = a.page_shift;
+  p.c = a.scale * kLog2e;
+  p.vec = a.vec;
+  return p;
+}
+
+}  // namespace
+}  // namespace dsp

@@ -123,6 +123,71 @@ int launch_attn_relpos(const RelposArgs& a, hipStream_t s);
 size_t attn_relpos_bwd_workspace_bytes(const RelposArgs& a);
 int launch_attn_relpos_bwd(const RelposArgs& a, hipStream_t s);
 
+// Attention with a window and first tokens that stay visible (attn_window.hip), its
+// gradient (attn_window_bwd.hip) and the same over a paged cache (attn_paged.hip).
+struct Window {
+  int32_t left, right, sinks;   // left, right < 0: no bound
+};
+constexpr int kWindowMaxD = 128;
+struct WindowArgs {
+  const void* q;
+  const void* k;           // [B, X, Lk] rows, or pages
+  const void* v;
+  void* o;
+  float* lse;              // [B * X * H][Lq], pages: [T][H]; or null
+  const int32_t* q_pos;    // [B] or null
+  const int32_t* kv_len;   // [B] or null; pages: [B]
+  float* workspace;
+  int64_t B, X, Lq, Lk;    // pages: sequences, 1, most new tokens of one, positions of a table's row
+  int H, Hkv, D;
+  int64_t q_strides[3], kv_strides[3], o_strides[3];   // pages: kv by page, slot, head; q, o: the last one
+  Window win;
+  float scale;
+  bool bf16, vec;          // vec: as in RelposArgs
+  // gradient
+  const void* dout;
+  void* dq;
+  void* dk;
+  void* dv;
+  // pages
+  const int32_t* q_start;  // [B + 1]
+  const int32_t* table;    // [B][max_pages]
+  const float* k_scale;    // [n_pages][Hkv], e4m3 only
+  const float* v_scale;
+  int64_t T, n_pages, max_pages;
+  int page_shift;
+  bool e4m3;
+};
+size_t attn_window_workspace_bytes(const WindowArgs& a);
+int launch_attn_window(const WindowArgs& a, hipStream_t s);
+size_t attn_paged_workspace_bytes(const WindowArgs& a);
+int launch_attn_paged(const WindowArgs& a, hipStream_t s);
+size_t attn_window_bwd_workspace_bytes(const WindowArgs& a);
+int launch_attn_window_bwd(const WindowArgs& a, hipStream_t s);
+
+// New keys and values into a paged cache, keys and queries turned on the way (kv_append.hip).
+struct AppendArgs {
+  const void* k;           // [T] rows
+  const void* v;
+  const void* q;           // or null
+  void* yq;
+  void* k_cache;
+  void* v_cache;
+  float* k_scale;
+  float* v_scale;
+  const int32_t* table;
+  const int32_t* q_start;
+  const int32_t* kv_len;
+  const int32_t* pos;      // [T] or null
+  const float* cos;
+  const float* sin;
+  int64_t N, T, P, n_pages, max_pages, k_row, v_row, q_row, y_row;
+  int64_t cache_strides[3];   // page, slot, head
+  int H, Hkv, D, rot, page_shift;
+  bool half, bf16, e4m3, vec;
+};
+int launch_kv_append(const AppendArgs& a, hipStream_t s);
+
 // Norm of queries and keys for each head with the position rotation, and its
 // gradient (qk_norm.hip).  Row (b, x, l, head) of x (and dy, y) sits at
 // b * st[0] + x * st[1] + l * st[2] + head * D.  part: qk_norm_workspace_bytes()
