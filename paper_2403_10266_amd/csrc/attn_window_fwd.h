@@ -190,7 +190,7 @@ struct Softmax {
 #pragma unroll
       for (int j = 0; j < QT; ++j) zero[j] = 0.0f;
       scores(s, kf, qf, key0, mask, gone, c, cols, zero, lane);
-      bool all = true;
+      bool have[QT];
 #pragma unroll
       for (int j = 0; j < QT; ++j) {
         float m = s[0][j][0];
@@ -203,15 +203,22 @@ struct Softmax {
         sum[j] *= f;
         o[j].scale(f, lane);
         ref[j] = m;
-        all &= m != -INFINITY || !sees_any(cols[j]);
+        have[j] = m != -INFINITY || !sees_any(cols[j]);
         const float by = m == -INFINITY ? 0.0f : m;   // nothing yet: every score is -inf
 #pragma unroll
         for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[kt][j][r] -= by;
       }
-      set = __all(all);
       probabilities(s, pf, add);
+      // a column that is not finite has all it will have: the others' way is the same
+      bool all = true;
+#pragma unroll
+      for (int j = 0; j < QT; ++j) {
+        const float both = add[j] + swap_halves(add[j]);
+        all &= have[j] || both != both;
+      }
+      set = __all(all);
     }
 #pragma unroll
     for (int j = 0; j < QT; ++j) sum[j] += add[j];
