@@ -15,6 +15,7 @@ int run_bf16(const WindowArgs& a, hipStream_t s) {
   if (a.D <= 32) return run<bf16, S, 32>(a, s);
   if (a.D <= 48) return run<bf16, S, 48>(a, s);
   if (a.D <= 64) return run<bf16, S, 64>(a, s);
+  if (a.D <= 72) return run<bf16, S, 72>(a, s);
   if (a.D <= 80) return run<bf16, S, 80>(a, s);
   if (a.D <= 96) return run<bf16, S, 96>(a, s);
   return run<bf16, S, 128>(a, s);

@@ -125,6 +125,42 @@ __device__ __forceinline__ void slab_mma(const bf16* t, int pitch, int row0, int
   acc[1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8, b1), acc[1], 0, 0, 0);
 }
 
+// The A operands of a column product over 32 rows of t from row0, read ahead of it.
+template <typename T, int DC>
+struct ColA;
+template <int DC>
+struct ColA<bf16, DC> {
+  using G = Geo<bf16, DC>;
+  bf16x8 t[G::NT > 0 ? G::NT : 1][2], s;
+  static __device__ __forceinline__ bf16x8 read(const bf16* at) {
+    const shortx4 lo = lds_read_tr(at), hi = lds_read_tr(at + 8 * G::P);
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  __device__ __forceinline__ void load(const bf16* lds, int row0, int lane) {
+    const int j16 = lane & 15, g = lane >> 5, c = lane >> 4;
+    const bf16* at = lds + (row0 + 4 * g + (j16 >> 2)) * G::P + 16 * (c & 1) + 4 * (j16 & 3);
+#pragma unroll
+    for (int i = 0; i < G::NT; ++i)
+#pragma unroll
+      for (int kk = 0; kk < 2; ++kk) t[i][kk] = read(at + 16 * kk * G::P + 32 * i);
+    if constexpr (G::SLAB)
+      s = read(lds + (row0 + ((c & 1) ? 16 : 0) + ((c & 2) ? 4 : 0) + (j16 >> 2)) * G::P + 32 * G::NT + 4 * (j16 & 3));
+  }
+};
+// the slab's B operands (as in slab_mma)
+__device__ __forceinline__ void slab_b(const ColB<bf16>& b, bf16x8 (&out)[2]) {
+  const u32x4 x = __builtin_bit_cast(u32x4, b.v[0]), y = __builtin_bit_cast(u32x4, b.v[1]);
+  u32x4 b0, b1;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x[w], y[w], false, false);
+    b0[w] = r[0];
+    b1[w] = r[1];
+  }
+  out[0] = __builtin_bit_cast(bf16x8, b0);
+  out[1] = __builtin_bit_cast(bf16x8, b1);
+}
+
 // The accumulators of a column product for one 32-row block: its tiles and slab.
 template <typename T, int DC>
 struct ColAcc {
@@ -145,6 +181,19 @@ struct ColAcc {
 #pragma unroll
     for (int i = 0; i < G::NT; ++i) t[i] = col_mma(lds, G::P, row0, 32 * i, lane, b, t[i]);
     if constexpr (G::SLAB) slab_mma(lds, G::P, row0, 32 * G::NT, lane, b, s);
+  }
+  __device__ __forceinline__ void add(const ColA<T, DC>& a, const ColB<T>& b) {
+    static_assert(sizeof(T) == 2, "operands read ahead are bf16");
+#pragma unroll
+    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+      for (int i = 0; i < G::NT; ++i) t[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.t[i][kk], b.v[kk], t[i], 0, 0, 0);
+    if constexpr (G::SLAB) {
+      bf16x8 half[2];
+      slab_b(b, half);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.s, half[h], s[h], 0, 0, 0);
+    }
   }
   // times a factor that each lane holds for its own column n = lane % 32
   __device__ __forceinline__ void scale(float f, int lane) {

@@ -25,6 +25,15 @@ __device__ __forceinline__ Seen seen(const Window& w, int64_t p, int32_t len) {
 __device__ __forceinline__ bool sees(const Seen& s, int32_t j) {
   return j < s.sink || (j >= s.lo && j < s.hi);
 }
+// 16 keys from key0 that all, or some, of the queries between two see, in full
+__device__ __forceinline__ bool whole_group(const Seen& first, const Seen& last, int32_t key0) {
+  return key0 + 16 <= last.sink || (key0 >= first.lo && key0 + 16 <= last.hi);
+}
+// bit i: whether key key0 + i is seen
+__device__ __forceinline__ uint32_t seen_bits(const Seen& s, int32_t key0) {
+  auto below = [](int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
+  return below(s.sink - key0) | (below(s.hi - key0) & ~below(s.lo - key0));
+}
 __device__ __forceinline__ bool sees_any(const Seen& s) { return s.sink > 0 || s.lo < s.hi; }
 
 // The keys that the queries between two see, in tiles of KB: `sinks` tiles from key 0,
@@ -59,7 +68,8 @@ struct Rows16 {
   R pre[N];
 
   struct Map {
-    uint32_t at, row, step;   // byte offset of the first chunk, its row, rows of a pass
+    uint32_t at[N];           // byte offset of each pass's chunk, kNone for a lane without one
+    uint32_t row, step;       // the first one's row, rows of a pass
     int to, col;              // element offset in LDS
   };
   static __device__ __forceinline__ Map map(int D, uint32_t row_bytes, uint32_t lane) {
@@ -69,27 +79,36 @@ struct Rows16 {
     m.row = lane / ch;
     const uint32_t col = lane - m.row * ch;
     if (m.row >= m.step) m.row = 16;   // a lane without chunks
-    m.at = m.row * row_bytes + col * (uint32_t)(E * sizeof(S));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t row = m.row + i * m.step;
+      m.at[i] = row < 16 ? row * row_bytes + col * (uint32_t)(E * sizeof(S)) : kNone;
+    }
     m.col = (int)(col * E);
     m.to = (int)(m.row * G::P) + m.col;
     return m;
   }
+  // whole: all 16 rows are taken, and nothing is asked of `on`
   template <typename F>
-  __device__ __forceinline__ void fetch(const Map& m, const S* base, uint32_t row_bytes, int D, bool vec, F on) {
+  __device__ __forceinline__ void fetch(const Map& m, const S* base, int D, bool vec, bool whole, F on) {
     const __amdgpu_buffer_rsrc_t rs = make_rsrc(base, 0x7FFFFFF0u);
+    if (whole) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const uint32_t row = m.row + i * m.step;
-      const uint32_t off = row < 16 && on((int)row) ? m.at + i * m.step * row_bytes : kNone;
-      if constexpr (sizeof(S) == 1) {
-        pre[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
-      } else if (sizeof(T) == 2 || vec) {
-        pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
-      } else {
+      for (int i = 0; i < N; ++i) load(rs, i, m, m.at[i], D, vec);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          pre[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, m.col + e < D && off != kNone ? off + 4u * e : kNone, 0, 0);
-      }
+      for (int i = 0; i < N; ++i) load(rs, i, m, on((int)(m.row + i * m.step)) ? m.at[i] : kNone, D, vec);
+    }
+  }
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t rs, int i, const Map& m, uint32_t off, int D, bool vec) {
+    if constexpr (sizeof(S) == 1) {
+      pre[i] = __builtin_amdgcn_raw_buffer_load_b64(rs, off, 0, 0);
+    } else if (sizeof(T) == 2 || vec) {
+      pre[i] = __builtin_amdgcn_raw_buffer_load_b128(rs, off, 0, 0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        pre[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, m.col + e < D && off != kNone ? off + 4u * e : kNone, 0, 0);
     }
   }
   __device__ __forceinline__ void stash(const Map& m, T* lds, float scale) const {

@@ -18,6 +18,7 @@ int launch_attn_window(const WindowArgs& a, hipStream_t s) {
     if (a.D <= 32) return run<bf16, 32>(a, s);
     if (a.D <= 48) return run<bf16, 48>(a, s);
     if (a.D <= 64) return run<bf16, 64>(a, s);
+    if (a.D <= 72) return run<bf16, 72>(a, s);
     if (a.D <= 80) return run<bf16, 80>(a, s);
     if (a.D <= 96) return run<bf16, 96>(a, s);
     return run<bf16, 128>(a, s);

@@ -84,7 +84,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
     for (int i = 0; i < NL; ++i) {
       const int li = wave + i * NW;
       const int32_t key0 = tiles.key0(t) + 16 * (li % GR);
-      rows[i].fetch(map, (li < GR ? kg : vg) + (int64_t)key0 * p.ks[2], row_bytes, D, p.vec, [&](int r) {
+      rows[i].fetch(map, (li < GR ? kg : vg) + (int64_t)key0 * p.ks[2], D, p.vec, whole_group(first, last, key0), [&](int r) {
         const int32_t j = key0 + r;
         return j < last.sink || (j >= first.lo && j < last.hi);
       });

@@ -100,17 +100,24 @@ __device__ __forceinline__ Unit<T, S, true> unit(const FwdParams& p, uint32_t n,
   return u;
 }
 
-// The softmax of QT blocks of 32 columns over NKT blocks of 32 keys at a time.
-// LAZY: the subtracted reference follows the running maximum only when it has to (it is
-// the maximum of the first tile until a tile's probabilities sum to more than 2^16);
-// otherwise every tile takes its maxima (few keys, and passes that memory bounds).
+// The softmax of QT blocks of 32 columns over NKT blocks of 32 keys at a time, less a
+// reference of each column (exp2 units).
+//  * exact(): takes the tile's maxima and moves the references to them.
+//  * fast() (LAZY): the references stay, 64 above the maximum of the tiles that set them, and
+//    probabilities are cut at 1, so that nothing stands between the exponentials and the
+//    product with v.  A score above its reference shows afterwards, as a sum of a half or
+//    more (probabilities below it add up to far less); then, rarely, fix() moves the
+//    reference and adds to the tile's probabilities what the cut took from them.
+// Sums are those of the fp32 probabilities (of the rounded ones, which a column of ones in v
+// would give with the product, the log-sum-exp would be off by their roundings: 9 times its
+// bound at 64 keys).
 template <typename T, int DC, int QT, int NKT, bool LAZY>
 struct Softmax {
   using G = Geo<T, DC>;
   using M = Mx<T>;
-  static constexpr float kMove = 65536.0f;
+  static constexpr float kRoom = LAZY ? 64.0f : 0.0f;
   ColAcc<T, DC> o[QT];
-  float ref[QT], sum[QT];   // exp2 units; the sum of this lane's keys
+  float ref[QT], sum[QT];   // the sum of this lane's keys
   bool set;                 // every column that sees a key has a reference
 
   __device__ __forceinline__ void init() {
@@ -122,6 +129,8 @@ struct Softmax {
     }
     set = false;
   }
+  // a column's sum over all keys
+  __device__ __forceinline__ float total(int j) const { return sum[j] + swap_halves(sum[j]); }
 
   // Scores of the tile from key0 in exp2 units, less `minus`.  mask: some column does not
   // see some key of it; gone: bits of its groups of 16 keys that are not there.
@@ -129,7 +138,6 @@ struct Softmax {
   static __device__ __forceinline__ void scores(floatx16 (&s)[NKT][QT], const KF& kf, const Q& qf, int32_t key0, bool mask,
                                                 uint32_t gone, float c, const Seen (&cols)[QT],
                                                 const float (&minus)[QT], int lane) {
-    const int g = lane >> 5;
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
@@ -145,107 +153,200 @@ struct Softmax {
         for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(a, qf[j][st], s[kt][j]);
       }
 #pragma unroll
-    for (int kt = 0; kt < NKT; ++kt)
+    for (int kt = 0; kt < NKT; ++kt) finish(s[kt], kt, key0, mask, gone, c, cols, minus, lane);
+  }
+  static __device__ __forceinline__ void scale(floatx16 (&s)[QT], float c, const float (&minus)[QT]) {
 #pragma unroll
-      for (int j = 0; j < QT; ++j)
+    for (int j = 0; j < QT; ++j)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[kt][j][r] = fmaf(s[kt][j][r], c, -minus[j]);
-    if (mask) {
+      for (int r = 0; r < 16; ++r) s[j][r] = fmaf(s[j][r], c, -minus[j]);
+  }
+  // products of block kt made scores
+  static __device__ __forceinline__ void finish(floatx16 (&s)[QT], int kt, int32_t key0, bool mask, uint32_t gone, float c,
+                                                const Seen (&cols)[QT], const float (&minus)[QT], int lane) {
+    scale(s, c, minus);
+    if (!mask) return;
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt)
+    for (int j = 0; j < QT; ++j) {
+      const int32_t at = key0 + 32 * kt + 4 * (lane >> 5);
+      const uint32_t from = (uint32_t)(at - cols[j].lo), width = (uint32_t)max(cols[j].hi - cols[j].lo, 0);
+      const int32_t left = cols[j].sink - at;
 #pragma unroll
-        for (int j = 0; j < QT; ++j) {
-          const int32_t at = key0 + 32 * kt + 4 * g;
-          const uint32_t from = (uint32_t)(at - cols[j].lo), width = (uint32_t)max(cols[j].hi - cols[j].lo, 0);
-          const int32_t left = cols[j].sink - at;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int k = 8 * (r / 4) + r % 4;
-            const bool off = gone >> (2 * kt + r / 8) & 1;
-            if (off || !(from + k < width || k < left)) s[kt][j][r] = -INFINITY;
-          }
-        }
+      for (int r = 0; r < 16; ++r) {
+        const int k = 8 * (r / 4) + r % 4;
+        const bool off = gone >> (2 * kt + r / 8) & 1;
+        if (off || !(from + k < width || k < left)) s[j][r] = -INFINITY;
+      }
     }
   }
-
-  // One tile: kf(kt, st) the fragments of its keys, vl its values in LDS.
-  template <typename KF, typename Q>
-  __device__ __forceinline__ void step(const KF& kf, const T* vl, const Q& qf, int32_t key0, bool mask, uint32_t gone,
-                                       float c, const Seen (&cols)[QT], int lane) {
-    ColB<T> pf[NKT][QT];
-    float add[QT];
-    bool move = !LAZY || !set;
-    if (LAZY && set) {
-      floatx16 s[NKT][QT];
-      float by[QT];
-#pragma unroll
-      for (int j = 0; j < QT; ++j) by[j] = ref[j] == -INFINITY ? 0.0f : ref[j];   // a column that sees nothing
-      scores(s, kf, qf, key0, mask, gone, c, cols, by, lane);
-      move = probabilities(s, pf, add);
-    }
-    if (!LAZY || __any(move)) {
-      // the scores themselves, their maxima, and the sums moved to those
-      floatx16 s[NKT][QT];
-      float zero[QT];
-#pragma unroll
-      for (int j = 0; j < QT; ++j) zero[j] = 0.0f;
-      scores(s, kf, qf, key0, mask, gone, c, cols, zero, lane);
-      bool have[QT];
-#pragma unroll
-      for (int j = 0; j < QT; ++j) {
-        float m = s[0][j][0];
-#pragma unroll
-        for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kt][j][r]);
-        m = fmaxf(fmaxf(m, swap_halves(m)), ref[j]);
-        const float f = ref[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[j] - m);
-        sum[j] *= f;
-        o[j].scale(f, lane);
-        ref[j] = m;
-        have[j] = m != -INFINITY || !sees_any(cols[j]);
-        const float by = m == -INFINITY ? 0.0f : m;   // nothing yet: every score is -inf
-#pragma unroll
-        for (int kt = 0; kt < NKT; ++kt)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[kt][j][r] -= by;
-      }
-      probabilities(s, pf, add);
-      // a column that is not finite has all it will have: the others' way is the same
-      bool all = true;
-#pragma unroll
-      for (int j = 0; j < QT; ++j) {
-        const float both = add[j] + swap_halves(add[j]);
-        all &= have[j] || both != both;
-      }
-      set = __all(all);
-    }
-#pragma unroll
-    for (int j = 0; j < QT; ++j) sum[j] += add[j];
+  __device__ __forceinline__ void product(const T* vl, const ColB<T> (&pf)[NKT][QT], int lane) {
 #pragma unroll
     for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
       for (int j = 0; j < QT; ++j) o[j].add(vl, 32 * kt, lane, pf[kt][j]);
   }
-  // exp2 of the scores, as operands and summed; whether some column's are too large
-  static __device__ __forceinline__ bool probabilities(const floatx16 (&s)[NKT][QT], ColB<T> (&pf)[NKT][QT],
-                                                       float (&add)[QT]) {
-    bool over = false;
+
+  // One tile: kf(kt, st) the fragments of its keys, vl its values in LDS.
+  template <typename KF, typename Q>
+  __device__ __forceinline__ void exact(const KF& kf, const T* vl, const Q& qf, int32_t key0, bool mask, uint32_t gone,
+                                        float c, const Seen (&cols)[QT], int lane) {
+    floatx16 s[NKT][QT];
+    float zero[QT];
+#pragma unroll
+    for (int j = 0; j < QT; ++j) zero[j] = 0.0f;
+    scores(s, kf, qf, key0, mask, gone, c, cols, zero, lane);
+    ColB<T> pf[NKT][QT];
+    bool all = true;
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
-      float a = 0.0f;
+      float m = s[0][j][0];
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kt][j][r]);
+      m = fmaxf(fmaxf(m, swap_halves(m)) + kRoom, ref[j]);
+      const float f = ref[j] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ref[j] - m);
+      sum[j] *= f;
+      o[j].scale(f, lane);
+      ref[j] = m;
+      const float by = m == -INFINITY ? 0.0f : m;   // nothing yet: every score is -inf
+      float add = 0.0f;
 #pragma unroll
       for (int kt = 0; kt < NKT; ++kt)
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float e = __builtin_amdgcn_exp2f(s[kt][j][r]);
-          a += e;
+          const float e = __builtin_amdgcn_exp2f(s[kt][j][r] - by);
+          add += e;
           pf[kt][j].set(r, e);
         }
-      add[j] = a;
-      over |= a > kMove;
+      sum[j] += add;
+      if constexpr (LAZY) {
+        // a column that is not finite has all it will have: the others' way is the same
+        add += swap_halves(add);
+        all &= m != -INFINITY || !sees_any(cols[j]) || add != add;
+      }
     }
-    return over;
+    if constexpr (LAZY) set = __all(all);
+    product(vl, pf, lane);
+  }
+
+  // Whether some column's reference has to move.  The operands of a block's products are
+  // read from LDS ahead of them, a block of 32 keys at a time, in the order written here (the
+  // fences keep it): left to itself the compiler reads each right before its MFMA, and a
+  // wave waits for LDS sixteen times a tile.
+  template <typename KF, typename Q>
+  __device__ __forceinline__ bool fast(const KF& kf, const T* vl, const Q& qf, int32_t key0, bool mask, uint32_t gone,
+                                       float c, const Seen (&cols)[QT], int lane) {
+    float by[QT];
+#pragma unroll
+    for (int j = 0; j < QT; ++j) by[j] = ref[j] == -INFINITY ? 0.0f : ref[j];   // a column that sees nothing
+    floatx16 s[NKT][QT];
+    ColB<T> pf[NKT][QT];
+    if constexpr (sizeof(T) == 2) {
+      typename M::frag ka[NKT][G::NS];
+#pragma unroll
+      for (int st = 0; st < G::NS; ++st) ka[0][st] = kf(0, st);
+      ColA<T, DC> va[NKT];
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (kt + 1 < NKT) {
+#pragma unroll
+          for (int st = 0; st < G::NS; ++st) ka[kt + 1][st] = kf(kt + 1, st);
+        } else {
+          va[0].load(vl, 0, lane);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < QT; ++j) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[kt][j][r] = 0.0f;
+        }
+#pragma unroll
+        for (int st = 0; st < G::NS; ++st)
+#pragma unroll
+          for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(ka[kt][st], qf[j][st], s[kt][j]);
+      }
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) {
+        scale(s[kt], c, by);
+        if (kt + 1 < NKT) va[kt + 1].load(vl, 32 * (kt + 1), lane);
+        cut(s[kt], pf[kt], kt, key0, mask, gone, cols, lane);
+#pragma unroll
+        for (int j = 0; j < QT; ++j) o[j].add(va[kt], pf[kt][j]);
+      }
+    } else {
+      scores(s, kf, qf, key0, false, 0, c, cols, by, lane);
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt) cut(s[kt], pf[kt], kt, key0, mask, gone, cols, lane);
+      product(vl, pf, lane);
+    }
+    bool over = false;
+#pragma unroll
+    for (int j = 0; j < QT; ++j) over |= sum[j] > 0.5f;
+    return __any(over);
+  }
+  // The probabilities of block kt, cut at 1, summed.  Masked ones are taken out by bits after
+  // the exponential (2 operations each; 5 by comparisons before it): cut, none is infinite.
+  __device__ __forceinline__ void cut(const floatx16 (&s)[QT], ColB<T> (&pf)[QT], int kt, int32_t key0, bool mask,
+                                      uint32_t gone, const Seen (&cols)[QT], int lane) {
+    auto at = [&](int j, uint32_t bits, bool all) {
+      float a = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        float e = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(s[j][r]), 0.0f, 1.0f);
+        if (!all) e = __uint_as_float(__float_as_uint(e) & (uint32_t)((int32_t)(bits << (31 - 8 * (r / 4) - r % 4)) >> 31));
+        a += e;
+        pf[j].set(r, e);
+      }
+      sum[j] += a;
+    };
+    if (!mask) {
+#pragma unroll
+      for (int j = 0; j < QT; ++j) at(j, 0, true);
+      return;
+    }
+    const uint32_t lost = (gone >> (2 * kt) & 1 ? 0xFFFFu : 0u) | (gone >> (2 * kt) & 2 ? 0xFFFF0000u : 0u);
+#pragma unroll
+    for (int j = 0; j < QT; ++j) at(j, (seen_bits(cols[j], key0 + 32 * kt) & ~lost) >> (4 * (lane >> 5)), false);
+  }
+
+  // After fast() of the same tile: for each column with a score above its reference, the
+  // reference goes d up, to that score and the room; sums are rescaled by 2^-d, and every
+  // key gets the difference between its probability and the one that was added.
+  template <typename KF, typename Q>
+  __device__ __forceinline__ void fix(const KF& kf, const T* vl, const Q& qf, int32_t key0, bool mask, uint32_t gone,
+                                      float c, const Seen (&cols)[QT], int lane) {
+    floatx16 s[NKT][QT];
+    float by[QT];
+#pragma unroll
+    for (int j = 0; j < QT; ++j) by[j] = ref[j] == -INFINITY ? 0.0f : ref[j];
+    scores(s, kf, qf, key0, mask, gone, c, cols, by, lane);
+    ColB<T> pf[NKT][QT];
+#pragma unroll
+    for (int j = 0; j < QT; ++j) {
+      float m = s[0][j][0];
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m = fmaxf(m, s[kt][j][r]);
+      m = fmaxf(m, swap_halves(m));
+      const float d = m > 0.0f ? m + kRoom : 0.0f;
+      ref[j] = by[j] + d;
+      const float f = __builtin_amdgcn_exp2f(-d);
+      sum[j] *= f;
+      o[j].scale(f, lane);
+#pragma unroll
+      for (int kt = 0; kt < NKT; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float x = s[kt][j][r];
+          const float e = x > 0.0f ? __builtin_amdgcn_exp2f(x - d) - f : 0.0f;
+          sum[j] += e;
+          pf[kt][j].set(r, e);
+        }
+    }
+    product(vl, pf, lane);
   }
 };
 
@@ -323,7 +424,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
       const auto gp = u.src.group(key0, id[i]);
       scale[i] = li < GR ? gp.ks : gp.vs;
       lost[i] = gp.gone;
-      rows[i].fetch(map, li < GR ? gp.k : gp.v, u.src.row_bytes, D, p.vec, [&](int r) {
+      rows[i].fetch(map, li < GR ? gp.k : gp.v, D, p.vec, !gp.gone && whole_group(we.first, we.last, key0), [&](int r) {
         const int32_t j = key0 + r;
         return !gp.gone && (j < we.last.sink || (j >= we.first.lo && j < we.last.hi));
       });
@@ -374,11 +475,16 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
         for (int i = 0; i < GR; ++i) lost_bits |= gone[buf * GR + i] << i;
         lost_bits = __builtin_amdgcn_readfirstlane(lost_bits);
       }
-      sm.step(
-          [&](int kt, int st) {
-            return *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
-          },
-          kl + TILE, qf, key0, lost_bits || !ed.all(key0, KB), lost_bits, p.c, col, lane);
+      auto kf = [&](int kt, int st) {
+        return *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
+      };
+      const bool mask = lost_bits || !ed.all(key0, KB);
+      if (sm.set) {
+        if (sm.fast(kf, kl + TILE, qf, key0, mask, lost_bits, p.c, col, lane))
+          sm.fix(kf, kl + TILE, qf, key0, mask, lost_bits, p.c, col, lane);
+      } else {
+        sm.exact(kf, kl + TILE, qf, key0, mask, lost_bits, p.c, col, lane);
+      }
     }
     if (more) stash(buf ^ 1);
     __syncthreads();
@@ -386,7 +492,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
 
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
-    const float l = sm.sum[j] + swap_halves(sm.sum[j]);
+    const float l = sm.total(j);
     sm.o[j].scale(l == 0.0f ? 0.0f : 1.0f / l, lane);
     const uint32_t j0 = c0 + 32 * (wave * QT + j);
     auto row = [&](int n) -> T* {
@@ -469,8 +575,9 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
         const int32_t j = key0 + r;
         return !gp.gone && (j < ed.last.sink || (j >= ed.first.lo && j < ed.last.hi));
       };
-      rk[i].fetch(map, gp.k, u.src.row_bytes, D, p.vec, on);
-      rv[i].fetch(map, gp.v, u.src.row_bytes, D, p.vec, on);
+      const bool whole = !gp.gone && whole_group(ed.first, ed.last, key0);
+      rk[i].fetch(map, gp.k, D, p.vec, whole, on);
+      rv[i].fetch(map, gp.v, D, p.vec, whole, on);
     }
   };
   const int32_t mine = (int32_t)split * part.per + wave;
@@ -501,13 +608,13 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
       ask(t + 2 * NW);
     }
     const int32_t key0 = tiles.key0(t);
-    sm.step(
+    sm.exact(
         [&](int, int st) {
           return *reinterpret_cast<const typename M::frag*>(kl + l32 * G::P + 2 * G::E * st + G::E * g);
         },
         vl, qf, key0, was_lost || !ed.all(key0, 32), was_lost, p.c, col, lane);
   }
-  float l = sm.sum[0] + swap_halves(sm.sum[0]);
+  float l = sm.total(0);
 
   // the waves' columns meet at the largest of their references, and are added in the
   // waves' order; the tiles are done with
