@@ -464,7 +464,7 @@ int dsp_attn_relpos_bwd(const void* q, const void* k, const void* v, const void*
  * dtype:   DSP_BF16 (fp32 scores, softmax and accumulation; probabilities are rounded to
  *          bf16 for the product with v), D a multiple of 8 up to 128, 16-byte aligned
  *          tensors and strides multiples of 8; or DSP_F32, any D up to 128.  Lq and Lk
- *          below 2^30, Lq * H / Hkv below 2^31, and 64 rows of each tensor within 2^31 bytes.
+ *          below 2^30, H / Hkv below 2^15, Lq * H / Hkv below 2^31, and 64 rows of each tensor within 2^31 bytes.
  * workspace: dsp_attn_window_workspace_bytes(...) bytes, 16-byte aligned (0 except for a
  *          few queries against many keys: there the keys are cut among work-groups, whose
  *          sums are joined).  Calls that may run at once, captured ones among them, have
@@ -541,8 +541,8 @@ int dsp_attn_window_bwd(const void* q, const void* k, const void* v, const void*
  * 16-byte aligned, of each call's own.
  *
  * Outputs lie apart from everything that the call reads and from one another (DSP_ERR_ARG;
- * the caches: from first element to last).  N <= 2^20, T * H and max_pages * page below
- * 2^30, 64 slots of a page within 2^31 bytes.
+ * the caches: from first element to last).  N <= 2^20, H / Hkv below 2^15, T * H and max_pages * page
+ * below 2^30, 64 slots of a page within 2^31 bytes.
  * Errors: DSP_ERR_NULL, DSP_ERR_SHAPE, DSP_ERR_DTYPE, DSP_ERR_ALIGN, DSP_ERR_ARG,
  *   DSP_ERR_WORKSPACE, DSP_ERR_HIP.  No sequences or no rows launch nothing.
  * ------------------------------------------------------------------------ */

@@ -11,12 +11,14 @@ using namespace dsp;
 namespace {
 
 constexpr int64_t kMaxL = int64_t(1) << 30;
+constexpr int kMaxGroup = 1 << 15;   // query heads of a key/value head
 
 // Sizes of dsp_attn_window that its workspaces depend on, checked.
 int window_sizes(WindowArgs& a, int64_t B, int64_t X, int64_t Lq, int64_t Lk, int H, int Hkv, int D, int left,
                  int right, int sinks, int dtype) {
   if (!valid_dtype(dtype)) return DSP_ERR_DTYPE;
-  if (B < 0 || X < 0 || Lq < 0 || Lk < 0 || H < 1 || Hkv < 1 || H % Hkv || D < 1 || D > kWindowMaxD) return DSP_ERR_SHAPE;
+  if (B < 0 || X < 0 || Lq < 0 || Lk < 0 || H < 1 || Hkv < 1 || H % Hkv || H / Hkv >= kMaxGroup || D < 1 || D > kWindowMaxD)
+    return DSP_ERR_SHAPE;
   if (dtype == DSP_BF16 && D % 8) return DSP_ERR_SHAPE;
   if (Lq >= kMaxL || Lk >= kMaxL) return DSP_ERR_SHAPE;
   if (sinks < 0) return DSP_ERR_ARG;
@@ -163,7 +165,8 @@ bool caches_apart(const Cache& c, const void* k, const void* v, int D) {
 int paged_sizes(WindowArgs& a, Cache& c, int64_t N, int64_t T, int64_t max_q, int64_t n_pages, int64_t max_pages, int page,
                 int H, int Hkv, int D, const int64_t* st, int left, int right, int sinks, int cache_dtype, int dtype) {
   if (!valid_dtype(dtype)) return DSP_ERR_DTYPE;
-  if (H < 1 || Hkv < 1 || H % Hkv || D < 1 || D > kWindowMaxD || T < 0 || max_q < 0) return DSP_ERR_SHAPE;
+  if (H < 1 || Hkv < 1 || H % Hkv || H / Hkv >= kMaxGroup || D < 1 || D > kWindowMaxD || T < 0 || max_q < 0)
+    return DSP_ERR_SHAPE;
   if (dtype == DSP_BF16 && D % 8) return DSP_ERR_SHAPE;
   int64_t n;
   if (!mul_ok(T, H, &n) || n >= kMaxL) return DSP_ERR_SHAPE;

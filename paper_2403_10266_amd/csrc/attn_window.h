@@ -52,10 +52,36 @@ struct Tiles {
   __device__ __forceinline__ int32_t key0(int32_t t) const { return t < sinks ? t * KB : band + (t - sinks) * KB; }
 };
 
+// Division by a number below 2^15 that the host knows: exact for n up to 2^16 (and n d below
+// 2^32), by one multiplication.
+struct Divisor {
+  uint32_t d, m;   // m = ceil(2^32 / d); 0 for d = 1
+  __device__ __forceinline__ uint32_t of(uint32_t n) const { return m ? __umulhi(n, m) : n; }
+};
+inline Divisor divisor(uint32_t d) { return {d, d > 1 ? (uint32_t)(((uint64_t(1) << 32) + d - 1) / d) : 0u}; }
+
+// Columns c0 + n (n below 2^15) of a unit as (query, head of the group) pairs.
+struct Columns {
+  Divisor grp;
+  uint32_t i0, r0;   // of c0
+  __device__ __forceinline__ Columns(const Divisor& g, uint32_t c0) : grp(g), i0(c0 / g.d), r0(c0 - c0 / g.d * g.d) {}
+  __device__ __forceinline__ uint32_t query(uint32_t n) const { return i0 + grp.of(r0 + n); }
+  __device__ __forceinline__ uint32_t head(uint32_t n, uint32_t query) const { return r0 + n - (query - i0) * grp.d; }
+};
+
+// zero in the columns D .. DP - 1 of `rows` LDS rows that the products take
+template <typename T, int DC>
+__device__ __forceinline__ void clear_cols(T* lds, int rows, int D, int tid, int nt) {
+  using G = Geo<T, DC>;
+  if (D >= G::DP) return;
+  for (int r = tid; r < rows; r += nt)
+    for (int c = (D + G::E - 1) / G::E * G::E; c < G::DP; c += G::E) *reinterpret_cast<u32x4*>(lds + r * G::P + c) = u32x4{0, 0, 0, 0};
+}
+
 // 16 keys of one tensor on their way from memory to LDS, by one wave: chunks of E
 // elements (16 bytes in LDS), in memory S: T itself, or e4m3 (8 bytes), whose values times
 // the page's scale, a power of two, are bf16 values exactly.  Rows that `on` leaves out
-// and columns past D come as 0 (the columns are cleared once, by clear_pad).
+// and columns past D come as 0 (the columns are cleared once, by clear_cols).
 template <typename T, typename S, int DC>
 struct Rows16 {
   using G = Geo<T, DC>;

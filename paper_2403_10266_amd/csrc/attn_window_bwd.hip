@@ -36,7 +36,8 @@ struct BwdParams {
   const int32_t* kv_len;
   int64_t qs[3], ks[3], os[3];
   Window win;
-  uint32_t X, H, Hkv, grp, Lq, Lk, D;
+  uint32_t X, H, Hkv, Lq, Lk, D;
+  Divisor grp;
   Order order;
   uint32_t parts, sink_blocks;   // parts of the first blocks of keys (0: they are like the others)
   uint32_t sink_groups;          // work-groups for them, the first of the grid
@@ -65,15 +66,16 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
   const Place pl = place(p.order);
   if (!pl.any) return;
   const uint32_t bx = pl.bx, e = pl.h, blk = p.order.blocks - 1 - pl.block, b = bx / p.X;
-  const uint32_t cols = p.Lq * p.grp, c0 = blk * CB;
+  const uint32_t c0 = blk * CB, nc = min(p.Lq * p.grp.d - c0, (uint32_t)CB);
   const int D = (int)p.D;
   const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D;
   const T* kg = static_cast<const T*>(p.k) + k_at;
   const T* vg = static_cast<const T*>(p.v) + k_at;
   const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
   const int64_t p0 = position(p.q_pos, b);
-  auto seen_by = [&](uint32_t c) { return seen(p.win, p0 + min(c, cols - 1) / p.grp, len); };
-  const Seen first = seen_by(c0), last = seen_by(c0 + CB - 1);
+  const Columns cs(p.grp, c0);
+  auto seen_by = [&](uint32_t n) { return seen(p.win, p0 + cs.query(min(n, nc - 1)), len); };
+  const Seen first = seen_by(0), last = seen_by(CB - 1);
   const Tiles<KB> tiles(first, last);
 
   const uint32_t row_bytes = (uint32_t)p.ks[2] * (uint32_t)sizeof(T);
@@ -98,8 +100,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
     }
   };
   if (tiles.n) fetch(0);
-  const uint32_t c = c0 + 32 * wave + l32, cc = min(c, cols - 1), qi = cc / p.grp, qh = e * p.grp + cc - qi * p.grp;
-  const bool on = c < cols;
+  const uint32_t n = 32 * wave + l32, qi = cs.query(min(n, nc - 1)), qh = e * p.grp.d + cs.head(min(n, nc - 1), qi);
+  const bool on = n < nc;
   const int64_t q_at = bx_at(p, bx, p.qs), o_at = bx_at(p, bx, p.os);
   auto at = [&](const void* base, int64_t from, int64_t row) {
     return on ? static_cast<const T*>(base) + from + (int64_t)qi * row + (int64_t)qh * D : nullptr;
@@ -123,9 +125,9 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
   const float lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
   if (on && g == 0) p.delta[stat] = delta;
   const Seen col = seen(p.win, p0 + qi, len);
-  const Seen wf = seen_by(c0 + 32 * wave), wl = seen_by(c0 + 32 * wave + 31);
-  const bool wave_on = c0 + 32 * wave < cols;
-  clear_pad<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
+  const Seen wf = seen_by(32 * wave), wl = seen_by(32 * wave + 31);
+  const bool wave_on = 32 * wave < nc;
+  clear_cols<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
   if (tiles.n) stash(0);
   __syncthreads();
 
@@ -170,10 +172,10 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
     __syncthreads();
   }
   dq.scale(p.scale, lane);
-  T* out = static_cast<T*>(p.dq) + q_at + (int64_t)e * p.grp * D;
-  auto row = [&](int n) -> T* {
-    const uint32_t k = c0 + 32 * wave + n, i = k / p.grp;
-    return k < cols ? out + (int64_t)i * p.qs[2] + (int64_t)(k - i * p.grp) * D : nullptr;
+  T* out = static_cast<T*>(p.dq) + q_at + (int64_t)e * p.grp.d * D;
+  auto row = [&](int k) -> T* {
+    const uint32_t n = 32 * wave + k, i = cs.query(n);
+    return n < nc ? out + (int64_t)i * p.qs[2] + (int64_t)cs.head(n, i) * D : nullptr;
   };
   if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, dq, lane, D, G::DP, row);
   else store_rows<T, DC>(dq, lane, D, false, row);
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
   TileT tq, to;
   static_assert(NT >= 2 * QB, "a statistic for each thread");
   float pre = 0.0f;
-  clear_pad<T, DC>(lds, 4 * QB, D, threadIdx.x, NT);
+  clear_cols<T, DC>(lds, 4 * QB, D, threadIdx.x, NT);
 
   ColAcc<T, DC> dk, dv;
   dk.zero();
@@ -260,7 +262,7 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
   const SeenBy highest = seen_by(p.win, p0, (int32_t)p.Lq, len, (int64_t)key_end - 1);
   const int32_t q_end = first_key < key_end ? max(lowest.end, highest.end) : 0;
   const uint32_t it0 = (uint32_t)lowest.first / QB, n_it = q_end > lowest.first ? ((uint32_t)q_end + QB - 1) / QB - it0 : 0;
-  uint32_t step = 0, steps = n_it * p.grp;
+  uint32_t step = 0, steps = n_it * p.grp.d;
   if (sink) {
     const uint32_t per = (steps + p.parts - 1) / p.parts;
     step = min(part * per, steps);
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
   }
   uint32_t hh = n_it ? step / n_it : 0, it = step - hh * n_it;   // the step to fetch
   auto fetch = [&]() {
-    const uint32_t h = e * p.grp + hh, q0 = (it0 + it) * QB, rows = min(p.Lq - q0, (uint32_t)QB);
+    const uint32_t h = e * p.grp.d + hh, q0 = (it0 + it) * QB, rows = min(p.Lq - q0, (uint32_t)QB);
     tq.fetch(mq, static_cast<const T*>(p.q) + q_bx + (int64_t)h * D + (int64_t)q0 * p.qs[2], rows, q_row, D, p.vec);
     to.fetch(mo, static_cast<const T*>(p.dout) + o_bx + (int64_t)h * D + (int64_t)q0 * p.os[2], rows, o_row, D, p.vec);
     if (threadIdx.x < 2 * QB) {
@@ -431,7 +433,7 @@ Sinks sinks_of(const WindowArgs& a) {
 template <typename T, int DC>
 int start_dq(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   constexpr int NW = 4, CB = 32 * NW, KB = 32, MINW = sizeof(T) == 2 && DC <= 64 ? 3 : sizeof(T) == 2 || DC <= 96 ? 2 : 1;
-  p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
+  p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp.d + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T);
   auto* kernel = window_bwd_dq_kernel<T, DC, NW, KB, MINW>;
   if (!grid_fits(order_blocks(p.order), NW * 64)) return DSP_ERR_SHAPE;
@@ -487,7 +489,7 @@ int launch_attn_window_bwd(const WindowArgs& a, hipStream_t s) {
   p.q_pos = a.q_pos, p.kv_len = a.kv_len;
   for (int i = 0; i < 3; ++i) p.qs[i] = a.q_strides[i], p.ks[i] = a.kv_strides[i], p.os[i] = a.o_strides[i];
   p.win = a.win;
-  p.X = (uint32_t)a.X, p.H = a.H, p.Hkv = a.Hkv, p.grp = a.H / a.Hkv, p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk;
+  p.X = (uint32_t)a.X, p.H = a.H, p.Hkv = a.Hkv, p.grp = divisor(a.H / a.Hkv), p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk;
   p.D = a.D;
   p.c = a.scale * kLog2e, p.scale = a.scale;
   p.vec = a.vec;

@@ -38,7 +38,8 @@ struct FwdParams {
   const float* v_scale;
   int64_t qs[3], ks[3], os[3];
   Window win;
-  uint32_t X, H, Hkv, grp, Lq, Lk, D;
+  uint32_t X, H, Hkv, Lq, Lk, D;
+  Divisor grp;       // heads of a key/value head's group
   uint32_t N, T, n_pages, max_pages, shift;   // pages
   Order order;       // many columns, rows of a tensor
   uint32_t n_blk;    // many columns, pages: blocks in all
@@ -62,7 +63,7 @@ struct Unit {
 template <typename T, typename S>
 __device__ __forceinline__ Unit<T, S, false> unit(const FwdParams& p, uint32_t bx, uint32_t e, Unit<T, S, false>*) {
   Unit<T, S, false> u;
-  const uint32_t b = bx / p.X, x = bx - b * p.X, h0 = e * p.grp;
+  const uint32_t b = bx / p.X, x = bx - b * p.X, h0 = e * p.grp.d;
   u.q = static_cast<const T*>(p.q) + (int64_t)b * p.qs[0] + (int64_t)x * p.qs[1] + (int64_t)h0 * p.D;
   u.o = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)h0 * p.D;
   u.lse = p.lse ? p.lse + ((uint64_t)bx * p.H + h0) * p.Lq : nullptr;
@@ -81,7 +82,7 @@ template <typename T, typename S>
 __device__ __forceinline__ Unit<T, S, true> unit(const FwdParams& p, uint32_t n, uint32_t e, Unit<T, S, true>*) {
   Unit<T, S, true> u;
   const Rows r = new_rows(p.q_start, n, p.T);
-  const uint32_t h0 = e * p.grp;
+  const uint32_t h0 = e * p.grp.d;
   u.q = static_cast<const T*>(p.q) + (int64_t)r.first * p.qs[2] + (int64_t)h0 * p.D;
   u.o = static_cast<T*>(p.o) + (int64_t)r.first * p.os[2] + (int64_t)h0 * p.D;
   u.lse = p.lse ? p.lse + (uint64_t)r.first * p.H + h0 : nullptr;
@@ -360,11 +361,10 @@ struct Edges {
     return key0 + n <= first.sink || (key0 >= last.lo && key0 + n <= first.hi);
   }
 };
-// The queries of columns c0 .. c0 + n - 1 of a unit (those that it has), as Edges.
+// The queries of columns n0 .. n1 from c0, as Edges.
 template <typename U>
-__device__ __forceinline__ Edges edges(const Window& w, const U& u, uint32_t grp, uint32_t c0, uint32_t n) {
-  const uint32_t cols = (uint32_t)u.nq * grp, c1 = min(c0 + n, cols) - 1;
-  return {seen(w, u.p0 + c0 / grp, u.len), seen(w, u.p0 + c1 / grp, u.len)};
+__device__ __forceinline__ Edges edges(const Window& w, const U& u, const Columns& c, uint32_t n0, uint32_t n1) {
+  return {seen(w, u.p0 + c.query(n0), u.len), seen(w, u.p0 + c.query(n1), u.len)};
 }
 
 // Many columns: QT blocks of 32 per wave, the keys in LDS tiles that all waves share,
@@ -390,8 +390,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   if constexpr (PAGED) {
     e = blockIdx.x % p.Hkv;
     const uint32_t w = p.n_blk - 1 - blockIdx.x / p.Hkv;   // a sequence's last blocks have the most keys
-    un = __builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, p.grp, CB, 1, w, lane));
-    const int32_t at = (int32_t)w - first_piece(p.q_start, un, p.T, p.grp, CB, 1);
+    un = __builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, p.grp.d, CB, 1, w, lane));
+    const int32_t at = (int32_t)w - first_piece(p.q_start, un, p.T, p.grp.d, CB, 1);
     if (at < 0) return;
     blk = (uint32_t)at;
   } else {
@@ -400,10 +400,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
     un = pl.bx, e = pl.h, blk = p.order.blocks - 1 - pl.block;
   }
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
-  const uint32_t cols = (uint32_t)u.nq * p.grp, c0 = blk * CB;
+  const uint32_t cols = (uint32_t)u.nq * p.grp.d, c0 = blk * CB;
   if (c0 >= cols || cols <= p.few_cols) return;
   const int D = (int)p.D;
-  const Edges we = edges(p.win, u, p.grp, c0, CB);           // of the work-group
+  const uint32_t nc = min(cols - c0, (uint32_t)CB);          // columns of the work-group
+  const Columns cs(p.grp, c0);
+  const Edges we = edges(p.win, u, cs, 0, nc - 1);
   const Tiles<KB> tiles(we.first, we.last);
 
   const typename R::Map map = R::map(D, u.src.row_bytes, lane);
@@ -447,14 +449,14 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   Seen col[QT];
 #pragma unroll
   for (int j = 0; j < QT; ++j) {
-    const uint32_t c = c0 + 32 * (wave * QT + j) + l32, cc = min(c, cols - 1), i = cc / p.grp, hh = cc - i * p.grp;
-    row_frags<T, DC>(c < cols ? u.q + (int64_t)i * u.q_row + (int64_t)hh * D : nullptr, g, D, p.vec, qf[j]);
+    const uint32_t n = 32 * (wave * QT + j) + l32, i = cs.query(min(n, nc - 1)), hh = cs.head(n, i);
+    row_frags<T, DC>(n < nc ? u.q + (int64_t)i * u.q_row + (int64_t)hh * D : nullptr, g, D, p.vec, qf[j]);
     col[j] = seen(p.win, u.p0 + i, u.len);
   }
-  const uint32_t w0 = c0 + 32 * QT * wave;
-  const bool on = w0 < cols;
-  const Edges ed = edges(p.win, u, p.grp, min(w0, cols - 1), 32 * QT);   // of the wave
-  clear_pad<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
+  const uint32_t w0 = 32 * QT * wave;
+  const bool on = w0 < nc;
+  const Edges ed = edges(p.win, u, cs, min(w0, nc - 1), min(w0 + 32 * QT, nc) - 1);   // of the wave
+  clear_cols<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
   if (tiles.n) stash(0);
   Softmax<T, DC, QT, NKT, true> sm;
   sm.init();
@@ -494,16 +496,16 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   for (int j = 0; j < QT; ++j) {
     const float l = sm.total(j);
     sm.o[j].scale(l == 0.0f ? 0.0f : 1.0f / l, lane);
-    const uint32_t j0 = c0 + 32 * (wave * QT + j);
-    auto row = [&](int n) -> T* {
-      const uint32_t c = j0 + n, i = c / p.grp;
-      return c < cols ? u.o + (int64_t)i * u.o_row + (int64_t)(c - i * p.grp) * D : nullptr;
+    const uint32_t j0 = 32 * (wave * QT + j);
+    auto row = [&](int k) -> T* {
+      const uint32_t n = j0 + k, i = cs.query(n);
+      return n < nc ? u.o + (int64_t)i * u.o_row + (int64_t)cs.head(n, i) * D : nullptr;
     };
     if (p.vec) store_rows_lds<T, DC>(lds + wave * 32 * G::P, sm.o[j], lane, D, G::DP, row);
     else store_rows<T, DC>(sm.o[j], lane, D, false, row);
-    const uint32_t c = j0 + l32, i = c / p.grp;
-    if (u.lse && g == 0 && c < cols)
-      u.lse[(int64_t)i * u.lse_i + (int64_t)(c - i * p.grp) * u.lse_h] =
+    const uint32_t n = j0 + l32, i = cs.query(n);
+    if (u.lse && g == 0 && n < nc)
+      u.lse[(int64_t)i * u.lse_i + (int64_t)cs.head(n, i) * u.lse_h] =
           l == 0.0f ? -INFINITY : kLn2 * (sm.ref[j] + log2f(l));
   }
 }
@@ -544,11 +546,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
   const uint32_t ec = j8 % he, e = ec / p.cblk, cb = ec - e * p.cblk;
   const uint32_t un = piece / p.n_split, split = piece - un * p.n_split;
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
-  const uint32_t cols = (uint32_t)u.nq * p.grp, c0 = 32 * cb;
+  const uint32_t cols = (uint32_t)u.nq * p.grp.d, c0 = 32 * cb;
   if (c0 >= cols || cols > p.few_cols) return;
   const uint32_t nc = min(cols - c0, 32u);
   const int D = (int)p.D;
-  const Edges ed = edges(p.win, u, p.grp, c0, 32);
+  const Columns cs(p.grp, c0);
+  const Edges ed = edges(p.win, u, cs, 0, nc - 1);
   const Tiles<32> tiles(ed.first, ed.last);
   const Cut part = cut(tiles.n, p.n_split, NW);
   if ((int32_t)split >= part.used) return;
@@ -586,8 +589,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
     fetch(mine);
     ask(mine + NW);
   }
-  clear_pad<T, DC>(kl, 64, D, lane, 64);
-  const uint32_t c = c0 + min((uint32_t)l32, nc - 1), ci = c / p.grp, ch = c - ci * p.grp;
+  clear_cols<T, DC>(kl, 64, D, lane, 64);
+  const uint32_t ci = cs.query(min((uint32_t)l32, nc - 1)), ch = cs.head(l32, ci);
   typename M::frag qf[1][G::NS];
   row_frags<T, DC>((uint32_t)l32 < nc ? u.q + (int64_t)ci * u.q_row + (int64_t)ch * D : nullptr, g, D, p.vec, qf[0]);
   const Seen col[1] = {seen(p.win, u.p0 + ci, u.len)};
@@ -619,13 +622,13 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
   // the waves' columns meet at the largest of their references, and are added in the
   // waves' order; the tiles are done with
   auto out = [&](uint32_t n) {
-    const uint32_t k = c0 + n, i = k / p.grp;
-    return u.o + (int64_t)i * u.o_row + (int64_t)(k - i * p.grp) * D;
+    const uint32_t i = cs.query(n);
+    return u.o + (int64_t)i * u.o_row + (int64_t)cs.head(n, i) * D;
   };
   auto put_lse = [&](uint32_t n, float m, float s) {
-    const uint32_t k = c0 + n, i = k / p.grp;
+    const uint32_t i = cs.query(n);
     if (u.lse)
-      u.lse[(int64_t)i * u.lse_i + (int64_t)(k - i * p.grp) * u.lse_h] = s == 0.0f ? -INFINITY : kLn2 * (m + log2f(s));
+      u.lse[(int64_t)i * u.lse_i + (int64_t)cs.head(n, i) * u.lse_h] = s == 0.0f ? -INFINITY : kLn2 * (m + log2f(s));
   };
   if constexpr (NW == 1) {
     if (part.used == 1) {
@@ -692,9 +695,10 @@ __global__ __launch_bounds__(256) void window_join_kernel(FwdParams p, int waves
   const uint32_t he = p.Hkv * p.cblk, n = blockIdx.x & 31u, uec = blockIdx.x >> 5, un = uec / he, ec = uec - un * he;
   const uint32_t e = ec / p.cblk, cb = ec - e * p.cblk;
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
-  const uint32_t cols = (uint32_t)u.nq * p.grp, c = 32 * cb + n;
+  const uint32_t cols = (uint32_t)u.nq * p.grp.d, c = 32 * cb + n;
   if (c >= cols || cols > p.few_cols) return;
-  const Edges ed = edges(p.win, u, p.grp, 32 * cb, 32);
+  const Columns cs(p.grp, 32 * cb);
+  const Edges ed = edges(p.win, u, cs, 0, min(cols - 32 * cb, 32u) - 1);
   const Tiles<32> tiles(ed.first, ed.last);
   const uint32_t used = (uint32_t)cut(tiles.n, p.n_split, waves).used;
   if (used == 1) return;
@@ -735,7 +739,7 @@ __global__ __launch_bounds__(256) void window_join_kernel(FwdParams p, int waves
   if (gr || d >= p.D) return;
 #pragma unroll
   for (int i = 1; i < GR; ++i) l += red[i * DP + d];
-  const uint32_t i = c / p.grp, hh = c - i * p.grp;
+  const uint32_t i = cs.query(n), hh = cs.head(n, i);
   u.o[(int64_t)i * u.o_row + (int64_t)hh * p.D + d] = (T)(l == 0.0f ? 0.0f : a / l);
   if (u.lse && d == 0)
     u.lse[(int64_t)i * u.lse_i + (int64_t)hh * u.lse_h] = l == 0.0f ? -INFINITY : kLn2 * (top + log2f(l));
@@ -758,10 +762,10 @@ int start_many(FwdParams& p, const WindowArgs& a, hipStream_t s) {
   constexpr int CB = NW * 32 * QT;
   int64_t blocks;
   if (PAGED) {
-    p.n_blk = (uint32_t)(a.T * p.grp / CB + a.B);
+    p.n_blk = (uint32_t)(a.T * p.grp.d / CB + a.B);
     blocks = (int64_t)p.n_blk * a.Hkv;
   } else {
-    p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
+    p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp.d + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
     blocks = order_blocks(p.order);
   }
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T) + 2 * (KB / 16) * 4;
@@ -833,7 +837,7 @@ inline FwdParams params(const WindowArgs& a) {
   p.k_scale = a.k_scale, p.v_scale = a.v_scale;
   for (int i = 0; i < 3; ++i) p.qs[i] = a.q_strides[i], p.ks[i] = a.kv_strides[i], p.os[i] = a.o_strides[i];
   p.win = a.win;
-  p.X = (uint32_t)a.X, p.H = a.H, p.Hkv = a.Hkv, p.grp = a.H / a.Hkv, p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk;
+  p.X = (uint32_t)a.X, p.H = a.H, p.Hkv = a.Hkv, p.grp = divisor(a.H / a.Hkv), p.Lq = (uint32_t)a.Lq, p.Lk = (uint32_t)a.Lk;
   p.D = a.D;
   p.N = (uint32_t)a.B, p.T = (uint32_t)a.T, p.n_pages = (uint32_t)a.n_pages, p.max_pages = (uint32_t)a.max_pages;
   p.shift = a.page_shift;
