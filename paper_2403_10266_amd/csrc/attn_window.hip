@@ -8,6 +8,11 @@ namespace {
 template <typename T, int DC>
 int run(const WindowArgs& a, hipStream_t s) {
   FwdParams p = params(a);
+  const int64_t cols = a.Lq * p.grp.d;
+  constexpr bool B16 = sizeof(T) == 2;
+  if (cols <= 32 && a.Lk <= 32) return start_short<T, DC, 1, 32, B16 ? (DC <= 80 ? 4 : 3) : 1>(p, a, s);
+  if (cols <= 64 && a.Lk <= 64) return start_short<T, DC, 2, 64, B16 ? 3 : 1>(p, a, s);
+  if (cols <= 128 && a.Lk <= 128) return start_short<T, DC, 4, 128, B16 ? (DC <= 96 ? 3 : 2) : 1>(p, a, s);
   return start<T, T, false, DC>(p, a, choose(a), s);
 }
 

@@ -510,6 +510,82 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   }
 }
 
+// Short units: all keys of one in LDS at once, with one barrier, and a wave per 32 columns,
+// which takes the blocks of 32 keys that it sees.  Memory bounds these: what counts is that
+// a work-group asks for all of its rows at once.
+template <typename T, int DC, int NW, int KEYS, int MINW>
+__global__ __launch_bounds__(NW * 64, MINW) void window_short_kernel(FwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  using U = Unit<T, T, false>;
+  using R = Rows16<T, T, DC>;
+  constexpr int NT = NW * 64, GR = KEYS / 16, TILE = KEYS * G::P;
+  constexpr int NL = 2 * GR / NW;   // group loads of a wave: K's groups, then V's
+  static_assert(2 * GR % NW == 0 && NW * 32 <= 2 * KEYS, "every wave loads the same; the output rows fit");
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* kl = reinterpret_cast<T*>(smem);   // [K, V][KEYS][P]
+  T* vl = kl + TILE;
+
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place pl = place(p.order);
+  if (!pl.any) return;
+  const U u = unit<T, T>(p, pl.bx, pl.h, (U*)nullptr);
+  const uint32_t nc = (uint32_t)u.nq * p.grp.d;
+  const int D = (int)p.D;
+  const Columns cs(p.grp, 0);
+  const Edges we = edges(p.win, u, cs, 0, nc - 1);
+  const typename R::Map map = R::map(D, u.src.row_bytes, lane);
+  R rows[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int li = wave + i * NW;
+    const int32_t key0 = 16 * (li % GR);
+    const auto gp = u.src.group(key0, 0);
+    rows[i].fetch(map, li < GR ? gp.k : gp.v, D, p.vec, whole_group(we.first, we.last, key0), [&](int r) {
+      const int32_t j = key0 + r;
+      return j < we.last.sink || (j >= we.first.lo && j < we.last.hi);
+    });
+  }
+  const uint32_t w0 = 32 * wave, n = w0 + l32, i = cs.query(min(n, nc - 1)), hh = cs.head(n, i);
+  typename M::frag qf[1][G::NS];
+  row_frags<T, DC>(n < nc ? u.q + (int64_t)i * u.q_row + (int64_t)hh * D : nullptr, g, D, p.vec, qf[0]);
+  const Seen col[1] = {seen(p.win, u.p0 + i, u.len)};
+  clear_cols<T, DC>(kl, 2 * KEYS, D, threadIdx.x, NT);
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int li = wave + i * NW;
+    rows[i].stash(map, (li < GR ? kl : vl) + 16 * (li % GR) * G::P, 1.0f);
+  }
+  if constexpr (NW > 1) __syncthreads();
+  else wave_order();
+  Softmax<T, DC, 1, 1, false> sm;
+  sm.init();
+  if (w0 < nc) {
+    const Edges ed = edges(p.win, u, cs, w0, min(w0 + 32, nc) - 1);
+    for (int32_t key0 = 0; key0 < ed.last.hi; key0 += 32) {
+      if (ed.none(key0, 32)) continue;
+      sm.exact(
+          [&](int, int st) {
+            return *reinterpret_cast<const typename M::frag*>(kl + (key0 + l32) * G::P + 2 * G::E * st + G::E * g);
+          },
+          vl + key0 * G::P, qf, key0, !ed.all(key0, 32), 0, p.c, col, lane);
+    }
+  }
+  const float l = sm.total(0);
+  sm.o[0].scale(l == 0.0f ? 0.0f : 1.0f / l, lane);
+  if constexpr (NW > 1) __syncthreads();   // the keys and values are done with
+  else wave_order();
+  auto row = [&](int k) -> T* {
+    const uint32_t c = w0 + k, i = cs.query(c);
+    return c < nc ? u.o + (int64_t)i * u.o_row + (int64_t)cs.head(c, i) * D : nullptr;
+  };
+  if (p.vec) store_rows_lds<T, DC>(kl + wave * 32 * G::P, sm.o[0], lane, D, G::DP, row);
+  else store_rows<T, DC>(sm.o[0], lane, D, false, row);
+  if (u.lse && g == 0 && n < nc)
+    u.lse[(int64_t)i * u.lse_i + (int64_t)hh * u.lse_h] = l == 0.0f ? -INFINITY : kLn2 * (sm.ref[0] + log2f(l));
+}
+
 // Few columns: a block of 32 of them, the keys' tiles of 32 cut among work-groups and,
 // inside one, among its waves, each with LDS rows of its own and no barrier until the
 // waves' sums are joined.  A pass over a cache is bound by memory: what counts is how
@@ -772,6 +848,13 @@ int start_many(FwdParams& p, const WindowArgs& a, hipStream_t s) {
   return launch(window_fwd_kernel<T, S, PAGED, DC, NW, QT, KB, MINW>, blocks, NW * 64, lds, p, s);
 }
 
+template <typename T, int DC, int NW, int KEYS, int MINW>
+int start_short(FwdParams& p, const WindowArgs& a, hipStream_t s) {
+  p.order = make_order(a.B * a.X, a.Hkv, 1, 1, false);
+  return launch(window_short_kernel<T, DC, NW, KEYS, MINW>, order_blocks(p.order), NW * 64,
+                (size_t)2 * KEYS * Geo<T, DC>::P * sizeof(T), p, s);
+}
+
 template <typename T, typename S, bool PAGED, int DC, int NW>
 int start_few(FwdParams& p, const WindowArgs& a, hipStream_t s) {
   constexpr int MINW = sizeof(T) == 4 ? 1 : DC <= 80 ? 3 : 2;
@@ -826,8 +909,13 @@ int start(FwdParams& p, const WindowArgs& a, const Choice& c, hipStream_t s) {
     if (int st = start_few<T, S, PAGED, DC, 4>(p, a, s)) return st;
   }
   if (!c.many) return DSP_OK;
-  constexpr bool B16 = sizeof(T) == 2;
-  return start_many<T, S, PAGED, DC, 4, 1, B16 ? 64 : 32, B16 ? (DC <= 64 ? 3 : 2) : 1>(p, a, s);
+  // Registers for three waves to a SIMD where they go without (many) spills, tiles of 64 keys
+  // where they do not: 8 x 16 units of 4096 x 72, window 257, 144 us with three waves and 32
+  // keys, 160 and 174 with two waves and 64 and 32; 32 heads of 8192 x 64, window 2048, 172 us
+  // with three waves and 64 keys, 198 with 32; 16 of 8192 x 128, window 1024, with two waves 218
+  // and 226.
+  constexpr bool B16 = sizeof(T) == 2, WIDE = DC > 64 && DC <= 96;
+  return start_many<T, S, PAGED, DC, 4, 1, B16 && !WIDE ? 64 : 32, B16 ? (DC <= 96 ? 3 : 2) : 1>(p, a, s);
 }
 
 inline FwdParams params(const WindowArgs& a) {
