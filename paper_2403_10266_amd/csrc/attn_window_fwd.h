@@ -45,6 +45,7 @@ struct FwdParams {
   uint32_t n_blk;    // many columns, pages: blocks in all
   uint32_t few_cols; // many columns: units of at most so many are left to the other form
   uint32_t pieces, n_split, cblk;   // few columns: units times splits, blocks of 32 columns
+  uint32_t block_cols;              // of a block, at most
   float c;           // scale * log2(e)
   bool vec;
 };
@@ -768,7 +769,8 @@ __global__ __launch_bounds__(256) void window_join_kernel(FwdParams p, int waves
   constexpr int GR = 256 / DP;
   __shared__ float f[kMaxSplit], red[256], m4[4];
   using U = Unit<T, S, PAGED>;
-  const uint32_t he = p.Hkv * p.cblk, n = blockIdx.x & 31u, uec = blockIdx.x >> 5, un = uec / he, ec = uec - un * he;
+  const uint32_t he = p.Hkv * p.cblk, uec = blockIdx.x / p.block_cols, n = blockIdx.x - uec * p.block_cols;
+  const uint32_t un = uec / he, ec = uec - un * he;
   const uint32_t e = ec / p.cblk, cb = ec - e * p.cblk;
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
   const uint32_t cols = (uint32_t)u.nq * p.grp.d, c = 32 * cb + n;
@@ -864,7 +866,8 @@ int start_few(FwdParams& p, const WindowArgs& a, hipStream_t s) {
   p.pieces = (uint32_t)pieces;
   int st = launch(window_few_kernel<T, S, PAGED, DC, NW, MINW>, (pieces + 7) / 8 * 8 * a.Hkv * p.cblk, NW * 64, lds, p, s);
   if (st != DSP_OK || p.n_split == 1) return st;
-  const int64_t cols = a.B * a.X * a.Hkv * p.cblk * 32;   // few units: they are why the keys are split
+  p.block_cols = (uint32_t)std::min<int64_t>(a.Lq * p.grp.d, 32);
+  const int64_t cols = a.B * a.X * a.Hkv * p.cblk * p.block_cols;   // few units: they are why the keys are split
   if (!grid_fits(cols, 256)) return DSP_ERR_SHAPE;
   if (a.D <= 64) window_join_kernel<T, S, PAGED, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
   else window_join_kernel<T, S, PAGED, 128><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
@@ -890,8 +893,13 @@ inline Choice choose(const WindowArgs& a) {
   int64_t keys = a.Lk;
   if (a.win.left >= 0 && a.win.right >= 0)
     keys = std::min<int64_t>(keys, (int64_t)a.win.left + a.win.right + a.win.sinks + 64);
+  // One sequence's units are alike: as many work-groups as the chip holds at once (100000 keys
+  // of 8 heads of 128: 87 us with 2 to a CU, 93 with 4, 104 with 8).  Sequences differ in
+  // length: 8 to a CU (64 of up to 16000 keys in 8 bits, 8 heads of 64: 166 us; 178 with 6, 196
+  // with 4, 174 with 16).
   const int64_t units = std::max<int64_t>(a.B * a.X * a.Hkv, 1);
-  const int64_t n = std::min<int64_t>({(256 * 8 + units - 1) / units, keys / 256, kMaxSplit});
+  const int64_t per_cu = a.B > 1 ? 8 : !a.bf16 ? 1 : a.D <= 64 ? 4 : a.D <= 80 ? 3 : 2;
+  const int64_t n = std::min<int64_t>({(256 * per_cu + units - 1) / units, keys / 256, kMaxSplit});
   if (n > 1) c.n_split = n;
   return c;
 }
