@@ -526,7 +526,7 @@ int dsp_attn_window_bwd(const void* q, const void* k, const void* v, const void*
  *   new tokens must hold what earlier calls wrote (or scale 0: nothing).
  *   Slots other than the new tokens' (8 bits: and those before them in the page) and rows of
  *   no sequence are left as they were.  A page that is written belongs to one sequence.
- *   D up to 256 at any alignment of an element; 16-byte aligned tensors and tables, with
+ *   D up to 256, H + 2 Hkv below 2048, at any alignment of an element; 16-byte aligned tensors and tables, with
  *   D and rot multiples of 8, are fastest.
  *
  * dsp_attn_paged -- attention of the new tokens (q, o: T rows of H heads, q_stride and

@@ -297,7 +297,7 @@ int dsp_kv_append(const void* k, const void* v, const void* q, void* yq, void* k
   if (!valid_dtype(dtype)) return DSP_ERR_DTYPE;
   if (H < 0 || Hkv < 1 || D < 1 || D > 256 || T < 0 || rot < 0 || rot % 2 || rot > D) return DSP_ERR_SHAPE;
   int64_t n;
-  if (!mul_ok(T, (int64_t)H + 2 * (int64_t)Hkv, &n) || n >= kMaxL) return DSP_ERR_SHAPE;
+  if (!mul_ok(T, (int64_t)H + 2 * (int64_t)Hkv, &n) || n >= kMaxL || (int64_t)H + 2 * (int64_t)Hkv >= 2048) return DSP_ERR_SHAPE;
   if (int st = cache_layout(c, N, n_pages, max_pages, page, Hkv, D, cache_strides, cache_dtype, dtype)) return st;
   if (flags & ~DSP_ROPE_ADJACENT) return DSP_ERR_ARG;
   if (k_stride < 0 || v_stride < 0 || q_stride < 0 || yq_stride < 0) return DSP_ERR_SHAPE;
@@ -320,12 +320,11 @@ int dsp_kv_append(const void* k, const void* v, const void* q, void* yq, void* k
   for (const int64_t* st : {sk, sv, sq, sy})
     if (st[2] >= (int64_t(1) << 40)) return DSP_ERR_SHAPE;
   if (H && sy[2] < wq) return DSP_ERR_ARG;
-  // whole items of eight, in halves of four
-  auto whole = [](const void* p, int64_t st, int size) { return aligned(p, 4 * size) && st % 4 == 0; };
+  // whole items of eight elements, at most 16 bytes at a time
+  auto whole = [](const void* p, int64_t st, int size) { return aligned(p, std::min(8 * size, 16)) && st % 8 == 0; };
   bool vec = D % 8 == 0 && rot % 8 == 0 && (!rot || (aligned(cos, 16) && aligned(sin, 16))) && whole(k, sk[2], es) &&
              whole(v, sv[2], es) && (!H || (whole(q, sq[2], es) && whole(yq, sy[2], es)));
-  for (int i = 0; i < 3; ++i) vec = vec && (c.e[i] <= 1 || c.st[i] % 4 == 0);
-  vec = vec && aligned(k_cache, 4 * c.es) && aligned(v_cache, 4 * c.es);
+  for (int i = 0; i < 3; ++i) vec = vec && whole(i ? v_cache : k_cache, c.e[i] <= 1 ? 0 : c.st[i], c.es);
   // what is written is apart from what is read and from one another; queries may stay in place
   const int64_t scales = e4m3 ? n_pages * Hkv * 4 : 0, angles = rot ? P * rot / 2 * 4 : 0;
   const Mem in[] = {{q, sq, wq, T}, {k, sk, wk, T}, {v, sv, wk, T}, mem_block(table, N * max_pages * 4),

@@ -10,8 +10,8 @@
 // |x| <= 448 s for every token since the page's first slot was written.  A work-group takes
 // one head of one page: it finds the new tokens' largest magnitude, rounds what the page
 // holds again where s has grown (a power of two: nothing but a lost last bit near the
-// least values), and writes.  A second reading of the tokens, from the cache that the
-// first left them in, costs less than registers for the largest page would.
+// least values), and writes.  Up to 1024 items of eight elements stay in registers between;
+// those of larger pages are read and turned twice.
 #include <type_traits>
 
 #include "attn_window.h"
@@ -36,13 +36,14 @@ struct AppendParams {
   const float* sin;
   int64_t k_row, v_row, q_row, y_row, page_st, slot_st, head_st;
   uint32_t N, T, P, n_pages, max_pages, shift, H, Hkv, D, rot;
-  uint32_t items;        // of a head: 8 elements each
+  Divisor items;         // of a head: 8 elements each
+  int32_t row_tokens;    // of a work-group that goes by rows: 16 at most, so that they lie in two pages at most
   uint32_t rot_items;    // the first of them, whose elements turn
   uint32_t page_groups;  // work-groups that write pages of 8 bits; the others go by rows
   bool half, e4m3, vec;
 };
 
-constexpr int kItem = 8, kRowTokens = 16;
+constexpr int kItem = 8;
 constexpr int kLeastExp = -64;   // of a scale
 
 // Item c of a head: elements at() .. of it, four pairs in the part that turns.
@@ -72,7 +73,13 @@ template <typename T, bool VEC>
 __device__ __forceinline__ void load8(const AppendParams& p, const T* head, const Place8& e, float (&x)[8]) {
   if constexpr (VEC) {
     if constexpr (sizeof(T) == 2) {
-      const uint2 lo = *reinterpret_cast<const uint2*>(head + e.a), hi = *reinterpret_cast<const uint2*>(head + e.b);
+      uint2 lo, hi;
+      if (e.b == e.a + 4) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(head + e.a);
+        lo = {v[0], v[1]}, hi = {v[2], v[3]};
+      } else {
+        lo = *reinterpret_cast<const uint2*>(head + e.a), hi = *reinterpret_cast<const uint2*>(head + e.b);
+      }
       const uint32_t w[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
@@ -144,8 +151,12 @@ __device__ __forceinline__ void store8(const AppendParams& p, T* head, const Pla
         const bf16x2 v = {(bf16)x[2 * i], (bf16)x[2 * i + 1]};
         w[i] = __builtin_bit_cast(uint32_t, v);
       }
-      *reinterpret_cast<uint2*>(head + e.a) = {w[0], w[1]};
-      *reinterpret_cast<uint2*>(head + e.b) = {w[2], w[3]};
+      if (e.b == e.a + 4) {
+        *reinterpret_cast<u32x4*>(head + e.a) = u32x4{w[0], w[1], w[2], w[3]};
+      } else {
+        *reinterpret_cast<uint2*>(head + e.a) = {w[0], w[1]};
+        *reinterpret_cast<uint2*>(head + e.b) = {w[2], w[3]};
+      }
     } else {
       *reinterpret_cast<floatx4*>(head + e.a) = floatx4{x[0], x[1], x[2], x[3]};
       *reinterpret_cast<floatx4*>(head + e.b) = floatx4{x[4], x[5], x[6], x[7]};
@@ -171,8 +182,12 @@ __device__ __forceinline__ void store8_e4m3(const AppendParams& p, uint8_t* head
     w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[4 * h + 2], y[4 * h + 3], v, true);
   }
   if constexpr (VEC) {
-    *reinterpret_cast<uint32_t*>(head + e.a) = w[0];
-    *reinterpret_cast<uint32_t*>(head + e.b) = w[1];
+    if (e.b == e.a + 4) {
+      *reinterpret_cast<uint2*>(head + e.a) = {w[0], w[1]};
+    } else {
+      *reinterpret_cast<uint32_t*>(head + e.a) = w[0];
+      *reinterpret_cast<uint32_t*>(head + e.b) = w[1];
+    }
   } else {
 #pragma unroll
     for (int t = 0; t < 8; ++t)
@@ -188,40 +203,66 @@ __device__ __forceinline__ int scale_exp(float top) {
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Rows: up to 16 tokens of one sequence, K, V and Q, or Q alone.
+// Rows: up to 16 tokens of one sequence, K, V and Q, or Q alone.  A thread takes four items
+// at a time, so that their loads are under way together; the rows lie in at most two pages.
 template <typename T, bool VEC, int NT>
 __device__ __forceinline__ void append_rows(const AppendParams& p, uint32_t w) {
+  constexpr int N = 4;
   const int lane = threadIdx.x & 63;
-  const uint32_t n = __builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, 1, kRowTokens, 1, w, lane));
-  const int32_t blk = (int32_t)w - first_piece(p.q_start, n, p.T, 1, kRowTokens, 1);
+  const uint32_t n = __builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, 1, p.row_tokens, 1, w, lane));
+  const int32_t blk = (int32_t)w - first_piece(p.q_start, n, p.T, 1, p.row_tokens, 1);
   const Rows r = new_rows(p.q_start, n, p.T);
-  if (blk < 0 || blk * kRowTokens >= r.n) return;
-  const uint32_t count = min((uint32_t)(r.n - blk * kRowTokens), (uint32_t)kRowTokens);
-  const int64_t p0 = (int64_t)p.kv_len[n] - r.n + blk * kRowTokens;   // position of the first
-  const int64_t row0 = (int64_t)r.first + blk * kRowTokens;
-  const uint32_t kv_heads = p.e4m3 ? 0 : p.Hkv, heads = p.H + 2 * kv_heads, per = heads * p.items;
-  for (uint32_t i = threadIdx.x; i < count * per; i += NT) {
-    const uint32_t t = i / per, in_row = i - t * per, hh = in_row / p.items;
-    const Place8 e = place8(p, in_row - hh * p.items);
-    const int64_t row = row0 + t, at = p0 + t;
-    float x[8];
-    if (hh < p.H) {
-      load8<T, VEC>(p, static_cast<const T*>(p.q) + row * p.q_row + (int64_t)hh * p.D, e, x);
-      turn8<VEC>(p, e, p.pos ? p.pos[row] : at, x);
-      store8<T, VEC>(p, static_cast<T*>(p.yq) + row * p.y_row + (int64_t)hh * p.D, e, x);
-      continue;
+  if (blk < 0 || blk * p.row_tokens >= r.n) return;
+  const uint32_t count = (uint32_t)min(r.n - blk * p.row_tokens, p.row_tokens);
+  const int64_t p0 = (int64_t)p.kv_len[n] - r.n + blk * p.row_tokens;   // position of the first
+  const int64_t row0 = (int64_t)r.first + blk * p.row_tokens;
+  const uint32_t kv_heads = p.e4m3 ? 0 : p.Hkv, per = (p.H + 2 * kv_heads) * p.items.d;
+  const int64_t first_pi = p0 >> p.shift;
+  auto page_at = [&](int64_t pi) {
+    return kv_heads && pi >= 0 && pi < (int64_t)p.max_pages ? p.table[(uint64_t)n * p.max_pages + (uint64_t)pi] : -1;
+  };
+  const int32_t page0 = page_at(first_pi), page1 = page_at(first_pi + 1);
+
+  uint32_t t = threadIdx.x / per, in_row = threadIdx.x - t * per;   // item
+  while (t < count) {
+    float x[N][8];
+    Place8 e[N];
+    T* to[N];
+    int64_t at[N];       // the table's row, or kNoTurn
+    constexpr int64_t kNoTurn = INT64_MIN;
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      to[q] = nullptr;
+      at[q] = kNoTurn;
+      if (t < count) {
+        const uint32_t hh = p.items.of(in_row);
+        e[q] = place8(p, in_row - hh * p.items.d);
+        const int64_t row = row0 + t, pos = p0 + t;
+        const bool is_q = hh < p.H, is_v = hh >= p.H + kv_heads;
+        const uint32_t h = is_q ? hh : hh - p.H - (is_v ? kv_heads : 0);
+        const T* from;
+        if (is_q) {
+          from = static_cast<const T*>(p.q) + row * p.q_row;
+          to[q] = static_cast<T*>(p.yq) + row * p.y_row + (int64_t)h * p.D;
+        } else {
+          from = is_v ? static_cast<const T*>(p.v) + row * p.v_row : static_cast<const T*>(p.k) + row * p.k_row;
+          const int32_t page = pos >> p.shift == first_pi ? page0 : page1;
+          if ((uint32_t)page < p.n_pages)
+            to[q] = static_cast<T*>(is_v ? p.v_cache : p.k_cache) + (int64_t)page * p.page_st +
+                    (pos & ((1 << p.shift) - 1)) * p.slot_st + (int64_t)h * p.head_st;
+        }
+        if (!is_v && e[q].turns) at[q] = p.pos ? p.pos[row] : pos;
+        load8<T, VEC>(p, from + (int64_t)h * p.D, e[q], x[q]);
+        in_row += NT;
+        while (in_row >= per) in_row -= per, ++t;
+      }
     }
-    const bool is_v = hh >= p.H + kv_heads;
-    const uint32_t h = hh - p.H - (is_v ? kv_heads : 0);
-    if (at < 0 || (uint64_t)at >= (uint64_t)p.max_pages << p.shift) continue;
-    const int32_t page = p.table[(uint64_t)n * p.max_pages + (uint64_t)(at >> p.shift)];
-    if ((uint32_t)page >= p.n_pages) continue;
-    const T* from = is_v ? static_cast<const T*>(p.v) + row * p.v_row : static_cast<const T*>(p.k) + row * p.k_row;
-    load8<T, VEC>(p, from + (int64_t)h * p.D, e, x);
-    if (!is_v) turn8<VEC>(p, e, p.pos ? p.pos[row] : at, x);
-    T* cache = static_cast<T*>(is_v ? p.v_cache : p.k_cache) + (int64_t)page * p.page_st +
-               (at & ((1 << p.shift) - 1)) * p.slot_st + (int64_t)h * p.head_st;
-    store8<T, VEC>(p, cache, e, x);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      if (!to[q]) continue;
+      if (at[q] != kNoTurn) turn8<VEC>(p, e[q], at[q], x[q]);
+      store8<T, VEC>(p, to[q], e[q], x[q]);
+    }
   }
 }
 
@@ -251,45 +292,62 @@ __device__ __forceinline__ void append_page(const AppendParams& p, uint32_t idx)
   float* scale_at = (is_v ? p.v_scale : p.k_scale) + (uint64_t)page * p.Hkv + h;
 
   auto token = [&](uint32_t i, uint32_t* slot, Place8* e, float (&x)[8]) {   // item i of the new tokens
-    const uint32_t t = i / p.items;
+    const uint32_t t = p.items.of(i);
     *slot = s0 + t;
-    *e = place8(p, i - t * p.items);
+    *e = place8(p, i - t * p.items.d);
     const int64_t row = row0 + *slot;
     load8<bf16, VEC>(p, x0 + row * x_row + (int64_t)h * p.D, *e, x);
-    if (!is_v) turn8<VEC>(p, *e, p.pos ? p.pos[row] : at0 + *slot, x);
   };
-  const uint32_t n_items = (s1 - s0) * p.items;
+  auto turn = [&](uint32_t slot, const Place8& e, float (&x)[8]) {
+    if (!is_v) turn8<VEC>(p, e, p.pos ? p.pos[row0 + slot] : at0 + slot, x);
+  };
+  const uint32_t n_items = (s1 - s0) * p.items.d;
   float top = 0.0f;
-  for (uint32_t i = threadIdx.x; i < n_items; i += NT) {
-    uint32_t slot;
-    Place8 e;
-    float x[8];
-    token(i, &slot, &e, x);
+  auto largest = [&](const float (&x)[8]) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) {
       const float m = fabsf(x[t]);
       if (m < INFINITY) top = fmaxf(top, m);
     }
+  };
+  // the thread's first items stay in registers, turned
+  constexpr int N = 4;
+  float x[N][8];
+  Place8 e[N];
+  uint32_t slot[N];
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+    if (threadIdx.x + q * NT < n_items) token(threadIdx.x + q * NT, &slot[q], &e[q], x[q]);
+  const float was = s0 ? *scale_at : 0.0f;
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+    if (threadIdx.x + q * NT < n_items) {
+      turn(slot[q], e[q], x[q]);
+      largest(x[q]);
+    }
+  for (uint32_t i = threadIdx.x + N * NT; i < n_items; i += NT) {
+    uint32_t sl;
+    Place8 pl;
+    float y[8];
+    token(i, &sl, &pl, y);
+    turn(sl, pl, y);
+    largest(y);
   }
 #pragma unroll
   for (int off = 32; off; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
-  if constexpr (NT > 64) {
-    if (lane == 0) red[threadIdx.x >> 6] = top;
-    __syncthreads();
+  if (lane == 0) red[threadIdx.x >> 6] = top;
+  __syncthreads();   // also: the scale is read before it is written
 #pragma unroll
-    for (int i = 0; i < NT / 64; ++i) top = fmaxf(top, red[i]);
-  }
+  for (int i = 0; i < NT / 64; ++i) top = fmaxf(top, red[i]);
   float scale = pow2(scale_exp(top));
   if (s0) {
-    const float was = *scale_at;
-    __syncthreads();   // before it is written
     if (was > scale && was < INFINITY) {
       scale = was;
     } else if (was > 0.0f && was < scale) {
       const float by = was / scale;   // what the page holds, rounded again
-      for (uint32_t i = threadIdx.x; i < s0 * p.items; i += NT) {
-        const uint32_t t = i / p.items;
-        const Place8 e = place8(p, i - t * p.items);
+      for (uint32_t i = threadIdx.x; i < s0 * p.items.d; i += NT) {
+        const uint32_t t = p.items.of(i);
+        const Place8 e = place8(p, i - t * p.items.d);
         uint8_t* head = cache + (int64_t)t * p.slot_st;
         float x[8];
         if constexpr (VEC) {
@@ -310,12 +368,16 @@ __device__ __forceinline__ void append_page(const AppendParams& p, uint32_t idx)
   }
   if (threadIdx.x == 0) *scale_at = scale;
   const float inv = 1.0f / scale;   // exact
-  for (uint32_t i = threadIdx.x; i < n_items; i += NT) {
-    uint32_t slot;
-    Place8 e;
-    float x[8];
-    token(i, &slot, &e, x);
-    store8_e4m3<VEC>(p, cache + (int64_t)slot * p.slot_st, e, x, inv);
+#pragma unroll
+  for (int q = 0; q < N; ++q)
+    if (threadIdx.x + q * NT < n_items) store8_e4m3<VEC>(p, cache + (int64_t)slot[q] * p.slot_st, e[q], x[q], inv);
+  for (uint32_t i = threadIdx.x + N * NT; i < n_items; i += NT) {
+    uint32_t sl;
+    Place8 pl;
+    float y[8];
+    token(i, &sl, &pl, y);
+    turn(sl, pl, y);
+    store8_e4m3<VEC>(p, cache + (int64_t)sl * p.slot_st, pl, y, inv);
   }
 }
 
@@ -333,7 +395,7 @@ __global__ __launch_bounds__(NT) void append_kernel(AppendParams p) {
 template <typename T, bool VEC, int NT>
 int run(AppendParams& p, hipStream_t s) {
   const int64_t pages = p.e4m3 ? ((int64_t)(p.T >> p.shift) + 2 * (int64_t)p.N) * 2 * p.Hkv : 0;
-  const int64_t rows = p.H || !p.e4m3 ? (int64_t)(p.T / kRowTokens) + p.N : 0;
+  const int64_t rows = p.H || !p.e4m3 ? (int64_t)p.T / p.row_tokens + p.N : 0;
   if (!grid_fits(pages + rows, NT)) return DSP_ERR_SHAPE;
   p.page_groups = (uint32_t)pages;
   if (pages + rows) append_kernel<T, VEC, NT><<<dim3((uint32_t)(pages + rows)), NT, 0, s>>>(p);
@@ -353,8 +415,10 @@ int launch_kv_append(const AppendArgs& a, hipStream_t s) {
   p.max_pages = (uint32_t)a.max_pages, p.shift = a.page_shift;
   p.H = a.H, p.Hkv = a.Hkv, p.D = a.D, p.rot = a.rot;
   p.rot_items = (a.rot + kItem - 1) / kItem;
-  p.items = p.rot_items + (a.D - a.rot + kItem - 1) / kItem;
+  p.items = divisor(p.rot_items + (a.D - a.rot + kItem - 1) / kItem);
   p.half = a.half, p.e4m3 = a.e4m3, p.vec = a.vec;
+  p.row_tokens = 16;
+  while (p.row_tokens > 1 && a.T / p.row_tokens < 4096) p.row_tokens /= 2;
   if (!a.bf16) return a.vec ? run<float, true, 256>(p, s) : run<float, false, 256>(p, s);
   return a.vec ? run<bf16, true, 256>(p, s) : run<bf16, false, 256>(p, s);
 }

@@ -46,6 +46,7 @@ def _window(lib, bwd=False, **kw):
     (dsp.DSP_ERR_NULL, dict(os=None)),
     (dsp.DSP_ERR_SHAPE, dict(X=-1)),
     (dsp.DSP_ERR_SHAPE, dict(Hkv=3)),
+    (dsp.DSP_ERR_SHAPE, dict(H=1 << 15, Hkv=1)),
     (dsp.DSP_ERR_SHAPE, dict(Hkv=0)),
     (dsp.DSP_ERR_SHAPE, dict(D=132)),
     (dsp.DSP_ERR_SHAPE, dict(D=68)),
@@ -197,6 +198,7 @@ def test_page_refusals(lib, call, status, kw):
     (dsp.DSP_ERR_SHAPE, dict(P=0)),
     (dsp.DSP_ERR_SHAPE, dict(H=-1)),
     (dsp.DSP_ERR_SHAPE, dict(D=260)),
+    (dsp.DSP_ERR_SHAPE, dict(H=2044, row=2044 * 72, orow=2044 * 72)),
     (dsp.DSP_ERR_SHAPE, dict(krow=-1)),
     (dsp.DSP_ERR_ARG, dict(flags=4)),
     (dsp.DSP_ERR_ALIGN, dict(sin=A[12] + 2)),
