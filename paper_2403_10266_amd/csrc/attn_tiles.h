@@ -15,6 +15,8 @@
 
 #include <math.h>
 
+#include <algorithm>
+
 #include "attn_bf16_common.h"
 #include "dsp_internal.h"
 
@@ -147,6 +149,12 @@ struct ColA<bf16, DC> {
       s = read(lds + (row0 + ((c & 1) ? 16 : 0) + ((c & 2) ? 4 : 0) + (j16 >> 2)) * G::P + 32 * G::NT + 4 * (j16 & 3));
   }
 };
+template <int DC>
+struct ColA<float, DC> {   // fp32 reads them as it goes
+  const float* lds;
+  int row0, lane;
+  __device__ __forceinline__ void load(const float* l, int r, int n) { lds = l, row0 = r, lane = n; }
+};
 // the slab's B operands (as in slab_mma)
 __device__ __forceinline__ void slab_b(const ColB<bf16>& b, bf16x8 (&out)[2]) {
   const u32x4 x = __builtin_bit_cast(u32x4, b.v[0]), y = __builtin_bit_cast(u32x4, b.v[1]);
@@ -183,16 +191,19 @@ struct ColAcc {
     if constexpr (G::SLAB) slab_mma(lds, G::P, row0, 32 * G::NT, lane, b, s);
   }
   __device__ __forceinline__ void add(const ColA<T, DC>& a, const ColB<T>& b) {
-    static_assert(sizeof(T) == 2, "operands read ahead are bf16");
+    if constexpr (sizeof(T) == 4) {
+      add(a.lds, a.row0, a.lane, b);
+    } else {
 #pragma unroll
-    for (int kk = 0; kk < 2; ++kk)
+      for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
-      for (int i = 0; i < G::NT; ++i) t[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.t[i][kk], b.v[kk], t[i], 0, 0, 0);
-    if constexpr (G::SLAB) {
-      bf16x8 half[2];
-      slab_b(b, half);
+        for (int i = 0; i < G::NT; ++i) t[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.t[i][kk], b.v[kk], t[i], 0, 0, 0);
+      if constexpr (G::SLAB) {
+        bf16x8 half[2];
+        slab_b(b, half);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.s, half[h], s[h], 0, 0, 0);
+        for (int h = 0; h < 2; ++h) s[h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.s, half[h], s[h], 0, 0, 0);
+      }
     }
   }
   // times a factor that each lane holds for its own column n = lane % 32
@@ -369,6 +380,7 @@ struct Order {
   uint32_t heads, blocks;       // of a chunk: heads, blocks of each head
   uint32_t chunks_bx;           // chunks of one (b, x)
   bool costly_first;
+  uint32_t run;                 // 0, or the other order below: n_chunks blocks, per_xcd runs of `run`
 };
 inline Order make_order(int64_t bx, int64_t groups, int64_t grp, int64_t blocks, bool costly_first) {
   const int64_t rows = blocks <= 2 && bx >= 64 ? groups : 1;   // key/value heads of a chunk
@@ -379,9 +391,25 @@ inline Order make_order(int64_t bx, int64_t groups, int64_t grp, int64_t blocks,
   o.heads = (uint32_t)(rows * grp);
   o.blocks = (uint32_t)blocks;
   o.costly_first = costly_first;
+  o.run = 0;
   return o;
 }
-inline int64_t order_blocks(const Order& o) { return (int64_t)8 * o.per_xcd * o.heads * o.blocks; }
+// Blocks that see a window only: neighbouring blocks share rows, and the heads of a token
+// share cache lines, so an XCD takes runs of neighbouring blocks, each with all its heads
+// side by side; runs go to the XCDs in turn.
+inline Order make_run_order(int64_t bx, int64_t heads, int64_t blocks) {
+  Order o = {};
+  o.n_chunks = (uint32_t)(bx * blocks);
+  o.run = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(8, bx * blocks / 8));
+  o.per_xcd = ((o.n_chunks + o.run - 1) / o.run + 7) / 8;
+  o.heads = (uint32_t)heads;
+  o.blocks = (uint32_t)blocks;
+  o.chunks_bx = 1;
+  return o;
+}
+inline int64_t order_blocks(const Order& o) {
+  return (int64_t)8 * o.per_xcd * o.heads * (o.run ? o.run : o.blocks);
+}
 struct Place {
   uint32_t bx, h, block;   // block 0 is the most costly
   bool any;                // the grid is rounded up: nothing to do
@@ -390,6 +418,15 @@ __device__ __forceinline__ Place place(const Order& o, uint32_t i = blockIdx.x) 
   const uint32_t xcd = i & 7u, j = i >> 3;
   Place p;
   uint32_t local, head;
+  if (o.run) {
+    local = j / o.heads;
+    const uint32_t k = local / o.run, block = (k * 8 + xcd) * o.run + local - k * o.run;
+    p.h = j - local * o.heads;
+    p.any = block < o.n_chunks;
+    p.bx = block / o.blocks;
+    p.block = block - p.bx * o.blocks;
+    return p;
+  }
   if (o.costly_first) {
     const uint32_t n = o.per_xcd * o.heads, r = j % n;
     p.block = j / n;

@@ -29,10 +29,15 @@ __device__ __forceinline__ bool sees(const Seen& s, int32_t j) {
 __device__ __forceinline__ bool whole_group(const Seen& first, const Seen& last, int32_t key0) {
   return key0 + 16 <= last.sink || (key0 >= first.lo && key0 + 16 <= last.hi);
 }
+// the lowest n bits
+__device__ __forceinline__ uint32_t low_bits(int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; }
 // bit i: whether key key0 + i is seen
 __device__ __forceinline__ uint32_t seen_bits(const Seen& s, int32_t key0) {
-  auto below = [](int32_t n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1u; };
-  return below(s.sink - key0) | (below(s.hi - key0) & ~below(s.lo - key0));
+  return low_bits(s.sink - key0) | (low_bits(s.hi - key0) & ~low_bits(s.lo - key0));
+}
+// x where bit k (a constant) of bits is set, else 0, whatever x is: 2 operations
+__device__ __forceinline__ float keep_bit(float x, uint32_t bits, int k) {
+  return __uint_as_float(__float_as_uint(x) & (uint32_t)((int32_t)(bits << (31 - k)) >> 31));
 }
 __device__ __forceinline__ bool sees_any(const Seen& s) { return s.sink > 0 || s.lo < s.hi; }
 
@@ -246,6 +251,16 @@ __device__ __forceinline__ uint32_t piece_owner(const int32_t* q_start, uint32_t
     count = min(step, count - skip);
   }
   return lo;
+}
+
+// The order of blocks of `rows` rows whose other side is a window of `span` rows more, where
+// an XCD's L2 (4 MB) holds what the heads of such a block read; else that of whole sequences.
+inline Order window_order(const WindowArgs& a, int64_t blocks, int64_t rows) {
+  const int64_t es = a.bf16 ? 2 : 4;
+  const int64_t span = a.win.left < 0 || a.win.right < 0 ? INT64_MAX / 4096 : (int64_t)a.win.left + a.win.right + 1;
+  const int64_t bytes = (span + rows) * 2 * std::max(a.H, a.Hkv) * a.D * es;
+  if (blocks > 2 && span < INT64_MAX / 4096 && bytes <= (int64_t(5) << 19)) return make_run_order(a.B * a.X, a.Hkv, blocks);
+  return make_order(a.B * a.X, a.Hkv, 1, blocks, a.win.right >= 0 && a.win.left < 0);
 }
 
 }  // namespace

@@ -49,6 +49,28 @@ __device__ __forceinline__ int64_t bx_at(const BwdParams& p, uint32_t bx, const 
   return (int64_t)(bx / p.X) * st[0] + (int64_t)(bx % p.X) * st[1];
 }
 
+// The operands of a block's products, read from LDS ahead of them: the order is the one
+// written (in bf16, where a wave would otherwise wait for LDS before every MFMA).
+template <typename T>
+__device__ __forceinline__ void ahead() {
+  if constexpr (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
+}
+template <typename T, int DC>
+__device__ __forceinline__ void row_operand(const T* lds, int row0, int l32, int g, typename Mx<T>::frag (&a)[Geo<T, DC>::NS]) {
+  using G = Geo<T, DC>;
+#pragma unroll
+  for (int st = 0; st < G::NS; ++st)
+    a[st] = *reinterpret_cast<const typename Mx<T>::frag*>(lds + (row0 + l32) * G::P + 2 * G::E * st + G::E * g);
+}
+template <typename T, int DC>
+__device__ __forceinline__ void row_product(floatx16& s, const typename Mx<T>::frag (&a)[Geo<T, DC>::NS],
+                                            const typename Mx<T>::frag (&b)[Geo<T, DC>::NS]) {
+#pragma unroll
+  for (int r = 0; r < 16; ++r) s[r] = 0.0f;
+#pragma unroll
+  for (int st = 0; st < Geo<T, DC>::NS; ++st) s = Mx<T>::mma(a[st], b[st], s);
+}
+
 // dQ and Delta: 32 columns per wave, keys on the rows of the products.
 template <typename T, int DC, int NW, int KB, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams p) {
@@ -142,31 +164,28 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
     for (int kt = 0; kt < NKT; ++kt) {
       const int32_t key0 = tiles.key0(it) + 32 * kt;
       if (!wave_on || (key0 >= wl.sink && (key0 + 32 <= wf.lo || key0 >= wl.hi))) continue;
+      const bool mask = !(key0 + 32 <= wf.sink || (key0 >= wl.lo && key0 + 32 <= wf.hi));
       floatx16 s, dp;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
-#pragma unroll
-      for (int st = 0; st < G::NS; ++st) {
-        const int a = (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g;
-        s = M::mma(*reinterpret_cast<const typename M::frag*>(kl + a), qf[st], s);
-        dp = M::mma(*reinterpret_cast<const typename M::frag*>(vl + a), df[st], dp);
-      }
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = fmaf(s[r], p.c, -lse2);
-      if (!(key0 + 32 <= wf.sink || (key0 >= wl.lo && key0 + 32 <= wf.hi))) {
-        const int32_t j = key0 + 4 * g;
-        const uint32_t from = (uint32_t)(j - col.lo), width = (uint32_t)max(col.hi - col.lo, 0);
-        const int32_t left = col.sink - j;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int k = 8 * (r / 4) + r % 4;
-          if (!(from + k < width || k < left)) s[r] = -INFINITY;
-        }
-      }
+      typename M::frag ka[G::NS], va[G::NS];
+      row_operand<T, DC>(kl, 32 * kt, l32, g, ka);
+      row_operand<T, DC>(vl, 32 * kt, l32, g, va);
+      ahead<T>();
+      row_product<T, DC>(s, ka, qf);
+      ColA<T, DC> kt_a;
+      kt_a.load(kl, 32 * kt, lane);
+      ahead<T>();
+      row_product<T, DC>(dp, va, df);
+      const uint32_t bits = mask ? seen_bits(col, key0) >> (4 * g) : ~0u;
       ColB<T> z;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z.set(r, __builtin_amdgcn_exp2f(s[r]) * (dp[r] - delta));
-      dq.add(kl, 32 * kt, lane, z);
+      for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -lse2));
+      if (mask) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = keep_bit(s[r], bits, 8 * (r / 4) + r % 4);
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) z.set(r, s[r] * (dp[r] - delta));
+      dq.add(kt_a, z);
     }
     if (more) stash((it + 1) & 1);
     __syncthreads();
@@ -307,27 +326,28 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
       const int sub = i * QS + qs;
       const int32_t q0 = qt0 + 32 * sub;
       if (q0 >= any1 || q0 + 32 <= any0) continue;
+      const bool mask = q0 < all0 || q0 + 32 > all1;
       floatx16 s, dp;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.0f;
-#pragma unroll
-      for (int st = 0; st < G::NS; ++st) {
-        const int a = (32 * sub + l32) * G::P + 2 * G::E * st + G::E * g;
-        s = M::mma(*reinterpret_cast<const typename M::frag*>(ql + a), kf[st], s);
-        dp = M::mma(*reinterpret_cast<const typename M::frag*>(ol + a), vf[st], dp);
-      }
+      typename M::frag qa[G::NS], oa[G::NS];
+      row_operand<T, DC>(ql, 32 * sub, l32, g, qa);
+      row_operand<T, DC>(ol, 32 * sub, l32, g, oa);
+      ahead<T>();
+      row_product<T, DC>(s, qa, kf);
+      ColA<T, DC> o_a, q_a;
+      o_a.load(ol, 32 * sub, lane);
+      ahead<T>();
+      row_product<T, DC>(dp, oa, vf);
       // lane (n + 32 g): key n, queries 8 (r / 4) + 4 g + r % 4
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         const floatx4 l = *reinterpret_cast<const floatx4*>(sl + 32 * sub + 8 * q + 4 * g);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[4 * q + j] = fmaf(s[4 * q + j], p.c, -l[j]);
+        for (int j = 0; j < 4; ++j) s[4 * q + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], p.c, -l[j]));
       }
-      if (q0 < all0 || q0 + 32 > all1) {
-        const uint32_t from = (uint32_t)(q0 + 4 * g - mine.first), width = (uint32_t)max(mine.end - mine.first, 0);
+      if (mask) {
+        const uint32_t bits = (low_bits(mine.end - q0) & ~low_bits(mine.first - q0)) >> (4 * g);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (!(from + 8 * (r / 4) + r % 4 < width)) s[r] = -INFINITY;
+        for (int r = 0; r < 16; ++r) s[r] = keep_bit(s[r], bits, 8 * (r / 4) + r % 4);
       }
       ColB<T> pb, zb;
 #pragma unroll
@@ -335,13 +355,14 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
         const floatx4 dl = *reinterpret_cast<const floatx4*>(sl + QB + 32 * sub + 8 * q + 4 * g);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const float e = __builtin_amdgcn_exp2f(s[4 * q + j]);
-          pb.set(4 * q + j, e);
-          zb.set(4 * q + j, e * (dp[4 * q + j] - dl[j]));
+          pb.set(4 * q + j, s[4 * q + j]);
+          zb.set(4 * q + j, s[4 * q + j] * (dp[4 * q + j] - dl[j]));
         }
       }
-      dv.add(ol, 32 * sub, lane, pb);
-      dk.add(ql, 32 * sub, lane, zb);
+      q_a.load(ql, 32 * sub, lane);
+      ahead<T>();
+      dv.add(o_a, pb);
+      dk.add(q_a, zb);
     }
     if (more) stash(buf ^ 1);
     __syncthreads();
@@ -433,7 +454,7 @@ Sinks sinks_of(const WindowArgs& a) {
 template <typename T, int DC>
 int start_dq(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   constexpr int NW = 4, CB = 32 * NW, KB = 32, MINW = sizeof(T) == 2 && DC <= 64 ? 3 : sizeof(T) == 2 || DC <= 96 ? 2 : 1;
-  p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp.d + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
+  p.order = window_order(a, (a.Lq * p.grp.d + CB - 1) / CB, CB / p.grp.d + 1);
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T);
   auto* kernel = window_bwd_dq_kernel<T, DC, NW, KB, MINW>;
   if (!grid_fits(order_blocks(p.order), NW * 64)) return DSP_ERR_SHAPE;
@@ -446,7 +467,7 @@ template <typename T, int DC, int KW, int QS, int QT, int MINW>
 int start_dkv(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   static_assert(32 * KW == kDkvKeys, "the sinks' workspace");
   constexpr int QB = 32 * QT;
-  p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lk + 32 * KW - 1) / (32 * KW), a.win.right >= 0 && a.win.left < 0);
+  p.order = window_order(a, (a.Lk + 32 * KW - 1) / (32 * KW), 32 * KW);
   const Sinks sk = sinks_of(a);
   p.parts = (uint32_t)sk.parts, p.sink_blocks = (uint32_t)sk.blocks;
   const int64_t first = a.B * a.X * a.Hkv * sk.blocks * sk.parts, blocks = first + order_blocks(p.order);

@@ -297,7 +297,7 @@ struct Softmax {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         float e = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(s[j][r]), 0.0f, 1.0f);
-        if (!all) e = __uint_as_float(__float_as_uint(e) & (uint32_t)((int32_t)(bits << (31 - 8 * (r / 4) - r % 4)) >> 31));
+        if (!all) e = keep_bit(e, bits, 8 * (r / 4) + r % 4);
         a += e;
         pf[j].set(r, e);
       }
@@ -843,7 +843,7 @@ int start_many(FwdParams& p, const WindowArgs& a, hipStream_t s) {
     p.n_blk = (uint32_t)(a.T * p.grp.d / CB + a.B);
     blocks = (int64_t)p.n_blk * a.Hkv;
   } else {
-    p.order = make_order(a.B * a.X, a.Hkv, 1, (a.Lq * p.grp.d + CB - 1) / CB, a.win.right >= 0 && a.win.left < 0);
+    p.order = window_order(a, (a.Lq * p.grp.d + CB - 1) / CB, CB / p.grp.d + 1);
     blocks = order_blocks(p.order);
   }
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T) + 2 * (KB / 16) * 4;
