@@ -427,6 +427,171 @@ __global__ __launch_bounds__(256) void window_bwd_sink_kernel(BwdParams p, uint3
   }
 }
 
+// Short units, of at most 32 NW keys and columns: one work-group reads each row once.  Wave w
+// first takes columns 32 w .. against all keys, which lie in LDS (Delta = sum_j P dP, with
+// no need of o, then dQ); then its Q and dO, which it held in registers as operands, take the
+// place of the keys in LDS, it keeps keys 32 w .. in registers, and dK and dV follow with the
+// scores computed the other way round.  Memory bounds these.
+template <typename T, int DC, int NW, int MINW>
+__global__ __launch_bounds__(NW * 64, MINW) void window_bwd_short_kernel(BwdParams p) {
+  using G = Geo<T, DC>;
+  using M = Mx<T>;
+  using R = Rows16<T, T, DC>;
+  constexpr int NT = NW * 64, N = NW * 32, TILE = N * G::P;
+  constexpr int NL = 4;   // group loads of a wave: two of K, two of V
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  T* t0 = reinterpret_cast<T*>(smem);      // K, then Q: [N][P]
+  T* t1 = t0 + TILE;                       // V, then dO
+  float* st_lse = reinterpret_cast<float*>(t1 + TILE);   // [N], exp2 units
+  float* st_del = st_lse + N;
+
+  const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Place pl = place(p.order);
+  if (!pl.any) return;
+  const uint32_t bx = pl.bx, e = pl.h, b = bx / p.X, nc = p.Lq * p.grp.d;
+  const int D = (int)p.D;
+  const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D, q_at = bx_at(p, bx, p.qs), o_at = bx_at(p, bx, p.os);
+  const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
+  const int64_t p0 = position(p.q_pos, b);
+  const Columns cs(p.grp, 0);
+  const Seen first = seen(p.win, p0, len), last = seen(p.win, p0 + p.Lq - 1, len);
+  const typename R::Map map = R::map(D, (uint32_t)p.ks[2] * (uint32_t)sizeof(T), lane);
+  R rows[NL];
+#pragma unroll
+  for (int i = 0; i < NL; ++i) {
+    const int32_t key0 = 32 * wave + 16 * (i & 1);
+    rows[i].fetch(map, static_cast<const T*>(i < 2 ? p.k : p.v) + k_at + (int64_t)key0 * p.ks[2], D, p.vec,
+                  whole_group(first, last, key0), [&](int r) {
+                    const int32_t j = key0 + r;
+                    return j < last.sink || (j >= first.lo && j < last.hi);
+                  });
+  }
+  const uint32_t w0 = 32 * wave, n = w0 + l32, qi = cs.query(min(n, nc - 1)), qh = e * p.grp.d + cs.head(min(n, nc - 1), qi);
+  const bool on = n < nc;
+  auto at = [&](const void* base, int64_t from, int64_t row) {
+    return on ? static_cast<const T*>(base) + from + (int64_t)qi * row + (int64_t)qh * D : nullptr;
+  };
+  typename M::frag qf[G::NS], df[G::NS];
+  row_frags<T, DC>(at(p.q, q_at, p.qs[2]), g, D, p.vec, qf);
+  row_frags<T, DC>(at(p.dout, o_at, p.os[2]), g, D, p.vec, df);
+  const float l = on ? p.lse[((uint64_t)bx * p.H + qh) * p.Lq + qi] : -INFINITY;
+  const float lse2 = l == -INFINITY ? INFINITY : l * kLog2e;   // sees nothing, or past the end: P = 0
+  const Seen col = seen(p.win, p0 + qi, len);
+  clear_cols<T, DC>(t0, 2 * N, D, threadIdx.x, NT);
+#pragma unroll
+  for (int i = 0; i < NL; ++i) rows[i].stash(map, (i < 2 ? t0 : t1) + (32 * wave + 16 * (i & 1)) * G::P, 1.0f);
+  __syncthreads();
+
+  // columns against the keys
+  const bool wave_on = w0 < nc;
+  const Seen wf = seen(p.win, p0 + cs.query(min(w0, nc - 1)), len), wl = seen(p.win, p0 + cs.query(min(w0 + 31, nc - 1)), len);
+  float delta = 0.0f;
+  ColAcc<T, DC> dq;
+  dq.zero();
+  auto block = [&](int key0, floatx16& s, floatx16& dp) {   // P and dP
+    typename M::frag a[G::NS];
+    row_operand<T, DC>(t0, key0, l32, g, a);
+    row_product<T, DC>(s, a, qf);
+    row_operand<T, DC>(t1, key0, l32, g, a);
+    row_product<T, DC>(dp, a, df);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -lse2));
+    if (!(key0 + 32 <= wf.sink || (key0 >= wl.lo && key0 + 32 <= wf.hi))) {
+      const uint32_t bits = seen_bits(col, key0) >> (4 * g);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = keep_bit(s[r], bits, 8 * (r / 4) + r % 4);
+    }
+  };
+  auto none = [&](int key0) { return !wave_on || (key0 >= wl.sink && (key0 + 32 <= wf.lo || key0 >= wl.hi)); };
+  for (int key0 = 0; key0 < N; key0 += 32) {
+    if (none(key0)) continue;
+    floatx16 s, dp;
+    block(key0, s, dp);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) delta += s[r] * dp[r];
+  }
+  delta += swap_halves(delta);
+  for (int key0 = 0; key0 < N; key0 += 32) {
+    if (none(key0)) continue;
+    floatx16 s, dp;
+    block(key0, s, dp);
+    ColB<T> z;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) z.set(r, s[r] * (dp[r] - delta));
+    dq.add(t0, key0, lane, z);
+  }
+  if (g == 0) st_lse[n] = lse2, st_del[n] = delta;
+  typename M::frag kf[G::NS], vf[G::NS];
+  row_operand<T, DC>(t0, w0, l32, g, kf);
+  row_operand<T, DC>(t1, w0, l32, g, vf);
+  __syncthreads();   // the keys are done with
+  dq.scale(p.scale, lane);
+  T* out = static_cast<T*>(p.dq) + q_at + (int64_t)e * p.grp.d * D;
+  auto q_row = [&](int k) -> T* {
+    const uint32_t c = w0 + k, i = cs.query(c);
+    return c < nc ? out + (int64_t)i * p.qs[2] + (int64_t)cs.head(c, i) * D : nullptr;
+  };
+  if (p.vec) store_rows_lds<T, DC>(t0 + w0 * G::P, dq, lane, D, G::DP, q_row);
+  else store_rows<T, DC>(dq, lane, D, false, q_row);
+  wave_order();
+#pragma unroll
+  for (int st = 0; st < G::NS; ++st) {
+    const int to = (w0 + l32) * G::P + 2 * G::E * st + G::E * g;
+    *reinterpret_cast<typename M::frag*>(t0 + to) = qf[st];
+    *reinterpret_cast<typename M::frag*>(t1 + to) = df[st];
+  }
+  __syncthreads();
+
+  // keys against the columns: key j's are those of the queries that see it
+  const int32_t key = (int32_t)w0 + l32, grp = (int32_t)p.grp.d;
+  const SeenBy mine = seen_by(p.win, p0, (int32_t)p.Lq, len, key);
+  const int32_t c_first = mine.first * grp, c_end = mine.end * grp;
+  ColAcc<T, DC> dk, dv;
+  dk.zero();
+  dv.zero();
+  for (int c0 = 0; c0 < N; c0 += 32) {
+    const uint32_t all = low_bits(c_end - c0) & ~low_bits(c_first - c0);
+    if (c0 >= (int32_t)nc || !__any(all != 0)) continue;
+    const uint32_t bits = all >> (4 * g);
+    floatx16 s, dp;
+    typename M::frag a[G::NS];
+    row_operand<T, DC>(t0, c0, l32, g, a);
+    row_product<T, DC>(s, a, kf);
+    row_operand<T, DC>(t1, c0, l32, g, a);
+    row_product<T, DC>(dp, a, vf);
+    ColB<T> pb, zb;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const floatx4 ll = *reinterpret_cast<const floatx4*>(st_lse + c0 + 8 * q + 4 * g);
+      const floatx4 dl = *reinterpret_cast<const floatx4*>(st_del + c0 + 8 * q + 4 * g);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float pr = keep_bit(__builtin_amdgcn_exp2f(fmaf(s[4 * q + j], p.c, -ll[j])), bits, 8 * q + j);
+        pb.set(4 * q + j, pr);
+        zb.set(4 * q + j, pr * (dp[4 * q + j] - dl[j]));
+      }
+    }
+    dv.add(t1, c0, lane, pb);
+    dk.add(t0, c0, lane, zb);
+  }
+  __syncthreads();   // Q and dO are done with
+  dk.scale(p.scale, lane);
+  auto k_row = [&](void* base) {
+    return [&, base](int k) -> T* {
+      const uint32_t r = w0 + k;
+      return r < p.Lk ? static_cast<T*>(base) + k_at + (int64_t)r * p.ks[2] : nullptr;
+    };
+  };
+  if (p.vec) {
+    store_rows_lds<T, DC>(t0 + w0 * G::P, dk, lane, D, G::DP, k_row(p.dk));
+    store_rows_lds<T, DC>(t1 + w0 * G::P, dv, lane, D, G::DP, k_row(p.dv));
+  } else {
+    store_rows<T, DC>(dk, lane, D, false, k_row(p.dk));
+    store_rows<T, DC>(dv, lane, D, false, k_row(p.dv));
+  }
+}
+
 template <typename K>
 int lds_limit(K* kernel, size_t lds) {
   if (lds <= 64 * 1024) return DSP_OK;
@@ -484,8 +649,30 @@ int start_dkv(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   return last_launch_status();
 }
 
+// Waves of the short form, 0: the unit is too long.
+int short_waves(const WindowArgs& a) {
+  const int64_t most = std::max<int64_t>(a.Lq * (a.H / a.Hkv), a.Lk);
+  return a.Lq == 0 || a.Lk == 0 || most > 128 ? 0 : most <= 32 ? 1 : most <= 64 ? 2 : 4;
+}
+template <typename T, int DC, int NW, int MINW>
+int start_short(BwdParams& p, const WindowArgs& a, hipStream_t s) {
+  p.order = make_order(a.B * a.X, a.Hkv, 1, 1, false);
+  const size_t lds = (size_t)2 * 32 * NW * Geo<T, DC>::P * sizeof(T) + (size_t)2 * 32 * NW * 4;
+  auto* kernel = window_bwd_short_kernel<T, DC, NW, MINW>;
+  if (!grid_fits(order_blocks(p.order), NW * 64)) return DSP_ERR_SHAPE;
+  if (int st = lds_limit(kernel, lds)) return st;
+  kernel<<<dim3((uint32_t)order_blocks(p.order)), NW * 64, lds, s>>>(p);
+  return last_launch_status();
+}
+
 template <typename T, int DC>
 int start(BwdParams& p, const WindowArgs& a, hipStream_t s) {
+  constexpr int MS = sizeof(T) == 4 ? 1 : DC <= 48 ? 3 : DC <= 96 ? 2 : 1;
+  switch (short_waves(a)) {
+    case 1: return start_short<T, DC, 1, MS>(p, a, s);
+    case 2: return start_short<T, DC, 2, MS>(p, a, s);
+    case 4: return start_short<T, DC, 4, MS>(p, a, s);
+  }
   if (a.Lq > 0)
     if (int st = start_dq<T, DC>(p, a, s)) return st;
   if (a.Lk == 0) return DSP_OK;
@@ -496,6 +683,7 @@ int start(BwdParams& p, const WindowArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t attn_window_bwd_workspace_bytes(const WindowArgs& a) {
+  if (short_waves(a)) return 0;
   const int64_t stats = (a.B * a.X * a.H * a.Lq + 63) / 64 * 64;
   const Sinks s = sinks_of(a);
   return (size_t)(stats + a.B * a.X * a.Hkv * s.blocks * s.parts * 2 * kDkvKeys * a.D) * 4;

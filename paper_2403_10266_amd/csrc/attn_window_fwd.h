@@ -370,17 +370,17 @@ __device__ __forceinline__ Edges edges(const Window& w, const U& u, const Column
 
 // Many columns: QT blocks of 32 per wave, the keys in LDS tiles that all waves share,
 // the next tile on its way in registers.
-template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int MINW>
+template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int NKT, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) {
   using G = Geo<T, DC>;
   using M = Mx<T>;
   using U = Unit<T, S, PAGED>;
   using R = Rows16<T, S, DC>;
-  constexpr int NT = NW * 64, CB = NW * 32 * QT, NKT = KB / 32, GR = KB / 16;
+  constexpr int NT = NW * 64, CB = NW * 32 * QT, GR = KB / 16;
   constexpr int TILE = KB * G::P;
   constexpr int NL = (2 * GR + NW - 1) / NW;   // group loads of a wave: K's groups, then V's
   static_assert(2 * GR % NW == 0, "every wave loads the same");
-  static_assert(NW <= 4 * NKT, "the output rows fit the tiles");
+  static_assert(NW * 32 <= 4 * KB && KB % (32 * NKT) == 0, "the output rows fit the tiles, a tile is whole steps");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   T* lds = reinterpret_cast<T*>(smem);                       // [2][K, V][KB][P]
   uint32_t* gone = reinterpret_cast<uint32_t*>(lds + 4 * TILE);   // [2][GR]: pages that are not there
@@ -478,15 +478,21 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
         for (int i = 0; i < GR; ++i) lost_bits |= gone[buf * GR + i] << i;
         lost_bits = __builtin_amdgcn_readfirstlane(lost_bits);
       }
-      auto kf = [&](int kt, int st) {
-        return *reinterpret_cast<const typename M::frag*>(kl + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
-      };
-      const bool mask = lost_bits || !ed.all(key0, KB);
-      if (sm.set) {
-        if (sm.fast(kf, kl + TILE, qf, key0, mask, lost_bits, p.c, col, lane))
-          sm.fix(kf, kl + TILE, qf, key0, mask, lost_bits, p.c, col, lane);
-      } else {
-        sm.exact(kf, kl + TILE, qf, key0, mask, lost_bits, p.c, col, lane);
+      for (int k0 = 0; k0 < KB; k0 += 32 * NKT) {
+        const int32_t at = key0 + k0;
+        if (KB > 32 * NKT && ed.none(at, 32 * NKT)) continue;
+        const T* ks = kl + k0 * G::P;
+        auto kf = [&](int kt, int st) {
+          return *reinterpret_cast<const typename M::frag*>(ks + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
+        };
+        const uint32_t lost_here = lost_bits >> (k0 / 16) & ((1u << (2 * NKT)) - 1);
+        const bool mask = lost_here || !ed.all(at, 32 * NKT);
+        if (sm.set) {
+          if (sm.fast(kf, ks + TILE, qf, at, mask, lost_here, p.c, col, lane))
+            sm.fix(kf, ks + TILE, qf, at, mask, lost_here, p.c, col, lane);
+        } else {
+          sm.exact(kf, ks + TILE, qf, at, mask, lost_here, p.c, col, lane);
+        }
       }
     }
     if (more) stash(buf ^ 1);
@@ -835,7 +841,7 @@ int launch(K* kernel, int64_t blocks, int threads, size_t lds, FwdParams& p, hip
   return last_launch_status();
 }
 
-template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int MINW>
+template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int NKT, int MINW>
 int start_many(FwdParams& p, const WindowArgs& a, hipStream_t s) {
   constexpr int CB = NW * 32 * QT;
   int64_t blocks;
@@ -847,7 +853,7 @@ int start_many(FwdParams& p, const WindowArgs& a, hipStream_t s) {
     blocks = order_blocks(p.order);
   }
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T) + 2 * (KB / 16) * 4;
-  return launch(window_fwd_kernel<T, S, PAGED, DC, NW, QT, KB, MINW>, blocks, NW * 64, lds, p, s);
+  return launch(window_fwd_kernel<T, S, PAGED, DC, NW, QT, KB, NKT, MINW>, blocks, NW * 64, lds, p, s);
 }
 
 template <typename T, int DC, int NW, int KEYS, int MINW>
@@ -922,8 +928,9 @@ int start(FwdParams& p, const WindowArgs& a, const Choice& c, hipStream_t s) {
   // keys, 160 and 174 with two waves and 64 and 32; 32 heads of 8192 x 64, window 2048, 172 us
   // with three waves and 64 keys, 198 with 32; 16 of 8192 x 128, window 1024, with two waves 218
   // and 226.
+  // Steps of 32 keys inside a tile of 64 above that: 209 us.
   constexpr bool B16 = sizeof(T) == 2, WIDE = DC > 64 && DC <= 96;
-  return start_many<T, S, PAGED, DC, 4, 1, B16 && !WIDE ? 64 : 32, B16 ? (DC <= 96 ? 3 : 2) : 1>(p, a, s);
+  return start_many<T, S, PAGED, DC, 4, 1, B16 && !WIDE ? 64 : 32, B16 && DC <= 64 ? 2 : 1, B16 ? (DC <= 96 ? 3 : 2) : 1>(p, a, s);
 }
 
 inline FwdParams params(const WindowArgs& a) {

@@ -91,12 +91,14 @@ def test_window_workspaces(lib):
         assert _window(lib, **LONG, **kw) == dsp.DSP_ERR_WORKSPACE
     for at in (A[0], A[1], A[2], A[3], A[4], A[3] - need + 16):
         assert _window(lib, **LONG, ws=at) == dsp.DSP_ERR_ARG, hex(at)
-    need = lib.dsp_attn_window_bwd_workspace_bytes(2, 3, 5, 7, 4, 2, 72, 3, 0, 1, BF)
+    assert lib.dsp_attn_window_bwd_workspace_bytes(2, 3, 5, 7, 4, 2, 72, 3, 0, 1, BF) == 0     # short units need none
+    need = lib.dsp_attn_window_bwd_workspace_bytes(2, 3, 5, 150, 4, 2, 72, 3, 0, 1, BF)
     assert need > 0
+    more = dict(Lk=150, ks=_st(450 * 144, 150 * 144, 144))
     for kw in (dict(ws=None), dict(nws=need - 1), dict(ws=A[7] + 8)):
-        assert _window(lib, True, **kw) == dsp.DSP_ERR_WORKSPACE
+        assert _window(lib, True, **more, **kw) == dsp.DSP_ERR_WORKSPACE
     for at in (A[0], A[1], A[2], A[3], A[4], A[8], A[9], A[10], A[11]):
-        assert _window(lib, True, ws=at) == dsp.DSP_ERR_ARG, hex(at)
+        assert _window(lib, True, **more, ws=at) == dsp.DSP_ERR_ARG, hex(at)
     assert lib.dsp_attn_window_workspace_bytes(-1, 1, 1, 5000, 8, 2, 72, -1, 0, 0, BF) == 0
     assert lib.dsp_attn_window_bwd_workspace_bytes(2, 3, 5, 7, 4, 3, 72, 3, 0, 1, BF) == 0
     # long windows and short ones; sinks that every query sees ask for partial sums
