@@ -57,6 +57,12 @@ struct Tiles {
   __device__ __forceinline__ int32_t key0(int32_t t) const { return t < sinks ? t * KB : band + (t - sinks) * KB; }
 };
 
+// x where bit k is set, else -inf: 2 operations
+__device__ __forceinline__ float mask_bit(float x, uint32_t bits, int k) {
+  const uint32_t t = (uint32_t)((int32_t)(bits << (31 - k)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & t) | (~t & 0xFF800000u));
+}
+
 // Division by a number below 2^15 that the host knows: exact for n up to 2^16 (and n d below
 // 2^32), by one multiplication.
 struct Divisor {

@@ -170,16 +170,17 @@ struct Softmax {
     if (!mask) return;
 #pragma unroll
     for (int j = 0; j < QT; ++j) {
-      const int32_t at = key0 + 32 * kt + 4 * (lane >> 5);
-      const uint32_t from = (uint32_t)(at - cols[j].lo), width = (uint32_t)max(cols[j].hi - cols[j].lo, 0);
-      const int32_t left = cols[j].sink - at;
+      uint32_t bits = block_bits(cols[j], kt, key0, gone) >> (4 * (lane >> 5));
+      // formed again here: kept from fast() to fix() they take 32 registers, which spill (3.7 times the time)
+      asm volatile("" : "+v"(bits));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int k = 8 * (r / 4) + r % 4;
-        const bool off = gone >> (2 * kt + r / 8) & 1;
-        if (off || !(from + k < width || k < left)) s[j][r] = -INFINITY;
-      }
+      for (int r = 0; r < 16; ++r) s[j][r] = mask_bit(s[j][r], bits, 8 * (r / 4) + r % 4);
     }
+  }
+  // bit i: whether the column sees key key0 + 32 kt + i
+  static __device__ __forceinline__ uint32_t block_bits(const Seen& col, int kt, int32_t key0, uint32_t gone) {
+    const uint32_t lost = (gone >> (2 * kt) & 1 ? 0xFFFFu : 0u) | (gone >> (2 * kt) & 2 ? 0xFFFF0000u : 0u);
+    return seen_bits(col, key0 + 32 * kt) & ~lost;
   }
   __device__ __forceinline__ void product(const T* vl, const ColB<T> (&pf)[NKT][QT], int lane) {
 #pragma unroll
@@ -308,9 +309,8 @@ struct Softmax {
       for (int j = 0; j < QT; ++j) at(j, 0, true);
       return;
     }
-    const uint32_t lost = (gone >> (2 * kt) & 1 ? 0xFFFFu : 0u) | (gone >> (2 * kt) & 2 ? 0xFFFF0000u : 0u);
 #pragma unroll
-    for (int j = 0; j < QT; ++j) at(j, (seen_bits(cols[j], key0 + 32 * kt) & ~lost) >> (4 * (lane >> 5)), false);
+    for (int j = 0; j < QT; ++j) at(j, block_bits(cols[j], kt, key0, gone) >> (4 * (lane >> 5)), false);
   }
 
   // After fast() of the same tile: for each column with a score above its reference, the
@@ -462,41 +462,63 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   Softmax<T, DC, QT, NKT, true> sm;
   sm.init();
   __syncthreads();
-  for (int32_t it = 0; it < tiles.n; ++it) {
-    const int32_t key0 = tiles.key0(it);
-    const bool more = it + 1 < tiles.n;
-    if (more) {
-      fetch(it + 1);
-      ask(it + 2);
-    }
-    const int buf = it & 1;
-    const T* kl = lds + buf * 2 * TILE;
-    if (on && !ed.none(key0, KB)) {
-      uint32_t lost_bits = 0;
-      if constexpr (PAGED) {
-#pragma unroll
-        for (int i = 0; i < GR; ++i) lost_bits |= gone[buf * GR + i] << i;
-        lost_bits = __builtin_amdgcn_readfirstlane(lost_bits);
-      }
-      for (int k0 = 0; k0 < KB; k0 += 32 * NKT) {
-        const int32_t at = key0 + k0;
-        if (KB > 32 * NKT && ed.none(at, 32 * NKT)) continue;
-        const T* ks = kl + k0 * G::P;
-        auto kf = [&](int kt, int st) {
-          return *reinterpret_cast<const typename M::frag*>(ks + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
-        };
-        const uint32_t lost_here = lost_bits >> (k0 / 16) & ((1u << (2 * NKT)) - 1);
-        const bool mask = lost_here || !ed.all(at, 32 * NKT);
-        if (sm.set) {
-          if (sm.fast(kf, ks + TILE, qf, at, mask, lost_here, p.c, col, lane))
-            sm.fix(kf, ks + TILE, qf, at, mask, lost_here, p.c, col, lane);
-        } else {
-          sm.exact(kf, ks + TILE, qf, at, mask, lost_here, p.c, col, lane);
-        }
-      }
-    }
-    if (more) stash(buf ^ 1);
+  // A tile's steps of 32 NKT keys: exact ones until every column has a reference, then fast
+  // ones, in a loop that the rare fix() stands outside of (inside, its registers weigh on it:
+  // 8192 causal tokens 173 and 185 us).  Waves go from one loop to the other by themselves;
+  // each meets every tile's barrier once.
+  int32_t it = 0, k0 = 0;
+  auto begin = [&]() {   // the tile after it sets out
+    if (it + 1 >= tiles.n) return;
+    fetch(it + 1);
+    ask(it + 2);
+  };
+  auto advance = [&]() {
+    k0 += 32 * NKT;
+    if (k0 < KB) return;
+    if (it + 1 < tiles.n) stash((it + 1) & 1);
     __syncthreads();
+    k0 = 0;
+    if (++it < tiles.n) begin();
+  };
+  // f(operands, values, first key, mask, keys not there) for a step that the wave's columns see
+  auto step = [&](auto f) {
+    const int32_t key0 = tiles.key0(it) + k0;
+    if (!on || ed.none(key0, 32 * NKT)) return false;
+    uint32_t lost_bits = 0;
+    if constexpr (PAGED) {
+      const uint32_t* flag = gone + (it & 1) * GR + k0 / 16;
+#pragma unroll
+      for (int i = 0; i < 2 * NKT; ++i) lost_bits |= flag[i] << i;
+      lost_bits = __builtin_amdgcn_readfirstlane(lost_bits);
+    }
+    const T* ks = lds + (it & 1) * 2 * TILE + k0 * G::P;
+    auto kf = [&](int kt, int st) {
+      return *reinterpret_cast<const typename M::frag*>(ks + (32 * kt + l32) * G::P + 2 * G::E * st + G::E * g);
+    };
+    return f(kf, ks + TILE, key0, lost_bits || !ed.all(key0, 32 * NKT), lost_bits);
+  };
+  if (tiles.n) begin();
+  while (it < tiles.n && !sm.set) {
+    step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) {
+      sm.exact(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
+      return false;
+    });
+    advance();
+  }
+  while (it < tiles.n) {
+    bool moved = false;
+    for (; it < tiles.n && !moved;) {
+      moved = step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) {
+        return sm.fast(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
+      });
+      if (!moved) advance();
+    }
+    if (!moved) break;
+    step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) {
+      sm.fix(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
+      return true;
+    });
+    advance();
   }
 
 #pragma unroll
