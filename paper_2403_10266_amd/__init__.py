@@ -883,29 +883,38 @@ def dsp_attn_window_bwd(q, k, v, o, dout, lse, H: int, Hkv: int, left: int = -1,
     return dq, dk, dv
 
 
-def _rows2(w, name, t, dt, shape, like):
+def _rows2(w, name, t, dt, shape, dev, like):
     """Packed rows: a 2-D view with a unit last stride."""
-    if not (_as(t, dt, shape, like.get_device()) and t.stride(1) == 1):
+    if not (_as(t, dt, shape, dev) and t.stride(1) == 1):
         _check(w, name, t, dtype=dt, shape=shape, contiguous=False, like=like)
         raise ValueError(f"{w}: {name} must have a unit last stride")
     return t
 
 
-def _paged_args(w, like, k_cache, v_cache, table, q_start, kv_len, k_scale, v_scale):
-    """Checks what the calls on a paged cache share; returns (N, n_pages, max_pages, page, Hkv, D, cache dtype)."""
+def _cache_refusal(w, like, caches):
+    """Says what is wrong with a pair of caches."""
     torch = _torch()
-    dt, f8, dev = _float_dtype(w, like), torch.float8_e4m3fn, like.get_device()
-    for name, c in (("k_cache", k_cache), ("v_cache", v_cache)):
+    dt, f8 = like.dtype, torch.float8_e4m3fn
+    for name, c in zip(("k_cache", "v_cache"), caches):
         _check(w, name, c, contiguous=False, like=like)
         if c.dtype not in (dt, f8) or (c.dtype == f8 and dt != torch.bfloat16):
             raise ValueError(f"{w}: {name} must be {dt}" + (" or float8_e4m3fn" if dt == torch.bfloat16 else "")
                              + f", got {c.dtype}")
         if c.dim() != 4 or c.stride(3) != 1:
             raise ValueError(f"{w}: {name} must be a view [pages, page, Hkv, D] with a unit last stride")
-    if k_cache.dtype != v_cache.dtype or k_cache.shape != v_cache.shape or not _same_layout(k_cache, v_cache):
-        raise ValueError(f"{w}: k_cache and v_cache must have one type, shape and layout")
+    raise ValueError(f"{w}: k_cache and v_cache must have one type, shape and layout")
+
+
+def _paged_args(w, like, dt, dev, k_cache, v_cache, table, q_start, kv_len, k_scale, v_scale):
+    """Checks what the calls on a paged cache share; returns (N, n_pages, max_pages, page, Hkv, D, cache dtype)."""
+    torch = _torch()
+    i32 = torch.int32
+    ct = k_cache.dtype if k_cache is not None else None
+    e4m3 = ct is torch.float8_e4m3fn
+    if (ct is not dt and not (e4m3 and dt is torch.bfloat16)) or k_cache.dim() != 4 or k_cache.get_device() != dev \
+            or k_cache.stride(3) != 1 or not _as(v_cache, ct, k_cache.shape, dev) or not _same_layout(k_cache, v_cache):
+        _cache_refusal(w, like, (k_cache, v_cache))
     n_pages, page, Hkv, D = k_cache.shape
-    e4m3 = k_cache.dtype == f8
     for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
         if (t is not None) != e4m3:
             raise ValueError(f"{w}: {name} comes with float8_e4m3fn caches, and only with them")
@@ -913,11 +922,11 @@ def _paged_args(w, like, k_cache, v_cache, table, q_start, kv_len, k_scale, v_sc
             _check(w, name, t, dtype=torch.float32, shape=(n_pages, Hkv), like=like)
     if table is None or table.dim() != 2 or kv_len is None or q_start is None:
         raise ValueError(f"{w}: table [N, max_pages], q_start [N + 1] and kv_len [N] are required")
-    N = table.shape[0]
-    _lengths(w, like, tuple(table.shape), table=table)
-    _lengths(w, like, (N + 1,), q_start=q_start)
-    _lengths(w, like, (N,), kv_len=kv_len)
-    return N, n_pages, table.shape[1], page, Hkv, D, DSP_E4M3 if e4m3 else _dtype_code(like)
+    N, max_pages = table.shape
+    for name, t, shape in (("table", table, (N, max_pages)), ("q_start", q_start, (N + 1,)), ("kv_len", kv_len, (N,))):
+        if not (_as(t, i32, shape, dev) and t.is_contiguous()):
+            _check(w, name, t, dtype=i32, shape=shape, like=like)
+    return N, n_pages, max_pages, page, Hkv, D, DSP_E4M3 if e4m3 else DSP_BF16 if dt is torch.bfloat16 else DSP_F32
 
 
 def dsp_kv_append(k, v, k_cache, v_cache, table, q_start, kv_len, k_scale=None, v_scale=None, cos=None, sin=None,
@@ -934,19 +943,20 @@ def dsp_kv_append(k, v, k_cache, v_cache, table, q_start, kv_len, k_scale=None, 
     torch = _torch()
     w = "dsp_kv_append"
     _check(w, "k", k, contiguous=False)
-    N, n_pages, max_pages, page, Hkv, D, cdt = _paged_args(w, k, k_cache, v_cache, table, q_start, kv_len, k_scale, v_scale)
+    dt, dev = _float_dtype(w, k), k.get_device()
+    N, n_pages, max_pages, page, Hkv, D, cdt = _paged_args(w, k, dt, dev, k_cache, v_cache, table, q_start, kv_len, k_scale,
+                                                           v_scale)
     if k.dim() != 2:
         raise ValueError(f"{w}: k and v must be packed rows [T, Hkv * D]")
-    T, dt = k.shape[0], k.dtype
-    _rows2(w, "k", k, dt, (T, Hkv * D), k)
-    _rows2(w, "v", v, dt, (T, Hkv * D), k)
+    T = k.shape[0]
+    _rows2(w, "k", k, dt, (T, Hkv * D), dev, k)
+    _rows2(w, "v", v, dt, (T, Hkv * D), dev, k)
     H = 0
     if q is not None:
-        _check(w, "q", q, dtype=dt, contiguous=False, like=k)
         if q.dim() != 2 or q.shape[0] != T or q.shape[1] % D or q.shape[1] == 0:
             raise ValueError(f"{w}: q must be packed rows [T, H * D]")
         H = q.shape[1] // D
-        _rows2(w, "q", q, dt, (T, H * D), k)
+        _rows2(w, "q", q, dt, (T, H * D), dev, k)
     elif out_q is not None:
         raise ValueError(f"{w}: out_q without q")
     if (cos is None) != (sin is None):
@@ -956,14 +966,15 @@ def dsp_kv_append(k, v, k_cache, v_cache, table, q_start, kv_len, k_scale=None, 
         if cos.dim() != 2:
             raise ValueError(f"{w}: cos must be [P, rot / 2]")
         for name, t in (("cos", cos), ("sin", sin)):
-            if not (_as(t, torch.float32, cos.shape, k.get_device()) and t.is_contiguous()):
+            if not (_as(t, torch.float32, cos.shape, dev) and t.is_contiguous()):
                 _check(w, name, t, dtype=torch.float32, shape=cos.shape, like=k)
         P, rot = cos.shape[0], 2 * cos.shape[1]
-    _lengths(w, k, (T,), pos=pos)
+    if pos is not None:
+        _lengths(w, k, (T,), pos=pos)
     with _on_device(k, stream) as s:
         if q is not None:
             out_q = torch.empty((T, H * D), dtype=dt, device=k.device) if out_q is None else out_q
-            _rows2(w, "out_q", out_q, dt, (T, H * D), k)
+            _rows2(w, "out_q", out_q, dt, (T, H * D), dev, k)
         _check_status(lib().dsp_kv_append(
             k.data_ptr(), v.data_ptr(), _at(q), _at(out_q), k_cache.data_ptr(), v_cache.data_ptr(), _at(k_scale),
             _at(v_scale), table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), _at(cos), _at(sin), _at(pos), P, rot,
@@ -984,16 +995,18 @@ def dsp_attn_paged(q, k_cache, v_cache, table, q_start, kv_len, H: int, max_q: i
     torch = _torch()
     w = "dsp_attn_paged"
     _check(w, "q", q, contiguous=False)
-    N, n_pages, max_pages, page, Hkv, D, cdt = _paged_args(w, q, k_cache, v_cache, table, q_start, kv_len, k_scale, v_scale)
+    dt, dev = _float_dtype(w, q), q.get_device()
+    N, n_pages, max_pages, page, Hkv, D, cdt = _paged_args(w, q, dt, dev, k_cache, v_cache, table, q_start, kv_len, k_scale,
+                                                           v_scale)
     if H < 1 or H % Hkv or q.dim() != 2:
         raise ValueError(f"{w}: q must be packed rows [T, H * D], H a multiple of the cache's heads")
-    T, dt = q.shape[0], q.dtype
-    _rows2(w, "q", q, dt, (T, H * D), q)
+    T = q.shape[0]
+    _rows2(w, "q", q, dt, (T, H * D), dev, q)
     win = _window(w, left, right, sinks)
     max_q = T if max_q is None else int(max_q)
     with _on_device(q, stream) as s:
         out = torch.empty((T, H * D), dtype=dt, device=q.device) if out is None else out
-        _rows2(w, "out", out, dt, (T, H * D), q)
+        _rows2(w, "out", out, dt, (T, H * D), dev, q)
         if with_lse and lse is None:
             lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
         if lse is not None:

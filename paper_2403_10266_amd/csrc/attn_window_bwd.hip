@@ -645,7 +645,7 @@ int start_dkv(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   if (int st = last_launch_status()) return st;
   if (!sk.parts) return DSP_OK;
   const int64_t ub = a.B * a.X * a.Hkv * sk.blocks;
-  window_bwd_sink_kernel<T><<<dim3((uint32_t)ub, 8), 256, 0, s>>>(p, 32 * KW);
+  window_bwd_sink_kernel<T><<<dim3((uint32_t)ub, 32), 256, 0, s>>>(p, 32 * KW);   // few units and parts: latency counts
   return last_launch_status();
 }
 

@@ -951,8 +951,8 @@ int start(FwdParams& p, const WindowArgs& a, const Choice& c, hipStream_t s) {
   // with three waves and 64 keys, 198 with 32; 16 of 8192 x 128, window 1024, with two waves 218
   // and 226.
   // Steps of 32 keys inside a tile of 64 above that: 209 us.
-  constexpr bool B16 = sizeof(T) == 2, WIDE = DC > 64 && DC <= 96;
-  return start_many<T, S, PAGED, DC, 4, 1, B16 && !WIDE ? 64 : 32, B16 && DC <= 64 ? 2 : 1, B16 ? (DC <= 96 ? 3 : 2) : 1>(p, a, s);
+  constexpr bool B16 = sizeof(T) == 2, MID = DC > 64 && DC <= 80;
+  return start_many<T, S, PAGED, DC, 4, 1, B16 && !MID ? 64 : 32, B16 && DC <= 64 ? 2 : 1, B16 ? (DC <= 80 ? 3 : 2) : 1>(p, a, s);
 }
 
 inline FwdParams params(const WindowArgs& a) {
