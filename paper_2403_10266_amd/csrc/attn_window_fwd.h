@@ -378,8 +378,8 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   using R = Rows16<T, S, DC>;
   constexpr int NT = NW * 64, CB = NW * 32 * QT, GR = KB / 16;
   constexpr int TILE = KB * G::P;
-  constexpr int NL = (2 * GR + NW - 1) / NW;   // group loads of a wave: K's groups, then V's
-  static_assert(2 * GR % NW == 0, "every wave loads the same");
+  constexpr int NL = 2 * GR / NW;   // a wave loads a group of 16 keys of K and V, or of one of them
+  static_assert(NW == GR || NW == 2 * GR, "every wave loads the same");
   static_assert(NW * 32 <= 4 * KB && KB % (32 * NKT) == 0, "the output rows fit the tiles, a tile is whole steps");
   extern __shared__ __attribute__((aligned(16))) char smem[];
   T* lds = reinterpret_cast<T*>(smem);                       // [2][K, V][KB][P]
@@ -412,34 +412,32 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   const typename R::Map map = R::map(D, u.src.row_bytes, lane);
   R rows[NL];
   float scale[NL];
-  bool lost[NL];
-  int32_t id[NL];
-  auto ask = [&](int32_t t) {      // the pages of this wave's groups
-#pragma unroll
-    for (int i = 0; i < NL; ++i)
-      id[i] = u.src.page_of(tiles.key0(t) + 16 * ((wave + i * NW) % GR), t < tiles.n ? we.last.hi : 0);
-  };
+  const int grp16 = 16 * (wave % GR);   // the wave's group in a tile
+  const bool of_v = NL == 1 && wave >= GR;
+  bool lost = false;
+  int32_t id = -1;
+  auto ask = [&](int32_t t) { id = t < tiles.n ? u.src.page_of(tiles.key0(t) + grp16, we.last.hi) : -1; };   // its page
   auto fetch = [&](int32_t t) {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int li = wave + i * NW;
-      const int32_t key0 = tiles.key0(t) + 16 * (li % GR);
-      const auto gp = u.src.group(key0, id[i]);
-      scale[i] = li < GR ? gp.ks : gp.vs;
-      lost[i] = gp.gone;
-      rows[i].fetch(map, li < GR ? gp.k : gp.v, D, p.vec, !gp.gone && whole_group(we.first, we.last, key0), [&](int r) {
-        const int32_t j = key0 + r;
-        return !gp.gone && (j < we.last.sink || (j >= we.first.lo && j < we.last.hi));
-      });
+    const int32_t key0 = tiles.key0(t) + grp16;
+    const auto gp = u.src.group(key0, id);
+    lost = gp.gone;
+    const bool whole = !gp.gone && whole_group(we.first, we.last, key0);
+    auto on = [&](int r) {
+      const int32_t j = key0 + r;
+      return !gp.gone && (j < we.last.sink || (j >= we.first.lo && j < we.last.hi));
+    };
+    rows[0].fetch(map, of_v ? gp.v : gp.k, D, p.vec, whole, on);
+    scale[0] = of_v ? gp.vs : gp.ks;
+    if constexpr (NL == 2) {
+      rows[1].fetch(map, gp.v, D, p.vec, whole, on);
+      scale[1] = gp.vs;
     }
   };
   auto stash = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int li = wave + i * NW;
-      rows[i].stash(map, lds + buf * 2 * TILE + (li < GR ? 0 : TILE) + 16 * (li % GR) * G::P, scale[i]);
-      if (PAGED && li < GR && lane == 0) gone[buf * GR + li] = lost[i];
-    }
+    T* to = lds + buf * 2 * TILE + grp16 * G::P;
+    rows[0].stash(map, to + (of_v ? TILE : 0), scale[0]);
+    if constexpr (NL == 2) rows[1].stash(map, to + TILE, scale[1]);
+    if (PAGED && !of_v && lane == 0) gone[buf * GR + wave % GR] = lost;
   };
   if (tiles.n) {
     ask(0);
