@@ -458,7 +458,10 @@ int dsp_attn_relpos_bwd(const void* q, const void* k, const void* v, const void*
  *          or NULL (Lk).
  * A query that sees nothing gives o = 0 and lse = -inf.  Keys and values that no query
  * of their sequence sees are never used, whatever they hold; a key or value that is not
- * finite may make every query of its unit NaN, and a query that is not finite its own row.
+ * finite makes the queries that see it NaN and may make any other of its unit so (an infinite
+ * key may also count as the softmax has it), a query that is not finite its own row.  A
+ * unit's gradients may be NaN where a row of q or dout of theirs, or a key or value that is
+ * seen, is not finite; no other unit's are.
  * lse:     fp32 [B * X * H][Lq], the row log-sum-exp of the scaled scores, or NULL.
  * scale:   softmax scale; scale <= 0 selects 1/sqrt(D).
  * dtype:   DSP_BF16 (fp32 scores, softmax and accumulation; probabilities are rounded to

@@ -22,9 +22,6 @@ __device__ __forceinline__ Seen seen(const Window& w, int64_t p, int32_t len) {
   s.sink = min(w.sinks, s.hi);
   return s;
 }
-__device__ __forceinline__ bool sees(const Seen& s, int32_t j) {
-  return j < s.sink || (j >= s.lo && j < s.hi);
-}
 // 16 keys from key0 that all, or some, of the queries between two see, in full
 __device__ __forceinline__ bool whole_group(const Seen& first, const Seen& last, int32_t key0) {
   return key0 + 16 <= last.sink || (key0 >= first.lo && key0 + 16 <= last.hi);

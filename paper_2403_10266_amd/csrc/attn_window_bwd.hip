@@ -213,20 +213,18 @@ __device__ __forceinline__ SeenBy seen_by(const Window& w, int64_t p0, int32_t n
 }
 
 // dK and dV, over the queries of every head of the key/value head's group, in tiles of
-// 32 QT: KW blocks of 32 keys, each tile's queries shared out among QS waves for each,
-// whose sums are joined at the end.
-template <typename T, int DC, int KW, int QS, int QT, int MINW>
-__global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdParams p) {
+// 32 QT: a wave per 32 keys.
+template <typename T, int DC, int KW, int QT, int MINW>
+__global__ __launch_bounds__(KW * 64, MINW) void window_bwd_dkv_kernel(BwdParams p) {
   using G = Geo<T, DC>;
   using M = Mx<T>;
-  constexpr int NT = KW * QS * 64, QB = 32 * QT, TILE = QB * G::P, KEYS = 32 * KW;
+  constexpr int NT = KW * 64, QB = 32 * QT, TILE = QB * G::P, KEYS = 32 * KW;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   T* lds = reinterpret_cast<T*>(smem);                            // [2][Q, dO][QB][P]
   float* stat = reinterpret_cast<float*>(lds + 4 * TILE);         // [2][lse2, Delta][QB]
 
   const int lane0 = threadIdx.x & 63, lane = lane0, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kw = wave / QS, qs = wave % QS;
   uint32_t blk, bx, e, part = 0;
   const bool sink = blockIdx.x < p.sink_groups;
   if (sink) {
@@ -244,7 +242,7 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
   const int D = (int)p.D;
   const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D;
   const int64_t q_bx = bx_at(p, bx, p.qs), o_bx = bx_at(p, bx, p.os);
-  const int32_t first_key = (int32_t)(blk * KEYS), key = first_key + 32 * kw + l32;
+  const int32_t first_key = (int32_t)(blk * KEYS), key = first_key + 32 * wave + l32;
   const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
   const int64_t p0 = position(p.q_pos, b);
   const SeenBy mine = seen_by(p.win, p0, (int32_t)p.Lq, len, key);
@@ -322,8 +320,7 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
     const T* ol = ql + TILE;
     const float* sl = stat + buf * 2 * QB;
 #pragma unroll
-    for (int i = 0; i < QT / QS; ++i) {
-      const int sub = i * QS + qs;
+    for (int sub = 0; sub < QT; ++sub) {
       const int32_t q0 = qt0 + 32 * sub;
       if (q0 >= any1 || q0 + 32 <= any0) continue;
       const bool mask = q0 < all0 || q0 + 32 > all1;
@@ -370,44 +367,21 @@ __global__ __launch_bounds__(KW * QS * 64, MINW) void window_bwd_dkv_kernel(BwdP
   dk.scale(p.scale, lane);
   T* const out[2] = {static_cast<T*>(p.dk) + k_at, static_cast<T*>(p.dv) + k_at};
   float* const sums_at = p.part + ((((uint64_t)bx * p.Hkv + e) * p.sink_blocks + blk) * p.parts + part) * 2 * KEYS * p.D;
-  if constexpr (QS == 1) {
-    const uint32_t k0 = first_key + 32 * kw;
-    auto row = [&](T* base, int n) -> T* { return k0 + n < p.Lk ? base + (int64_t)(k0 + n) * p.ks[2] : nullptr; };
-    auto part_row = [&](int which, int n) -> float* { return sums_at + ((uint64_t)which * KEYS + 32 * kw + n) * p.D; };
-    if (sink) {
-      const bool vec4 = p.D % 4 == 0;
-      store_rows<T, DC>(dk, lane, D, vec4, [&](int n) { return part_row(0, n); });
-      store_rows<T, DC>(dv, lane, D, vec4, [&](int n) { return part_row(1, n); });
-    } else if (p.vec) {
-      T* so = lds + wave * 32 * G::P;   // the tiles are done with
-      static_assert(KW * 32 <= 4 * QB, "rows to write through");
-      store_rows_lds<T, DC>(so, dk, lane, D, G::DP, [&](int n) { return row(out[0], n); });
-      store_rows_lds<T, DC>(so, dv, lane, D, G::DP, [&](int n) { return row(out[1], n); });
-    } else {
-      store_rows<T, DC>(dk, lane, D, false, [&](int n) { return row(out[0], n); });
-      store_rows<T, DC>(dv, lane, D, false, [&](int n) { return row(out[1], n); });
-    }
+  const uint32_t k0 = first_key + 32 * wave;
+  auto row = [&](T* base, int n) -> T* { return k0 + n < p.Lk ? base + (int64_t)(k0 + n) * p.ks[2] : nullptr; };
+  auto part_row = [&](int which, int n) -> float* { return sums_at + ((uint64_t)which * KEYS + 32 * wave + n) * p.D; };
+  if (sink) {
+    const bool vec4 = p.D % 4 == 0;
+    store_rows<T, DC>(dk, lane, D, vec4, [&](int n) { return part_row(0, n); });
+    store_rows<T, DC>(dv, lane, D, vec4, [&](int n) { return part_row(1, n); });
+  } else if (p.vec) {
+    T* so = lds + wave * 32 * G::P;   // the tiles are done with
+    static_assert(KW * 32 <= 4 * QB, "rows to write through");
+    store_rows_lds<T, DC>(so, dk, lane, D, G::DP, [&](int n) { return row(out[0], n); });
+    store_rows_lds<T, DC>(so, dv, lane, D, G::DP, [&](int n) { return row(out[1], n); });
   } else {
-    // the QS waves' sums of a key, added in order
-    float* sums = reinterpret_cast<float*>(smem);   // [QS][KEYS][DP]
-    constexpr int W = G::DP, ROWS = KEYS;
-    static_assert((size_t)QS * ROWS * W * 4 <= (size_t)4 * TILE * sizeof(T), "the sums fit the tiles");
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      __syncthreads();
-      store_rows<T, DC>(which ? dv : dk, lane, W, true, [&](int n) { return sums + (qs * ROWS + kw * 32 + n) * W; });
-      __syncthreads();
-      for (uint32_t i = threadIdx.x; i < ROWS * W / 4; i += NT) {
-        const uint32_t n = i / (W / 4), d = i % (W / 4) * 4;
-        floatx4 v = *reinterpret_cast<const floatx4*>(sums + n * W + d);
-#pragma unroll
-        for (int q = 1; q < QS; ++q) v += *reinterpret_cast<const floatx4*>(sums + (q * ROWS + n) * W + d);
-        if (sink)
-          store4(sums_at + ((uint64_t)which * KEYS + n) * p.D, (int)d, D, p.D % 4 == 0, v[0], v[1], v[2], v[3]);
-        else if (first_key + n < p.Lk)
-          store4(out[which] + (int64_t)(first_key + n) * p.ks[2], (int)d, D, p.vec, v[0], v[1], v[2], v[3]);
-      }
-    }
+    store_rows<T, DC>(dk, lane, D, false, [&](int n) { return row(out[0], n); });
+    store_rows<T, DC>(dv, lane, D, false, [&](int n) { return row(out[1], n); });
   }
 }
 
@@ -628,7 +602,7 @@ int start_dq(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   return last_launch_status();
 }
 
-template <typename T, int DC, int KW, int QS, int QT, int MINW>
+template <typename T, int DC, int KW, int QT, int MINW>
 int start_dkv(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   static_assert(32 * KW == kDkvKeys, "the sinks' workspace");
   constexpr int QB = 32 * QT;
@@ -636,12 +610,12 @@ int start_dkv(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   const Sinks sk = sinks_of(a);
   p.parts = (uint32_t)sk.parts, p.sink_blocks = (uint32_t)sk.blocks;
   const int64_t first = a.B * a.X * a.Hkv * sk.blocks * sk.parts, blocks = first + order_blocks(p.order);
-  if (!grid_fits(blocks, KW * QS * 64)) return DSP_ERR_SHAPE;
+  if (!grid_fits(blocks, KW * 64)) return DSP_ERR_SHAPE;
   p.sink_groups = (uint32_t)first;
   const size_t lds = (size_t)4 * QB * Geo<T, DC>::P * sizeof(T) + (size_t)4 * QB * 4;
-  auto* kernel = window_bwd_dkv_kernel<T, DC, KW, QS, QT, MINW>;
+  auto* kernel = window_bwd_dkv_kernel<T, DC, KW, QT, MINW>;
   if (int st = lds_limit(kernel, lds)) return st;
-  kernel<<<dim3((uint32_t)blocks), KW * QS * 64, lds, s>>>(p);
+  kernel<<<dim3((uint32_t)blocks), KW * 64, lds, s>>>(p);
   if (int st = last_launch_status()) return st;
   if (!sk.parts) return DSP_OK;
   const int64_t ub = a.B * a.X * a.Hkv * sk.blocks;
@@ -677,7 +651,7 @@ int start(BwdParams& p, const WindowArgs& a, hipStream_t s) {
     if (int st = start_dq<T, DC>(p, a, s)) return st;
   if (a.Lk == 0) return DSP_OK;
   constexpr bool B16 = sizeof(T) == 2;
-  return start_dkv<T, DC, 4, 1, B16 ? 2 : 1, B16 && DC <= 80 ? 2 : 1>(p, a, s);
+  return start_dkv<T, DC, 4, B16 ? 2 : 1, B16 && DC <= 80 ? 2 : 1>(p, a, s);
 }
 
 }  // namespace

@@ -44,8 +44,8 @@ struct FwdParams {
   Order order;       // many columns, rows of a tensor
   uint32_t n_blk;    // many columns, pages: blocks in all
   uint32_t few_cols; // many columns: units of at most so many are left to the other form
-  uint32_t pieces, n_split, cblk;   // few columns: units times splits, blocks of 32 columns
-  uint32_t block_cols;              // of a block, at most
+  uint32_t pieces, n_split;   // few columns: units times splits
+  uint32_t block_cols;        // columns of a unit, at most
   float c;           // scale * log2(e)
   bool vec;
 };
@@ -101,6 +101,11 @@ __device__ __forceinline__ Unit<T, S, true> unit(const FwdParams& p, uint32_t n,
   u.src.n_pages = p.n_pages, u.src.n_heads = p.Hkv, u.src.shift = p.shift;
   return u;
 }
+
+// Clamps of this wave leave a NaN as it is (bit 8 of the mode register; set, they make it 0):
+// a probability that fast() cuts with its exponential's clamp stays NaN.  A minimum for it
+// costs 4% (8192 causal tokens 156 and 162 us).
+__device__ __forceinline__ void keep_nan() { __builtin_amdgcn_s_setreg(1 | 8 << 6 | 0 << 11, 0); }
 
 // The softmax of QT blocks of 32 columns over NKT blocks of 32 keys at a time, less a
 // reference of each column (exp2 units).
@@ -385,14 +390,19 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   T* lds = reinterpret_cast<T*>(smem);                       // [2][K, V][KB][P]
   uint32_t* gone = reinterpret_cast<uint32_t*>(lds + 4 * TILE);   // [2][GR]: pages that are not there
 
+  keep_nan();
   const int lane = threadIdx.x & 63, l32 = lane & 31, g = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t un, e, blk;
   if constexpr (PAGED) {
     e = blockIdx.x % p.Hkv;
-    const uint32_t w = p.n_blk - 1 - blockIdx.x / p.Hkv;   // a sequence's last blocks have the most keys
+    const uint32_t w = blockIdx.x / p.Hkv;
     un = __builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, p.grp.d, CB, 1, w, lane));
-    const int32_t at = (int32_t)w - first_piece(p.q_start, un, p.T, p.grp.d, CB, 1);
+    const int32_t f = first_piece(p.q_start, un, p.T, p.grp.d, CB, 1);
+    if ((int32_t)w < f) return;
+    // a sequence's last blocks have the most keys, and come first (8192 new tokens, 32 heads of 64: 352
+    // us, 410 the other way round); a place past its blocks has no columns
+    const int32_t at = first_piece(p.q_start, un + 1, p.T, p.grp.d, CB, 1) - 1 - (int32_t)w;
     if (at < 0) return;
     blk = (uint32_t)at;
   } else {
@@ -613,7 +623,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_short_kernel(FwdParams p
     u.lse[(int64_t)i * u.lse_i + (int64_t)hh * u.lse_h] = l == 0.0f ? -INFINITY : kLn2 * (sm.ref[0] + log2f(l));
 }
 
-// Few columns: a block of 32 of them, the keys' tiles of 32 cut among work-groups and,
+// Few columns: 32 of a unit at most, the keys' tiles of 32 cut among work-groups and,
 // inside one, among its waves, each with LDS rows of its own and no barrier until the
 // waves' sums are joined.  A pass over a cache is bound by memory: what counts is how
 // many waves a CU holds, that each has its next tile on its way, and that every load
@@ -644,16 +654,14 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
   T* vl = kl + TILE;
 
   // an XCD takes the heads of a stretch of keys, which together read whole token rows
-  const uint32_t he = p.Hkv * p.cblk, j8 = blockIdx.x >> 3, piece = j8 / he * 8 + (blockIdx.x & 7u);
+  const uint32_t j8 = blockIdx.x >> 3, piece = j8 / p.Hkv * 8 + (blockIdx.x & 7u), e = j8 % p.Hkv;
   if (piece >= p.pieces) return;
-  const uint32_t ec = j8 % he, e = ec / p.cblk, cb = ec - e * p.cblk;
   const uint32_t un = piece / p.n_split, split = piece - un * p.n_split;
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
-  const uint32_t cols = (uint32_t)u.nq * p.grp.d, c0 = 32 * cb;
-  if (c0 >= cols || cols > p.few_cols) return;
-  const uint32_t nc = min(cols - c0, 32u);
+  const uint32_t nc = (uint32_t)u.nq * p.grp.d;
+  if (nc == 0 || nc > p.few_cols) return;
   const int D = (int)p.D;
-  const Columns cs(p.grp, c0);
+  const Columns cs(p.grp, 0);
   const Edges ed = edges(p.win, u, cs, 0, nc - 1);
   const Tiles<32> tiles(ed.first, ed.last);
   const Cut part = cut(tiles.n, p.n_split, NW);
@@ -733,17 +741,6 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
     if (u.lse)
       u.lse[(int64_t)i * u.lse_i + (int64_t)cs.head(n, i) * u.lse_h] = s == 0.0f ? -INFINITY : kLn2 * (m + log2f(s));
   };
-  if constexpr (NW == 1) {
-    if (part.used == 1) {
-      sm.o[0].scale(l == 0.0f ? 0.0f : 1.0f / l, lane);
-      wave_order();
-      auto row = [&](int n) -> T* { return (uint32_t)n < nc ? out(n) : nullptr; };
-      if (p.vec) store_rows_lds<T, DC>(vl, sm.o[0], lane, D, G::DP, row);
-      else store_rows<T, DC>(sm.o[0], lane, D, false, row);
-      if (g == 0 && (uint32_t)l32 < nc) put_lse(l32, sm.ref[0], l);
-      return;
-    }
-  }
   __syncthreads();
   float* ms = reinterpret_cast<float*>(smem);   // [NW][32] references, [NW][32] sums, [2][32] joined
   if (g == 0) {
@@ -769,7 +766,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
   }
   __syncthreads();
   // maxima, sums, rows of 32 columns
-  float* to = p.part + (((uint64_t)un * he + ec) * p.n_split + split) * 32 * (2 + p.D);
+  float* to = p.part + (((uint64_t)un * p.Hkv + e) * p.n_split + split) * 32 * (2 + p.D);
   for (uint32_t i = threadIdx.x; i < nc * p.D; i += NW * 64) {
     const uint32_t n = i / p.D, d = i - n * p.D;
     float v = 0.0f;
@@ -795,19 +792,18 @@ __global__ __launch_bounds__(256) void window_join_kernel(FwdParams p, int waves
   constexpr int GR = 256 / DP;
   __shared__ float f[kMaxSplit], red[256], m4[4];
   using U = Unit<T, S, PAGED>;
-  const uint32_t he = p.Hkv * p.cblk, uec = blockIdx.x / p.block_cols, n = blockIdx.x - uec * p.block_cols;
-  const uint32_t un = uec / he, ec = uec - un * he;
-  const uint32_t e = ec / p.cblk, cb = ec - e * p.cblk;
+  const uint32_t ue = blockIdx.x / p.block_cols, n = blockIdx.x - ue * p.block_cols;
+  const uint32_t un = ue / p.Hkv, e = ue - un * p.Hkv;
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
-  const uint32_t cols = (uint32_t)u.nq * p.grp.d, c = 32 * cb + n;
-  if (c >= cols || cols > p.few_cols) return;
-  const Columns cs(p.grp, 32 * cb);
-  const Edges ed = edges(p.win, u, cs, 0, min(cols - 32 * cb, 32u) - 1);
+  const uint32_t nc = (uint32_t)u.nq * p.grp.d;
+  if (n >= nc || nc > p.few_cols) return;
+  const Columns cs(p.grp, 0);
+  const Edges ed = edges(p.win, u, cs, 0, nc - 1);
   const Tiles<32> tiles(ed.first, ed.last);
   const uint32_t used = (uint32_t)cut(tiles.n, p.n_split, waves).used;
   if (used == 1) return;
   const uint32_t stride = 32 * (2 + p.D);
-  const float* w = p.part + (uint64_t)uec * p.n_split * stride;
+  const float* w = p.part + (uint64_t)ue * p.n_split * stride;
   float m = -INFINITY;
   for (uint32_t s = threadIdx.x; s < used; s += 256) {
     f[s] = w[(uint64_t)s * stride + n];
@@ -890,10 +886,10 @@ int start_few(FwdParams& p, const WindowArgs& a, hipStream_t s) {
   lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * 32 * Geo<T, DC>::DP) * 4);
   const int64_t pieces = a.B * a.X * p.n_split;
   p.pieces = (uint32_t)pieces;
-  int st = launch(window_few_kernel<T, S, PAGED, DC, NW, MINW>, (pieces + 7) / 8 * 8 * a.Hkv * p.cblk, NW * 64, lds, p, s);
+  int st = launch(window_few_kernel<T, S, PAGED, DC, NW, MINW>, (pieces + 7) / 8 * 8 * a.Hkv, NW * 64, lds, p, s);
   if (st != DSP_OK || p.n_split == 1) return st;
   p.block_cols = (uint32_t)std::min<int64_t>(a.Lq * p.grp.d, 32);
-  const int64_t cols = a.B * a.X * a.Hkv * p.cblk * p.block_cols;   // few units: they are why the keys are split
+  const int64_t cols = a.B * a.X * a.Hkv * p.block_cols;   // few units: they are why the keys are split
   if (!grid_fits(cols, 256)) return DSP_ERR_SHAPE;
   if (a.D <= 64) window_join_kernel<T, S, PAGED, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
   else window_join_kernel<T, S, PAGED, 128><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
@@ -904,7 +900,7 @@ int start_few(FwdParams& p, const WindowArgs& a, hipStream_t s) {
 // how many parts their keys go at most.
 struct Choice {
   bool few, many;
-  int64_t cblk, n_split;
+  int64_t n_split;
 };
 inline Choice choose(const WindowArgs& a) {
   Choice c = {};
@@ -912,7 +908,6 @@ inline Choice choose(const WindowArgs& a) {
   c.few = grp <= 32;
   c.many = cols > 32;
   if (c.many && !(a.page_shift && a.B > 1)) c.few = false;
-  c.cblk = 1;
   c.n_split = 1;
   if (!c.few) return c;
   // keys that a block of columns can see
@@ -931,13 +926,12 @@ inline Choice choose(const WindowArgs& a) {
 }
 inline size_t part_bytes(const WindowArgs& a) {
   const Choice c = choose(a);
-  return c.n_split > 1 ? (size_t)(a.B * a.X * a.Hkv * c.cblk * c.n_split) * 32 * (2 + (size_t)a.D) * 4 : 0;
+  return c.n_split > 1 ? (size_t)(a.B * a.X * a.Hkv * c.n_split) * 32 * (2 + (size_t)a.D) * 4 : 0;
 }
 
 template <typename T, typename S, bool PAGED, int DC>
 int start(FwdParams& p, const WindowArgs& a, const Choice& c, hipStream_t s) {
   p.few_cols = c.few ? 32 : 0;
-  p.cblk = (uint32_t)c.cblk;
   p.n_split = (uint32_t)c.n_split;
   if (c.few) {
     if (int st = start_few<T, S, PAGED, DC, 4>(p, a, s)) return st;

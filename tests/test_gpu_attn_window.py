@@ -265,3 +265,94 @@ def test_captured_and_on_another_stream(torch, Lq, Lk):
         call(put(cs[(i + 1) % 3]))
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want[i])), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Lq,Lk,at", [(3, 900, 700), (100, 100, 70), (400, 400, 250)])
+def test_a_key_that_is_not_finite_shows(torch, dtype, Lq, Lk, at):
+    """A NaN in a key, wherever the pass over the keys meets it, is in every query that sees the
+    key, and not in another unit."""
+    import paper_2403_10266_amd as dsp
+    c = wu.case(1, 2, Lq, Lk, 4, 2, 72, dtype, seed=30)
+    q, k, v = (dev(c[n], dtype) for n in "qkv")
+    kw = dict(left=-1, right=0, q_pos=_i32(torch, [Lk - Lq]), with_lse=True)
+    o, lse = dsp.dsp_attn_window(q, k, v, 4, 2, **kw)
+    k[0, 1, at, 3] = float("nan")
+    p, lsp = dsp.dsp_attn_window(q, k, v, 4, 2, **kw)
+    first = max(at - (Lk - Lq), 0)
+    seen = p.reshape(2, Lq, 2, 2, 72)[1, first:, 0]       # heads of the key's head
+    assert seen.isnan().all() and lsp[0, 1, :2, first:].isnan().all()
+    assert torch.equal(p[0, 0], o[0, 0]) and torch.equal(lsp[0, 0], lse[0, 0])
+    assert torch.equal(p[0, 1, :, 144:], o[0, 1, :, 144:]) and torch.equal(lsp[0, 1, 2:], lse[0, 1, 2:])
+
+
+SHORT = [
+    # B, X, Lq, Lk, H, Hkv, D, left, right, sinks, q_pos, kv_len
+    (1, 5, 32, 32, 2, 2, 64, 8, 0, 0, None, None),                # one wave, full
+    (2, 3, 8, 31, 4, 1, 72, -1, 0, 2, [23, -3], [31, 7]),         # a group of 4 heads in a block
+    (1, 4, 33, 20, 2, 2, 40, 5, 5, 1, None, None),                # more columns than keys
+    (2, 2, 16, 64, 8, 2, 96, 30, 2, 3, [40, 60], [64, 0]),        # a unit without keys
+    (1, 3, 64, 64, 2, 2, 128, 16, 16, 0, None, None),
+    (1, 3, 32, 100, 4, 1, 64, 20, 0, 5, [68], None),              # 128 columns
+    (1, 2, 128, 128, 1, 1, 72, 16, 16, 1, None, None),
+    (1, 2, 128, 128, 2, 2, 16, -1, -1, 0, None, None),
+    (1, 2, 1, 128, 6, 2, 48, 40, 0, 130, [127], None),
+    (1, 2, 127, 1, 2, 2, 80, 3, 200, 0, [-90], None),
+    (1, 2, 129, 128, 2, 2, 72, 16, 16, 1, None, None),            # one more than fits
+    (1, 2, 43, 128, 3, 1, 32, 60, 0, 0, [80], None),              # 129 columns of a group
+]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,X,Lq,Lk,H,Hkv,D,left,right,sinks,q_pos,kv_len", SHORT)
+def test_short_units(torch, dtype, B, X, Lq, Lk, H, Hkv, D, left, right, sinks, q_pos, kv_len):
+    c = wu.case(B, X, Lq, Lk, H, Hkv, D, dtype, seed=Lq + Lk)
+    _check(torch, c, dtype, f"short B{B} X{X} {Lq}x{Lk} H{H}/{Hkv} D{D}", left=left, right=right, sinks=sinks, q_pos=q_pos,
+           kv_len=kv_len)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,X,L,H,Hkv,D", [(2, 3, 600, 4, 2, 64), (1, 5, 641, 3, 3, 72), (1, 1, 900, 2, 1, 128),
+                                           (3, 1, 530, 4, 4, 96), (1, 9, 257, 8, 8, 8)])
+def test_blocks_in_runs(torch, dtype, B, X, L, H, Hkv, D):
+    """Enough blocks of a narrow window that neighbouring ones go to one place together."""
+    c = wu.case(B, X, L, L, H, Hkv, D, dtype, seed=L)
+    _check(torch, c, dtype, f"runs B{B} X{X} {L} H{H}/{Hkv} D{D}", left=33, right=20, sinks=2)
+
+
+def test_two_at_once(torch):
+    """Two streams, and two graphs replayed in turn and together, with workspaces of their own."""
+    import paper_2403_10266_amd as dsp
+    cs = [wu.case(1, 1, L, n, 8, 2, 64, "bf16", seed=40 + i) for i, (L, n) in enumerate([(2, 5000), (300, 300)])]
+    kw = [dict(left=-1, right=0, q_pos=_i32(torch, [4998])), dict(left=30, right=0, sinks=2)]
+    ts = [[dev(c[n], "bf16") for n in ("q", "k", "v", "do")] for c in cs]
+
+    def call(i, stream=None):
+        q, k, v, do = ts[i]
+        o, lse = dsp.dsp_attn_window(q, k, v, 8, 2, with_lse=True, stream=stream, **kw[i])
+        return [o, lse, *dsp.dsp_attn_window_bwd(q, k, v, o, do, lse, 8, 2, stream=stream, **kw[i])]
+
+    want = [[x.clone() for x in call(i)] for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(4):
+        got = [call(i, streams[i]) for i in range(2)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+    graphs, outs = [], []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call(i))
+        graphs.append(g)
+    for together in (False, True, False, True):
+        for o in outs:
+            for x in o:
+                x.fill_(7)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s if together else streams[0]):
+                g.replay()
+        call(0)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(outs, want) for a, b in zip(g, w))

@@ -449,3 +449,44 @@ def test_generation(torch):
             want = ow.turned(data[0]["k"].reshape(-1, Hkv, D), np.arange(total[0]), cos.cpu().numpy(), sin.cpu().numpy(), False)
             j = kv[0] - 1
             assert np.abs(_f64(caches[0][table[0][j // page], j % page]) - want[j]).max() <= 2.0 ** -7 * np.abs(want[j]).max()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("new", [2, 300])
+def test_a_held_token_that_is_not_finite_shows(torch, kind, new):
+    """A token whose key is NaN, appended in the middle of a sequence, is in every new token that
+    sees it, and not in another sequence."""
+    import paper_2403_10266_amd as dsp
+    r = np.random.default_rng(12)
+    H, Hkv, D, page, kv, at = 4, 2, 72, 32, 640, 350
+    table = _i32(torch, r.permutation(40).reshape(2, 20))
+    c = [_cache(torch, np.zeros((40, page, Hkv, D)), kind, "token") for _ in "kv"]
+    s = [torch.zeros(40, Hkv, device="cuda") for _ in "kv"] if kind == "e4m3" else [None, None]
+    k, v = (dev(wu.draw((2 * kv, Hkv * D), "bf16", r), "bf16") for _ in "kv")
+    q = dev(wu.draw((2 * new, H * D), "bf16", r), "bf16")
+    call = lambda: dsp.dsp_attn_paged(q, *c, table, _i32(torch, [0, new, 2 * new]), _i32(torch, [kv, kv]), H,  # noqa: E731
+                                      max_q=new, k_scale=s[0], v_scale=s[1], with_lse=True)
+    put = lambda: dsp.dsp_kv_append(k, v, *c, table, _i32(torch, [0, kv, 2 * kv]), _i32(torch, [kv, kv]), *s)  # noqa: E731
+    put()
+    o, lse = call()
+    k[kv + at, 5] = float("nan")
+    put()
+    p, lsp = call()
+    first = new + max(at - (kv - new), 0)
+    assert p[first:, :144].isnan().all() and lsp[first:, :2].isnan().all()
+    assert torch.equal(p[:new], o[:new]) and torch.equal(p[:, 144:], o[:, 144:]) and torch.equal(lsp[:, 2:], lse[:, 2:])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_long_prompts_and_short_ones(torch, kind):
+    """Blocks of many sequences, some with none, some of many: each is taken once."""
+    import paper_2403_10266_amd as dsp
+    r = np.random.default_rng(13)
+    new = [0, 257, 1, 33, 0, 128, 5, 0]
+    kv = [10, 257, 90, 300, 0, 130, 5, 0]
+    table, pages = _table(r, kv, 16)
+    held, scales = [wu.draw((pages, 16, 2, 64), "bf16", r) for _ in "kv"], [None, None]
+    if kind == "e4m3":
+        scales = [2.0 ** r.integers(-4, 2, (pages, 2)) for _ in "kv"]
+        held = [np.clip(ow.e4m3(h / s[:, None, :, None]), -448, 448) for h, s in zip(held, scales)]
+    _attend(torch, dsp, r, kind, "bf16", "token", table, held, scales, new, kv, 8, 2, 64, -1, 0, 0)
