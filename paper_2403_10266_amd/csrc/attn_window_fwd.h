@@ -105,7 +105,9 @@ __device__ __forceinline__ Unit<T, S, true> unit(const FwdParams& p, uint32_t n,
 // Clamps of this wave leave a NaN as it is (bit 8 of the mode register; set, they make it 0):
 // a probability that fast() cuts with its exponential's clamp stays NaN.  A minimum for it
 // costs 4% (8192 causal tokens 156 and 162 us).
-__device__ __forceinline__ void keep_nan() { __builtin_amdgcn_s_setreg(1 | 8 << 6 | 0 << 11, 0); }
+__device__ __forceinline__ void keep_nan() {
+  asm volatile("s_setreg_imm32_b32 hwreg(HW_REG_MODE, 8, 1), 0");
+}
 
 // The softmax of QT blocks of 32 columns over NKT blocks of 32 keys at a time, less a
 // reference of each column (exp2 units).
@@ -373,6 +375,38 @@ __device__ __forceinline__ Edges edges(const Window& w, const U& u, const Column
   return {seen(w, u.p0 + c.query(n0), u.len), seen(w, u.p0 + c.query(n1), u.len)};
 }
 
+// The w-th block of `size` columns of all sequences' new tokens; n < 0: none.  The last block
+// of a sequence, which has the most keys, comes first (8192 new tokens of one, 32 heads of 64:
+// 352 us, 410 the other way round), and up to 64 sequences go by falling length, so that
+// the longest passes do not start last.
+struct BlockOf {
+  int32_t n, blk;
+};
+__device__ __forceinline__ BlockOf block_of(const FwdParams& p, uint32_t size, uint32_t w, int lane) {
+  if (p.N <= 64) {
+    const bool on = (uint32_t)lane < p.N;
+    const uint32_t cols = on ? (uint32_t)min(new_rows(p.q_start, lane, p.T).n, (int32_t)p.Lq) * p.grp.d : 0u;
+    const int32_t len = on ? p.kv_len[lane] : 0;
+    const uint32_t blocks = cols > p.few_cols ? (cols + size - 1) / size : 0;
+    uint32_t first = 0;   // of the lane's sequence: the blocks of those before it
+    for (int j = 0; j < (int)p.N; ++j) {
+      const int32_t other = __builtin_amdgcn_readlane(len, j);
+      const uint32_t theirs = __builtin_amdgcn_readlane(blocks, j);
+      first += other > len || (other == len && j < lane) ? theirs : 0u;
+    }
+    const uint64_t it = __ballot(w >= first && w - first < blocks);
+    if (!it) return {-1, 0};
+    const int n = __ffsll((unsigned long long)it) - 1;
+    const uint32_t f = __builtin_amdgcn_readlane(first, n), b = __builtin_amdgcn_readlane(blocks, n);
+    return {n, (int32_t)(f + b - 1 - w)};
+  }
+  const int32_t n = (int32_t)__builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, p.grp.d, size, 1, w, lane));
+  if ((int32_t)w < first_piece(p.q_start, n, p.T, p.grp.d, size, 1)) return {-1, 0};
+  // a place past the sequence's blocks has no columns
+  const int32_t blk = first_piece(p.q_start, n + 1, p.T, p.grp.d, size, 1) - 1 - (int32_t)w;
+  return {blk < 0 ? -1 : n, blk};
+}
+
 // Many columns: QT blocks of 32 per wave, the keys in LDS tiles that all waves share,
 // the next tile on its way in registers.
 template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int NKT, int MINW>
@@ -396,15 +430,9 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   uint32_t un, e, blk;
   if constexpr (PAGED) {
     e = blockIdx.x % p.Hkv;
-    const uint32_t w = blockIdx.x / p.Hkv;
-    un = __builtin_amdgcn_readfirstlane(piece_owner(p.q_start, p.N, p.T, p.grp.d, CB, 1, w, lane));
-    const int32_t f = first_piece(p.q_start, un, p.T, p.grp.d, CB, 1);
-    if ((int32_t)w < f) return;
-    // a sequence's last blocks have the most keys, and come first (8192 new tokens, 32 heads of 64: 352
-    // us, 410 the other way round); a place past its blocks has no columns
-    const int32_t at = first_piece(p.q_start, un + 1, p.T, p.grp.d, CB, 1) - 1 - (int32_t)w;
-    if (at < 0) return;
-    blk = (uint32_t)at;
+    const BlockOf at = block_of(p, CB, blockIdx.x / p.Hkv, lane);
+    if (at.n < 0) return;
+    un = (uint32_t)at.n, blk = (uint32_t)at.blk;
   } else {
     const Place pl = place(p.order);
     if (!pl.any) return;
@@ -475,12 +503,12 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   // 8192 causal tokens 173 and 185 us).  Waves go from one loop to the other by themselves;
   // each meets every tile's barrier once.
   int32_t it = 0, k0 = 0;
-  auto begin = [&]() {   // the tile after it sets out
+  auto begin = [&]() __attribute__((always_inline)) {   // the tile after it sets out
     if (it + 1 >= tiles.n) return;
     fetch(it + 1);
     ask(it + 2);
   };
-  auto advance = [&]() {
+  auto advance = [&]() __attribute__((always_inline)) {
     k0 += 32 * NKT;
     if (k0 < KB) return;
     if (it + 1 < tiles.n) stash((it + 1) & 1);
@@ -489,7 +517,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
     if (++it < tiles.n) begin();
   };
   // f(operands, values, first key, mask, keys not there) for a step that the wave's columns see
-  auto step = [&](auto f) {
+  auto step = [&](auto f) __attribute__((always_inline)) {
     const int32_t key0 = tiles.key0(it) + k0;
     if (!on || ed.none(key0, 32 * NKT)) return false;
     uint32_t lost_bits = 0;
@@ -507,7 +535,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   };
   if (tiles.n) begin();
   while (it < tiles.n && !sm.set) {
-    step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) {
+    step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) __attribute__((always_inline)) {
       sm.exact(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
       return false;
     });
@@ -516,13 +544,13 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   while (it < tiles.n) {
     bool moved = false;
     for (; it < tiles.n && !moved;) {
-      moved = step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) {
+      moved = step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) __attribute__((always_inline)) {
         return sm.fast(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
       });
       if (!moved) advance();
     }
     if (!moved) break;
-    step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) {
+    step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) __attribute__((always_inline)) {
       sm.fix(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
       return true;
     });
