@@ -112,7 +112,8 @@ __device__ __forceinline__ void keep_nan() {
 // The softmax of QT blocks of 32 columns over NKT blocks of 32 keys at a time, less a
 // reference of each column (exp2 units).
 //  * exact(): takes the tile's maxima and moves the references to them.
-//  * fast() (LAZY): the references stay, 64 above the maximum of the tiles that set them, and
+//  * fast() (LAZY, bf16: a reference so far off costs an fp32 exponent 6 of its bits, fp32 results
+//    1.3e-6 of their value where exact() gives 2e-7): the references stay, 64 above the maximum of the tiles that set them, and
 //    probabilities are cut at 1, so that nothing stands between the exponentials and the
 //    product with v.  A score above its reference shows afterwards, as a sum of a half or
 //    more (probabilities below it add up to far less); then, rarely, fix() moves the
@@ -252,44 +253,37 @@ struct Softmax {
     for (int j = 0; j < QT; ++j) by[j] = ref[j] == -INFINITY ? 0.0f : ref[j];   // a column that sees nothing
     floatx16 s[NKT][QT];
     ColB<T> pf[NKT][QT];
-    if constexpr (sizeof(T) == 2) {
-      typename M::frag ka[NKT][G::NS];
+    typename M::frag ka[NKT][G::NS];
 #pragma unroll
-      for (int st = 0; st < G::NS; ++st) ka[0][st] = kf(0, st);
-      ColA<T, DC> va[NKT];
+    for (int st = 0; st < G::NS; ++st) ka[0][st] = kf(0, st);
+    ColA<T, DC> va[NKT];
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (kt + 1 < NKT) {
+    for (int kt = 0; kt < NKT; ++kt) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (kt + 1 < NKT) {
 #pragma unroll
-          for (int st = 0; st < G::NS; ++st) ka[kt + 1][st] = kf(kt + 1, st);
-        } else {
-          va[0].load(vl, 0, lane);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        for (int st = 0; st < G::NS; ++st) ka[kt + 1][st] = kf(kt + 1, st);
+      } else {
+        va[0].load(vl, 0, lane);
+      }
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < QT; ++j) {
+      for (int j = 0; j < QT; ++j) {
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[kt][j][r] = 0.0f;
-        }
-#pragma unroll
-        for (int st = 0; st < G::NS; ++st)
-#pragma unroll
-          for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(ka[kt][st], qf[j][st], s[kt][j]);
+        for (int r = 0; r < 16; ++r) s[kt][j][r] = 0.0f;
       }
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) {
-        scale(s[kt], c, by);
-        if (kt + 1 < NKT) va[kt + 1].load(vl, 32 * (kt + 1), lane);
-        cut(s[kt], pf[kt], kt, key0, mask, gone, cols, lane);
+      for (int st = 0; st < G::NS; ++st)
 #pragma unroll
-        for (int j = 0; j < QT; ++j) o[j].add(va[kt], pf[kt][j]);
-      }
-    } else {
-      scores(s, kf, qf, key0, false, 0, c, cols, by, lane);
+        for (int j = 0; j < QT; ++j) s[kt][j] = M::mma(ka[kt][st], qf[j][st], s[kt][j]);
+    }
 #pragma unroll
-      for (int kt = 0; kt < NKT; ++kt) cut(s[kt], pf[kt], kt, key0, mask, gone, cols, lane);
-      product(vl, pf, lane);
+    for (int kt = 0; kt < NKT; ++kt) {
+      scale(s[kt], c, by);
+      if (kt + 1 < NKT) va[kt + 1].load(vl, 32 * (kt + 1), lane);
+      cut(s[kt], pf[kt], kt, key0, mask, gone, cols, lane);
+#pragma unroll
+      for (int j = 0; j < QT; ++j) o[j].add(va[kt], pf[kt][j]);
     }
     bool over = false;
 #pragma unroll
@@ -495,10 +489,10 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
   const Edges ed = edges(p.win, u, cs, min(w0, nc - 1), min(w0 + 32 * QT, nc) - 1);   // of the wave
   clear_cols<T, DC>(lds, 4 * KB, D, threadIdx.x, NT);
   if (tiles.n) stash(0);
-  Softmax<T, DC, QT, NKT, true> sm;
+  Softmax<T, DC, QT, NKT, sizeof(T) == 2> sm;
   sm.init();
   __syncthreads();
-  // A tile's steps of 32 NKT keys: exact ones until every column has a reference, then fast
+  // A tile's steps of 32 NKT keys: exact ones (fp32: all) until every column has a reference, then fast
   // ones, in a loop that the rare fix() stands outside of (inside, its registers weigh on it:
   // 8192 causal tokens 173 and 185 us).  Waves go from one loop to the other by themselves;
   // each meets every tile's barrier once.
@@ -541,20 +535,22 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) 
     });
     advance();
   }
-  while (it < tiles.n) {
-    bool moved = false;
-    for (; it < tiles.n && !moved;) {
-      moved = step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) __attribute__((always_inline)) {
-        return sm.fast(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
+  if constexpr (sizeof(T) == 2) {
+    while (it < tiles.n) {
+      bool moved = false;
+      for (; it < tiles.n && !moved;) {
+        moved = step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) __attribute__((always_inline)) {
+          return sm.fast(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
+        });
+        if (!moved) advance();
+      }
+      if (!moved) break;
+      step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) __attribute__((always_inline)) {
+        sm.fix(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
+        return true;
       });
-      if (!moved) advance();
+      advance();
     }
-    if (!moved) break;
-    step([&](const auto& kf, const T* vl, int32_t key0, bool mask, uint32_t lost_bits) __attribute__((always_inline)) {
-      sm.fix(kf, vl, qf, key0, mask, lost_bits, p.c, col, lane);
-      return true;
-    });
-    advance();
   }
 
 #pragma unroll

@@ -124,20 +124,17 @@ __device__ __forceinline__ void turn8(const AppendParams& p, const Place8& e, in
       }
     }
   }
-  if (p.half) {
+  float a[4], b[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float xa = x[i], xb = x[4 + i];
-      x[i] = xa * c[i] - xb * s[i];
-      x[4 + i] = xb * c[i] + xa * s[i];
-    }
-  } else {
+  for (int i = 0; i < 4; ++i) {
+    const float xa = p.half ? x[i] : x[2 * i], xb = p.half ? x[4 + i] : x[2 * i + 1];
+    a[i] = xa * c[i] - xb * s[i];
+    b[i] = xb * c[i] + xa * s[i];
+  }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float xa = x[2 * i], xb = x[2 * i + 1];
-      x[2 * i] = xa * c[i] - xb * s[i];
-      x[2 * i + 1] = xb * c[i] + xa * s[i];
-    }
+  for (int i = 0; i < 4; ++i) {
+    x[i] = p.half ? a[i] : i % 2 ? b[i / 2] : a[i / 2];
+    x[4 + i] = p.half ? b[i] : i % 2 ? b[2 + i / 2] : a[2 + i / 2];
   }
 }
 
