@@ -402,8 +402,8 @@ __device__ __forceinline__ BlockOf block_of(const FwdParams& p, uint32_t size, u
 }
 
 // Many columns: QT blocks of 32 per wave, the keys in LDS tiles that all waves share,
-// the next tile on its way in registers.  Vector units bound it (busy 77 - 87%: for a score an
-// exponential, its scaling, cut, sum and half a conversion; matrix cores 34%): 8192 causal
+// the next tile on its way in registers.  Vector units bound it (busy 64%: for a score an
+// exponential, its scaling, cut, sum and half a conversion; matrix cores 38%): 8192 causal
 // tokens, 32 heads of 64 over 8, window 2048, 158 us, 764 TFLOP/s of the 120 GF of its mask;
 // 8 x 16 units of 4096 x 72, window 257, 122 us.
 template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int NKT, int MINW>
