@@ -535,8 +535,8 @@ int dsp_attn_window_bwd(const void* q, const void* k, const void* v, const void*
  * dsp_attn_paged -- attention of the new tokens (q, o: T rows of H heads, q_stride and
  * o_stride elements apart) over their sequences' cached positions, with the visibility,
  * scale and precision of dsp_attn_window (left -1, right 0: causal without a window).
- * max_q:    no sequence has more new tokens (rows past it are left as they were); with
- *           max_q * H / Hkv <= 32 the keys are cut among work-groups.
+ * max_q:    no sequence has more new tokens (rows past it are left as they were); a small one
+ *           lets the keys be cut among work-groups.
  * lse:      fp32 [T][H], or NULL.
  * Rows of no sequence are left as they were.  DSP_BF16: D a multiple of 8 up to 128,
  * 16-byte aligned q and o and bf16 caches (8-byte for DSP_E4M3) with strides multiples of 8;

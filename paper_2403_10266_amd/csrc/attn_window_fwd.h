@@ -44,8 +44,8 @@ struct FwdParams {
   Order order;       // many columns, rows of a tensor
   uint32_t n_blk;    // many columns, pages: blocks in all
   uint32_t few_cols; // many columns: units of at most so many are left to the other form
-  uint32_t pieces, n_split;   // few columns: units times splits
-  uint32_t block_cols;        // columns of a unit, at most
+  uint32_t pieces, n_split, cblk;   // few columns: units times splits, blocks of 32 columns
+  uint32_t block_cols;              // of a block, at most
   float c;           // scale * log2(e)
   bool vec;
 };
@@ -651,7 +651,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_short_kernel(FwdParams p
     u.lse[(int64_t)i * u.lse_i + (int64_t)hh * u.lse_h] = l == 0.0f ? -INFINITY : kLn2 * (sm.ref[0] + log2f(l));
 }
 
-// Few columns: 32 of a unit at most, the keys' tiles of 32 cut among work-groups and,
+// Few columns: blocks of 32 of a unit's, the keys' tiles of 32 cut among work-groups and,
 // inside one, among its waves, each with LDS rows of its own and no barrier until the
 // waves' sums are joined.  A pass over a cache is bound by memory: what counts is how
 // many waves a CU holds, that each has its next tile on its way, and that every load
@@ -682,15 +682,17 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
   T* kl = reinterpret_cast<T*>(smem) + wave * 2 * TILE;   // [NW][K, V][32][P]
   T* vl = kl + TILE;
 
-  // an XCD takes the heads of a stretch of keys, which together read whole token rows
-  const uint32_t j8 = blockIdx.x >> 3, piece = j8 / p.Hkv * 8 + (blockIdx.x & 7u), e = j8 % p.Hkv;
+  // an XCD takes the heads of a stretch of keys, which together read whole token rows, and the blocks of a head's columns
+  const uint32_t he = p.Hkv * p.cblk, j8 = blockIdx.x >> 3, piece = j8 / he * 8 + (blockIdx.x & 7u);
   if (piece >= p.pieces) return;
+  const uint32_t ec = j8 % he, e = ec / p.cblk, c0 = 32 * (ec - e * p.cblk);
   const uint32_t un = piece / p.n_split, split = piece - un * p.n_split;
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
-  const uint32_t nc = (uint32_t)u.nq * p.grp.d;
-  if (nc == 0 || nc > p.few_cols) return;
+  const uint32_t cols = (uint32_t)u.nq * p.grp.d;
+  if (c0 >= cols || cols > p.few_cols) return;
+  const uint32_t nc = min(cols - c0, 32u);
   const int D = (int)p.D;
-  const Columns cs(p.grp, 0);
+  const Columns cs(p.grp, c0);
   const Edges ed = edges(p.win, u, cs, 0, nc - 1);
   const Tiles<32> tiles(ed.first, ed.last);
   const Cut part = cut(tiles.n, p.n_split, NW);
@@ -795,7 +797,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_few_kernel(FwdParams p) 
   }
   __syncthreads();
   // maxima, sums, rows of 32 columns
-  float* to = p.part + (((uint64_t)un * p.Hkv + e) * p.n_split + split) * 32 * (2 + p.D);
+  float* to = p.part + (((uint64_t)un * he + ec) * p.n_split + split) * 32 * (2 + p.D);
   for (uint32_t i = threadIdx.x; i < nc * p.D; i += NW * 64) {
     const uint32_t n = i / p.D, d = i - n * p.D;
     float v = 0.0f;
@@ -821,18 +823,18 @@ __global__ __launch_bounds__(256) void window_join_kernel(FwdParams p, int waves
   constexpr int GR = 256 / DP;
   __shared__ float f[kMaxSplit], red[256], m4[4];
   using U = Unit<T, S, PAGED>;
-  const uint32_t ue = blockIdx.x / p.block_cols, n = blockIdx.x - ue * p.block_cols;
-  const uint32_t un = ue / p.Hkv, e = ue - un * p.Hkv;
+  const uint32_t he = p.Hkv * p.cblk, uec = blockIdx.x / p.block_cols, n = blockIdx.x - uec * p.block_cols;
+  const uint32_t un = uec / he, ec = uec - un * he, e = ec / p.cblk, c0 = 32 * (ec - e * p.cblk);
   const U u = unit<T, S>(p, un, e, (U*)nullptr);
-  const uint32_t nc = (uint32_t)u.nq * p.grp.d;
-  if (n >= nc || nc > p.few_cols) return;
-  const Columns cs(p.grp, 0);
-  const Edges ed = edges(p.win, u, cs, 0, nc - 1);
+  const uint32_t cols = (uint32_t)u.nq * p.grp.d;
+  if (c0 + n >= cols || cols > p.few_cols) return;
+  const Columns cs(p.grp, c0);
+  const Edges ed = edges(p.win, u, cs, 0, min(cols - c0, 32u) - 1);
   const Tiles<32> tiles(ed.first, ed.last);
   const uint32_t used = (uint32_t)cut(tiles.n, p.n_split, waves).used;
   if (used == 1) return;
   const uint32_t stride = 32 * (2 + p.D);
-  const float* w = p.part + (uint64_t)ue * p.n_split * stride;
+  const float* w = p.part + (uint64_t)uec * p.n_split * stride;
   float m = -INFINITY;
   for (uint32_t s = threadIdx.x; s < used; s += 256) {
     f[s] = w[(uint64_t)s * stride + n];
@@ -915,10 +917,10 @@ int start_few(FwdParams& p, const WindowArgs& a, hipStream_t s) {
   lds = std::max(lds, ((2 * NW + 2) * 32 + (size_t)NW * 32 * Geo<T, DC>::DP) * 4);
   const int64_t pieces = a.B * a.X * p.n_split;
   p.pieces = (uint32_t)pieces;
-  int st = launch(window_few_kernel<T, S, PAGED, DC, NW, MINW>, (pieces + 7) / 8 * 8 * a.Hkv, NW * 64, lds, p, s);
+  int st = launch(window_few_kernel<T, S, PAGED, DC, NW, MINW>, (pieces + 7) / 8 * 8 * a.Hkv * p.cblk, NW * 64, lds, p, s);
   if (st != DSP_OK || p.n_split == 1) return st;
   p.block_cols = (uint32_t)std::min<int64_t>(a.Lq * p.grp.d, 32);
-  const int64_t cols = a.B * a.X * a.Hkv * p.block_cols;   // few units: they are why the keys are split
+  const int64_t cols = a.B * a.X * a.Hkv * p.cblk * p.block_cols;   // few units: they are why the keys are split
   if (!grid_fits(cols, 256)) return DSP_ERR_SHAPE;
   if (a.D <= 64) window_join_kernel<T, S, PAGED, 64><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
   else window_join_kernel<T, S, PAGED, 128><<<dim3((uint32_t)cols), 256, 0, s>>>(p, NW);
@@ -929,38 +931,48 @@ int start_few(FwdParams& p, const WindowArgs& a, hipStream_t s) {
 // how many parts their keys go at most.
 struct Choice {
   bool few, many;
-  int64_t n_split;
+  int64_t cblk, n_split;
 };
 inline Choice choose(const WindowArgs& a) {
   Choice c = {};
-  const int64_t grp = a.H / a.Hkv, cols = a.Lq * grp;
-  c.few = grp <= 32;
-  c.many = cols > 32;
-  if (c.many && !(a.page_shift && a.B > 1)) c.few = false;
-  c.n_split = 1;
-  if (!c.few) return c;
+  const int64_t grp = a.H / a.Hkv, cols = a.Lq * grp, units = std::max<int64_t>(a.B * a.X * a.Hkv, 1);
   // keys that a block of columns can see
   int64_t keys = a.Lk;
   if (a.win.left >= 0 && a.win.right >= 0)
     keys = std::min<int64_t>(keys, (int64_t)a.win.left + a.win.right + a.win.sinks + 64);
+  // More columns than a block has take several of this form where the other one, with whole
+  // passes over the keys, would leave most of the chip idle: each block reads the keys again, out
+  // of L2.  Heads of 64, groups of 4; blocks of all units, keys: this form and the other in us:
+  // 16, 8000: 21 and 124; 128, 2000: 33 and 37; 256, 2000: 53 and 37; 512, 8000: 115 - 135 and
+  // 146 - 173; 1024, 8000: 220 and 171; 16, 100000: 58 and 1760; 512, 100000: 842 and 2183.
+  const int64_t blocks = (cols + 31) / 32;
+  c.cblk = cols > 32 && units * blocks <= std::min<int64_t>(512, keys / 16) ? blocks : 1;
+  c.few = grp <= 32 || c.cblk > 1;
+  c.many = cols > 32 * c.cblk;
+  if (c.many && !(a.page_shift && a.B > 1)) c.few = false;
+  c.n_split = 1;
+  if (!c.few) return c;
   // One sequence's units are alike: as many work-groups as the chip holds at once (100000 keys
   // of 8 heads of 128: 87 us with 2 to a CU, 93 with 4, 104 with 8).  Sequences differ in
   // length: 8 to a CU (64 of up to 16000 keys in 8 bits, 8 heads of 64: 166 us; 178 with 6, 196
   // with 4, 174 with 16).
-  const int64_t units = std::max<int64_t>(a.B * a.X * a.Hkv, 1);
   const int64_t per_cu = a.B > 1 ? 8 : !a.bf16 ? 1 : a.D <= 64 ? 4 : a.D <= 80 ? 3 : 2;
-  const int64_t n = std::min<int64_t>({(256 * per_cu + units - 1) / units, keys / 256, kMaxSplit});
+  int64_t n = (256 * per_cu + units * c.cblk - 1) / (units * c.cblk);
+  // a part's blocks and heads run on one XCD: as many parts for each of the eight
+  if (c.cblk > 1) n = (n + 7) / 8 * 8;
+  n = std::min<int64_t>({n, keys / 256, kMaxSplit});
   if (n > 1) c.n_split = n;
   return c;
 }
 inline size_t part_bytes(const WindowArgs& a) {
   const Choice c = choose(a);
-  return c.n_split > 1 ? (size_t)(a.B * a.X * a.Hkv * c.n_split) * 32 * (2 + (size_t)a.D) * 4 : 0;
+  return c.n_split > 1 ? (size_t)(a.B * a.X * a.Hkv * c.cblk * c.n_split) * 32 * (2 + (size_t)a.D) * 4 : 0;
 }
 
 template <typename T, typename S, bool PAGED, int DC>
 int start(FwdParams& p, const WindowArgs& a, const Choice& c, hipStream_t s) {
-  p.few_cols = c.few ? 32 : 0;
+  p.few_cols = c.few ? (uint32_t)(32 * c.cblk) : 0;
+  p.cblk = (uint32_t)c.cblk;
   p.n_split = (uint32_t)c.n_split;
   if (c.few) {
     if (int st = start_few<T, S, PAGED, DC, 4>(p, a, s)) return st;

@@ -356,3 +356,13 @@ def test_two_at_once(torch):
         call(0)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for g, w in zip(outs, want) for a, b in zip(g, w))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,Lq,Lk,H,Hkv,D,left,right,sinks", [
+    (1, 16, 3000, 8, 2, 64, -1, 0, 0), (2, 33, 1500, 4, 2, 72, -1, 0, 0), (1, 3, 2500, 40, 1, 40, 1200, 0, 5),
+    (1, 129, 2200, 2, 2, 128, -1, 3, 0), (1, 9, 1025, 4, 1, 96, 700, 40, 2)])
+def test_several_blocks_of_columns_against_many_keys(torch, dtype, B, Lq, Lk, H, Hkv, D, left, right, sinks):
+    c = wu.case(B, 1, Lq, Lk, H, Hkv, D, dtype, seed=Lq)
+    _check(torch, c, dtype, f"blocks B{B} {Lq}x{Lk} H{H}/{Hkv} D{D}", left=left, right=right, sinks=sinks,
+           q_pos=[Lk - Lq - 7 * b for b in range(B)], kv_len=[Lk - 7 * b for b in range(B)])

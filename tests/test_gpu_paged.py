@@ -490,3 +490,18 @@ def test_long_prompts_and_short_ones(torch, kind):
         scales = [2.0 ** r.integers(-4, 2, (pages, 2)) for _ in "kv"]
         held = [np.clip(ow.e4m3(h / s[:, None, :, None]), -448, 448) for h, s in zip(held, scales)]
     _attend(torch, dsp, r, kind, "bf16", "token", table, held, scales, new, kv, 8, 2, 64, -1, 0, 0)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("new,kv,H,Hkv,D,left", [([20, 9, 0, 1], [2100, 1500, 40, 90], 8, 2, 64, -1), ([40], [3000], 4, 1, 72, -1),
+                                                 ([17, 33], [1800, 33], 6, 2, 128, 900)])
+def test_several_blocks_of_columns_against_a_long_cache(torch, kind, new, kv, H, Hkv, D, left):
+    import paper_2403_10266_amd as dsp
+    r = np.random.default_rng(14)
+    dtype = "f32" if kind == "f32" else "bf16"
+    table, pages = _table(r, kv, 32)
+    held, scales = [wu.draw((pages, 32, Hkv, D), dtype, r) for _ in "kv"], [None, None]
+    if kind == "e4m3":
+        scales = [2.0 ** r.integers(-4, 2, (pages, Hkv)) for _ in "kv"]
+        held = [np.clip(ow.e4m3(h / s[:, None, :, None]), -448, 448) for h, s in zip(held, scales)]
+    _attend(torch, dsp, r, kind, dtype, "token", table, held, scales, new, kv, H, Hkv, D, left, 0, 0)
