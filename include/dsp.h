@@ -507,7 +507,8 @@ int dsp_attn_window_bwd(const void* q, const void* k, const void* v, const void*
  * table[n][j / page].
  * table:    DEVICE int32 [N][max_pages].  An entry outside 0 .. n_pages - 1 is no page:
  *           its keys are not seen and tokens for it are dropped (a page given back, or not
- *           yet needed).  Nothing outside the caches is read or written.
+ *           yet needed).  Nothing outside the caches is read or written.  A cache may have no
+ *           pages at all (n_pages 0, NULL caches and scales).
  * q_start:  DEVICE int32 [N + 1], rising: rows q_start[n] .. q_start[n + 1] - 1 of the T
  *           packed rows are sequence n's new tokens.  Values outside 0 .. T are clamped.
  * kv_len:   DEVICE int32 [N], the positions of each sequence, the new tokens being the

@@ -144,14 +144,14 @@ int cache_layout(Cache& c, int64_t N, int64_t n_pages, int64_t max_pages, int pa
     c.st[i] = st[i];
     if (st[i] < 0 || (c.e[i] > 1 && st[i] == 0)) return DSP_ERR_SHAPE;
   }
+  if (!n_pages) return DSP_OK;   // nothing to span: every token is dropped, no key is seen
   if (!spans_ok(n_pages, page, Hkv, st)) return DSP_ERR_SHAPE;
   if (st[1] >= (int64_t(1) << 31) / 64 / c.es) return DSP_ERR_SHAPE;   // 64 slots lie within 2^31 bytes
   if (!rows_disjoint(n_pages, page, Hkv, st, D)) return DSP_ERR_ARG;
-  c.bytes = n_pages ? ((n_pages - 1) * st[0] + (page - 1) * st[1] + (Hkv - 1) * st[2] + D) * c.es : 0;
+  c.bytes = ((n_pages - 1) * st[0] + (page - 1) * st[1] + (Hkv - 1) * st[2] + D) * c.es;
   return DSP_OK;
 }
 bool caches_apart(const Cache& c, const void* k, const void* v, int D) {
-  if (!c.e[0]) return true;
   int64_t off = (intptr_t)v - (intptr_t)k;
   off = off < 0 ? -off : off;
   if (off % c.es) return off >= c.bytes;

@@ -281,3 +281,18 @@ def test_binding_refusals():
         dsp.dsp_kv_append(x[0, 0], x[0, 0], torch.zeros(3, 16, 2, 72), torch.zeros(3, 16, 2, 72), i[None], i, i[:1])
     with pytest.raises(ValueError, match="device tensor"):
         dsp.dsp_attn_paged(x[0, 0], torch.zeros(3, 16, 2, 72), torch.zeros(3, 16, 2, 72), i[None], i, i[:1], 2)
+
+
+@pytest.mark.parametrize("call", [_append, _paged])
+def test_a_cache_of_no_pages(lib, call):
+    """No pages are a size like any other: with nothing to do the calls return, other
+    arguments are checked as ever."""
+    none = dict(q=None, k=None, v=None, o=None, kc=None, vc=None, table=None, start=None, lens=None, lse=None, ws=None, nws=0)
+    for more in (dict(N=0), dict(T=0)):
+        assert call(lib, n_pages=0, **more, **none) == dsp.DSP_OK
+        assert call(lib, n_pages=0, **more, **none, cs=_st(0, 0, 0)) == dsp.DSP_ERR_SHAPE   # slots over one another
+    bare = dict(n_pages=0, kc=None, vc=None)
+    assert call(lib, **bare, q=None) == dsp.DSP_ERR_NULL
+    assert call(lib, **bare, lens=None) == dsp.DSP_ERR_NULL
+    assert call(lib, **bare, o=A[9]) == dsp.DSP_ERR_ARG
+    assert call(lib, **bare, page=24) == dsp.DSP_ERR_SHAPE
