@@ -465,7 +465,8 @@ int dsp_attn_relpos_bwd(const void* q, const void* k, const void* v, const void*
  * lse:     fp32 [B * X * H][Lq], the row log-sum-exp of the scaled scores, or NULL.
  * scale:   softmax scale; scale <= 0 selects 1/sqrt(D).
  * dtype:   DSP_BF16 (fp32 scores, softmax and accumulation; probabilities are rounded to
- *          bf16 for the product with v), D a multiple of 8 up to 128, 16-byte aligned
+ *          bf16 for the product with v, whose sums may be held at 2^-16 of their size:
+ *          values below 2^-110 may lose bits), D a multiple of 8 up to 128, 16-byte aligned
  *          tensors and strides multiples of 8; or DSP_F32, any D up to 128.  Lq and Lk
  *          below 2^30, H / Hkv below 2^15, Lq * H / Hkv below 2^31, and 64 rows of each tensor within 2^31 bytes.
  * workspace: dsp_attn_window_workspace_bytes(...) bytes, 16-byte aligned (0 except for a

@@ -112,12 +112,16 @@ __device__ __forceinline__ void keep_nan() {
 // The softmax of QT blocks of 32 columns over NKT blocks of 32 keys at a time, less a
 // reference of each column (exp2 units).
 //  * exact(): takes the tile's maxima and moves the references to them.
-//  * fast() (LAZY, bf16: a reference so far off costs an fp32 exponent 6 of its bits, fp32 results
-//    1.3e-6 of their value where exact() gives 2e-7): the references stay, 64 above the maximum of the tiles that set them, and
-//    probabilities are cut at 1, so that nothing stands between the exponentials and the
+//  * fast() (LAZY, bf16: a reference off the maximum costs an exponent's last bits, fp32 results
+//    1.3e-6 of their value at 64 off where exact() gives 2e-7): the references stay, kRoom above the maximum of the
+//    tiles that set them, and probabilities are cut at 1, so that nothing stands between the exponentials and the
 //    product with v.  A score above its reference shows afterwards, as a sum of a half or
-//    more (probabilities below it add up to far less); then, rarely, fix() moves the
-//    reference and adds to the tile's probabilities what the cut took from them.
+//    more (probabilities below it add up to less, or are so many that the reference had better
+//    move too); then, rarely, fix() moves the reference and adds to the tile's probabilities
+//    what the cut took from them.
+// The room bounds the values: sums are of 2^-kRoom v, and with 16 those of any v above 2^-110 keep
+// fp32's normal range (with 64 above 2^-62 only), at the price of a fix for every 16 binary steps
+// that the scores climb.
 // Sums are those of the fp32 probabilities (of the rounded ones, which a column of ones in v
 // would give with the product, the log-sum-exp would be off by their roundings: 9 times its
 // bound at 64 keys).
@@ -125,7 +129,7 @@ template <typename T, int DC, int QT, int NKT, bool LAZY>
 struct Softmax {
   using G = Geo<T, DC>;
   using M = Mx<T>;
-  static constexpr float kRoom = LAZY ? 64.0f : 0.0f;
+  static constexpr float kRoom = LAZY ? 16.0f : 0.0f;
   ColAcc<T, DC> o[QT];
   float ref[QT], sum[QT];   // the sum of this lane's keys
   bool set;                 // every column that sees a key has a reference

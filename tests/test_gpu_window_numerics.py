@@ -2,10 +2,54 @@
 import numpy as np
 import pytest
 
-from tests.gpu_util import say
-from tests.test_gpu_attn_window import torch  # noqa: F401
+from oracle import window as ow
+from tests import window_util as wu
+from tests.gpu_util import dev, host, say
+from tests.test_gpu_attn_window import _i32, torch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("exp", [100, 60, -60, -80, -100])
+@pytest.mark.parametrize("Lq,Lk,left,kv_len", [(300, 300, -1, 300), (900, 1000, 300, 960), (200, 1400, 500, 1390), (20, 3000, -1, 2900),
+                                               (2, 3000, -1, 3000), (100, 100, 30, 90)])
+def test_values_of_any_magnitude(torch, exp, Lq, Lk, left, kv_len):  # noqa: F811
+    """Values times a power of two give outputs times that power, at the tolerances of values
+    around 1: every form of the kernel, scores that climb among them."""
+    import paper_2403_10266_amd as dsp
+    c = wu.case(1, 1, Lq, Lk, 4, 2, 64, "bf16", seed=50)
+    for climb in (0.0, 30.0):       # nats, over the keys
+        c["q"][..., 0::64] = 8.0
+        c["k"][..., 0::64] = wu.synth.bf16_round(np.linspace(0, climb, Lk, dtype=np.float32))[:, None]
+        kw = dict(left=left, right=0, sinks=3)
+        want = wu.wanted(c, "bf16", q_pos=[kv_len - Lq], kv_len=[kv_len], grads=False, **kw)
+        v = dev(c["v"], "bf16") * 2.0 ** exp
+        assert torch.isfinite(v).all()
+        o, lse = dsp.dsp_attn_window(dev(c["q"], "bf16"), dev(c["k"], "bf16"), v, 4, 2, q_pos=_i32(torch, [kv_len - Lq]),
+                                     kv_len=_i32(torch, [kv_len]), with_lse=True, **kw)
+        say(f"2^{exp}, climb {climb}")
+        wu.compare(dict(o=host(o) * 2.0 ** -exp, lse=host(lse)), want, say)
+
+
+@pytest.mark.parametrize("new", [1, 200])
+def test_8_bit_values_of_the_least_scale(torch, new):  # noqa: F811
+    """Scales of 2^-64 and 2^-40: values down to 2^-73 keep their bits."""
+    import paper_2403_10266_amd as dsp
+    r = np.random.default_rng(51)
+    H, Hkv, D, page, kv = 4, 2, 64, 32, 320
+    k = ow.e4m3(wu.draw((10, page, Hkv, D), "bf16", r) * 8)
+    v = np.clip(ow.e4m3(wu.draw((10, page, Hkv, D), "bf16", r)), -448, 448)
+    q = wu.draw((new, H * D), "bf16", r)
+    table = r.permutation(10)[None]
+    put = lambda t: torch.from_numpy(t.astype(np.float32)).cuda().to(torch.float8_e4m3fn)  # noqa: E731
+    ks = torch.full((10, Hkv), 0.125, device="cuda")
+    call = lambda e: dsp.dsp_attn_paged(dev(q, "bf16"), put(k), put(v), _i32(torch, table), _i32(torch, [0, new]),  # noqa: E731
+                                        _i32(torch, [kv]), H, max_q=new, k_scale=ks, v_scale=torch.full_like(ks, 2.0 ** e))
+    rows = lambda t: t[table[0]].reshape(1, 1, kv, Hkv * D)  # noqa: E731
+    c = dict(q=q[None, None], k=rows(k) * 0.125, v=rows(v), do=q[None, None], H=H, Hkv=Hkv)
+    want = wu.wanted(c, "bf16", right=0, q_pos=[kv - new], grads=False)
+    for e in (0, -40, -64):
+        wu.compare(dict(o=host(call(e)) * 2.0 ** -e), dict(o=want["o"]), say)
 
 
 @pytest.mark.parametrize("rise", [15.5, 63.5, 300.0])
