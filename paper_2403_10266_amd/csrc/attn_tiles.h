@@ -206,6 +206,21 @@ struct ColAcc {
       }
     }
   }
+  // plus f times b, f what each lane holds for its own column n = lane % 32
+  __device__ __forceinline__ void add(float f, const ColAcc& b, int lane) {
+#pragma unroll
+    for (int i = 0; i < G::NT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) t[i][r] = fmaf(f, b.t[i][r], t[i][r]);
+    if constexpr (G::SLAB) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float fh = __shfl(f, 16 * h + (lane & 15));
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[h][r] = fmaf(fh, b.s[h][r], s[h][r]);
+      }
+    }
+  }
   // times a factor that each lane holds for its own column n = lane % 32
   __device__ __forceinline__ void scale(float f, int lane) {
 #pragma unroll

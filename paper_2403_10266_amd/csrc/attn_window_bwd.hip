@@ -4,7 +4,7 @@
 //   dV = P^T dO,  dQ = scale dZ K,  dK = scale dZ^T Q.
 // P is recomputed from the forward's row log-sum-exp.  Two kernels, both deterministic:
 // the first owns blocks of (query, head) columns of a key/value head's group and visits
-// the keys that they see (dQ, Delta), the second owns blocks of keys and visits the
+// the keys that they see (dQ and Delta = sum_j P dP, as O is rounded in bf16), the second owns blocks of keys and visits the
 // queries that see them, head by head of the group (dK, dV).
 //
 // A first token that stays visible is seen by every later query, so its block of keys has
@@ -148,7 +148,6 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
   // a row that sees nothing, or past the end: P = exp2(-inf) = 0
   const float l = on ? p.lse[stat] : -INFINITY;
   const float lse2 = l == -INFINITY ? INFINITY : l * kLog2e;
-  if (on && g == 0) p.delta[stat] = delta;
   const Seen col = seen(p.win, p0 + qi, len);
   const Seen wf = seen_by(32 * wave), wl = seen_by(32 * wave + 31);
   const bool wave_on = 32 * wave < nc;
@@ -156,8 +155,15 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
   if (tiles.n) stash(0);
   __syncthreads();
 
-  ColAcc<T, DC> dq;
+  // bf16: Delta from the rounded o misses sum_j P dP by `off`, the sum of the column's dZ, and dQ by
+  // off times sum_j P k_j: one more product, of operands that are there.  Without it dQ and dK err
+  // 1.4 times as much where rows see few keys, and without limit where dP varies less over a row's
+  // keys than o's rounding does.
+  constexpr bool FIX = sizeof(T) == 2;
+  ColAcc<T, DC> dq, pk;
   dq.zero();
+  pk.zero();
+  float off = 0.0f;
   for (int32_t it = 0; it < tiles.n; ++it) {
     const bool more = it + 1 < tiles.n;
     if (more) fetch(it + 1);
@@ -171,28 +177,43 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
       floatx16 s, dp;
       typename M::frag ka[G::NS], va[G::NS];
       row_operand<T, DC>(kl, 32 * kt, l32, g, ka);
-      row_operand<T, DC>(vl, 32 * kt, l32, g, va);
       ahead<T>();
       row_product<T, DC>(s, ka, qf);
+      row_operand<T, DC>(vl, 32 * kt, l32, g, va);
+      ahead<T>();
+      row_product<T, DC>(dp, va, df);
       ColA<T, DC> kt_a;
       kt_a.load(kl, 32 * kt, lane);
       ahead<T>();
-      row_product<T, DC>(dp, va, df);
       const uint32_t bits = mask ? seen_bits(col, key0) >> (4 * g) : ~0u;
-      ColB<T> z;
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], p.c, -lse2));
       if (mask) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = keep_bit(s[r], bits, 8 * (r / 4) + r % 4);
       }
+      ColB<T> z, pb;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) z.set(r, s[r] * (dp[r] - delta));
+      for (int r = 0; r < 16; ++r) {
+        const float dz = s[r] * (dp[r] - delta);
+        z.set(r, dz);
+        if constexpr (FIX) {
+          off += dz;
+          pb.set(r, s[r]);
+        }
+      }
       dq.add(kt_a, z);
+      if constexpr (FIX) pk.add(kt_a, pb);
     }
     if (more) stash((it + 1) & 1);
     __syncthreads();
   }
+  if constexpr (FIX) {
+    off += swap_halves(off);
+    dq.add(-off, pk, lane);
+    delta += off;
+  }
+  if (on && g == 0) p.delta[stat] = delta;
   dq.scale(p.scale, lane);
   T* out = static_cast<T*>(p.dq) + q_at + (int64_t)e * p.grp.d * D;
   auto row = [&](int k) -> T* {
@@ -597,7 +618,7 @@ Sinks sinks_of(const WindowArgs& a) {
 
 template <typename T, int DC>
 int start_dq(BwdParams& p, const WindowArgs& a, hipStream_t s) {
-  constexpr int NW = 4, CB = 32 * NW, KB = 32, MINW = sizeof(T) == 2 && DC <= 64 ? 3 : sizeof(T) == 2 || DC <= 96 ? 2 : 1;
+  constexpr int NW = 4, CB = 32 * NW, KB = 32, MINW = DC <= 96 ? 2 : 1;
   p.order = window_order(a, (a.Lq * p.grp.d + CB - 1) / CB, CB / p.grp.d + 1);
   const size_t lds = (size_t)4 * KB * Geo<T, DC>::P * sizeof(T);
   auto* kernel = window_bwd_dq_kernel<T, DC, NW, KB, MINW>;

@@ -86,3 +86,58 @@ def test_scores_under_the_reference_cost_nothing(torch, rise):  # noqa: F811
     assert ((out[0, 0].double() - want).abs() <= tol).all()
     # steps of the pass are alike in number and kind; half as much again is a step taken twice
     assert min(times[1]) < 1.5 * min(times[0])
+
+
+def _tight(c, left, right, sinks, q_pos, kv_len, scale):
+    """{name: (value, tolerance)} of dq and dk with Delta in fp32.  With e = eta of window_util:
+    dZ = P (dP - Delta) is off by 4 e P (|dO| |v| + |Delta|), and by u |dZ| where it is rounded as
+    an operand (twice u P dD, dD the o's rounding in Delta, where a correction of it meets
+    rounded operands); the sum by as much and the result by u."""
+    H, Hkv, u = c["H"], c["Hkv"], 2.0 ** -8
+    q, k, v, do = (ow._heads(c[n], h) for n, h in (("q", H), ("k", Hkv), ("v", Hkv), ("do", H)))
+    D = q.shape[-1]
+    _, lse, dq, dk, _ = ow.attention_window(c["q"], c["k"], c["v"], H, Hkv, left, right, sinks, q_pos, kv_len, scale, c["do"])
+    tq, tk = np.zeros_like(dq), np.zeros_like(dk)
+    hd = lambda t, h: t.reshape(*t.shape[:3], h, D)  # noqa: E731
+    Lq, Lk = q.shape[2], k.shape[2]
+    for b in range(q.shape[0]):
+        ok = ow.visible(Lq, Lk, q_pos[b], kv_len[b], left, right, sinks)
+        for h in range(H):
+            qq, g, kk, vv = q[b, :, :, h], do[b, :, :, h], k[b, :, :, h // (H // Hkv)], v[b, :, :, h // (H // Hkv)]
+            ll = lse[b, :, h][..., None]
+            p = np.where(ok & ~np.isneginf(ll), np.exp(qq @ kk.swapaxes(-1, -2) * scale - np.where(np.isneginf(ll), 0, ll)), 0.0)
+            S = float((np.abs(qq) @ np.abs(kk).swapaxes(-1, -2)).max() * scale)
+            eta = (D + 16) * wu.N24 * (1 + S) + Lk * wu.N24
+            dp = g @ vv.swapaxes(-1, -2)
+            dl = (p * dp).sum(-1, keepdims=True)
+            dd = u * (np.abs(g) * np.abs(p @ vv)).sum(-1, keepdims=True)
+            mag = p * (np.abs(g) @ np.abs(vv).swapaxes(-1, -2) + np.abs(dl))
+            e = (4 * eta + 2.0 ** -22 + max(Lk, Lq) * wu.N24) * mag + u * np.abs(p * (dp - dl)) * (1 + u) + 2 * u * p * dd
+            hd(tq, H)[b, :, :, h] = scale * (e @ np.abs(kk))
+            hd(tk, Hkv)[b, :, :, h // (H // Hkv)] += scale * (e.swapaxes(-1, -2) @ np.abs(qq))
+    return dict(dq=(dq, tq + u * np.abs(dq)), dk=(dk, tk + u * np.abs(dk)))
+
+
+@pytest.mark.parametrize("B,Lq,Lk,H,Hkv,D,left,right,sinks,kv_len", [
+    (1, 200, 200, 2, 2, 64, 3, 0, 0, [200]),
+    (2, 150, 150, 4, 2, 72, 1, 1, 2, [150, 40]),       # later queries see two sinks only
+    (1, 300, 300, 2, 1, 128, -1, 0, 0, [300]),
+    (1, 140, 260, 3, 3, 40, 9, 0, 4, [250]),
+    (1, 700, 700, 2, 1, 96, 40, 0, 4, [700]),          # sinks in parts
+    (3, 140, 140, 8, 4, 80, 2, 0, 1, [140, 70, 0]),
+    (1, 190, 190, 2, 2, 16, 2, 2, 0, [190]),
+])
+def test_gradients_do_not_see_the_rounding_of_o(torch, B, Lq, Lk, H, Hkv, D, left, right, sinks, kv_len):  # noqa: F811
+    """Values 64 and a little: o is rounded to halves, and dP - Delta is of that size.  Delta has to be that of
+    the probabilities, not of the rounded o."""
+    import paper_2403_10266_amd as dsp
+    r = np.random.default_rng(Lq + D)
+    c = wu.case(B, 1, Lq, Lk, H, Hkv, D, "bf16", seed=Lq)
+    c["v"] = (64.0 + 0.5 * r.integers(0, 5, c["v"].shape)).astype(np.float32)
+    q_pos = [n - Lq if Lq < Lk else 0 for n in kv_len]
+    want = _tight(c, left, right, sinks, q_pos, kv_len, D ** -0.5)
+    q, k, v, do = (dev(c[n], "bf16") for n in ("q", "k", "v", "do"))
+    kw = dict(left=left, right=right, sinks=sinks, q_pos=_i32(torch, q_pos), kv_len=_i32(torch, kv_len))
+    o, lse = dsp.dsp_attn_window(q, k, v, H, Hkv, with_lse=True, **kw)
+    dq, dk, _ = dsp.dsp_attn_window_bwd(q, k, v, o, do, lse, H, Hkv, **kw)
+    wu.compare(dict(dq=host(dq), dk=host(dk)), want, say)
