@@ -8,8 +8,8 @@
 // queries that see them, head by head of the group (dK, dV).
 //
 // A first token that stays visible is seen by every later query, so its block of keys has
-// a window's queries many times over.  Those queries are cut into parts, work-groups of
-// about a window's work whose fp32 sums a third kernel adds in order.
+// a window's queries many times over.  Where units are few, those queries are cut into parts,
+// work-groups of about a window's work whose fp32 sums a third kernel adds in order.
 //
 // P and dZ are rounded to bf16 for the products that take them as operands (the matrix
 // cores' type; their sums are fp32).
@@ -31,7 +31,7 @@ struct BwdParams {
   void* dk;
   void* dv;
   float* delta;      // [B X H][Lq]
-  float* part;       // sinks: [unit and head][block][part][dK, dV][keys][D]
+  float* part;       // sinks in several parts: [unit and head][block][part][dK, dV][keys][D]
   const int32_t* q_pos;
   const int32_t* kv_len;
   int64_t qs[3], ks[3], os[3];
@@ -39,7 +39,7 @@ struct BwdParams {
   uint32_t X, H, Hkv, Lq, Lk, D;
   Divisor grp;
   Order order;
-  uint32_t parts, sink_blocks;   // parts of the first blocks of keys (0: they are like the others)
+  uint32_t parts, sink_blocks;   // parts of the first blocks of keys (0: they are like the others, 1: they only go first)
   uint32_t sink_groups;          // work-groups for them, the first of the grid
   float c, scale;
   bool vec;
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(KW * 64, MINW) void window_bwd_dkv_kernel(BwdParams
   const uint32_t k0 = first_key + 32 * wave;
   auto row = [&](T* base, int n) -> T* { return k0 + n < p.Lk ? base + (int64_t)(k0 + n) * p.ks[2] : nullptr; };
   auto part_row = [&](int which, int n) -> float* { return sums_at + ((uint64_t)which * KEYS + 32 * wave + n) * p.D; };
-  if (sink) {
+  if (sink && p.parts > 1) {
     const bool vec4 = p.D % 4 == 0;
     store_rows<T, DC>(dk, lane, D, vec4, [&](int n) { return part_row(0, n); });
     store_rows<T, DC>(dv, lane, D, vec4, [&](int n) { return part_row(1, n); });
@@ -600,10 +600,15 @@ int lds_limit(K* kernel, size_t lds) {
 }
 
 constexpr int kDkvKeys = 128;   // of a work-group
-// Parts of the first keys' queries: about a window's work each, where that is less than a
-// half of all.
+// Parts of the first keys' queries: about a window's work each, and no more work-groups than the
+// chip's 512 places for them: more only write and read more sums.  One part: the first blocks of keys
+// start first and write their gradients themselves.  Gradients in us with any number of parts, 512
+// work-groups, 256: 64 x 16 units of 8000 x 72, window 65, 4 sinks 6670 (2.4 GB of sums), 5470
+// (none), 5490; 8 x 16 of 8000 x 64, window 201, 768 (172 MB), 710 (38), 698; 8 of 8000 x 64 with 2000
+// sinks 237, 177, 209.
+constexpr int64_t kPlaces = 512;
 struct Sinks {
-  int64_t blocks, parts;
+  int64_t blocks, parts;   // parts 0: these blocks of keys are like the others
 };
 Sinks sinks_of(const WindowArgs& a) {
   Sinks s = {0, 0};
@@ -612,7 +617,7 @@ Sinks sinks_of(const WindowArgs& a) {
   const int64_t parts = std::min<int64_t>(a.Lq / std::max<int64_t>(band, 256), 64);
   if (parts < 2) return s;
   s.blocks = (std::min<int64_t>(a.win.sinks, a.Lk) + kDkvKeys - 1) / kDkvKeys;
-  s.parts = parts;
+  s.parts = std::min(parts, std::max<int64_t>(kPlaces / (a.B * a.X * a.Hkv * s.blocks), 1));
   return s;
 }
 
@@ -643,7 +648,7 @@ int start_dkv(BwdParams& p, const WindowArgs& a, hipStream_t s) {
   if (int st = lds_limit(kernel, lds)) return st;
   kernel<<<dim3((uint32_t)blocks), KW * 64, lds, s>>>(p);
   if (int st = last_launch_status()) return st;
-  if (!sk.parts) return DSP_OK;
+  if (sk.parts <= 1) return DSP_OK;
   const int64_t ub = a.B * a.X * a.Hkv * sk.blocks;
   window_bwd_sink_kernel<T><<<dim3((uint32_t)ub, 32), 256, 0, s>>>(p, 32 * KW);   // few units and parts: latency counts
   return last_launch_status();
@@ -686,7 +691,8 @@ size_t attn_window_bwd_workspace_bytes(const WindowArgs& a) {
   if (short_waves(a)) return 0;
   const int64_t stats = (a.B * a.X * a.H * a.Lq + 63) / 64 * 64;
   const Sinks s = sinks_of(a);
-  return (size_t)(stats + a.B * a.X * a.Hkv * s.blocks * s.parts * 2 * kDkvKeys * a.D) * 4;
+  const int64_t groups = s.parts > 1 ? a.B * a.X * a.Hkv * s.blocks * s.parts : 0;
+  return (size_t)(stats + groups * 2 * kDkvKeys * a.D) * 4;
 }
 
 int launch_attn_window_bwd(const WindowArgs& a, hipStream_t s) {

@@ -296,3 +296,14 @@ def test_a_cache_of_no_pages(lib, call):
     assert call(lib, **bare, lens=None) == dsp.DSP_ERR_NULL
     assert call(lib, **bare, o=A[9]) == dsp.DSP_ERR_ARG
     assert call(lib, **bare, page=24) == dsp.DSP_ERR_SHAPE
+
+
+def test_sinks_of_many_units_keep_no_sums(lib):
+    """The partial sums of first tokens fill the chip and no more, however many units there are."""
+    need = lambda X, L, left, sinks: lib.dsp_attn_window_bwd_workspace_bytes(1, X, L, L, 16, 16, 72, left, 0, sinks, BF)  # noqa: E731
+    for X, L, left in ((1024, 512, 33), (64, 8000, 65)):
+        assert need(X, L, left, 1) == need(X, L, left, 4) == need(X, L, left, 0) == X * 16 * L * 4
+    most = 512 * 2 * 128 * 72 * 4                       # work-groups, dK and dV, keys, columns
+    for X in range(1, 40):
+        for sinks in (1, 300):
+            assert 0 <= need(X, 9000, 50, sinks) - X * 16 * 9000 * 4 <= most, X

@@ -141,3 +141,25 @@ def test_gradients_do_not_see_the_rounding_of_o(torch, B, Lq, Lk, H, Hkv, D, lef
     o, lse = dsp.dsp_attn_window(q, k, v, H, Hkv, with_lse=True, **kw)
     dq, dk, _ = dsp.dsp_attn_window_bwd(q, k, v, o, do, lse, H, Hkv, **kw)
     wu.compare(dict(dq=host(dq), dk=host(dk)), want, say)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("X,L,H,Hkv,D,left,sinks", [(1, 1100, 2, 1, 40, 30, 3), (90, 560, 4, 2, 16, 9, 1), (150, 800, 2, 2, 8, 5, 140),
+                                                    (300, 520, 2, 2, 16, 3, 4)])
+def test_sinks_of_few_and_many_units(torch, dtype, X, L, H, Hkv, D, left, sinks):
+    """First tokens' gradients in many parts, in a few and in one: some units against the oracle."""
+    import paper_2403_10266_amd as dsp
+    r = np.random.default_rng(X)
+    q, do = (wu.draw((1, X, L, H * D), dtype, r) for _ in range(2))
+    k, v = (wu.draw((1, X, L, Hkv * D), dtype, r) for _ in range(2))
+    kw = dict(left=left, right=0, sinks=sinks)
+    n = L - 7
+    put = dict(kv_len=_i32(torch, [n]))
+    dq, dk, dv, dg = (dev(t, dtype) for t in (q, k, v, do))
+    o, lse = dsp.dsp_attn_window(dq, dk, dv, H, Hkv, with_lse=True, **put, **kw)
+    got = dict(zip(("dq", "dk", "dv"), dsp.dsp_attn_window_bwd(dq, dk, dv, o, dg, lse, H, Hkv, **put, **kw)))
+    for x in {0, X // 2, X - 1}:
+        c = dict(q=q[:, x:x + 1], k=k[:, x:x + 1], v=v[:, x:x + 1], do=do[:, x:x + 1], H=H, Hkv=Hkv)
+        want = wu.wanted(c, dtype, kv_len=[n], **kw)
+        say(f"unit {x} of {X}")
+        wu.compare({m: host(t[:, x:x + 1]) for m, t in got.items()}, {m: want[m] for m in got}, say)
