@@ -915,6 +915,8 @@ def _paged_args(w, like, dt, dev, k_cache, v_cache, table, q_start, kv_len, k_sc
             or k_cache.stride(3) != 1 or not _as(v_cache, ct, k_cache.shape, dev) or not _same_layout(k_cache, v_cache):
         _cache_refusal(w, like, (k_cache, v_cache))
     n_pages, page, Hkv, D = k_cache.shape
+    if Hkv < 1 or D < 1:
+        raise ValueError(f"{w}: k_cache and v_cache must hold at least one head, got {tuple(k_cache.shape)}")
     for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
         if (t is not None) != e4m3:
             raise ValueError(f"{w}: {name} comes with float8_e4m3fn caches, and only with them")

@@ -31,3 +31,14 @@ def test_no_pages(torch, kind, new):  # noqa: F811
     o, lse = dsp.dsp_attn_paged(got, *caches, table, start, kv, H, max_q=max(new), k_scale=s[0], v_scale=s[1],
                                 out=torch.full_like(q, 7.0), lse=torch.full((T, H), 7.0, device="cuda"))
     assert not o[:-1].any() and (lse[:-1] == -np.inf).all() and (o[-1] == 7).all() and (lse[-1] == 7).all()
+
+
+@pytest.mark.parametrize("Hkv,D", [(0, 72), (2, 0)])
+def test_caches_without_heads_are_refused(torch, Hkv, D):  # noqa: F811
+    import paper_2403_10266_amd as dsp
+    x, c = torch.zeros(3, 144, device="cuda"), torch.zeros(4, 16, Hkv, D, device="cuda")
+    k, args = torch.zeros(3, Hkv * D, device="cuda"), (_i32(torch, [[0, 1]]), _i32(torch, [0, 3]), _i32(torch, [9]))
+    with pytest.raises(ValueError, match="at least one head"):
+        dsp.dsp_attn_paged(x, c, c.clone(), *args, 2)
+    with pytest.raises(ValueError, match="at least one head"):
+        dsp.dsp_kv_append(k, k, c, c.clone(), *args, q=x)
