@@ -57,23 +57,23 @@ inline bool spans_ok(int64_t B, int64_t X, int64_t L, const int64_t* st) {
 }
 
 // Two row tensors of (B, X, La) and (B, X, Lb) rows share no element: their spans
-// are apart, or they have one grid and layout and lie in different columns of its rows.
+// are apart, or they have one layout and lie in different columns of its rows (the shorter
+// one's taken on to the longer one's end).
 inline bool rows_apart(const void* a, const int64_t* sa, int64_t wa, int64_t La, const void* b, const int64_t* sb, int64_t wb,
                 int64_t Lb, int64_t B, int64_t X, int es) {
   auto span = [&](const int64_t* st, int64_t w, int64_t L) {
     return (size_t)((B - 1) * st[0] + (X - 1) * st[1] + (L - 1) * st[2] + w) * es;
   };
   if (!wa || !wb || !La || !Lb || !overlap(a, span(sa, wa, La), b, span(sb, wb, Lb))) return true;
-  if (La != Lb) return false;
-  const int64_t L = La;
-  const int64_t ext[3] = {B, X, L};
+  const int64_t ext[3] = {B, X, std::max(La, Lb)};
+  const int64_t st[3] = {sa[0], sa[1], La > 1 ? sa[2] : sb[2]}, other[3] = {sb[0], sb[1], Lb > 1 ? sb[2] : sa[2]};
   int64_t pitch = INT64_MAX;
   for (int i = 0; i < 3; ++i) {
     if (ext[i] <= 1) continue;
-    if (sa[i] != sb[i] || sa[i] == 0) return false;
-    pitch = sa[i] < pitch ? sa[i] : pitch;
+    if (st[i] != other[i] || st[i] == 0) return false;
+    pitch = st[i] < pitch ? st[i] : pitch;
     for (int j = 0; j < 3; ++j)   // whole pitches: a larger stride starts after the smaller one's rows
-      if (j != i && ext[j] > 1 && sa[j] >= sa[i] && sa[j] / sa[i] < ext[i]) return false;
+      if (j != i && ext[j] > 1 && st[j] >= st[i] && st[j] / st[i] < ext[i]) return false;
   }
   const int64_t off = ((intptr_t)b - (intptr_t)a) / es;
   if (((intptr_t)b - (intptr_t)a) % es) return false;

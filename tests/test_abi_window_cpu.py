@@ -307,3 +307,18 @@ def test_sinks_of_many_units_keep_no_sums(lib):
     for X in range(1, 40):
         for sinks in (1, 300):
             assert 0 <= need(X, 9000, 50, sinks) - X * 16 * 9000 * 4 <= most, X
+
+
+@pytest.mark.parametrize("Lq", [1, 3, 150])
+def test_gradients_of_unequal_lengths_in_one_buffer(lib, Lq):
+    """dq, dk and dv as columns of one buffer's rows where queries are fewer than keys: apart (the
+    call goes on to its workspace), and refused where columns meet."""
+    row, L = 288 + 2 * 144, 150
+    st = _st(2 * L * row, L * row, row)
+    kw = dict(B=2, X=2, Lq=Lq, Lk=L, ws=None, os=_st(2 * Lq * 288, Lq * 288, 288))
+    packed = dict(qs=st, ks=st, q=A[0], k=A[0] + 2 * 288, v=A[0] + 2 * 432)
+    at = lambda q, k, v: _window(lib, True, **kw, **packed, dq=A[9] + 2 * q, dk=A[9] + 2 * k, dv=A[9] + 2 * v)  # noqa: E731
+    assert at(0, 288, 432) == at(288, 0, 144) == dsp.DSP_ERR_WORKSPACE
+    assert at(0, 280, 432) == at(8, 288, 440) == at(296, 0, 144) == dsp.DSP_ERR_ARG
+    assert at(row, 288, 432) == dsp.DSP_ERR_WORKSPACE      # a row on the columns are as far apart
+    assert at(row + 8, 288, 432) == at(row + 288, 288, 432) == dsp.DSP_ERR_ARG
