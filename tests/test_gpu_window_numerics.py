@@ -163,3 +163,32 @@ def test_sinks_of_few_and_many_units(torch, dtype, X, L, H, Hkv, D, left, sinks)
         want = wu.wanted(c, dtype, kv_len=[n], **kw)
         say(f"unit {x} of {X}")
         wu.compare({m: host(t[:, x:x + 1]) for m, t in got.items()}, {m: want[m] for m in got}, say)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Lq,sinks", [(300, 3), (3, 0)])
+def test_rows_far_apart(torch, dtype, Lq, sinks):  # noqa: F811
+    """Rows whose offsets inside one unit pass 32 bits, q, k and v columns of one buffer, and
+    their gradients of another: the bits of compact rows."""
+    import paper_2403_10266_amd as dsp
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GB of free GPU memory")
+    L, H, D = 300, 2, 64
+    step, C = (1 << 22 if dtype == "f32" else 1 << 23), H * D
+    c = wu.case(1, 1, Lq, L, H, H, D, dtype, seed=60)
+    q, k, v, do = (dev(c[n], dtype) for n in ("q", "k", "v", "do"))
+    kw = dict(left=40, right=0, sinks=sinks, q_pos=_i32(torch, [L - Lq]))
+
+    def views():
+        base = torch.empty(L * step, dtype=q.dtype, device="cuda")
+        assert (L - 1) * step * base.element_size() > 2 ** 32
+        return [base.as_strided((1, 1, n, C), (n * step, n * step, step, 1), i * C) for i, n in enumerate((Lq, L, L))]
+
+    far, grads, got = views(), views(), []
+    for t, x in zip(far, (q, k, v)):
+        t.copy_(x)
+    for t, g in (((q, k, v), [torch.empty_like(x) for x in (q, k, v)]), (far, grads)):
+        o, lse = dsp.dsp_attn_window(*t, H, H, with_lse=True, **kw)
+        got.append([o, lse, *dsp.dsp_attn_window_bwd(*t, o, do, lse, H, H, dq=g[0], dk=g[1], dv=g[2], **kw)])
+    assert torch.isfinite(got[0][0].float()).all()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
