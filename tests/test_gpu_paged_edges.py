@@ -196,3 +196,31 @@ def test_pages_far_apart(torch, kind, new):  # noqa: F811
         got.append([o, lse] + held + [t for t in s if t is not None])
     assert torch.isfinite(got[0][0].float()).all()
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_the_order_of_sequences_is_cheap(torch):  # noqa: F811
+    """64 sequences, put in order by length, take the time of 65, which are not, with as many
+    tokens: short passes over a narrow window, whose work-groups spend little else."""
+    import paper_2403_10266_amd as dsp
+    H, Hkv, D, page, T = 32, 8, 64, 64, 64 * 65 * 15
+    times, calls = [[], []], []
+    for N in (64, 65):
+        n = T // N
+        need = -(-n // page)
+        cache = [torch.randn(N * need, page, Hkv, D, device="cuda").bfloat16() for _ in "kv"]
+        q = torch.randn(T, H * D, device="cuda").bfloat16()
+        args = (_i32(torch, np.arange(N * need).reshape(N, need)), _i32(torch, np.arange(N + 1) * n), _i32(torch, [n] * N))
+        calls.append(lambda q=q, c=cache, a=args, n=n, o=torch.empty_like(q): dsp.dsp_attn_paged(q, *c, *a, H, max_q=n, left=31,
+                                                                                                  out=o))
+    ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+    for _ in range(12):
+        for t, call in zip(times, calls):
+            ev[0].record()
+            for _ in range(10):
+                call()
+            ev[1].record()
+            torch.cuda.synchronize()
+            t.append(ev[0].elapsed_time(ev[1]))
+    a, b = (min(t) * 100 for t in times)
+    say(f"64 sequences {a:.0f} us, 65 {b:.0f} us")
+    assert a < 1.3 * b
