@@ -9,6 +9,9 @@
 namespace dsp {
 namespace {
 
+// The position of a sequence's first query: any number of 32 bits, to be counted on in 64.
+__device__ __forceinline__ int64_t first_position(const int32_t* q_pos, uint32_t b) { return q_pos ? q_pos[b] : 0; }
+
 // A query at position p sees the keys j < sink and lo <= j < hi.  All three grow with p,
 // so a block's first and last query bound what its queries see.
 struct Seen {

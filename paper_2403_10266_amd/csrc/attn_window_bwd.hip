@@ -97,7 +97,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams 
   const T* kg = static_cast<const T*>(p.k) + k_at;
   const T* vg = static_cast<const T*>(p.v) + k_at;
   const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
-  const int64_t p0 = position(p.q_pos, b);
+  const int64_t p0 = first_position(p.q_pos, b);
   const Columns cs(p.grp, c0);
   auto seen_by = [&](uint32_t n) { return seen(p.win, p0 + cs.query(min(n, nc - 1)), len); };
   const Seen first = seen_by(0), last = seen_by(CB - 1);
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(KW * 64, MINW) void window_bwd_dkv_kernel(BwdParams
   const int64_t q_bx = bx_at(p, bx, p.qs), o_bx = bx_at(p, bx, p.os);
   const int32_t first_key = (int32_t)(blk * KEYS), key = first_key + 32 * wave + l32;
   const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
-  const int64_t p0 = position(p.q_pos, b);
+  const int64_t p0 = first_position(p.q_pos, b);
   const SeenBy mine = seen_by(p.win, p0, (int32_t)p.Lq, len, key);
   // of the wave's keys: the tiles that any is seen from, and those that all are
   int32_t any0 = mine.first < mine.end ? mine.first : INT32_MAX, any1 = mine.end, all0 = mine.first, all1 = mine.end;
@@ -453,7 +453,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_short_kernel(BwdPara
   const int D = (int)p.D;
   const int64_t k_at = bx_at(p, bx, p.ks) + (int64_t)e * D, q_at = bx_at(p, bx, p.qs), o_at = bx_at(p, bx, p.os);
   const int32_t len = (int32_t)length(p.kv_len, b, p.Lk);
-  const int64_t p0 = position(p.q_pos, b);
+  const int64_t p0 = first_position(p.q_pos, b);
   const Columns cs(p.grp, 0);
   const Seen first = seen(p.win, p0, len), last = seen(p.win, p0 + p.Lq - 1, len);
   const typename R::Map map = R::map(D, (uint32_t)p.ks[2] * (uint32_t)sizeof(T), lane);

@@ -69,7 +69,7 @@ __device__ __forceinline__ Unit<T, S, false> unit(const FwdParams& p, uint32_t b
   u.o = static_cast<T*>(p.o) + (int64_t)b * p.os[0] + (int64_t)x * p.os[1] + (int64_t)h0 * p.D;
   u.lse = p.lse ? p.lse + ((uint64_t)bx * p.H + h0) * p.Lq : nullptr;
   u.q_row = p.qs[2], u.o_row = p.os[2], u.lse_i = 1, u.lse_h = p.Lq;
-  u.p0 = position(p.q_pos, b);
+  u.p0 = first_position(p.q_pos, b);
   u.nq = (int32_t)p.Lq;
   u.len = (int32_t)length(p.kv_len, b, p.Lk);
   const int64_t at = (int64_t)b * p.ks[0] + (int64_t)x * p.ks[1] + (int64_t)e * p.D;

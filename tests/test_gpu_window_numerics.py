@@ -5,7 +5,7 @@ import pytest
 from oracle import window as ow
 from tests import window_util as wu
 from tests.gpu_util import dev, host, say
-from tests.test_gpu_attn_window import _i32, torch  # noqa: F401
+from tests.test_gpu_attn_window import _i32, _run, torch  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -192,3 +192,18 @@ def test_rows_far_apart(torch, dtype, Lq, sinks):  # noqa: F811
         got.append([o, lse, *dsp.dsp_attn_window_bwd(*t, o, do, lse, H, H, dq=g[0], dk=g[1], dv=g[2], **kw)])
     assert torch.isfinite(got[0][0].float()).all()
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Lq,Lk", [(2, 600), (40, 50), (150, 200)])
+def test_positions_at_the_ends_of_32_bits(torch, dtype, Lq, Lk):  # noqa: F811
+    """First queries at positions of any size, with windows that reach back to the keys, that just
+    do and that do not."""
+    far = 2 ** 31 - 1
+    c = wu.case(1, 1, Lq, Lk, 2, 1, 64, dtype, seed=70)
+    for q_pos, left, right in ((far, 2 ** 30 + 5, 0), (far, far - 30, 0), (far, far, -1), (-far - 1, -1, 2 ** 30 + 5),
+                               (-far - 1, 7, far), (-far - 1 + Lq, -1, far - 20), (2 ** 30 + 9, 2 ** 30, 3)):
+        kw = dict(left=left, right=right, sinks=0, q_pos=[q_pos])
+        say(kw)
+        got = _run(torch, c, dtype, **kw)
+        wu.compare({n: host(t) for n, t in got.items()}, wu.wanted(c, dtype, **kw), say)
