@@ -530,9 +530,10 @@ int dsp_attn_window_bwd(const void* q, const void* k, const void* v, const void*
  *   are not finite are held as NaN and do not count.  A page whose slot 0 is not among the
  *   new tokens must hold what earlier calls wrote (or scale 0: nothing).
  *   Slots other than the new tokens' (8 bits: and those before them in the page) and rows of
- *   no sequence are left as they were.  A page that is written belongs to one sequence.
- *   D up to 256, H + 2 Hkv below 2048, at any alignment of an element; 16-byte aligned tensors and tables, with
- *   D and rot multiples of 8, are fastest.
+ *   no sequence are left as they were.  A page that is written belongs to one sequence and to one
+ *   place of its table.
+ *   D up to 256 (dsp_attn_paged: 128), H + 2 Hkv below 2048, at any alignment of an element;
+ *   16-byte aligned tensors and tables, with D and rot multiples of 8, are fastest.
  *
  * dsp_attn_paged -- attention of the new tokens (q, o: T rows of H heads, q_stride and
  * o_stride elements apart) over their sequences' cached positions, with the visibility,

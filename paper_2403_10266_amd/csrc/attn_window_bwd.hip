@@ -72,9 +72,9 @@ __device__ __forceinline__ void row_product(floatx16& s, const typename Mx<T>::f
 }
 
 // dQ and Delta: 32 columns per wave, keys on the rows of the products.  Chains of product,
-// exponential and product bound it, at two or three waves to a SIMD (matrix cores 17 - 27%, waits 31 - 50%):
-// 8 x 16 units of 4096 x 72, window 257, 185 us; 4 sequences of 4000, 32 heads of 64 over 8,
-// window 501, 100 us.
+// exponential and product bound it, at two waves to a SIMD, one for heads above 96 (matrix cores
+// 22 - 26%, waits 36 - 45%): 8 x 16 units of 4096 x 72, window 257, 193 us; 4 sequences of 4000, 32
+// heads of 64 over 8, window 501, 134 us (without the correction of Delta 186 and, with three waves, 102).
 template <typename T, int DC, int NW, int KB, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_dq_kernel(BwdParams p) {
   using G = Geo<T, DC>;
@@ -237,8 +237,9 @@ __device__ __forceinline__ SeenBy seen_by(const Window& w, int64_t p0, int32_t n
 }
 
 // dK and dV, over the queries of every head of the key/value head's group, in tiles of
-// 32 QT: a wave per 32 keys, whose K, V and sums it holds (two waves to a SIMD).  The same two
-// calls: 225 and 174 us.
+// 32 QT: a wave per 32 keys, whose K, V and sums it holds (two waves to a SIMD that wait half of their
+// time, and in the second call a grid that is not a whole number of rounds).  The same two calls: 223
+// and 177 us.
 template <typename T, int DC, int KW, int QT, int MINW>
 __global__ __launch_bounds__(KW * 64, MINW) void window_bwd_dkv_kernel(BwdParams p) {
   using G = Geo<T, DC>;
@@ -430,8 +431,9 @@ __global__ __launch_bounds__(256) void window_bwd_sink_kernel(BwdParams p, uint3
 // first takes columns 32 w .. against all keys, which lie in LDS (Delta = sum_j P dP, with
 // no need of o, then dQ); then its Q and dO, which it held in registers as operands, take the
 // place of the keys in LDS, it keeps keys 32 w .. in registers, and dK and dV follow with the
-// scores computed the other way round.  Memory bounds these: 1024 x 16 units of 128 x 72, 665 us,
-// 3.2 TB/s (940 with the two kernels for long units); 1350 x 16 of 49 260, 2048 x 16 of 32 249.
+// scores computed the other way round.  Memory bounds those of one or two blocks: 1350 x 16 units of
+// 49 x 72 265 us, 2048 x 16 of 32 254, 4.0 - 4.2 TB/s.  At 128 it is the scores, formed three times by
+// two waves to a SIMD: 1024 x 16 units 665 us, 3.2 TB/s (940 with the two kernels for long units).
 template <typename T, int DC, int NW, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void window_bwd_short_kernel(BwdParams p) {
   using G = Geo<T, DC>;

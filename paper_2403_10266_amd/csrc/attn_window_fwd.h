@@ -415,10 +415,11 @@ __device__ __forceinline__ BlockOf block_of(const FwdParams& p, uint32_t size, u
 }
 
 // Many columns: QT blocks of 32 per wave, the keys in LDS tiles that all waves share,
-// the next tile on its way in registers.  Vector units bound it (busy 64%: for a score an
-// exponential, its scaling, cut, sum and half a conversion; matrix cores 38%): 8192 causal
-// tokens, 32 heads of 64 over 8, window 2048, 158 us, 764 TFLOP/s of the 120 GF of its mask;
-// 8 x 16 units of 4096 x 72, window 257, 122 us.
+// the next tile on its way in registers.  Vector units (busy 64%: for a score an exponential, its
+// scaling, cut, sum and half a conversion) and matrix cores (38%) take turns, which together is the
+// whole time: 8192 causal tokens, 32 heads of 64 over 8, window 2048, 159 us, 757 TFLOP/s of the
+// 120 GF of its mask; without a window 318 us, 865 TFLOP/s.  In narrow windows waves wait for tiles
+// that only their neighbours see (waits 50%): 8 x 16 units of 4096 x 72, window 257, 129 us.
 template <typename T, typename S, bool PAGED, int DC, int NW, int QT, int KB, int NKT, int MINW>
 __global__ __launch_bounds__(NW * 64, MINW) void window_fwd_kernel(FwdParams p) {
   using G = Geo<T, DC>;
@@ -669,7 +670,7 @@ __global__ __launch_bounds__(NW * 64, MINW) void window_short_kernel(FwdParams p
 // waves' sums are joined.  A pass over a cache is bound by memory: what counts is how
 // many waves a CU holds, that each has its next tile on its way, and that every load
 // runs along rows.  2 tokens over 100000 keys, 32 heads of 128 over 8: 80 us and 8 for the join,
-// 5.1 TB/s in the pass; 64 tokens over 8-bit caches of up to 16000 keys 164 us, 4.4 TB/s.
+// 5.1 TB/s in the pass; 64 tokens over 8-bit caches of up to 16000 keys 166 us, 4.4 TB/s in the pass.
 constexpr int kMinTiles = 4;   // of a work-group's wave, where the keys are cut
 struct Cut {                   // tiles of each part, and parts that have any
   int32_t per, used;
@@ -957,7 +958,8 @@ inline Choice choose(const WindowArgs& a) {
   // passes over the keys, would leave most of the chip idle: each block reads the keys again, out
   // of L2.  Heads of 64, groups of 4; blocks of all units, keys: this form and the other in us:
   // 16, 8000: 21 and 124; 128, 2000: 33 and 37; 256, 2000: 53 and 37; 512, 8000: 115 - 135 and
-  // 146 - 173; 1024, 8000: 220 and 171; 16, 100000: 58 and 1760; 512, 100000: 842 and 2183.
+  // 146 - 173; 1024, 8000: 220 and 171; 16, 100000: 58 and 1760; 512, 100000: 842 and 2183 (keys from
+  // the call before in the 256 MB cache; 16, 100000 with other keys in turn 73).
   const int64_t blocks = (cols + 31) / 32;
   c.cblk = cols > 32 && units * blocks <= std::min<int64_t>(512, keys / 16) ? blocks : 1;
   c.few = grp <= 32 || c.cblk > 1;
