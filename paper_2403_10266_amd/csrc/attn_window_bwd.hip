@@ -238,8 +238,8 @@ __device__ __forceinline__ SeenBy seen_by(const Window& w, int64_t p0, int32_t n
 
 // dK and dV, over the queries of every head of the key/value head's group, in tiles of
 // 32 QT: a wave per 32 keys, whose K, V and sums it holds (two waves to a SIMD that wait half of their
-// time, and in the second call a grid that is not a whole number of rounds).  The same two calls: 223
-// and 177 us.
+// time, and in the second call a grid that fills the chip one and a third times).  The same two calls:
+// 223 and 177 us.
 template <typename T, int DC, int KW, int QT, int MINW>
 __global__ __launch_bounds__(KW * 64, MINW) void window_bwd_dkv_kernel(BwdParams p) {
   using G = Geo<T, DC>;
