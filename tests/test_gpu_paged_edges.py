@@ -224,3 +224,49 @@ def test_the_order_of_sequences_is_cheap(torch):  # noqa: F811
     a, b = (min(t) * 100 for t in times)
     say(f"64 sequences {a:.0f} us, 65 {b:.0f} us")
     assert a < 1.3 * b
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_two_programs_at_once(torch, kind):  # noqa: F811
+    """Appending and attending on two streams, and from two graphs replayed in turn and together,
+    each with a cache and (its keys cut among work-groups) a workspace of its own."""
+    import paper_2403_10266_amd as dsp
+    r = np.random.default_rng(23)
+    H, Hkv, D, page, kv = 8, 2, 64, 16, [3000, 2000]
+    progs = []
+    for new in (1, 40):
+        table, pages = _table(r, kv, page)
+        caches = [_cache(torch, np.clip(ow.e4m3(wu.draw((pages, page, Hkv, D), "bf16", r)), -448, 448), kind, "token")
+                  for _ in "kv"]
+        s = [torch.full((pages, Hkv), 1.0, device="cuda") for _ in "kv"] if kind == "e4m3" else [None, None]
+        rows = [dev(wu.draw((2 * new, n * D), "bf16", r), "bf16") for n in (H, Hkv, Hkv)]
+        at = (_i32(torch, table), _i32(torch, [0, new, 2 * new]), _i32(torch, kv))
+
+        def call(stream=None, rows=rows, caches=caches, s=s, at=at, new=new):
+            q = dsp.dsp_kv_append(rows[1], rows[2], *caches, *at, *s, q=rows[0], stream=stream)
+            return [q, *dsp.dsp_attn_paged(q, *caches, *at, H, max_q=new, k_scale=s[0], v_scale=s[1], with_lse=True,
+                                           stream=stream)]
+        progs.append(call)
+    want = [[x.clone() for x in call()] for call in progs]      # appending the same tokens again changes nothing
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in progs]
+    for _ in range(4):
+        got = [call(s) for call, s in zip(progs, streams)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(got, want) for a, b in zip(g, w))
+    graphs, outs = [], []
+    for call in progs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(call())
+        graphs.append(g)
+    for together in (False, True, False, True):
+        for o in outs:
+            for x in o:
+                x.fill_(7)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s if together else streams[0]):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for g, w in zip(outs, want) for a, b in zip(g, w))
